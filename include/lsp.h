@@ -61,7 +61,9 @@ extern "C" {
 /* device error word bits (lsp_get_error) */
 #define LSP_DEV_TIMEOUT 1u        /* a bounded mbarrier/flag wait expired */
 #define LSP_DEV_BAD_TOKEN 2u      /* a token id outside [-1, V) (slot 0: outside [0, V)) */
-#define LSP_DEV_BAD_DELTA 4u      /* accepted_len outside [0, row capacity] */
+#define LSP_DEV_BAD_DELTA 4u      /* accepted_len outside [0, row capacity] (lsp_verify_probs: n_draft outside [0, B]) */
+#define LSP_DEV_BAD_SEQ 8u        /* a cache entry a call cannot use: sequence or page index, length, row range */
+#define LSP_DEV_NO_PAGE 16u       /* lsp_pages_reserve: not enough free pages */
 
 #define LSP_DTYPE_BF16 0
 #define LSP_DTYPE_F32 1
@@ -372,6 +374,158 @@ int lsp_get_error(lsp_state* st, uint32_t* dev_error, int clear, lsp_stream_t st
  *   t int64 [C]. */
 int lsp_state_export(lsp_state* st, void* host_buf, size_t bytes, lsp_stream_t stream);
 int lsp_state_import(lsp_state* st, const void* host_buf, size_t bytes, lsp_stream_t stream);
+
+/* ---------------------------------------------------------------- target side of a round
+ *
+ * The round's other half runs in the target: its candidate rows (the committed
+ * token and the drafted block) are appended to the target's key/value cache,
+ * attend over it, and the proposals are accepted or rejected (Sec. 2.1).  The
+ * calls below are its operators over a paged cache that the caller owns.  They
+ * need no lsp_state, allocate nothing, and follow the conventions above; a
+ * condition that only the device can see sets bits of the optional device word
+ * `dev_error` (OR-ed in; NULL: not reported) and the entry concerned is left
+ * as it was.  A round, for sequences that share a prompt:
+ *   lsp_pages_fork     branches hold the prompt's pages (no data is copied)
+ *   lsp_pages_reserve  room for the new rows of each sequence; a page that is
+ *                      only partly filled and shared is copied first
+ *   per target layer:  lsp_pages_write, lsp_prefix_attention
+ *   lsp_verify_probs   (or lsp_verify) accepts r of the drafted tokens
+ *   lsp_pages_trim     gives back the rejected rows' pages
+ */
+
+/*
+ * A paged key/value cache; every pointer is device memory of the caller.
+ *   k, v   element (layer, page, head, slot, dim) at
+ *          layer*s_layer + page*s_page + head*s_head + slot*s_slot + dim
+ *          (strides in elements, the same for k and v, any order; each a
+ *          positive multiple of 16 bytes; k and v 16-byte aligned)
+ *   table  [seqs][max_pages]: the page of tokens [i*page, (i+1)*page) of a
+ *          sequence, -1 past its last page
+ *   len    [seqs] tokens of each sequence
+ *   refs   [pages] how many sequences hold each page; 0 = free
+ * An empty cache has table = -1, len = 0, refs = 0.
+ * Supported: page 16, 32, 64, 128 or 256; d 64 or 128; dtype BF16 or F32;
+ * pages <= 2^20; seqs * max_pages <= 2^30; max_pages * page <= 2^30.
+ */
+typedef struct lsp_kv_cache {
+  void* k;
+  void* v;
+  int32_t* table;
+  int32_t* len;
+  int32_t* refs;
+  int64_t s_layer, s_page, s_head, s_slot;
+  int layers, pages, page, nkv, d, dtype, seqs, max_pages;
+} lsp_kv_cache;
+
+/* Bytes of device workspace that lsp_pages_reserve and lsp_pages_compact need
+ * for this cache (0 for one that is not supported).  Host only. */
+size_t lsp_pages_workspace_bytes(const lsp_kv_cache* cache);
+
+/* Sequence dst[i] becomes another holder of src[i]'s pages, and as long (i < n
+ * <= 1024; device int32).  What dst[i] held is let go first.  A pair with an
+ * index outside [0, seqs), a dst listed before or a dst listed as a src sets
+ * LSP_DEV_BAD_SEQ and is skipped.  One launch; no key or value is copied. */
+int lsp_pages_fork(const lsp_kv_cache* cache, const int32_t* src, const int32_t* dst, int n,
+                   uint32_t* dev_error, lsp_stream_t stream);
+
+/* Make room for add[i] more tokens of sequence seqs[i] (i < n <= 1024; device
+ * int32): its len grows by add[i] and its table by the pages this takes.  If
+ * its last page is partly filled and other sequences hold it too, it gets its
+ * own copy first (the filled slots, every layer); of several such entries of
+ * one call the last holder keeps the page.  Pages are handed out in list order,
+ * an entry's copy first, each the lowest free one.  An entry with an index
+ * outside [0, seqs), listed before, add < 0 or too long for max_pages is
+ * skipped (LSP_DEV_BAD_SEQ).  If the free pages do not suffice
+ * (LSP_DEV_NO_PAGE), the first entry that does not fit and all after it are
+ * left as they were.  workspace: lsp_pages_workspace_bytes, 16-byte aligned,
+ * not initialised, not shared with a call that may overlap. */
+int lsp_pages_reserve(const lsp_kv_cache* cache, const int32_t* seqs, const int32_t* add, int n,
+                      void* workspace, size_t workspace_bytes, uint32_t* dev_error,
+                      lsp_stream_t stream);
+
+/* Store the keys and values of new rows in one layer: rows [start[i],
+ * start[i+1]) (device int32 [n+1]) become the last start[i+1] - start[i]
+ * tokens of sequence seqs[i].  k_new, v_new: device dtype, row r at r *
+ * row_stride elements, [nkv][d] dense within (row_stride and the pointers
+ * multiples of 16 bytes); total: rows in all.  Rows of an entry whose sequence,
+ * range or page is outside the cache are dropped (LSP_DEV_BAD_SEQ). */
+int lsp_pages_write(const lsp_kv_cache* cache, int layer, const int32_t* seqs, const int32_t* start,
+                    int n, const void* k_new, const void* v_new, int64_t row_stride, int total,
+                    uint32_t* dev_error, lsp_stream_t stream);
+
+/* Cut sequence seqs[i] down to its first new_len[i] tokens (i < n <= 1024;
+ * device int32; 0 frees it, more than it has changes nothing): the pages past
+ * them lose a holder.  An index outside [0, seqs), one listed before or a
+ * negative length is skipped (LSP_DEV_BAD_SEQ). */
+int lsp_pages_trim(const lsp_kv_cache* cache, const int32_t* seqs, const int32_t* new_len, int n,
+                   uint32_t* dev_error, lsp_stream_t stream);
+
+/* Move the live pages (refs > 0) to the front of the pool, every layer: with
+ * `live` of them, the k-th live page at an index >= live goes to the k-th free
+ * index < live; table and refs follow.  live: device int32, receives the
+ * count, or NULL.  workspace as for lsp_pages_reserve. */
+int lsp_pages_compact(const lsp_kv_cache* cache, int32_t* live, void* workspace,
+                      size_t workspace_bytes, lsp_stream_t stream);
+
+/* Bytes of device workspace of lsp_prefix_attention for n sequences and
+ * total rows (0 for what it does not support).  The greatest over the calls a
+ * program makes is enough for all.  Host only, but it asks the current device
+ * for its size. */
+size_t lsp_prefix_attention_workspace_bytes(const lsp_kv_cache* cache, int nq, int n, int total);
+
+/* Causal attention of the batch's newest rows over their sequences in one
+ * layer of the cache, the pages that all of them share read once for the batch.
+ *   q       device dtype, row t at t * q_stride elements, [nq][d] within
+ *           (q_stride and q multiples of 16 bytes); nq / nkv a whole number <= 64
+ *   seqs    device int32 [n], n <= 1024: the batch's sequences
+ *   start   device int32 [n+1]: rows [start[i], start[i+1]) of q, c of them, are
+ *           the last c tokens of sequence seqs[i] (already in the cache)
+ *   total   rows of q in all
+ *   shared_len  the first shared_len tokens of every listed sequence are in the
+ *           same pages (as lsp_pages_fork leaves them); 0: nothing is shared.
+ *           Only whole pages of it before every row's position are read for
+ *           all, from the table of the first sequence that has rows.
+ *   scale   > 0, of the scores (d^-1/2 as a rule)
+ *   out     device dtype [total][nq][d]; 16-byte aligned
+ *   lse     device float [total][nq] or NULL: log sum exp of the scaled scores
+ * A row at position t sees tokens 0..t:  out = softmax(scale q K^T) V.  A row
+ * with no token to see (a sequence shorter than its rows) gives 0 and lse
+ * -inf, and so does one of no sequence, or of one outside the cache
+ * (LSP_DEV_BAD_SEQ); table entries outside the pool read as zero keys and values
+ * (LSP_DEV_BAD_SEQ).  What lies in unused slots of a page is never seen,
+ * whatever its bits; the keys and values of a sequence's own tokens are taken
+ * to be finite.  bf16: scores and sums in fp32, weights rounded to bf16 for
+ * the product with V; f32: fp32 throughout. */
+int lsp_prefix_attention(const lsp_kv_cache* cache, int layer, const void* q, int64_t q_stride,
+                         int nq, const int32_t* seqs, const int32_t* start, int n, int total,
+                         int shared_len, float scale, void* out, float* lse, void* workspace,
+                         size_t workspace_bytes, uint32_t* dev_error, lsp_stream_t stream);
+
+/* Acceptance of drafted tokens (Eq. acceptance, Eq. residual) from
+ * probabilities and random numbers that the caller gives: lsp_verify for
+ * programs that shape their distributions (top-k, top-p, ...) or draw their
+ * randomness elsewhere.
+ *   target_probs  device dtype, row (b, i) of [C][B+1] at (b (B+1) + i) ld_target
+ *           elements, V within: p_{i+1}; need not be normalised
+ *   draft_probs  the same for [C][B] with ld_draft: q_{i+1}; NULL: the drafts were
+ *           not drawn (each q a point mass on its token)
+ *   draft_tokens  device int32 [C][B];  n_draft: device int32 [C], how many of
+ *           them count, in [0, B] (else clamped, LSP_DEV_BAD_DELTA); NULL: all
+ *   u       device float [C][B], uniforms of the acceptance tests
+ *   e       device float [C][V], Exp(1) variates of the draw
+ * y_i is accepted iff u_i q_i(y_i) < p_i(y_i), in order, in fp32; with r accepted,
+ * next_token = argmax_v w_v / e_v over w_v > 0, w = [p_{r+1} - q_{r+1}]_+ if y_{r+1}
+ * was rejected (p_{r+1} where that is 0 throughout), w = p_{r+1} if none was left;
+ * ties go to the lowest index, -1 if no w_v > 0.  A drafted token outside [0, V)
+ * is rejected (LSP_DEV_BAD_TOKEN).
+ *   accepted_len, next_token  device int32 [C]
+ *   out_tokens  device int32 [C][B+1] or NULL: the accepted tokens, next_token, -1
+ * C >= 1, B in [0, 1024], V in [1, 2^30], ld >= V.  One launch. */
+int lsp_verify_probs(const void* target_probs, const void* draft_probs, int dtype,
+                     const int32_t* draft_tokens, const int32_t* n_draft, const float* u,
+                     const float* e, int C, int B, int V, int64_t ld_target, int64_t ld_draft,
+                     int32_t* accepted_len, int32_t* next_token, int32_t* out_tokens,
+                     uint32_t* dev_error, lsp_stream_t stream);
 
 #ifdef __cplusplus
 }

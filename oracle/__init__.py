@@ -16,14 +16,17 @@ written from the paper's text in its own order and notation:
                 over a Philox4x32-10 stream.
 * verify.py  -- target-side verification of a drafted block (Eq. acceptance,
                 Eq. residual, the bonus draw of Sec. 2.1).
+* target.py  -- the target's paged cache, the attention of the round's rows over
+                it, and acceptance from given probabilities and random numbers.
 * philox.py  -- Philox4x32-10 (Salmon et al., SC'11) from its published definition.
 
 Only tests/, __graft_entry__.smoke() and bench.py's CPU-baseline leg may import
 it; the CUDA library never does, and this package imports nothing from it.
 Every function works in float64 on inputs upcast from the stored bf16/fp32
-bytes, and never rounds an intermediate.
+bytes, and never rounds an intermediate (target.verify_probs decides in fp32,
+as its definition says).
 """
-from . import philox, views, drafter, sampler, verify  # noqa: F401
+from . import philox, views, drafter, sampler, verify, target  # noqa: F401
 from .views import OracleState, state_init, view_update, full_summary, state_bytes_per_request  # noqa: F401
 from .drafter import OracleWeights, draft_base_logits  # noqa: F401
 from .sampler import sample_block, gumbel  # noqa: F401

@@ -1,0 +1,378 @@
+// Attention of a batch's newest rows over a paged cache whose sequences share
+// a prefix (contract: include/lsp.h, work distribution: prefix_sched.cuh).
+//
+//   s_j = scale q.k_j,  m = max_j s_j,  l = sum_j exp(s_j - m),
+//   o = (1/l) sum_j exp(s_j - m) v_j,   lse = m + log l
+//
+// with the keys cut into segments, each leaving (sum_j 2^(s2_j - m2) v_j, m2,
+// l) in base 2, s2 = s log2(e); prefix_join_kernel adds a row's segments with
+// weights 2^(m2_seg - max m2).
+//
+// prefix_attn_fma_kernel: fp32 multiply-adds, 64 rows x 64 keys a step.
+#include <algorithm>
+
+#include "prefix_sched.cuh"
+
+namespace lsp {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.69314718055994531f;
+
+__device__ __forceinline__ float ex2a(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// The schedule goes to the workspace for the joining kernel (CTA 0).
+__device__ __forceinline__ void publish_sched(const PrefixAttnParams& p, const PrefixSched& s, const int64_t* step_base) {
+  if (threadIdx.x == 0) *reinterpret_cast<PrefixSched*>(p.sched) = s;
+  int64_t* out = reinterpret_cast<int64_t*>(p.sched + kSchedHdrBytes);
+  for (int i = threadIdx.x; i <= p.n; i += blockDim.x) out[i] = step_base[i];
+}
+
+constexpr int kFmaRows = 64, kFmaKeys = 64, kFmaThreads = 256;
+
+template <typename T>
+__device__ __forceinline__ float4 load4(const T* p);
+template <>
+__device__ __forceinline__ float4 load4<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
+template <>
+__device__ __forceinline__ float4 load4<bf16>(const bf16* p) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  const __nv_bfloat162 a = *reinterpret_cast<const __nv_bfloat162*>(&u.x), b = *reinterpret_cast<const __nv_bfloat162*>(&u.y);
+  return make_float4(__low2float(a), __high2float(a), __low2float(b), __high2float(b));
+}
+
+template <int HD>
+struct FmaSmem {
+  float q[kFmaRows][HD + 4];
+  float kv[kFmaKeys][HD + 4];
+  float p[kFmaRows][kFmaKeys + 4];
+  int64_t at[kFmaKeys];                          // element offset of each key of the block, -1: none
+  int64_t step_base[kPrefixMaxSeqs + 1];
+  PrefixSched sched;
+};
+
+// One segment: rows of one tile of `tokens` rows of q from token t0, head g,
+// key blocks [kb0, kb1) of the tokens [k0, k_end) of table row `tab`.  Row (i,
+// head) sees tokens below see0 + i (the shared part: k_end for all).
+template <typename T, int HD>
+__device__ void fma_segment(const PrefixAttnParams& p, FmaSmem<HD>& sm, const int32_t* tab, int g, int t0, int tokens, int k0,
+                            int k_end, int kb0, int kb1, int see0, bool causal, int64_t out_row) {
+  constexpr int kD4 = HD / 4, kCols = HD / 64;   // float4 of a row; float4 output columns of a thread
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  const int rows = tokens * p.rep;
+  const T* q = static_cast<const T*>(p.q);
+  __syncthreads();
+  for (int i = tid; i < kFmaRows * kD4; i += kFmaThreads) {
+    const int r = i / kD4, c = i % kD4;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r < rows) x = load4<T>(q + (int64_t)(t0 + r / p.rep) * p.q_stride + (int64_t)(g * p.rep + r % p.rep) * HD + 4 * c);
+    *reinterpret_cast<float4*>(&sm.q[r][4 * c]) = x;
+  }
+  float m[4], l[4], o[4][kCols][4];
+  int lim[4];
+  const float sl = p.scale * kLog2e;
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    m[a] = -INFINITY;
+    l[a] = 0.f;
+    const int r = 4 * ty + a;
+    lim[a] = r >= rows ? 0 : (causal ? min(see0 + r / p.rep, k_end) : k_end);
+#pragma unroll
+    for (int c = 0; c < kCols; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[a][c][e] = 0.f;
+  }
+  for (int kb = kb0; kb < kb1; ++kb) {
+    const int key0 = k0 + kb * kFmaKeys;
+    __syncthreads();                             // q is stored; kv and p of the block before are read
+    if (tid < kFmaKeys) {
+      const int pos = key0 + tid;
+      int64_t at = -1;
+      if (pos < k_end) {
+        const int pg = tab[pos / p.page];
+        if (pg >= 0 && pg < p.pages)
+          at = (int64_t)pg * p.s_page + (int64_t)(pos % p.page) * p.s_slot + (int64_t)g * p.s_head;
+        else
+          set_err(p.err, LSP_DEV_BAD_SEQ);
+      }
+      sm.at[tid] = at;
+    }
+    __syncthreads();
+    auto load_kv = [&](const char* pool) {
+      for (int i = tid; i < kFmaKeys * kD4; i += kFmaThreads) {
+        const int r = i / kD4, c = i % kD4;
+        const int64_t at = sm.at[r];
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (at >= 0) x = load4<T>(reinterpret_cast<const T*>(pool) + at + 4 * c);
+        *reinterpret_cast<float4*>(&sm.kv[r][4 * c]) = x;
+      }
+    };
+    load_kv(p.k);
+    __syncthreads();
+    float s[4][4];
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[a][c] = 0.f;
+#pragma unroll 4
+    for (int d = 0; d < HD; d += 4) {
+      float4 x[4], y[4];
+#pragma unroll
+      for (int a = 0; a < 4; ++a) x[a] = *reinterpret_cast<const float4*>(&sm.q[4 * ty + a][d]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) y[c] = *reinterpret_cast<const float4*>(&sm.kv[tx + 16 * c][d]);
+#pragma unroll
+      for (int a = 0; a < 4; ++a)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          s[a][c] = fmaf(x[a].x, y[c].x, s[a][c]);
+          s[a][c] = fmaf(x[a].y, y[c].y, s[a][c]);
+          s[a][c] = fmaf(x[a].z, y[c].z, s[a][c]);
+          s[a][c] = fmaf(x[a].w, y[c].w, s[a][c]);
+        }
+    }
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        s[a][c] = key0 + tx + 16 * c < lim[a] ? s[a][c] * sl : -INFINITY;
+        mx = fmaxf(mx, s[a][c]);
+      }
+#pragma unroll
+      for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+      const float nm = fmaxf(m[a], mx), mb = nm == -INFINITY ? 0.f : nm;
+      const float keep = ex2a(m[a] - mb);
+      float sum = 0.f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const float w = ex2a(s[a][c] - mb);
+        sum += w;
+        sm.p[4 * ty + a][tx + 16 * c] = w;
+      }
+#pragma unroll
+      for (int w = 8; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+      l[a] = l[a] * keep + sum;
+      m[a] = nm;
+#pragma unroll
+      for (int c = 0; c < kCols; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[a][c][e] *= keep;
+    }
+    __syncthreads();                             // p is stored, k is read
+    load_kv(p.v);
+    __syncthreads();
+#pragma unroll 2
+    for (int j = 0; j < kFmaKeys; j += 4) {
+      float4 w[4];
+#pragma unroll
+      for (int a = 0; a < 4; ++a) w[a] = *reinterpret_cast<const float4*>(&sm.p[4 * ty + a][j]);
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj)
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) {
+          const float4 y = *reinterpret_cast<const float4*>(&sm.kv[j + jj][4 * tx + 64 * c]);
+#pragma unroll
+          for (int a = 0; a < 4; ++a) {
+            const float x = jj == 0 ? w[a].x : jj == 1 ? w[a].y : jj == 2 ? w[a].z : w[a].w;
+            o[a][c][0] = fmaf(x, y.x, o[a][c][0]);
+            o[a][c][1] = fmaf(x, y.y, o[a][c][1]);
+            o[a][c][2] = fmaf(x, y.z, o[a][c][2]);
+            o[a][c][3] = fmaf(x, y.w, o[a][c][3]);
+          }
+        }
+    }
+  }
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    const int r = 4 * ty + a;
+    if (r >= rows) continue;
+    const int64_t at = out_row + r;
+#pragma unroll
+    for (int c = 0; c < kCols; ++c)
+      *reinterpret_cast<float4*>(p.part_o + at * HD + 4 * tx + 64 * c) = make_float4(o[a][c][0], o[a][c][1], o[a][c][2], o[a][c][3]);
+    if (tx == 0) p.part_ml[at] = make_float2(m[a], l[a]);
+  }
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(kFmaThreads) prefix_attn_fma_kernel(const PrefixAttnParams p) {
+  extern __shared__ __align__(16) uint8_t fma_raw[];
+  FmaSmem<HD>& sm = *reinterpret_cast<FmaSmem<HD>*>(fma_raw);
+  griddep_wait();
+  griddep_launch();
+  const int cta = blockIdx.x;
+  if (threadIdx.x < 32) {
+    const PrefixSched s = build_sched<1, kFmaKeys>(p, sm.step_base, cta == 0);
+    if (threadIdx.x == 0) sm.sched = s;
+  }
+  __syncthreads();
+  const PrefixSched s = sm.sched;
+  if (cta == 0) publish_sched(p, s, sm.step_base);
+  if (s.items > 0) {
+    const int32_t* tab = nullptr;
+    for (int i = 0; i < p.n && !tab; ++i) {      // the first sequence with rows stands for all
+      const PrefixSeq r = prefix_seq(p, i, false);
+      if (r.rows > 0) tab = p.table + (size_t)r.seq * p.max_pages;
+    }
+    for (int j = cta; j < s.items; j += p.grid) {
+      const int u = j % p.units, gs = j / p.units, split = gs % p.splits, g = gs / p.splits;
+      const int kb0 = split * s.per_split, kb1 = min(kb0 + s.per_split, s.blocks);
+      if (kb0 >= kb1) continue;
+      const int t0 = u * p.tok_tile, tokens = min(p.tok_tile, p.total - t0);
+      fma_segment<T, HD>(p, sm, tab, g, t0, tokens, 0, s.base, kb0, kb1, 0, false, shared_rows<1>(p, g, split, u).row);
+    }
+  }
+  int64_t x = own_begin(s, p.grid, cta);
+  const int64_t end = own_begin(s, p.grid, cta + 1);
+  while (x < end) {
+    const OwnSpot o = own_spot<1, kFmaKeys>(p, s, sm.step_base, x);
+    const PrefixSeq r = prefix_seq(p, o.i, false);
+    const int count = (int)min((int64_t)(o.blocks - o.block), end - x);
+    const int i0 = o.unit * p.tok_tile, tokens = min(p.tok_tile, r.rows - i0);
+    fma_segment<T, HD>(p, sm, p.table + (size_t)r.seq * p.max_pages, o.head, r.first + i0, tokens, s.base, r.len, o.block,
+                       o.block + count, r.len - r.rows + i0 + 1, true, own_rows<1>(p, r, o.unit, o.head, cta).row);
+    x += count;
+  }
+}
+
+// Joins the segments of one output row: a warp per (token, query head), lane l
+// holds dims [l HD/32, (l + 1) HD/32).
+constexpr int kJoinThreads = 256;
+template <typename T, int HD, int kUnitTiles, int kBlock>
+__global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixAttnParams p) {
+  constexpr int kVec = HD / 32;
+  griddep_wait();
+  griddep_launch();
+  const int lane = threadIdx.x & 31;
+  const int64_t w = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) >> 5;
+  if (w >= (int64_t)p.total * p.nq) return;
+  const int t = (int)(w / p.nq), h = (int)(w % p.nq), g = h / p.rep, hr = h % p.rep;
+  const PrefixSched s = *reinterpret_cast<const PrefixSched*>(p.sched);
+  const int64_t* step_base = reinterpret_cast<const int64_t*>(p.sched + kSchedHdrBytes);
+  float m = -INFINITY, l = 0.f, o[kVec];
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) o[e] = 0.f;
+  auto add = [&](int64_t row) {
+    const float2 ml = p.part_ml[row];
+    if (ml.x == -INFINITY) return;               // the segment saw nothing of this row
+    const float nm = fmaxf(m, ml.x), a = ex2a(m - nm), b = ex2a(ml.x - nm);
+    l = l * a + ml.y * b;
+    const float* x = p.part_o + row * HD + lane * kVec;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) o[e] = o[e] * a + x[e] * b;
+    m = nm;
+  };
+  int lo = 0, hi = p.n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (p.start[mid] <= t) lo = mid; else hi = mid;
+  }
+  const PrefixSeq r = prefix_seq(p, lo, false);
+  if (t >= r.first && t < r.first + r.rows) {
+    if (s.items > 0) {
+      const int tile = t / p.tok_tile, unit = tile / kUnitTiles, sub = tile % kUnitTiles;
+      const bool lone = kUnitTiles > 1 && (unit * kUnitTiles + 1) * p.tok_tile >= p.total;
+      for (int split = 0; split < p.splits && split * s.per_split < s.blocks; ++split) {
+        const PartRows at = shared_rows<kUnitTiles>(p, g, split, unit);
+        const int64_t row = at.row + sub * at.second + (t % p.tok_tile) * p.rep + hr;
+        add(row);
+        if (lone) add(row + at.second);
+      }
+    }
+    const int i = t - r.first, tile = i / p.tok_tile, unit = tile / kUnitTiles, sub = tile % kUnitTiles;
+    const bool lone = kUnitTiles > 1 && (unit * kUnitTiles + 1) * p.tok_tile >= r.rows;
+    int64_t first = step_base[lo];
+    for (int u = 0; u < unit; ++u) first += (int64_t)own_blocks<kUnitTiles, kBlock>(p, r, s.base, u) * p.nkv;
+    const int blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, unit);
+    first += (int64_t)g * blocks;
+    int c0 = 0, c1 = p.grid;                     // the CTA that has step `first`
+    while (c1 - c0 > 1) {
+      const int mid = (c0 + c1) >> 1;
+      if (own_begin(s, p.grid, mid) <= first) c0 = mid; else c1 = mid;
+    }
+    for (int c = c0; blocks > 0 && c < p.grid && own_begin(s, p.grid, c) < first + blocks; ++c) {
+      if (own_begin(s, p.grid, c + 1) <= max(first, own_begin(s, p.grid, c))) continue;   // a CTA without steps
+      const PartRows at = own_rows<kUnitTiles>(p, r, unit, g, c);
+      const int64_t row = at.row + sub * at.second + (i % p.tok_tile) * p.rep + hr;
+      add(row);
+      if (lone) add(row + at.second);
+    }
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  T* out = static_cast<T*>(p.out) + w * HD + lane * kVec;
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) out[e] = from_f<T>(o[e] * inv);
+  if (p.lse && lane == 0) p.lse[w] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+template <typename T, int HD>
+int launch_fma(const PrefixAttnParams& p, cudaStream_t s) {
+  static bool set[8] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return LSP_ERR_CUDA;
+  if (dev >= 8 || !set[dev]) {
+    if (cudaFuncSetAttribute(prefix_attn_fma_kernel<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)sizeof(FmaSmem<HD>)) != cudaSuccess)
+      return LSP_ERR_CUDA;
+    if (dev < 8) set[dev] = true;
+  }
+  if (launch_pdl(prefix_attn_fma_kernel<T, HD>, dim3(p.grid), dim3(kFmaThreads), sizeof(FmaSmem<HD>), s, p) != cudaSuccess)
+    return LSP_ERR_CUDA;
+  const int64_t warps = (int64_t)p.total * p.nq;
+  const unsigned grid = (unsigned)((warps * 32 + kJoinThreads - 1) / kJoinThreads);
+  return launch_pdl(prefix_join_kernel<T, HD, 1, kFmaKeys>, dim3(grid), dim3(kJoinThreads), 0, s, p) == cudaSuccess ? LSP_OK
+                                                                                                                  : LSP_ERR_CUDA;
+}
+
+inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Key ranges of the shared part.  Items (heads x units x ranges) of equal size
+// run in turns of `grid`: for each number of turns the most ranges that fit,
+// and of those the fewest key blocks on the longest CTA, each item counted
+// kItemBlocks more for its query loads and partial sums.
+constexpr int kMaxTurns = 4;
+int choose_splits(int groups, int blocks, int grid) {
+  constexpr double kItemBlocks = 3.0;
+  int best = 1;
+  double cost = 0.0;
+  for (int t = 0; t <= kMaxTurns; ++t) {
+    const int s = std::max(1, std::min(t * grid / groups, blocks));
+    const int turns = (groups * s + grid - 1) / grid, per = (blocks + s - 1) / s;
+    const double c = turns * (per + kItemBlocks);
+    if (t == 0 || c < cost) { best = s; cost = c; }
+  }
+  return best;
+}
+
+}  // namespace
+
+size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms) {
+  const int tile = kFmaRows, unit_tiles = 1, block = kFmaKeys, per_sm = 2;
+  p->tok_tile = tile / p->rep;
+  p->units = (p->total + p->tok_tile * unit_tiles - 1) / (p->tok_tile * unit_tiles);
+  p->grid = num_sms * per_sm;
+  p->splits = choose_splits(p->nkv * p->units, (p->shared_len + block - 1) / block, p->grid);
+  const int64_t rows = (int64_t)p->tok_tile * p->rep * unit_tiles, groups = (int64_t)p->nkv * p->units;
+  p->part_rows = std::max<int64_t>(groups, kMaxTurns * p->grid) * rows + (int64_t)unit_tiles * p->nkv * p->rep * p->total +
+                 p->grid * rows;
+  return align256(kSchedHdrBytes + (p->n + 1) * sizeof(int64_t)) + align256((size_t)p->part_rows * sizeof(float2)) +
+         (size_t)p->part_rows * p->d * sizeof(float);
+}
+
+int launch_prefix_attention(PrefixAttnParams p, int dtype, void* ws, cudaStream_t s) {
+  char* w = static_cast<char*>(ws);
+  p.sched = w;
+  w += align256(kSchedHdrBytes + (p.n + 1) * sizeof(int64_t));
+  p.part_ml = reinterpret_cast<float2*>(w);
+  w += align256((size_t)p.part_rows * sizeof(float2));
+  p.part_o = reinterpret_cast<float*>(w);
+  if (dtype == LSP_DTYPE_BF16) return p.d == 128 ? launch_fma<bf16, 128>(p, s) : launch_fma<bf16, 64>(p, s);
+  return p.d == 128 ? launch_fma<float, 128>(p, s) : launch_fma<float, 64>(p, s);
+}
+
+}  // namespace lsp

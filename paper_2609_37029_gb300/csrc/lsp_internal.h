@@ -265,4 +265,76 @@ int sample_launches(const SampleParams& p, int dtype);
 int launch_philox_words(uint64_t seed, uint32_t round, uint32_t b, uint32_t i, uint32_t* out,
                         int count, cudaStream_t s);
 
+// ------------------------------------------------------------------ paged cache (target side)
+// lsp_kv_cache with byte-addressed pools; strides in elements.
+struct KvCache {
+  char* k;
+  char* v;
+  int32_t* table;
+  int32_t* len;
+  int32_t* refs;
+  int64_t s_layer, s_page, s_head, s_slot;
+  int layers, pages, page, nkv, d, seqs, max_pages;
+};
+constexpr int kPagesMaxSeqs = 1024;   // entries of one page call
+size_t pages_ws_bytes(int pages);
+int launch_pages_fork(const KvCache& c, const int* src, const int* dst, int n, unsigned* err, cudaStream_t s);
+int launch_pages_trim(const KvCache& c, const int* seqs, const int* new_len, int n, unsigned* err, cudaStream_t s);
+int launch_pages_write(const KvCache& c, const int* seqs, const int* start, int n, const void* k_new, const void* v_new,
+                       int64_t row_bytes, int total, int es, unsigned* err, cudaStream_t s);
+int launch_pages_reserve(const KvCache& c, const int* seqs, const int* add, int n, void* ws, int es, int num_sms,
+                         unsigned* err, cudaStream_t s);
+int launch_pages_compact(const KvCache& c, int* live, void* ws, int es, int num_sms, cudaStream_t s);
+
+// ------------------------------------------------------------------ shared-prefix attention
+struct PrefixAttnParams {
+  const char* k;            // the layer's pools
+  const char* v;
+  const void* q;
+  void* out;                // [total][nq][d]
+  float* lse;               // [total][nq] or null
+  const int32_t* table;
+  const int32_t* len;
+  const int32_t* seqs;
+  const int32_t* start;
+  int64_t q_stride, s_page, s_head, s_slot;   // elements
+  int n, total, nq, nkv, rep, d;
+  int page, pages, max_pages, n_seqs;
+  int shared_len;
+  float scale;
+  unsigned* err;
+  // plan (prefix_attn_plan) and workspace
+  int tok_tile;             // rows of q (tokens) in a tile: tile rows / rep
+  int units;                // units of tiles that cover all rows
+  int splits;               // key ranges of the shared pages
+  int grid;                 // CTAs of the main kernel
+  int64_t part_rows;        // rows of partial results the workspace holds
+  char* sched;              // the schedule, for the joining kernel
+  float* part_o;            // [part_rows][d] unnormalised sums
+  float2* part_ml;          // [part_rows] (running maximum of the base-2 scores, sum)
+};
+constexpr int kPrefixMaxSeqs = 1024;
+constexpr int kPrefixMaxRep = 64;
+// Fills the plan fields; returns the workspace bytes.
+size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms);
+// ws: prefix_attn_plan's bytes, 256-byte aligned.
+int launch_prefix_attention(PrefixAttnParams p, int dtype, void* ws, cudaStream_t s);
+
+// ------------------------------------------------------------------ verification from probabilities
+struct VerifyProbsParams {
+  const void* pt;           // [C][B+1] rows of V, ld_t apart
+  const void* pq;           // [C][B] rows, ld_q apart, or null
+  const int32_t* y;         // [C][B]
+  const int32_t* n;         // [C] or null
+  const float* u;           // [C][B]
+  const float* e;           // [C][V]
+  int32_t* accepted;
+  int32_t* next_token;
+  int32_t* out_tokens;      // [C][B+1] or null
+  unsigned* err;
+  int C, B, V;
+  int64_t ld_t, ld_q;
+};
+int launch_verify_probs(const VerifyProbsParams& p, int dtype, cudaStream_t s);
+
 }  // namespace lsp

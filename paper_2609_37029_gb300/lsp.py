@@ -10,8 +10,8 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import (POINTER, Structure, c_char_p, c_float, c_int, c_size_t, c_uint32, c_uint64,
-                    c_void_p)
+from ctypes import (POINTER, Structure, c_char_p, c_float, c_int, c_int64, c_size_t, c_uint32,
+                    c_uint64, c_void_p)
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "liblsp.so")
@@ -20,6 +20,7 @@ LSP_MAX_DRAFT_LAYERS = 16
 LSP_OK, LSP_ERR_ARG, LSP_ERR_SHAPE, LSP_ERR_CUDA = 0, -1, -2, -3
 LSP_ERR_TIMEOUT, LSP_ERR_STATE, LSP_ERR_NOMEM, LSP_ERR_UNSUPPORTED = -4, -5, -6, -7
 LSP_DEV_TIMEOUT, LSP_DEV_BAD_TOKEN, LSP_DEV_BAD_DELTA = 1, 2, 4
+LSP_DEV_BAD_SEQ, LSP_DEV_NO_PAGE = 8, 16
 LSP_NO_BOUNDARY = 1
 LSP_DTYPE_BF16, LSP_DTYPE_F32 = 0, 1
 
@@ -55,6 +56,12 @@ class lsp_weights(Structure):
 
 class lsp_sample_params(Structure):
     _fields_ = [("temperature", c_float), ("round", c_uint32), ("seed", c_uint64)]
+
+
+class lsp_kv_cache(Structure):
+    _fields_ = [(n, c_void_p) for n in "k v table len refs".split()] + [
+        (n, c_int64) for n in "s_layer s_page s_head s_slot".split()] + [
+        (n, c_int) for n in "layers pages page nkv d dtype seqs max_pages".split()]
 
 
 class LspError(RuntimeError):
@@ -103,6 +110,25 @@ _f = {
     "lsp_set_stage_events": _sig("lsp_set_stage_events", c_int, c_void_p, POINTER(c_void_p), c_int),
     "lsp_state_export": _sig("lsp_state_export", c_int, c_void_p, c_void_p, c_size_t, c_void_p),
     "lsp_state_import": _sig("lsp_state_import", c_int, c_void_p, c_void_p, c_size_t, c_void_p),
+    "lsp_pages_workspace_bytes": _sig("lsp_pages_workspace_bytes", c_size_t, POINTER(lsp_kv_cache)),
+    "lsp_pages_fork": _sig("lsp_pages_fork", c_int, POINTER(lsp_kv_cache), c_void_p, c_void_p, c_int,
+                           c_void_p, c_void_p),
+    "lsp_pages_reserve": _sig("lsp_pages_reserve", c_int, POINTER(lsp_kv_cache), c_void_p, c_void_p,
+                              c_int, c_void_p, c_size_t, c_void_p, c_void_p),
+    "lsp_pages_write": _sig("lsp_pages_write", c_int, POINTER(lsp_kv_cache), c_int, c_void_p, c_void_p,
+                            c_int, c_void_p, c_void_p, c_int64, c_int, c_void_p, c_void_p),
+    "lsp_pages_trim": _sig("lsp_pages_trim", c_int, POINTER(lsp_kv_cache), c_void_p, c_void_p, c_int,
+                           c_void_p, c_void_p),
+    "lsp_pages_compact": _sig("lsp_pages_compact", c_int, POINTER(lsp_kv_cache), c_void_p, c_void_p,
+                              c_size_t, c_void_p),
+    "lsp_prefix_attention_workspace_bytes": _sig("lsp_prefix_attention_workspace_bytes", c_size_t,
+                                                 POINTER(lsp_kv_cache), c_int, c_int, c_int),
+    "lsp_prefix_attention": _sig("lsp_prefix_attention", c_int, POINTER(lsp_kv_cache), c_int, c_void_p,
+                                 c_int64, c_int, c_void_p, c_void_p, c_int, c_int, c_int, c_float,
+                                 c_void_p, c_void_p, c_void_p, c_size_t, c_void_p, c_void_p),
+    "lsp_verify_probs": _sig("lsp_verify_probs", c_int, c_void_p, c_void_p, c_int, c_void_p, c_void_p,
+                             c_void_p, c_void_p, c_int, c_int, c_int, c_int64, c_int64, c_void_p,
+                             c_void_p, c_void_p, c_void_p, c_void_p),
 }
 
 
@@ -152,6 +178,29 @@ def make_weights(w: dict) -> lsp_weights:
         for n in _LAYER_FIELDS:
             setattr(s.layer[j], n, _ptr(lw[n]))
     return s
+
+
+def make_kv_cache(k, v, table, lens, refs) -> lsp_kv_cache:
+    """lsp_kv_cache of device pointers: k, v [layers][pages][nkv][page][d] in any order of the first
+    four axes (their strides are taken), int32 table [seqs][max_pages], lens [seqs], refs [pages].
+    The struct holds addresses only: the caller keeps the tensors."""
+    import torch
+    if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.dim() != 5 or k.stride(4) != 1:
+        raise ValueError("k and v: the same 5-D shape, type and strides, the last axis dense")
+    if k.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("k and v: bfloat16 or float32")
+    for t in (table, lens, refs):
+        if t.dtype != torch.int32 or not t.is_contiguous():
+            raise ValueError("table, lens and refs: contiguous int32")
+    if table.dim() != 2 or lens.numel() != table.shape[0] or refs.numel() != k.shape[1]:
+        raise ValueError("table [seqs][max_pages], lens [seqs], refs [pages]")
+    c = lsp_kv_cache()
+    c.k, c.v, c.table, c.len, c.refs = (t.data_ptr() for t in (k, v, table, lens, refs))
+    c.s_layer, c.s_page, c.s_head, c.s_slot = k.stride()[:4]
+    c.layers, c.pages, c.nkv, c.page, c.d = k.shape
+    c.dtype = LSP_DTYPE_BF16 if k.dtype == torch.bfloat16 else LSP_DTYPE_F32
+    c.seqs, c.max_pages = table.shape
+    return c
 
 
 def make_sample_params(temperature=0.0, seed=0, rnd=0) -> lsp_sample_params:
@@ -290,6 +339,82 @@ def lsp_state_export(st, host_buf, stream=None) -> None:
 def lsp_state_import(st, host_buf, stream=None) -> None:
     _check(_f["lsp_state_import"](st, _ptr(host_buf), host_buf.numel() * host_buf.element_size(),
                                   _stream(stream)), "lsp_state_import")
+
+
+def lsp_pages_workspace_bytes(cache: lsp_kv_cache) -> int:
+    return _f["lsp_pages_workspace_bytes"](cache)
+
+
+def lsp_pages_fork(cache: lsp_kv_cache, src, dst, dev_error=None, stream=None) -> None:
+    _check(_f["lsp_pages_fork"](cache, _ptr(src), _ptr(dst), dst.numel(), _ptr(dev_error), _stream(stream)),
+           "lsp_pages_fork")
+
+
+def lsp_pages_reserve(cache: lsp_kv_cache, seqs, add, workspace, dev_error=None, stream=None) -> None:
+    _check(_f["lsp_pages_reserve"](cache, _ptr(seqs), _ptr(add), seqs.numel(), _ptr(workspace),
+                                   workspace.numel() * workspace.element_size(), _ptr(dev_error),
+                                   _stream(stream)), "lsp_pages_reserve")
+
+
+def lsp_pages_write(cache: lsp_kv_cache, layer, seqs, start, k_new, v_new, dev_error=None, stream=None) -> None:
+    """k_new, v_new: [total][nkv][d], dense within a row, the same stride between rows."""
+    if k_new.stride() != v_new.stride() or k_new.stride()[1:] != (cache.d, 1) or k_new.shape[1:] != (cache.nkv, cache.d):
+        raise ValueError("k_new and v_new: [total][nkv][d] of the same strides, dense within a row")
+    _check(_f["lsp_pages_write"](cache, int(layer), _ptr(seqs), _ptr(start), seqs.numel(), _ptr(k_new),
+                                 _ptr(v_new), k_new.stride(0), k_new.shape[0], _ptr(dev_error),
+                                 _stream(stream)), "lsp_pages_write")
+
+
+def lsp_pages_trim(cache: lsp_kv_cache, seqs, new_len, dev_error=None, stream=None) -> None:
+    _check(_f["lsp_pages_trim"](cache, _ptr(seqs), _ptr(new_len), seqs.numel(), _ptr(dev_error),
+                                _stream(stream)), "lsp_pages_trim")
+
+
+def lsp_pages_compact(cache: lsp_kv_cache, live, workspace, stream=None) -> None:
+    """live: int32 [1] that receives the number of live pages, or None."""
+    _check(_f["lsp_pages_compact"](cache, _ptr(live), _ptr(workspace),
+                                   workspace.numel() * workspace.element_size(), _stream(stream)),
+           "lsp_pages_compact")
+
+
+def lsp_prefix_attention_workspace_bytes(cache: lsp_kv_cache, nq: int, n: int, total: int) -> int:
+    return _f["lsp_prefix_attention_workspace_bytes"](cache, nq, n, total)
+
+
+def lsp_prefix_attention(cache: lsp_kv_cache, layer, q, seqs, start, out, lse=None, *, shared_len, scale,
+                         workspace, dev_error=None, stream=None) -> None:
+    """q: [total][nq][d], dense within a row (a slice of a fused q/k/v row will do); out: dense."""
+    if q.stride()[1:] != (cache.d, 1) or q.shape[2] != cache.d or out.shape != q.shape or not out.is_contiguous():
+        raise ValueError("q: [total][nq][d], dense within a row; out: the same shape, contiguous")
+    _check(_f["lsp_prefix_attention"](cache, int(layer), _ptr(q), q.stride(0), q.shape[1], _ptr(seqs),
+                                      _ptr(start), seqs.numel(), q.shape[0], int(shared_len), float(scale),
+                                      _ptr(out), _ptr(lse), _ptr(workspace),
+                                      workspace.numel() * workspace.element_size(), _ptr(dev_error),
+                                      _stream(stream)), "lsp_prefix_attention")
+
+
+def lsp_verify_probs(target_probs, draft_probs, draft_tokens, u, e, accepted_len, next_token, n_draft=None,
+                     out_tokens=None, dev_error=None, stream=None) -> None:
+    """target_probs [C][B+1][V], draft_probs [C][B][V] (or None) of one type, bfloat16 or float32; the
+    stride between their rows may exceed V."""
+    import torch
+    C, B = draft_tokens.shape
+    V = target_probs.shape[2]
+    ld = [0, 0]
+    for i, (t, rows) in enumerate(((target_probs, B + 1), (draft_probs, B))):
+        if t is None or t.numel() == 0:
+            continue
+        ld[i] = t.stride(1) if rows > 1 else t.stride(0) if C > 1 else max(V, t.stride(1))
+        if t.dtype != target_probs.dtype or t.shape != (C, rows, V) or (V > 1 and t.stride(2) != 1) or (
+                C > 1 and t.stride(0) != rows * ld[i]):
+            raise ValueError("target_probs [C][B+1][V] and draft_probs [C][B][V]: one type, rows evenly spaced")
+    if target_probs.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("target_probs: bfloat16 or float32")
+    dtype = LSP_DTYPE_BF16 if target_probs.dtype == torch.bfloat16 else LSP_DTYPE_F32
+    _check(_f["lsp_verify_probs"](_ptr(target_probs), _ptr(draft_probs), dtype, _ptr(draft_tokens),
+                                  _ptr(n_draft), _ptr(u), _ptr(e), C, B, V, ld[0], ld[1],
+                                  _ptr(accepted_len), _ptr(next_token), _ptr(out_tokens),
+                                  _ptr(dev_error), _stream(stream)), "lsp_verify_probs")
 
 
 EXPORTED = sorted(_f)
