@@ -464,6 +464,23 @@ int tmap_2d_bf16_sw128(CUtensorMap* m, const void* ptr, uint64_t inner, uint64_t
   return r == CUDA_SUCCESS ? LSP_OK : LSP_ERR_CUDA;
 }
 
+int tmap_bf16_sw128(CUtensorMap* m, const void* ptr, int rank, const uint64_t* dims, const uint64_t* stride_bytes,
+                    const uint32_t* box) {
+  auto enc = encoder();
+  if (!enc) return LSP_ERR_UNSUPPORTED;
+  cuuint64_t d[5], st[4];
+  cuuint32_t b[5], es[5] = {1, 1, 1, 1, 1};
+  for (int i = 0; i < rank; ++i) {
+    d[i] = dims[i];
+    b[i] = box[i];
+    if (i > 0) st[i - 1] = stride_bytes[i - 1];
+  }
+  const CUresult r = enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(ptr), d, st, b, es,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? LSP_OK : LSP_ERR_CUDA;
+}
+
 // [splits][M][N] view of the output (row stride ldy) for TMA stores of
 // box (cols features, tok tokens, 1 split); no swizzle.
 static int make_out_map(CUtensorMap* m, bool f32, const void* Y, int N, int M, int splits, int ldy,

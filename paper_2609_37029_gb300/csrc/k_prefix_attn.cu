@@ -8,7 +8,8 @@
 // l) in base 2, s2 = s log2(e); prefix_join_kernel adds a row's segments with
 // weights 2^(m2_seg - max m2).
 //
-// prefix_attn_fma_kernel: fp32 multiply-adds, 64 rows x 64 keys a step.
+// prefix_attn_fma_kernel: f32 storage, fp32 multiply-adds, 64 rows x 64 keys a
+// step.  bf16 storage: k_prefix_attn_tc.cu.
 #include <algorithm>
 
 #include "prefix_sched.cuh"
@@ -25,25 +26,7 @@ __device__ __forceinline__ float ex2a(float x) {
   return y;
 }
 
-// The schedule goes to the workspace for the joining kernel (CTA 0).
-__device__ __forceinline__ void publish_sched(const PrefixAttnParams& p, const PrefixSched& s, const int64_t* step_base) {
-  if (threadIdx.x == 0) *reinterpret_cast<PrefixSched*>(p.sched) = s;
-  int64_t* out = reinterpret_cast<int64_t*>(p.sched + kSchedHdrBytes);
-  for (int i = threadIdx.x; i <= p.n; i += blockDim.x) out[i] = step_base[i];
-}
-
 constexpr int kFmaRows = 64, kFmaKeys = 64, kFmaThreads = 256;
-
-template <typename T>
-__device__ __forceinline__ float4 load4(const T* p);
-template <>
-__device__ __forceinline__ float4 load4<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
-template <>
-__device__ __forceinline__ float4 load4<bf16>(const bf16* p) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
-  const __nv_bfloat162 a = *reinterpret_cast<const __nv_bfloat162*>(&u.x), b = *reinterpret_cast<const __nv_bfloat162*>(&u.y);
-  return make_float4(__low2float(a), __high2float(a), __low2float(b), __high2float(b));
-}
 
 template <int HD>
 struct FmaSmem {
@@ -52,24 +35,21 @@ struct FmaSmem {
   float p[kFmaRows][kFmaKeys + 4];
   int64_t at[kFmaKeys];                          // element offset of each key of the block, -1: none
   int64_t step_base[kPrefixMaxSeqs + 1];
+  PrefixSeq info[kPrefixMaxSeqs];
   PrefixSched sched;
 };
 
-// One segment: rows of one tile of `tokens` rows of q from token t0, head g,
-// key blocks [kb0, kb1) of the tokens [k0, k_end) of table row `tab`.  Row (i,
-// head) sees tokens below see0 + i (the shared part: k_end for all).
-template <typename T, int HD>
-__device__ void fma_segment(const PrefixAttnParams& p, FmaSmem<HD>& sm, const int32_t* tab, int g, int t0, int tokens, int k0,
-                            int k_end, int kb0, int kb1, int see0, bool causal, int64_t out_row) {
+template <int HD>
+__device__ void fma_segment(const PrefixAttnParams& p, FmaSmem<HD>& sm, const PrefixSeg& seg) {
   constexpr int kD4 = HD / 4, kCols = HD / 64;   // float4 of a row; float4 output columns of a thread
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  const int rows = tokens * p.rep;
-  const T* q = static_cast<const T*>(p.q);
+  const int rows = seg.tokens * p.rep, g = seg.head;
+  const float* q = static_cast<const float*>(p.q);
   __syncthreads();
   for (int i = tid; i < kFmaRows * kD4; i += kFmaThreads) {
     const int r = i / kD4, c = i % kD4;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (r < rows) x = load4<T>(q + (int64_t)(t0 + r / p.rep) * p.q_stride + (int64_t)(g * p.rep + r % p.rep) * HD + 4 * c);
+    if (r < rows) x = *reinterpret_cast<const float4*>(q + (int64_t)(seg.t0 + r / p.rep) * p.q_stride + (int64_t)(g * p.rep + r % p.rep) * HD + 4 * c);
     *reinterpret_cast<float4*>(&sm.q[r][4 * c]) = x;
   }
   float m[4], l[4], o[4][kCols][4];
@@ -80,20 +60,20 @@ __device__ void fma_segment(const PrefixAttnParams& p, FmaSmem<HD>& sm, const in
     m[a] = -INFINITY;
     l[a] = 0.f;
     const int r = 4 * ty + a;
-    lim[a] = r >= rows ? 0 : (causal ? min(see0 + r / p.rep, k_end) : k_end);
+    lim[a] = r >= rows ? 0 : min(seg.see0 + r / p.rep, seg.k_end);
 #pragma unroll
     for (int c = 0; c < kCols; ++c)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[a][c][e] = 0.f;
   }
-  for (int kb = kb0; kb < kb1; ++kb) {
-    const int key0 = k0 + kb * kFmaKeys;
+  for (int kb = seg.kb0; kb < seg.kb1; ++kb) {
+    const int key0 = seg.k0 + kb * kFmaKeys;
     __syncthreads();                             // q is stored; kv and p of the block before are read
     if (tid < kFmaKeys) {
       const int pos = key0 + tid;
       int64_t at = -1;
-      if (pos < k_end) {
-        const int pg = tab[pos / p.page];
+      if (pos < seg.k_end) {
+        const int pg = seg.tab[pos / p.page];
         if (pg >= 0 && pg < p.pages)
           at = (int64_t)pg * p.s_page + (int64_t)(pos % p.page) * p.s_slot + (int64_t)g * p.s_head;
         else
@@ -107,7 +87,7 @@ __device__ void fma_segment(const PrefixAttnParams& p, FmaSmem<HD>& sm, const in
         const int r = i / kD4, c = i % kD4;
         const int64_t at = sm.at[r];
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (at >= 0) x = load4<T>(reinterpret_cast<const T*>(pool) + at + 4 * c);
+        if (at >= 0) x = *reinterpret_cast<const float4*>(pool + 4 * (at + 4 * c));
         *reinterpret_cast<float4*>(&sm.kv[r][4 * c]) = x;
       }
     };
@@ -191,7 +171,7 @@ __device__ void fma_segment(const PrefixAttnParams& p, FmaSmem<HD>& sm, const in
   for (int a = 0; a < 4; ++a) {
     const int r = 4 * ty + a;
     if (r >= rows) continue;
-    const int64_t at = out_row + r;
+    const int64_t at = seg.part.row + r;
 #pragma unroll
     for (int c = 0; c < kCols; ++c)
       *reinterpret_cast<float4*>(p.part_o + at * HD + 4 * tx + 64 * c) = make_float4(o[a][c][0], o[a][c][1], o[a][c][2], o[a][c][3]);
@@ -199,7 +179,7 @@ __device__ void fma_segment(const PrefixAttnParams& p, FmaSmem<HD>& sm, const in
   }
 }
 
-template <typename T, int HD>
+template <int HD>
 __global__ void __launch_bounds__(kFmaThreads) prefix_attn_fma_kernel(const PrefixAttnParams p) {
   extern __shared__ __align__(16) uint8_t fma_raw[];
   FmaSmem<HD>& sm = *reinterpret_cast<FmaSmem<HD>*>(fma_raw);
@@ -207,37 +187,14 @@ __global__ void __launch_bounds__(kFmaThreads) prefix_attn_fma_kernel(const Pref
   griddep_launch();
   const int cta = blockIdx.x;
   if (threadIdx.x < 32) {
-    const PrefixSched s = build_sched<1, kFmaKeys>(p, sm.step_base, cta == 0);
+    const PrefixSched s = build_sched<1, kFmaKeys>(p, sm.step_base, sm.info, cta == 0);
     if (threadIdx.x == 0) sm.sched = s;
   }
   __syncthreads();
-  const PrefixSched s = sm.sched;
-  if (cta == 0) publish_sched(p, s, sm.step_base);
-  if (s.items > 0) {
-    const int32_t* tab = nullptr;
-    for (int i = 0; i < p.n && !tab; ++i) {      // the first sequence with rows stands for all
-      const PrefixSeq r = prefix_seq(p, i, false);
-      if (r.rows > 0) tab = p.table + (size_t)r.seq * p.max_pages;
-    }
-    for (int j = cta; j < s.items; j += p.grid) {
-      const int u = j % p.units, gs = j / p.units, split = gs % p.splits, g = gs / p.splits;
-      const int kb0 = split * s.per_split, kb1 = min(kb0 + s.per_split, s.blocks);
-      if (kb0 >= kb1) continue;
-      const int t0 = u * p.tok_tile, tokens = min(p.tok_tile, p.total - t0);
-      fma_segment<T, HD>(p, sm, tab, g, t0, tokens, 0, s.base, kb0, kb1, 0, false, shared_rows<1>(p, g, split, u).row);
-    }
-  }
-  int64_t x = own_begin(s, p.grid, cta);
-  const int64_t end = own_begin(s, p.grid, cta + 1);
-  while (x < end) {
-    const OwnSpot o = own_spot<1, kFmaKeys>(p, s, sm.step_base, x);
-    const PrefixSeq r = prefix_seq(p, o.i, false);
-    const int count = (int)min((int64_t)(o.blocks - o.block), end - x);
-    const int i0 = o.unit * p.tok_tile, tokens = min(p.tok_tile, r.rows - i0);
-    fma_segment<T, HD>(p, sm, p.table + (size_t)r.seq * p.max_pages, o.head, r.first + i0, tokens, s.base, r.len, o.block,
-                       o.block + count, r.len - r.rows + i0 + 1, true, own_rows<1>(p, r, o.unit, o.head, cta).row);
-    x += count;
-  }
+  if (cta == 0) publish_sched(p, sm.sched, sm.step_base);
+  PrefixSegs<1, kFmaKeys> segs(p, sm.sched, sm.step_base, sm.info, cta);
+  PrefixSeg seg;
+  while (segs.next(seg)) fma_segment<HD>(p, sm, seg);
 }
 
 // Joins the segments of one output row: a warp per (token, query head), lane l
@@ -310,23 +267,35 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixA
   if (p.lse && lane == 0) p.lse[w] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-template <typename T, int HD>
+template <typename T, int HD, int kUnitTiles, int kBlock>
+int launch_join(const PrefixAttnParams& p, cudaStream_t s) {
+  const int64_t warps = (int64_t)p.total * p.nq;
+  const unsigned grid = (unsigned)((warps * 32 + kJoinThreads - 1) / kJoinThreads);
+  return launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock>, dim3(grid), dim3(kJoinThreads), 0, s, p) == cudaSuccess
+             ? LSP_OK
+             : LSP_ERR_CUDA;
+}
+
+template <int HD>
 int launch_fma(const PrefixAttnParams& p, cudaStream_t s) {
   static bool set[8] = {};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return LSP_ERR_CUDA;
   if (dev >= 8 || !set[dev]) {
-    if (cudaFuncSetAttribute(prefix_attn_fma_kernel<T, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)sizeof(FmaSmem<HD>)) != cudaSuccess)
+    if (cudaFuncSetAttribute(prefix_attn_fma_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(FmaSmem<HD>)) !=
+        cudaSuccess)
       return LSP_ERR_CUDA;
     if (dev < 8) set[dev] = true;
   }
-  if (launch_pdl(prefix_attn_fma_kernel<T, HD>, dim3(p.grid), dim3(kFmaThreads), sizeof(FmaSmem<HD>), s, p) != cudaSuccess)
+  if (launch_pdl(prefix_attn_fma_kernel<HD>, dim3(p.grid), dim3(kFmaThreads), sizeof(FmaSmem<HD>), s, p) != cudaSuccess)
     return LSP_ERR_CUDA;
-  const int64_t warps = (int64_t)p.total * p.nq;
-  const unsigned grid = (unsigned)((warps * 32 + kJoinThreads - 1) / kJoinThreads);
-  return launch_pdl(prefix_join_kernel<T, HD, 1, kFmaKeys>, dim3(grid), dim3(kJoinThreads), 0, s, p) == cudaSuccess ? LSP_OK
-                                                                                                                  : LSP_ERR_CUDA;
+  return launch_join<float, HD, 1, kFmaKeys>(p, s);
+}
+
+template <int HD>
+int launch_tc(const PrefixAttnParams& p, cudaStream_t s) {
+  const int rc = launch_prefix_attn_tc(p, s);
+  return rc == LSP_OK ? launch_join<bf16, HD, kPrefixTcTiles, kPrefixTcKeys>(p, s) : rc;
 }
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -352,7 +321,9 @@ int choose_splits(int groups, int blocks, int grid) {
 }  // namespace
 
 size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms) {
-  const int tile = kFmaRows, unit_tiles = 1, block = kFmaKeys, per_sm = 2;
+  const bool tc = dtype == LSP_DTYPE_BF16;
+  const int tile = tc ? kPrefixTcRows : kFmaRows, unit_tiles = tc ? kPrefixTcTiles : 1;
+  const int block = tc ? kPrefixTcKeys : kFmaKeys, per_sm = tc ? 1 : 2;
   p->tok_tile = tile / p->rep;
   p->units = (p->total + p->tok_tile * unit_tiles - 1) / (p->tok_tile * unit_tiles);
   p->grid = num_sms * per_sm;
@@ -371,8 +342,8 @@ int launch_prefix_attention(PrefixAttnParams p, int dtype, void* ws, cudaStream_
   p.part_ml = reinterpret_cast<float2*>(w);
   w += align256((size_t)p.part_rows * sizeof(float2));
   p.part_o = reinterpret_cast<float*>(w);
-  if (dtype == LSP_DTYPE_BF16) return p.d == 128 ? launch_fma<bf16, 128>(p, s) : launch_fma<bf16, 64>(p, s);
-  return p.d == 128 ? launch_fma<float, 128>(p, s) : launch_fma<float, 64>(p, s);
+  if (dtype == LSP_DTYPE_BF16) return p.d == 128 ? launch_tc<128>(p, s) : launch_tc<64>(p, s);
+  return p.d == 128 ? launch_fma<128>(p, s) : launch_fma<64>(p, s);
 }
 
 }  // namespace lsp

@@ -1,0 +1,518 @@
+// Shared-prefix attention on the tcgen05 tensor cores: bf16, head dim 64 or 128
+// (mathematics: k_prefix_attn.cu, work distribution: prefix_sched.cuh).
+//
+// A persistent CTA per SM works through its segments.  Two softmax warpgroups
+// ("streams") keep two score tiles of 128 rows x 128 keys in flight, so that
+// the tensor cores multiply for one while the other takes exponentials.  A
+// segment with two row tiles gives each stream one, both over every key block;
+// a segment with one (few rows: decoding) gives both streams the same rows and
+// alternate key blocks, and each leaves its own partial result.
+//
+//   warps 0-3, 4-7  streams 0 and 1: thread = row; scores from TMEM, running
+//                   maximum and sum, weights rounded to bf16 back to TMEM
+//                   over the scores, at the end the sums to the workspace
+//   warp 8          loads: query tiles, then key and value blocks, page by page
+//                   (TMA, 128-byte swizzle), into a ring of tiles
+//   warp 9          products: S = Q K^T (both from shared memory) and O += P V
+//                   (P from TMEM, V MN-major from shared memory)
+//
+// Job j of a segment is a (stream j & 1, key block); the order of the products
+// is S(0) S(1) [PV(j) S(j + 2)]...: S(j + 2) overwrites the weights PV(j) reads,
+// and products complete in order.  The ring's tiles follow the order of first
+// use.  TMEM: scores of stream t at columns 128 t, sums at 256 + 128 t.
+//
+// The maximum is raised (and the sums rescaled) only when it would grow by more
+// than 2^8: weights stay below 2^8 and the sums, in fp32, lose nothing.
+#include <algorithm>
+
+#include "prefix_sched.cuh"
+
+namespace lsp {
+namespace {
+
+constexpr int kRows = kPrefixTcRows, kKeys = kPrefixTcKeys, kTiles = kPrefixTcTiles;
+constexpr int kThreads = 320;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kRaise = 8.0f;                   // log2 of the most a weight may exceed 1
+
+template <int HD>
+struct TcShape {
+  static constexpr int kHalves = HD / 64;                    // 128-byte column blocks of a row
+  static constexpr uint32_t kHalf = 128 * 128;               // bytes of a column block of a tile
+  static constexpr uint32_t kTile = kHalves * kHalf;
+  static constexpr int kStages = HD == 128 ? 4 : 8;
+  static constexpr uint32_t kRing = kTiles * kTile;          // offset of the ring behind the query tiles
+  static constexpr uint32_t kMisc = kRing + kStages * kTile;
+};
+
+struct TcMisc {
+  uint64_t full[8], empty[8], q_full, q_empty, s_full[2], p_full[2], o_full[2], o_free[2], drain;
+  uint32_t tmem;
+  int abort;
+  PrefixSched sched;
+  int64_t step_base[kPrefixMaxSeqs + 1];
+  PrefixSeq info[kPrefixMaxSeqs];
+};
+
+template <int HD>
+constexpr size_t tc_smem() { return TcShape<HD>::kMisc + sizeof(TcMisc) + 1024; }
+
+// Bounded wait that also gives up when another role has.
+__device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity, volatile int* abort, unsigned* err) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = global_ns();
+  for (uint32_t i = 1;; ++i) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((i & 31u) == 0) {
+      if (*abort) return false;
+      if (global_ns() - t0 > kWaitLimitNs) {
+        *abort = 1;
+        set_err(err, LSP_DEV_TIMEOUT);
+        return false;
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* map, uint32_t bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const void* map, uint32_t bar, int x, int y, int z, int w) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(
+          dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
+      : "memory");
+}
+
+// D[tmem] (+)= A[tmem] * B[smem desc], 16-bit inputs (A: two per 32-bit column).
+__device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// MN-major operand, 128-byte swizzle: 64 contiguous N elements per 128-byte row,
+// 8 K rows per 1024-byte group; `lbo` bytes between 64-element N blocks.
+__device__ __forceinline__ uint64_t sdesc_mn(uint32_t saddr, uint32_t lbo) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)((lbo >> 4) & 0x3FFFu) << 16;
+  d |= (uint64_t)(1024u >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+// kind::f16: bf16 A and B, fp32 D, M = 128, N = n; B K-major or MN-major.
+__device__ constexpr uint32_t idesc_bf16(int n, bool b_mn) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | (b_mn ? (1u << 16) : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kRows >> 4) << 24);
+}
+
+#define LSP_R4(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3])
+#define LSP_R16(v, i) LSP_R4(v, i), LSP_R4(v, i + 4), LSP_R4(v, i + 8), LSP_R4(v, i + 12)
+#define LSP_I4(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3])
+#define LSP_I16(v, i) LSP_I4(v, i), LSP_I4(v, i + 4), LSP_I4(v, i + 8), LSP_I4(v, i + 12)
+
+// 32 lanes x 128 consecutive columns (one row per thread), one wait.
+__device__ __forceinline__ void tmem_ld128(uint32_t taddr, uint32_t (&r)[128]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x128.b32 {"
+      "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
+      "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63,"
+      "%64,%65,%66,%67,%68,%69,%70,%71,%72,%73,%74,%75,%76,%77,%78,%79,%80,%81,%82,%83,%84,%85,%86,%87,%88,%89,%90,%91,%92,%93,%94,%95,"
+      "%96,%97,%98,%99,%100,%101,%102,%103,%104,%105,%106,%107,%108,%109,%110,%111,%112,%113,%114,%115,%116,%117,%118,%119,%120,%121,%122,%123,%124,%125,%126,%127"
+      "}, [%128];\n"
+      "tcgen05.wait::ld.sync.aligned;"
+      : LSP_R16(r, 0), LSP_R16(r, 16), LSP_R16(r, 32), LSP_R16(r, 48), LSP_R16(r, 64), LSP_R16(r, 80), LSP_R16(r, 96), LSP_R16(r, 112)
+      : "r"(taddr)
+      : "memory");
+}
+
+// 32 lanes x 32 consecutive columns; complete after tmem_wait_st.
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {"
+      "%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+      LSP_I16(v, 0), LSP_I16(v, 16)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ float ex2a(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// (a0, a1) * (b, b) + (c, c) and (a0, a1) + (b0, b1): two fp32 operations an instruction
+__device__ __forceinline__ float2 fma2(float a0, float a1, float b, float c) {
+  float2 d;
+  asm("{\n .reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %4};\n mov.b64 z, {%5, %5};\n"
+      " fma.rn.f32x2 x, x, y, z;\n mov.b64 {%0, %1}, x;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a0), "f"(a1), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+// How a segment's key blocks fall to the streams.
+struct Jobs {
+  bool lone;          // one row tile: the streams take alternate blocks
+  int count;          // jobs of both streams
+};
+__device__ __forceinline__ Jobs seg_jobs(const PrefixAttnParams& p, const PrefixSeg& g) {
+  const int blocks = g.kb1 - g.kb0;
+  const bool lone = g.tokens <= p.tok_tile;
+  return {lone, lone ? blocks : 2 * blocks};
+}
+__device__ __forceinline__ int stream_jobs(const Jobs& j, int stream) { return (j.count + 1 - stream) >> 1; }
+
+template <int HD>
+__device__ __forceinline__ void load_role(const PrefixAttnParams& p, const CUtensorMap* mq, const CUtensorMap* mk,
+                                          const CUtensorMap* mv, uint32_t sm, TcMisc* m, PrefixSegs<kTiles, kKeys>& segs) {
+  using Sh = TcShape<HD>;
+  const int lane = threadIdx.x & 31;
+  const int box = min(p.page, kKeys), boxes = kKeys / box;
+  uint32_t fill = 0, nseg = 0;
+  PrefixSeg g;
+  for (; segs.next(g); ++nseg) {
+    const Jobs jobs = seg_jobs(p, g);
+    if (!tc_wait(smem_u32(&m->q_empty), (nseg & 1) ^ 1, &m->abort, p.err)) return;
+    const int tiles = jobs.lone ? 1 : 2;
+    if (lane == 0) {
+      const uint32_t bar = smem_u32(&m->q_full);
+      mbar_expect_tx(bar, (uint32_t)(tiles * Sh::kHalves * p.tok_tile * p.rep * 128));
+      for (int t = 0; t < tiles; ++t)
+        for (int h = 0; h < Sh::kHalves; ++h)
+          tma_load_3d(sm + t * Sh::kTile + h * Sh::kHalf, mq, bar, 64 * h, g.head * p.rep, g.t0 + t * p.tok_tile);
+    }
+    // lane l loads page l of a block; a page past the keys or outside the pool reads as zeros
+    auto entry = [&](int kb) {
+      const int pos = g.k0 + kb * kKeys + lane * box;
+      int pg = p.pages;
+      if (lane < boxes && kb < g.kb1 && pos < g.k_end) {
+        pg = __ldg(g.tab + pos / p.page);
+        if (pg < 0 || pg >= p.pages) {
+          set_err(p.err, LSP_DEV_BAD_SEQ);
+          pg = p.pages;
+        }
+      }
+      return pg;
+    };
+    auto load = [&](const CUtensorMap* map, int kb, int pg) {
+      const uint32_t st = fill % Sh::kStages, bar = smem_u32(&m->full[st]);
+      if (!tc_wait(smem_u32(&m->empty[st]), ((fill / Sh::kStages) & 1) ^ 1, &m->abort, p.err)) return false;
+      if (lane == 0) mbar_expect_tx(bar, Sh::kTile);
+      __syncwarp();
+      if (lane < boxes) {
+        const uint32_t dst = sm + Sh::kRing + st * Sh::kTile + (uint32_t)(lane * box) * 128u;
+        const int slot = (g.k0 + kb * kKeys + lane * box) % p.page;
+        for (int h = 0; h < Sh::kHalves; ++h) tma_load_4d(dst + h * Sh::kHalf, map, bar, 64 * h, slot, g.head, pg);
+      }
+      ++fill;
+      return true;
+    };
+    // first uses: keys lead values by one job (two streams' worth where both take every block)
+    const int lead = jobs.lone ? 2 : 1;
+    int ahead[3] = {entry(g.kb0), entry(g.kb0 + 1), 0};
+    const int blocks = g.kb1 - g.kb0;
+    for (int i = 0; i < lead && i < blocks; ++i)
+      if (!load(mk, g.kb0 + i, ahead[i])) return;
+    for (int i = 0; i < blocks; ++i) {
+      ahead[2] = entry(g.kb0 + i + 2);
+      if (!load(mv, g.kb0 + i, ahead[0])) return;
+      if (i + lead < blocks && !load(mk, g.kb0 + i + lead, ahead[lead])) return;
+      ahead[0] = ahead[1];
+      ahead[1] = ahead[2];
+    }
+  }
+}
+
+template <int HD>
+__device__ __forceinline__ void mma_role(const PrefixAttnParams& p, uint32_t sm, uint8_t* smp, uint32_t tmem, TcMisc* m,
+                                         PrefixSegs<kTiles, kKeys>& segs) {
+  using Sh = TcShape<HD>;
+  const int lane = threadIdx.x & 31;
+  constexpr uint32_t is = idesc_bf16(kKeys, false), io = idesc_bf16(HD, true);
+  uint32_t use = 0, nseg = 0, np[2] = {0, 0}, no[2] = {0, 0};
+  PrefixSeg g;
+  for (; segs.next(g); ++nseg) {
+    const Jobs jobs = seg_jobs(p, g);
+    if (!tc_wait(smem_u32(&m->q_full), nseg & 1, &m->abort, p.err)) return;
+    uint32_t kst = 0, vst = 0;
+    auto take = [&](uint32_t* st) {
+      *st = use % Sh::kStages;
+      const bool ok = tc_wait(smem_u32(&m->full[*st]), (use / Sh::kStages) & 1, &m->abort, p.err);
+      ++use;
+      return ok;
+    };
+    auto scores = [&](int j) {
+      const int t = j & 1;
+      if ((jobs.lone || t == 0) && !take(&kst)) return false;
+      if (lane == 0) {
+        tc_fence_after();
+        const uint32_t q = sm + (jobs.lone ? 0u : (uint32_t)t * Sh::kTile), k = sm + Sh::kRing + kst * Sh::kTile;
+#pragma unroll
+        for (int s = 0; s < HD / 16; ++s) {
+          const uint32_t at = (uint32_t)(s >> 2) * Sh::kHalf + (uint32_t)(s & 3) * 32u;
+          umma_f16(tmem + 128u * t, sdesc_sw128(q + at), sdesc_sw128(k + at), is, s > 0 ? 1u : 0u);
+        }
+        umma_commit(smem_u32(&m->s_full[t]));
+        if (jobs.lone || t == 1) umma_commit(smem_u32(&m->empty[kst]));
+        if (j == jobs.count - 1) umma_commit(smem_u32(&m->q_empty));
+      }
+      __syncwarp();
+      return true;
+    };
+    for (int j = 0; j < 2 && j < jobs.count; ++j)
+      if (!scores(j)) return;
+    for (int j = 0; j < jobs.count; ++j) {
+      const int t = j & 1, kb = g.kb0 + (jobs.lone ? j : j >> 1);
+      if (jobs.lone || t == 0) {
+        if (!take(&vst)) return;
+        // slots of a page past the last key hold anything: their weights are 0, and 0 x V must be 0
+        const int valid = g.k_end - (g.k0 + kb * kKeys);
+        if (valid < kKeys) {
+          const int upto = min(kKeys, (valid + p.page - 1) / p.page * p.page);
+          uint8_t* v = smp + Sh::kRing + vst * Sh::kTile;
+          for (int i = valid * 8 + lane; i < upto * 8; i += 32)
+            for (int h = 0; h < Sh::kHalves; ++h) *reinterpret_cast<uint4*>(v + h * Sh::kHalf + i * 16) = make_uint4(0, 0, 0, 0);
+          fence_proxy_async_smem();
+          __syncwarp();
+        }
+      }
+      if (j < 2) {                               // the stream's sums of the segment before are read
+        if (!tc_wait(smem_u32(&m->o_free[t]), (no[t] & 1) ^ 1, &m->abort, p.err)) return;
+        ++no[t];
+      }
+      if (!tc_wait(smem_u32(&m->p_full[t]), np[t] & 1, &m->abort, p.err)) return;
+      ++np[t];
+      if (lane == 0) {
+        tc_fence_after();
+        const uint32_t v = sm + Sh::kRing + vst * Sh::kTile;
+#pragma unroll
+        for (int s = 0; s < kKeys / 16; ++s)
+          umma_f16_ts(tmem + 256u + 128u * t, tmem + 128u * t + 8u * s, sdesc_mn(v + 2048u * s, Sh::kHalf), io,
+                      (j >= 2 || s > 0) ? 1u : 0u);
+        if (jobs.lone || t == 1) umma_commit(smem_u32(&m->empty[vst]));
+        if (j >= jobs.count - 2) umma_commit(smem_u32(&m->o_full[t]));
+      }
+      __syncwarp();
+      if (j + 2 < jobs.count && !scores(j + 2)) return;
+    }
+  }
+}
+
+template <int HD>
+__device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, uint32_t tmem, TcMisc* m,
+                                             PrefixSegs<kTiles, kKeys>& segs) {
+  const int lane = threadIdx.x & 31, quad = (threadIdx.x >> 5) & 3, row = quad * 32 + lane;
+  const uint32_t ts = tmem + ((uint32_t)(quad * 32) << 16) + 128u * t, to = ts + 256u;
+  const int tok = row / p.rep;
+  const float sl = p.scale * kLog2e;
+  uint32_t ns = 0, no = 0;
+  PrefixSeg g;
+  while (segs.next(g)) {
+    const Jobs jobs = seg_jobs(p, g);
+    const int mine = stream_jobs(jobs, t), i = (jobs.lone ? 0 : t * p.tok_tile) + tok;
+    const bool valid = tok < p.tok_tile && i < g.tokens;
+    const int lim = valid ? min(g.see0 + i, g.k_end) - g.k0 : kKeys * g.kb1;   // keys this row sees, from k0 on
+    float mx = -INFINITY, sum = 0.f;             // maximum of the raw scores, sum of the weights
+    for (int n = 0; n < mine; ++n) {
+      const int kb = g.kb0 + (jobs.lone ? 2 * n + t : n), left = lim - kb * kKeys;
+      if (!tc_wait(smem_u32(&m->s_full[t]), ns & 1, &m->abort, p.err)) return;
+      ++ns;
+      tc_fence_after();
+      uint32_t r[128];
+      tmem_ld128(ts, r);
+      if (!__all_sync(0xffffffffu, left >= kKeys)) {
+#pragma unroll
+        for (int c = 0; c < 128; ++c)
+          if (c >= left) r[c] = 0xff800000u;     // -inf
+      }
+      float b = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < 128; c += 4)
+        b = fmaxf(fmaxf(fmaxf(b, __uint_as_float(r[c])), fmaxf(__uint_as_float(r[c + 1]), __uint_as_float(r[c + 2]))),
+                  __uint_as_float(r[c + 3]));
+      if (n == 0) {
+        mx = b;
+      } else {
+        const bool raise = (b - mx) * sl > kRaise || (mx == -INFINITY && b > -INFINITY);
+        if (__any_sync(0xffffffffu, raise)) {
+          // PV of the job before is complete: its product was issued before this score's
+          const float keep = !raise || mx == -INFINITY ? 1.f : ex2a((mx - b) * sl);
+#pragma unroll 1
+          for (int c = 0; c < HD; c += 32) {
+            float o[32];
+            tmem_ld32(to + c, o);
+            uint32_t w[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(o[e] * keep);
+            tmem_st32(to + c, w);
+          }
+          sum *= keep;
+          if (raise) mx = b;
+        }
+      }
+      const float base = mx == -INFINITY ? 0.f : -mx * sl;
+      float2 acc = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t w[32];
+#pragma unroll
+        for (int c = 0; c < 64; c += 2) {
+          const float2 x = fma2(__uint_as_float(r[64 * h + c]), __uint_as_float(r[64 * h + c + 1]), sl, base);
+          const float2 e = make_float2(ex2a(x.x), ex2a(x.y));
+          acc = add2(acc, e);
+          w[c >> 1] = pack_bf16(e.x, e.y);
+        }
+        tmem_st32(ts + 32 * h, w);
+      }
+      sum += acc.x + acc.y;
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&m->p_full[t]));
+    }
+    const int64_t at = g.part.row + (t ? g.part.second : 0) + row;
+    if (mine > 0) {
+      if (!tc_wait(smem_u32(&m->o_full[t]), no & 1, &m->abort, p.err)) return;
+      ++no;
+      tc_fence_after();
+#pragma unroll 1
+      for (int c = 0; c < HD; c += 32) {
+        float o[32];
+        tmem_ld32(to + c, o);
+        if (c + 32 == HD) {                      // the sums are in registers: the next segment may start
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&m->o_free[t]));
+        }
+        if (valid) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            *reinterpret_cast<float4*>(p.part_o + at * HD + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        }
+      }
+    }
+    if (valid) p.part_ml[at] = make_float2(mx == -INFINITY ? mx : mx * sl, sum);
+  }
+}
+
+template <int HD>
+__global__ void __launch_bounds__(kThreads, 1)
+    prefix_attn_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+                          const __grid_constant__ CUtensorMap mv, const PrefixAttnParams p) {
+  extern __shared__ uint8_t tc_raw[];
+  uint8_t* smp = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tc_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  TcMisc* m = reinterpret_cast<TcMisc*>(smp + TcShape<HD>::kMisc);
+  const uint32_t sm = smem_u32(smp);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x;
+  if (threadIdx.x == 256) {
+    for (int i = 0; i < 8; ++i) {
+      mbar_init(smem_u32(&m->full[i]), 1);
+      mbar_init(smem_u32(&m->empty[i]), 1);
+    }
+    mbar_init(smem_u32(&m->q_full), 1);
+    mbar_init(smem_u32(&m->q_empty), 1);
+    mbar_init(smem_u32(&m->drain), 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&m->s_full[i]), 1);
+      mbar_init(smem_u32(&m->p_full[i]), 4);
+      mbar_init(smem_u32(&m->o_full[i]), 1);
+      mbar_init(smem_u32(&m->o_free[i]), 4);
+    }
+    m->abort = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(&mq);
+    tma_prefetch_desc(&mk);
+    tma_prefetch_desc(&mv);
+  }
+  if (warp == 9) tmem_alloc(smem_u32(&m->tmem), 512);
+  griddep_wait();
+  griddep_launch();
+  if (warp == 0) {
+    const PrefixSched s = build_sched<kTiles, kKeys>(p, m->step_base, m->info, cta == 0);
+    if (lane == 0) m->sched = s;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = m->tmem;
+  PrefixSegs<kTiles, kKeys> segs(p, m->sched, m->step_base, m->info, cta);
+  if (warp == 8)
+    load_role<HD>(p, &mq, &mk, &mv, sm, m, segs);
+  else if (warp == 9)
+    mma_role<HD>(p, sm, smp, tmem, m, segs);
+  else
+    softmax_role<HD>(p, warp >> 2, tmem, m, segs);
+  if (cta == 0) publish_sched(p, m->sched, m->step_base);
+  tc_fence_before();
+  __syncthreads();
+  // Every load has been waited for by its product, unless a wait gave up: then
+  // loads may still be landing, and the CTA stays for them (bounded).
+  if (m->abort && threadIdx.x == 0) {
+    const uint64_t t0 = global_ns();
+    while (global_ns() - t0 < 1000000ull) {}
+  }
+  if (warp == 9) {
+    tc_fence_after();
+    if (lane == 0) {
+      umma_commit(smem_u32(&m->drain));
+      mbar_wait(smem_u32(&m->drain), 0, p.err);
+    }
+    __syncwarp();
+    tmem_dealloc(tmem, 512);
+  }
+  __syncthreads();
+}
+
+template <int HD>
+int launch(const PrefixAttnParams& p, cudaStream_t s) {
+  static bool set[8] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return LSP_ERR_CUDA;
+  if (dev >= 8 || !set[dev]) {
+    if (cudaFuncSetAttribute(prefix_attn_tc_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc_smem<HD>()) != cudaSuccess)
+      return LSP_ERR_CUDA;
+    if (dev < 8) set[dev] = true;
+  }
+  CUtensorMap mq, mk, mv;
+  int rc;
+  {
+    const uint64_t dims[3] = {HD, (uint64_t)p.nq, (uint64_t)p.total}, st[2] = {HD * 2, (uint64_t)p.q_stride * 2};
+    const uint32_t box[3] = {64, (uint32_t)p.rep, (uint32_t)p.tok_tile};
+    if ((rc = tmap_bf16_sw128(&mq, p.q, 3, dims, st, box)) != LSP_OK) return rc;
+  }
+  const uint64_t dims[4] = {HD, (uint64_t)p.page, (uint64_t)p.nkv, (uint64_t)p.pages};
+  const uint64_t st[3] = {(uint64_t)p.s_slot * 2, (uint64_t)p.s_head * 2, (uint64_t)p.s_page * 2};
+  const uint32_t box[4] = {64, (uint32_t)std::min(p.page, kKeys), 1, 1};
+  if ((rc = tmap_bf16_sw128(&mk, p.k, 4, dims, st, box)) != LSP_OK || (rc = tmap_bf16_sw128(&mv, p.v, 4, dims, st, box)) != LSP_OK)
+    return rc;
+  return launch_pdl(prefix_attn_tc_kernel<HD>, dim3(p.grid), dim3(kThreads), tc_smem<HD>(), s, mq, mk, mv, p) == cudaSuccess
+             ? LSP_OK
+             : LSP_ERR_CUDA;
+}
+
+}  // namespace
+
+int launch_prefix_attn_tc(const PrefixAttnParams& p, cudaStream_t s) { return p.d == 128 ? launch<128>(p, s) : launch<64>(p, s); }
+
+}  // namespace lsp

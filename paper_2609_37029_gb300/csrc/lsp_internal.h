@@ -188,6 +188,9 @@ int launch_attention_tc(const AttnParams& p, const AttnTcPlan& pl, cudaStream_t 
 // row_bytes), box (box_inner <= 64, box_rows <= 256).
 int tmap_2d_bf16_sw128(CUtensorMap* m, const void* ptr, uint64_t inner, uint64_t rows, uint64_t row_bytes,
                        uint32_t box_inner, uint32_t box_rows);
+// The same for rank 2..5: dims and box innermost first, stride_bytes of dims 1.. (multiples of 16).
+int tmap_bf16_sw128(CUtensorMap* m, const void* ptr, int rank, const uint64_t* dims, const uint64_t* stride_bytes,
+                    const uint32_t* box);
 
 // ------------------------------------------------------------------ prefill
 struct PrefillParams {
@@ -317,6 +320,9 @@ constexpr int kPrefixMaxSeqs = 1024;
 constexpr int kPrefixMaxRep = 64;
 // Fills the plan fields; returns the workspace bytes.
 size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms);
+// bf16 on the tensor cores; the joining kernel is the caller's.
+int launch_prefix_attn_tc(const PrefixAttnParams& p, cudaStream_t s);
+constexpr int kPrefixTcRows = 128, kPrefixTcKeys = 128, kPrefixTcTiles = 2;   // tile rows, key block, tiles of a unit
 // ws: prefix_attn_plan's bytes, 256-byte aligned.
 int launch_prefix_attention(PrefixAttnParams p, int dtype, void* ws, cudaStream_t s);
 

@@ -78,16 +78,20 @@ __device__ __forceinline__ int own_units(const PrefixAttnParams& p, const Prefix
   return cdiv(r.rows, unit_tiles * p.tok_tile);
 }
 
-// Built by one warp of every CTA; step_base: [n + 1] in shared memory.
+// Built by one warp of every CTA; step_base [n + 1], info [n] in shared memory.
 template <int kUnitTiles, int kBlock>
-__device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, int64_t* step_base, bool report) {
+__device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, int64_t* step_base, PrefixSeq* info, bool report) {
   const int lane = threadIdx.x & 31;
   PrefixSched s;
   int base = p.shared_len;
+  bool any = false;
   for (int i = lane; i < p.n; i += 32) {
     const PrefixSeq r = prefix_seq(p, i, report);
+    info[i] = r;
     if (r.rows > 0) base = min(base, r.len - r.rows);
+    any |= r.rows > 0;
   }
+  if (!__any_sync(0xffffffffu, any)) base = 0;   // rows of no sequence have nothing to see
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) base = min(base, __shfl_xor_sync(0xffffffffu, base, o));
   s.base = max(base, 0) / p.page * p.page;
@@ -99,7 +103,7 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
     const int i = i0 + lane;
     int64_t mine = 0;
     if (i < p.n) {
-      const PrefixSeq r = prefix_seq(p, i, false);
+      const PrefixSeq r = info[i];               // this lane's own store
       for (int u = 0, units = own_units(p, r, kUnitTiles); u < units; ++u)
         mine += own_blocks<kUnitTiles, kBlock>(p, r, s.base, u);
       mine *= p.nkv;
@@ -129,34 +133,6 @@ __device__ __forceinline__ int64_t own_begin(const PrefixSched& s, int grid, int
   return even * c / grid + (more > 0 && c > more ? (int64_t)(c - more) * s.per_split : 0);
 }
 
-// Where a step of the own line lies.
-struct OwnSpot {
-  int i, unit, head, blocks, block;
-};
-template <int kUnitTiles, int kBlock>
-__device__ __forceinline__ OwnSpot own_spot(const PrefixAttnParams& p, const PrefixSched& s, const int64_t* step_base,
-                                            int64_t step) {
-  int lo = 0, hi = p.n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (step_base[mid] <= step) lo = mid; else hi = mid;
-  }
-  const PrefixSeq r = prefix_seq(p, lo, false);
-  const int units = own_units(p, r, kUnitTiles);
-  int64_t rel = step - step_base[lo];
-  OwnSpot o;
-  o.i = lo;
-  o.unit = 0;
-  o.blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, 0);
-  while (rel >= (int64_t)o.blocks * p.nkv && o.unit + 1 < units) {
-    rel -= (int64_t)o.blocks * p.nkv;
-    o.blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, ++o.unit);
-  }
-  o.head = (int)(rel / max(o.blocks, 1));
-  o.block = (int)(rel - (int64_t)o.head * o.blocks);
-  return o;
-}
-
 // Workspace rows: the first row of a segment, and where its second tile (or the
 // second stream of a unit with one tile) starts.
 struct PartRows {
@@ -174,6 +150,93 @@ __device__ __forceinline__ PartRows own_rows(const PrefixAttnParams& p, const Pr
   const int64_t before = (int64_t)p.nkv * (r.first + t0) + (int64_t)head * tokens;
   const int64_t own0 = (int64_t)p.nkv * p.splits * p.units * kUnitTiles * p.tok_tile * p.rep;
   return {own0 + kUnitTiles * (before * p.rep + (int64_t)cta * p.tok_tile * p.rep), min(tokens, p.tok_tile) * p.rep};
+}
+
+// What a CTA works on at a time: the rows of a unit and a range of key blocks.
+struct PrefixSeg {
+  const int32_t* tab;   // row of the table
+  int head;             // KV head
+  int t0, tokens;       // rows of q
+  int k0, k_end;        // keys: tokens [k0, k_end) of the sequence
+  int kb0, kb1;         // blocks of them, from k0 on
+  int see0;             // token i of the unit sees tokens below min(see0 + i, k_end)
+  PartRows part;
+};
+
+// The segments of a CTA in order: its shared items, then its piece of the own line.
+template <int kUnitTiles, int kBlock>
+struct PrefixSegs {
+  const PrefixAttnParams& p;
+  const PrefixSched s;
+  const int64_t* step_base;
+  const PrefixSeq* info;
+  const int cta;
+  const int32_t* shared_tab;
+  int j;
+  int64_t x, end;
+
+  __device__ PrefixSegs(const PrefixAttnParams& p_, const PrefixSched& s_, const int64_t* base, const PrefixSeq* info_, int cta_)
+      : p(p_), s(s_), step_base(base), info(info_), cta(cta_), shared_tab(nullptr), j(cta_) {
+    x = own_begin(s, p.grid, cta);
+    end = own_begin(s, p.grid, cta + 1);
+    if (s.items > 0) {                           // base > 0: some sequence has rows
+      int i = 0;
+      while (i + 1 < p.n && info[i].rows == 0) ++i;
+      shared_tab = p.table + (size_t)info[i].seq * p.max_pages;
+    }
+  }
+
+  __device__ bool next(PrefixSeg& g) {
+    for (; j < s.items; j += p.grid) {
+      const int u = j % p.units, gs = j / p.units, split = gs % p.splits;
+      g.kb0 = split * s.per_split;
+      g.kb1 = min(g.kb0 + s.per_split, s.blocks);
+      if (g.kb0 >= g.kb1) continue;
+      g.tab = shared_tab;
+      g.head = gs / p.splits;
+      g.t0 = u * kUnitTiles * p.tok_tile;
+      g.tokens = min(kUnitTiles * p.tok_tile, p.total - g.t0);
+      g.k0 = 0;
+      g.k_end = g.see0 = s.base;
+      g.part = shared_rows<kUnitTiles>(p, g.head, split, u);
+      j += p.grid;
+      return true;
+    }
+    if (x >= end) return false;
+    int lo = 0, hi = p.n;                        // the last sequence that starts at or before step x
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (step_base[mid] <= x) lo = mid; else hi = mid;
+    }
+    const PrefixSeq r = info[lo];
+    const int units = own_units(p, r, kUnitTiles);
+    int64_t rel = x - step_base[lo];
+    int u = 0, blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, 0);
+    while (rel >= (int64_t)blocks * p.nkv && u + 1 < units) {
+      rel -= (int64_t)blocks * p.nkv;
+      blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, ++u);
+    }
+    g.head = (int)(rel / blocks);
+    g.kb0 = (int)(rel - (int64_t)g.head * blocks);
+    g.kb1 = (int)min((int64_t)blocks, g.kb0 + (end - x));
+    g.tab = p.table + (size_t)r.seq * p.max_pages;
+    const int i0 = u * kUnitTiles * p.tok_tile;
+    g.t0 = r.first + i0;
+    g.tokens = min(kUnitTiles * p.tok_tile, r.rows - i0);
+    g.k0 = s.base;
+    g.k_end = r.len;
+    g.see0 = r.len - r.rows + i0 + 1;
+    g.part = own_rows<kUnitTiles>(p, r, u, g.head, cta);
+    x += g.kb1 - g.kb0;
+    return true;
+  }
+};
+
+// The schedule goes to the workspace for the joining kernel (CTA 0).
+__device__ __forceinline__ void publish_sched(const PrefixAttnParams& p, const PrefixSched& s, const int64_t* step_base) {
+  if (threadIdx.x == 0) *reinterpret_cast<PrefixSched*>(p.sched) = s;
+  int64_t* out = reinterpret_cast<int64_t*>(p.sched + kSchedHdrBytes);
+  for (int i = threadIdx.x; i <= p.n; i += blockDim.x) out[i] = step_base[i];
 }
 
 }  // namespace lsp
