@@ -144,7 +144,9 @@ def _ptr(x):
 def _stream(stream):
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        if not torch.cuda.is_initialized():
+            return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())   # the same, without a Stream object
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -352,7 +354,7 @@ def lsp_pages_fork(cache: lsp_kv_cache, src, dst, dev_error=None, stream=None) -
 
 def lsp_pages_reserve(cache: lsp_kv_cache, seqs, add, workspace, dev_error=None, stream=None) -> None:
     _check(_f["lsp_pages_reserve"](cache, _ptr(seqs), _ptr(add), seqs.numel(), _ptr(workspace),
-                                   workspace.numel() * workspace.element_size(), _ptr(dev_error),
+                                   workspace.nbytes, _ptr(dev_error),
                                    _stream(stream)), "lsp_pages_reserve")
 
 
@@ -373,7 +375,7 @@ def lsp_pages_trim(cache: lsp_kv_cache, seqs, new_len, dev_error=None, stream=No
 def lsp_pages_compact(cache: lsp_kv_cache, live, workspace, stream=None) -> None:
     """live: int32 [1] that receives the number of live pages, or None."""
     _check(_f["lsp_pages_compact"](cache, _ptr(live), _ptr(workspace),
-                                   workspace.numel() * workspace.element_size(), _stream(stream)),
+                                   workspace.nbytes, _stream(stream)),
            "lsp_pages_compact")
 
 
@@ -389,7 +391,7 @@ def lsp_prefix_attention(cache: lsp_kv_cache, layer, q, seqs, start, out, lse=No
     _check(_f["lsp_prefix_attention"](cache, int(layer), _ptr(q), q.stride(0), q.shape[1], _ptr(seqs),
                                       _ptr(start), seqs.numel(), q.shape[0], int(shared_len), float(scale),
                                       _ptr(out), _ptr(lse), _ptr(workspace),
-                                      workspace.numel() * workspace.element_size(), _ptr(dev_error),
+                                      workspace.nbytes, _ptr(dev_error),
                                       _stream(stream)), "lsp_prefix_attention")
 
 
