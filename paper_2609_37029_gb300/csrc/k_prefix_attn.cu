@@ -11,6 +11,7 @@
 // prefix_attn_fma_kernel: f32 storage, fp32 multiply-adds, 64 rows x 64 keys a
 // step.  bf16 storage: k_prefix_attn_tc.cu.
 #include <algorithm>
+#include <cstdint>
 
 #include "prefix_sched.cuh"
 
@@ -191,89 +192,158 @@ __global__ void __launch_bounds__(kFmaThreads) prefix_attn_fma_kernel(const Pref
     if (threadIdx.x == 0) sm.sched = s;
   }
   __syncthreads();
-  if (cta == 0) publish_sched(p, sm.sched, sm.step_base);
+  if (cta == 0) publish_sched(p, sm.sched, sm.step_base, sm.info);
   PrefixSegs<1, kFmaKeys> segs(p, sm.sched, sm.step_base, sm.info, cta);
   PrefixSeg seg;
   while (segs.next(seg)) fma_segment<HD>(p, sm, seg);
 }
 
-// Joins the segments of one output row: a warp per (token, query head), lane l
-// holds dims [l HD/32, (l + 1) HD/32).
-constexpr int kJoinThreads = 256;
-template <typename T, int HD, int kUnitTiles, int kBlock>
+// Joins the segments of an output row (token, query head): kWarps warps a row
+// take its segments in turn, lane l holds dims [l HD/32, (l + 1) HD/32).  The
+// running maxima come first, one segment a lane, so that the sums themselves
+// are independent loads.  Four warps where the rows alone would leave most of
+// the GPU idle (few rows have many segments), one where they fill it.
+constexpr int kJoinThreads = 128;
+template <typename T, int HD, int kUnitTiles, int kBlock, int kWarps>
 __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixAttnParams p) {
-  constexpr int kVec = HD / 32;
+  constexpr int kVec = HD / 32, kRowsCta = kJoinThreads / 32 / kWarps, kAhead = 8;
+  __shared__ float s_o[kWarps > 1 ? kJoinThreads / 32 : 1][HD], s_l[kJoinThreads / 32];
   griddep_wait();
   griddep_launch();
-  const int lane = threadIdx.x & 31;
-  const int64_t w = ((int64_t)blockIdx.x * kJoinThreads + threadIdx.x) >> 5;
-  if (w >= (int64_t)p.total * p.nq) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % kWarps;
+  const int64_t w = (int64_t)blockIdx.x * kRowsCta + warp / kWarps;
+  if (w >= (int64_t)p.total * p.nq) return;      // kWarps > 1: one row a CTA, all of it leaves
   const int t = (int)(w / p.nq), h = (int)(w % p.nq), g = h / p.rep, hr = h % p.rep;
-  const PrefixSched s = *reinterpret_cast<const PrefixSched*>(p.sched);
-  const int64_t* step_base = reinterpret_cast<const int64_t*>(p.sched + kSchedHdrBytes);
-  float m = -INFINITY, l = 0.f, o[kVec];
-#pragma unroll
-  for (int e = 0; e < kVec; ++e) o[e] = 0.f;
-  auto add = [&](int64_t row) {
-    const float2 ml = p.part_ml[row];
-    if (ml.x == -INFINITY) return;               // the segment saw nothing of this row
-    const float nm = fmaxf(m, ml.x), a = ex2a(m - nm), b = ex2a(ml.x - nm);
-    l = l * a + ml.y * b;
-    const float* x = p.part_o + row * HD + lane * kVec;
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) o[e] = o[e] * a + x[e] * b;
-    m = nm;
-  };
-  int lo = 0, hi = p.n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (p.start[mid] <= t) lo = mid; else hi = mid;
-  }
-  const PrefixSeq r = prefix_seq(p, lo, false);
+  const SchedView v = sched_view(p);
+  const PrefixSched s = *v.s;
+  int lo = -1;                                   // the last sequence that starts at or before t
+  for (int i0 = 0; i0 < p.n; i0 += 32)
+    lo += __popc(__ballot_sync(0xffffffffu, i0 + lane < p.n && p.start[i0 + lane] <= t));
+  PrefixSeq r = {-1, 0, 0, 0};
+  if (lo >= 0) r = v.info[lo];
+  // segments: the shared part's ranges, then the CTAs of the own item; two of each where a unit has one tile
+  int shared = 0, shared_f = 1, own = 0, own_f = 1, c0 = 0;
+  int64_t shared_row = 0, shared_step = 0, first = 0, last = 0;
+  int shared_second = 0, unit = 0, own_at = 0;
   if (t >= r.first && t < r.first + r.rows) {
     if (s.items > 0) {
-      const int tile = t / p.tok_tile, unit = tile / kUnitTiles, sub = tile % kUnitTiles;
-      const bool lone = kUnitTiles > 1 && (unit * kUnitTiles + 1) * p.tok_tile >= p.total;
-      for (int split = 0; split < p.splits && split * s.per_split < s.blocks; ++split) {
-        const PartRows at = shared_rows<kUnitTiles>(p, g, split, unit);
-        const int64_t row = at.row + sub * at.second + (t % p.tok_tile) * p.rep + hr;
-        add(row);
-        if (lone) add(row + at.second);
-      }
+      const int tile = t / p.tok_tile, u = tile / kUnitTiles;
+      shared_f = kUnitTiles > 1 && (u * kUnitTiles + 1) * p.tok_tile >= p.total ? 2 : 1;
+      shared = cdiv(s.blocks, s.per_split);
+      const PartRows at = shared_rows<kUnitTiles>(p, g, 0, u);
+      shared_second = at.second;
+      shared_row = at.row + (tile % kUnitTiles) * at.second + (t % p.tok_tile) * p.rep + hr;
+      shared_step = shared_rows<kUnitTiles>(p, g, 1, u).row - at.row;
     }
-    const int i = t - r.first, tile = i / p.tok_tile, unit = tile / kUnitTiles, sub = tile % kUnitTiles;
-    const bool lone = kUnitTiles > 1 && (unit * kUnitTiles + 1) * p.tok_tile >= r.rows;
-    int64_t first = step_base[lo];
+    const int i = t - r.first, tile = i / p.tok_tile;
+    unit = tile / kUnitTiles;
+    own_f = kUnitTiles > 1 && (unit * kUnitTiles + 1) * p.tok_tile >= r.rows ? 2 : 1;
+    own_at = (i % p.tok_tile) * p.rep + hr;
+    const int tokens = min(r.rows - unit * kUnitTiles * p.tok_tile, kUnitTiles * p.tok_tile);
+    own_at += (tile % kUnitTiles) * min(tokens, p.tok_tile) * p.rep;
+    first = v.step_base[lo];
     for (int u = 0; u < unit; ++u) first += (int64_t)own_blocks<kUnitTiles, kBlock>(p, r, s.base, u) * p.nkv;
     const int blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, unit);
     first += (int64_t)g * blocks;
-    int c0 = 0, c1 = p.grid;                     // the CTA that has step `first`
-    while (c1 - c0 > 1) {
-      const int mid = (c0 + c1) >> 1;
-      if (own_begin(s, p.grid, mid) <= first) c0 = mid; else c1 = mid;
+    last = first + blocks;
+    if (blocks > 0) {                            // CTAs [c0, c1): those that begin before `last`, from the one that has `first`
+      int c1 = 0;
+      c0 = -1;
+      for (int i0 = 0; i0 < p.grid; i0 += 32) {
+        const int64_t b = i0 + lane < p.grid ? v.cta_begin[i0 + lane] : INT64_MAX;
+        c0 += __popc(__ballot_sync(0xffffffffu, b <= first));
+        c1 += __popc(__ballot_sync(0xffffffffu, b < last));
+      }
+      own = c1 - c0;
     }
-    for (int c = c0; blocks > 0 && c < p.grid && own_begin(s, p.grid, c) < first + blocks; ++c) {
-      if (own_begin(s, p.grid, c + 1) <= max(first, own_begin(s, p.grid, c))) continue;   // a CTA without steps
-      const PartRows at = own_rows<kUnitTiles>(p, r, unit, g, c);
-      const int64_t row = at.row + sub * at.second + (i % p.tok_tile) * p.rep + hr;
-      add(row);
-      if (lone) add(row + at.second);
+  }
+  const int ns = shared * shared_f, all = ns + own * own_f;
+  auto row_of = [&](int q) -> int64_t {          // -1: no such segment
+    if (q >= all) return -1;
+    if (q < ns) return shared_row + (q / shared_f) * shared_step + (q % shared_f) * shared_second;
+    const int c = c0 + (q - ns) / own_f;
+    if (v.cta_begin[c + 1] <= (first > v.cta_begin[c] ? first : v.cta_begin[c])) return -1;   // a CTA without steps
+    const PartRows at = own_rows<kUnitTiles>(p, r, unit, g, c);
+    return at.row + own_at + ((q - ns) % own_f) * at.second;
+  };
+  float m = -INFINITY, l = 0.f, o[kVec];
+  for (int q = lane; q < all; q += 32) {
+    const int64_t row = row_of(q);
+    if (row >= 0) m = fmaxf(m, p.part_ml[row].x);
+  }
+  m = warp_max(m);
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) o[e] = 0.f;
+  for (int q0 = 0; q0 < all && m > -INFINITY; q0 += 32 * kWarps) {
+    const int64_t row = row_of(q0 + lane * kWarps + part);
+    float x = 0.f;
+    if (row >= 0) {
+      const float2 ml = p.part_ml[row];
+      x = ml.x == -INFINITY ? 0.f : ex2a(ml.x - m);
+      l += x * ml.y;
+    }
+    const unsigned has = __ballot_sync(0xffffffffu, x > 0.f);
+    for (unsigned left = has; left;) {
+      float y[kAhead][kVec], f[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int src = left ? __ffs(left) - 1 : 0;
+        const bool on = left != 0;
+        left &= left - 1;
+        const int64_t at = __shfl_sync(0xffffffffu, row, src);
+        f[k] = on ? __shfl_sync(0xffffffffu, x, src) : 0.f;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) y[k][e] = 0.f;
+        if (on) {
+          const float* from = p.part_o + at * HD + lane * kVec;
+          if constexpr (kVec == 4) {
+            const float4 z = *reinterpret_cast<const float4*>(from);
+            y[k][0] = z.x; y[k][1] = z.y; y[k][2] = z.z; y[k][3] = z.w;
+          } else {
+            const float2 z = *reinterpret_cast<const float2*>(from);
+            y[k][0] = z.x; y[k][1] = z.y;
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) o[e] = fmaf(y[k][e], f[k], o[e]);
+    }
+  }
+  l = warp_sum(l);
+  if constexpr (kWarps > 1) {
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) s_o[warp][lane * kVec + e] = o[e];
+    if (lane == 0) s_l[warp] = l;
+    __syncthreads();
+    if (warp > 0) return;
+    l = 0.f;
+    for (int k = 0; k < kWarps; ++k) l += s_l[k];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      o[e] = 0.f;
+      for (int k = 0; k < kWarps; ++k) o[e] += s_o[k][lane * kVec + e];
     }
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
   T* out = static_cast<T*>(p.out) + w * HD + lane * kVec;
+  if constexpr (sizeof(T) == 2 && kVec == 4)
+    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+  else
 #pragma unroll
-  for (int e = 0; e < kVec; ++e) out[e] = from_f<T>(o[e] * inv);
+    for (int e = 0; e < kVec; ++e) out[e] = from_f<T>(o[e] * inv);
   if (p.lse && lane == 0) p.lse[w] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 template <typename T, int HD, int kUnitTiles, int kBlock>
 int launch_join(const PrefixAttnParams& p, cudaStream_t s) {
-  const int64_t warps = (int64_t)p.total * p.nq;
-  const unsigned grid = (unsigned)((warps * 32 + kJoinThreads - 1) / kJoinThreads);
-  return launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock>, dim3(grid), dim3(kJoinThreads), 0, s, p) == cudaSuccess
-             ? LSP_OK
-             : LSP_ERR_CUDA;
+  const int64_t rows = (int64_t)p.total * p.nq;
+  const bool few = rows < 16 * (int64_t)p.num_sms;
+  const cudaError_t e =
+      few ? launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 4>, dim3((unsigned)rows), dim3(kJoinThreads), 0, s, p)
+          : launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(kJoinThreads), 0, s, p);
+  return e == cudaSuccess ? LSP_OK : LSP_ERR_CUDA;
 }
 
 template <int HD>
@@ -326,19 +396,20 @@ size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms) {
   const int block = tc ? kPrefixTcKeys : kFmaKeys, per_sm = tc ? 1 : 2;
   p->tok_tile = tile / p->rep;
   p->units = (p->total + p->tok_tile * unit_tiles - 1) / (p->tok_tile * unit_tiles);
+  p->num_sms = num_sms;
   p->grid = num_sms * per_sm;
   p->splits = choose_splits(p->nkv * p->units, (p->shared_len + block - 1) / block, p->grid);
   const int64_t rows = (int64_t)p->tok_tile * p->rep * unit_tiles, groups = (int64_t)p->nkv * p->units;
   p->part_rows = std::max<int64_t>(groups, kMaxTurns * p->grid) * rows + (int64_t)unit_tiles * p->nkv * p->rep * p->total +
                  p->grid * rows;
-  return align256(kSchedHdrBytes + (p->n + 1) * sizeof(int64_t)) + align256((size_t)p->part_rows * sizeof(float2)) +
+  return align256(sched_bytes(p->n, p->grid)) + align256((size_t)p->part_rows * sizeof(float2)) +
          (size_t)p->part_rows * p->d * sizeof(float);
 }
 
 int launch_prefix_attention(PrefixAttnParams p, int dtype, void* ws, cudaStream_t s) {
   char* w = static_cast<char*>(ws);
   p.sched = w;
-  w += align256(kSchedHdrBytes + (p.n + 1) * sizeof(int64_t));
+  w += align256(sched_bytes(p.n, p.grid));
   p.part_ml = reinterpret_cast<float2*>(w);
   w += align256((size_t)p.part_rows * sizeof(float2));
   p.part_o = reinterpret_cast<float*>(w);

@@ -31,7 +31,7 @@ namespace lsp {
 namespace {
 
 constexpr int kRows = kPrefixTcRows, kKeys = kPrefixTcKeys, kTiles = kPrefixTcTiles;
-constexpr int kThreads = 320;
+constexpr int kThreads = 384;                   // warps 10 and 11 only share their registers out
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRaise = 8.0f;                   // log2 of the most a weight may exceed 1
 
@@ -46,7 +46,7 @@ struct TcShape {
 };
 
 struct TcMisc {
-  uint64_t full[8], empty[8], q_full, q_empty, s_full[2], p_full[2], o_full[2], o_free[2], drain;
+  uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], o_free[2], drain;
   uint32_t tmem;
   int abort;
   PrefixSched sched;
@@ -92,25 +92,27 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void* map, uint3
       : "memory");
 }
 
-// D[tmem] (+)= A[tmem] * B[smem desc], 16-bit inputs (A: two per 32-bit column).
-__device__ __forceinline__ void umma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+// Shared-memory matrix descriptors of 128-byte swizzled tiles (8-row groups 1024
+// bytes apart).  Only the start address differs between the products of a CTA:
+// the low word is formed per product (address / 16, plus the offset between
+// 64-element blocks of an MN-major operand), the high word is a constant.
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);   // group stride, version, 128-byte swizzle
+__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr, uint32_t lbo) { return ((saddr & 0x3FFFFu) >> 4) | ((lbo >> 4) << 16); }
+
+// D[tmem] (+)= A[smem] B[smem] and A[tmem] B[smem], bf16 (A in TMEM: two per 32-bit column).
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      "{\n .reg .pred p;\n .reg .b64 x, y;\n setp.ne.b32 p, %4, 0;\n mov.b64 x, {%1, %5};\n mov.b64 y, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n}" ::"r"(d),
+      "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
       : "memory");
 }
-
-// MN-major operand, 128-byte swizzle: 64 contiguous N elements per 128-byte row,
-// 8 K rows per 1024-byte group; `lbo` bytes between 64-element N blocks.
-__device__ __forceinline__ uint64_t sdesc_mn(uint32_t saddr, uint32_t lbo) {
-  uint64_t d = 0;
-  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)((lbo >> 4) & 0x3FFFu) << 16;
-  d |= (uint64_t)(1024u >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 y;\n setp.ne.b32 p, %4, 0;\n mov.b64 y, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n}" ::"r"(d),
+      "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi)
+      : "memory");
 }
 
 // kind::f16: bf16 A and B, fp32 D, M = 128, N = n; B K-major or MN-major.
@@ -120,22 +122,25 @@ __device__ constexpr uint32_t idesc_bf16(int n, bool b_mn) {
 
 #define LSP_R4(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3])
 #define LSP_R16(v, i) LSP_R4(v, i), LSP_R4(v, i + 4), LSP_R4(v, i + 8), LSP_R4(v, i + 12)
+#define LSP_T4(v, i) "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3])
+#define LSP_T16(v, i) LSP_T4(v, i), LSP_T4(v, i + 4), LSP_T4(v, i + 8), LSP_T4(v, i + 12)
 #define LSP_I4(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3])
 #define LSP_I16(v, i) LSP_I4(v, i), LSP_I4(v, i + 4), LSP_I4(v, i + 8), LSP_I4(v, i + 12)
 
-// 32 lanes x 128 consecutive columns (one row per thread), one wait.
-__device__ __forceinline__ void tmem_ld128(uint32_t taddr, uint32_t (&r)[128]) {
+// 32 lanes x 64 consecutive columns (one row per thread): the values may be used
+// after tmem_wait_ld64 of the same registers, which ties them to the wait.
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t* r) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x128.b32 {"
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
       "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,"
-      "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63,"
-      "%64,%65,%66,%67,%68,%69,%70,%71,%72,%73,%74,%75,%76,%77,%78,%79,%80,%81,%82,%83,%84,%85,%86,%87,%88,%89,%90,%91,%92,%93,%94,%95,"
-      "%96,%97,%98,%99,%100,%101,%102,%103,%104,%105,%106,%107,%108,%109,%110,%111,%112,%113,%114,%115,%116,%117,%118,%119,%120,%121,%122,%123,%124,%125,%126,%127"
-      "}, [%128];\n"
-      "tcgen05.wait::ld.sync.aligned;"
-      : LSP_R16(r, 0), LSP_R16(r, 16), LSP_R16(r, 32), LSP_R16(r, 48), LSP_R16(r, 64), LSP_R16(r, 80), LSP_R16(r, 96), LSP_R16(r, 112)
+      "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63"
+      "}, [%64];"
+      : LSP_R16(r, 0), LSP_R16(r, 16), LSP_R16(r, 32), LSP_R16(r, 48)
       : "r"(taddr)
       : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld64(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : LSP_T16(r, 0), LSP_T16(r, 16), LSP_T16(r, 32), LSP_T16(r, 48)::"memory");
 }
 
 // 32 lanes x 32 consecutive columns; complete after tmem_wait_st.
@@ -144,6 +149,12 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* v) {
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {"
       "%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
       LSP_I16(v, 0), LSP_I16(v, 16)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      LSP_I16(v, 0)
       : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -171,6 +182,23 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   return d;
 }
 
+// Maximum of 64 scores of a row (four chains); edge: those from `left` on become -inf.
+__device__ __forceinline__ float row_max64(uint32_t* r, int left, bool edge) {
+  if (edge) {
+#pragma unroll
+    for (int c = 0; c < 64; ++c)
+      if (c >= left) r[c] = 0xff800000u;
+  }
+  float b[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) b[k] = fmaxf(__uint_as_float(r[k]), __uint_as_float(r[k + 4]));
+#pragma unroll
+  for (int c = 8; c < 64; c += 8)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) b[k] = fmaxf(fmaxf(b[k], __uint_as_float(r[c + k])), __uint_as_float(r[c + k + 4]));
+  return fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3]));
+}
+
 // How a segment's key blocks fall to the streams.
 struct Jobs {
   bool lone;          // one row tile: the streams take alternate blocks
@@ -189,18 +217,19 @@ __device__ __forceinline__ void load_role(const PrefixAttnParams& p, const CUten
   using Sh = TcShape<HD>;
   const int lane = threadIdx.x & 31;
   const int box = min(p.page, kKeys), boxes = kKeys / box;
-  uint32_t fill = 0, nseg = 0;
+  uint32_t fill = 0, nq = 0;
   PrefixSeg g;
-  for (; segs.next(g); ++nseg) {
+  while (segs.next(g)) {
     const Jobs jobs = seg_jobs(p, g);
-    if (!tc_wait(smem_u32(&m->q_empty), (nseg & 1) ^ 1, &m->abort, p.err)) return;
     const int tiles = jobs.lone ? 1 : 2;
-    if (lane == 0) {
-      const uint32_t bar = smem_u32(&m->q_full);
-      mbar_expect_tx(bar, (uint32_t)(tiles * Sh::kHalves * p.tok_tile * p.rep * 128));
-      for (int t = 0; t < tiles; ++t)
+    for (int t = 0; t < tiles; ++t, ++nq) {
+      const uint32_t slot = nq & 1, bar = smem_u32(&m->q_full[slot]);
+      if (!tc_wait(smem_u32(&m->q_empty[slot]), ((nq >> 1) & 1) ^ 1, &m->abort, p.err)) return;
+      if (lane == 0) {
+        mbar_expect_tx(bar, (uint32_t)(Sh::kHalves * p.tok_tile * p.rep * 128));
         for (int h = 0; h < Sh::kHalves; ++h)
-          tma_load_3d(sm + t * Sh::kTile + h * Sh::kHalf, mq, bar, 64 * h, g.head * p.rep, g.t0 + t * p.tok_tile);
+          tma_load_3d(sm + slot * Sh::kTile + h * Sh::kHalf, mq, bar, 64 * h, g.head * p.rep, g.t0 + t * p.tok_tile);
+      }
     }
     // lane l loads page l of a block; a page past the keys or outside the pool reads as zeros
     auto entry = [&](int kb) {
@@ -230,103 +259,179 @@ __device__ __forceinline__ void load_role(const PrefixAttnParams& p, const CUten
     };
     // first uses: keys lead values by one job (two streams' worth where both take every block)
     const int lead = jobs.lone ? 2 : 1;
-    int ahead[3] = {entry(g.kb0), entry(g.kb0 + 1), 0};
+    int e0 = entry(g.kb0), e1 = entry(g.kb0 + 1);
     const int blocks = g.kb1 - g.kb0;
-    for (int i = 0; i < lead && i < blocks; ++i)
-      if (!load(mk, g.kb0 + i, ahead[i])) return;
+    if (!load(mk, g.kb0, e0)) return;
+    if (lead == 2 && blocks > 1 && !load(mk, g.kb0 + 1, e1)) return;
     for (int i = 0; i < blocks; ++i) {
-      ahead[2] = entry(g.kb0 + i + 2);
-      if (!load(mv, g.kb0 + i, ahead[0])) return;
-      if (i + lead < blocks && !load(mk, g.kb0 + i + lead, ahead[lead])) return;
-      ahead[0] = ahead[1];
-      ahead[1] = ahead[2];
+      const int e2 = entry(g.kb0 + i + 2);
+      if (!load(mv, g.kb0 + i, e0)) return;
+      if (i + lead < blocks && !load(mk, g.kb0 + i + lead, lead == 2 ? e2 : e1)) return;
+      e0 = e1;
+      e1 = e2;
     }
   }
 }
 
+__device__ __forceinline__ bool elect_one() {
+  uint32_t e;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(e));
+  return e != 0;
+}
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+
+// The products.  The whole warp runs this, in step, and one lane issues: a job's
+// 16 products take the tensor cores only about 1000 cycles, so their operands
+// have to stay in uniform registers (one thread's own branch cost 2.7 times as
+// much).  Barrier addresses and descriptors are sums of 32-bit words; the two
+// kinds of segment have a loop each.
 template <int HD>
-__device__ __forceinline__ void mma_role(const PrefixAttnParams& p, uint32_t sm, uint8_t* smp, uint32_t tmem, TcMisc* m,
-                                         PrefixSegs<kTiles, kKeys>& segs) {
+struct MmaWarp {
   using Sh = TcShape<HD>;
-  const int lane = threadIdx.x & 31;
-  constexpr uint32_t is = idesc_bf16(kKeys, false), io = idesc_bf16(HD, true);
-  uint32_t use = 0, nseg = 0, np[2] = {0, 0}, no[2] = {0, 0};
-  PrefixSeg g;
-  for (; segs.next(g); ++nseg) {
-    const Jobs jobs = seg_jobs(p, g);
-    if (!tc_wait(smem_u32(&m->q_full), nseg & 1, &m->abort, p.err)) return;
-    uint32_t kst = 0, vst = 0;
-    auto take = [&](uint32_t* st) {
-      *st = use % Sh::kStages;
-      const bool ok = tc_wait(smem_u32(&m->full[*st]), (use / Sh::kStages) & 1, &m->abort, p.err);
-      ++use;
-      return ok;
-    };
-    auto scores = [&](int j) {
-      const int t = j & 1;
-      if ((jobs.lone || t == 0) && !take(&kst)) return false;
-      if (lane == 0) {
-        tc_fence_after();
-        const uint32_t q = sm + (jobs.lone ? 0u : (uint32_t)t * Sh::kTile), k = sm + Sh::kRing + kst * Sh::kTile;
+  static constexpr uint32_t kIdescS = idesc_bf16(kKeys, false), kIdescO = idesc_bf16(HD, true);
+  uint32_t tmem, qd, rd;                         // descriptors of query tile 0 and ring tile 0, as K-major operands
+  uint32_t full, empty, q_full, q_empty, s_full, p_full, o_full, o_free;
+  uint32_t st = 0, par = 0;                      // ring place and its phase
+  uint32_t kst = 0, vst = 0;
+  uint32_t pp = 0, po = 3, pq = 0;               // phase bits by stream (p_full, o_free) and query tile
+  uint32_t qs = 0;                               // query tile of the segment's stream 0
+  volatile int* abort;
+  unsigned* err;
+
+  __device__ MmaWarp(uint32_t sm, uint32_t tm, TcMisc* m, unsigned* e) : tmem(tm), abort(&m->abort), err(e) {
+    qd = desc_lo(sm, 16);
+    rd = desc_lo(sm + Sh::kRing, 16);
+    full = smem_u32(m->full); empty = smem_u32(m->empty);
+    q_full = smem_u32(m->q_full); q_empty = smem_u32(m->q_empty);
+    s_full = smem_u32(m->s_full); p_full = smem_u32(m->p_full);
+    o_full = smem_u32(m->o_full); o_free = smem_u32(m->o_free);
+  }
+  __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    return __all_sync(0xffffffffu, tc_wait(bar, parity, abort, err));
+  }
+  __device__ __forceinline__ bool take(uint32_t& at) {
+    at = st;
+    const bool ok = wait(full + 8 * st, par);
+    if (++st == Sh::kStages) { st = 0; par ^= 1; }
+    return ok;
+  }
+  // S of stream t: query tile slot times ring tile kst
+  __device__ __forceinline__ void scores(int t, uint32_t slot, bool free_k, bool free_q) {
+    const uint32_t a = qd + slot * (Sh::kTile >> 4), b = rd + kst * (Sh::kTile >> 4), d = tmem + 128u * t;
+    tc_fence_after();
+    if (elect_one()) {
 #pragma unroll
-        for (int s = 0; s < HD / 16; ++s) {
-          const uint32_t at = (uint32_t)(s >> 2) * Sh::kHalf + (uint32_t)(s & 3) * 32u;
-          umma_f16(tmem + 128u * t, sdesc_sw128(q + at), sdesc_sw128(k + at), is, s > 0 ? 1u : 0u);
-        }
-        umma_commit(smem_u32(&m->s_full[t]));
-        if (jobs.lone || t == 1) umma_commit(smem_u32(&m->empty[kst]));
-        if (j == jobs.count - 1) umma_commit(smem_u32(&m->q_empty));
+      for (int s = 0; s < HD / 16; ++s) {
+        const uint32_t at = ((uint32_t)(s >> 2) * Sh::kHalf + (uint32_t)(s & 3) * 32u) >> 4;
+        mma_ss(d, a + at, b + at, kIdescS, s > 0 ? 1u : 0u);
       }
-      __syncwarp();
-      return true;
-    };
-    for (int j = 0; j < 2 && j < jobs.count; ++j)
-      if (!scores(j)) return;
-    for (int j = 0; j < jobs.count; ++j) {
-      const int t = j & 1, kb = g.kb0 + (jobs.lone ? j : j >> 1);
-      if (jobs.lone || t == 0) {
-        if (!take(&vst)) return;
-        // slots of a page past the last key hold anything: their weights are 0, and 0 x V must be 0
-        const int valid = g.k_end - (g.k0 + kb * kKeys);
-        if (valid < kKeys) {
-          const int upto = min(kKeys, (valid + p.page - 1) / p.page * p.page);
-          uint8_t* v = smp + Sh::kRing + vst * Sh::kTile;
-          for (int i = valid * 8 + lane; i < upto * 8; i += 32)
-            for (int h = 0; h < Sh::kHalves; ++h) *reinterpret_cast<uint4*>(v + h * Sh::kHalf + i * 16) = make_uint4(0, 0, 0, 0);
-          fence_proxy_async_smem();
-          __syncwarp();
-        }
-      }
-      if (j < 2) {                               // the stream's sums of the segment before are read
-        if (!tc_wait(smem_u32(&m->o_free[t]), (no[t] & 1) ^ 1, &m->abort, p.err)) return;
-        ++no[t];
-      }
-      if (!tc_wait(smem_u32(&m->p_full[t]), np[t] & 1, &m->abort, p.err)) return;
-      ++np[t];
-      if (lane == 0) {
-        tc_fence_after();
-        const uint32_t v = sm + Sh::kRing + vst * Sh::kTile;
-#pragma unroll
-        for (int s = 0; s < kKeys / 16; ++s)
-          umma_f16_ts(tmem + 256u + 128u * t, tmem + 128u * t + 8u * s, sdesc_mn(v + 2048u * s, Sh::kHalf), io,
-                      (j >= 2 || s > 0) ? 1u : 0u);
-        if (jobs.lone || t == 1) umma_commit(smem_u32(&m->empty[vst]));
-        if (j >= jobs.count - 2) umma_commit(smem_u32(&m->o_full[t]));
-      }
-      __syncwarp();
-      if (j + 2 < jobs.count && !scores(j + 2)) return;
+      umma_commit(s_full + 8 * t);
+      if (free_k) umma_commit(empty + 8 * kst);
+      if (free_q) umma_commit(q_empty + 8 * slot);
     }
+    __syncwarp();
+  }
+  // O of stream t (+)= its weights times ring tile vst
+  __device__ __forceinline__ bool weighted(int t, bool first, bool free_v, bool last) {
+    if (first) {                                 // the stream's sums of the segment before are read
+      if (!wait(o_free + 8 * t, (po >> t) & 1)) return false;
+      po ^= 1u << t;
+    }
+    if (!wait(p_full + 8 * t, (pp >> t) & 1)) return false;
+    pp ^= 1u << t;
+    tc_fence_after();
+    // as an MN-major operand: the distance between its 64-column blocks in place of the K-major one's
+    const uint32_t b = rd + vst * (Sh::kTile >> 4) + (((Sh::kHalf - 16) >> 4) << 16), d = tmem + 256u + 128u * t;
+    if (elect_one()) {
+#pragma unroll
+      for (int s = 0; s < kKeys / 16; ++s) mma_ts(d, tmem + 128u * t + 8u * s, b + 128u * s, kIdescO, s > 0 || !first ? 1u : 0u);
+      if (free_v) umma_commit(empty + 8 * vst);
+      if (last) umma_commit(o_full + 8 * t);
+    }
+    __syncwarp();
+    return true;
+  }
+  __device__ __forceinline__ bool query(uint32_t slot) {
+    const bool ok = wait(q_full + 8 * slot, (pq >> slot) & 1);
+    pq ^= 1u << slot;
+    return ok;
+  }
+  // The first score product of stream t of a segment with `count` jobs (qn: its first query tile).
+  __device__ __forceinline__ bool open(const Jobs& jobs, int t, uint32_t qn) {
+    if (t >= jobs.count) return true;
+    const uint32_t slot = jobs.lone ? qn : qn ^ (uint32_t)t;
+    if ((!jobs.lone || t == 0) && !query(slot)) return false;
+    if ((jobs.lone || t == 0) && !take(kst)) return false;
+    scores(t, slot, jobs.lone || t == 1, jobs.count <= (jobs.lone ? t + 1 : 2));
+    return true;
+  }
+  // The rest of a segment, and the first score products of the next one.
+  template <bool kLone>
+  __device__ __forceinline__ bool run(const Jobs& jobs, bool more, const Jobs& next, uint32_t qn) {
+    const int pairs = (jobs.count + 1) >> 1;
+    uint32_t vlast = 0;
+    for (int i = 0; i < pairs; ++i) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int j = 2 * i + t;
+        if (!kLone || t == 0 || j < jobs.count) {
+          if (kLone && t == 1 && i + 1 == pairs)
+            vst = vlast;
+          else if ((kLone || t == 0) && !take(vst))
+            return false;
+          // the next segment's first keys lie behind this one's last values in the ring
+          if (kLone && t == 0 && i + 1 == pairs && j + 1 < jobs.count && !take(vlast)) return false;
+          if (!weighted(t, i == 0, kLone || t == 1, j + 2 >= jobs.count)) return false;
+        }
+        if (j + 2 < jobs.count) {
+          if ((kLone || t == 0) && !take(kst)) return false;
+          scores(t, kLone ? qs : qs ^ (uint32_t)t, kLone || t == 1, kLone ? j + 3 == jobs.count : j + 4 >= jobs.count);
+        } else if (i + 1 == pairs && more && !open(next, t, qn)) {
+          return false;
+        }
+      }
+    }
+    return true;
+  }
+};
+
+template <int HD>
+__device__ __forceinline__ void mma_role(const PrefixAttnParams& p, uint32_t sm, uint32_t tmem, TcMisc* m,
+                                         PrefixSegs<kTiles, kKeys>& segs) {
+  MmaWarp<HD> x(sm, tmem, m, p.err);
+  PrefixSeg g;
+  Jobs jobs = {false, 0}, next = {false, 0};
+  auto advance = [&](Jobs& j) {
+    const bool more = uniform(segs.next(g)) != 0;
+    if (more) {
+      const Jobs x = seg_jobs(p, g);
+      j.lone = uniform(x.lone) != 0;
+      j.count = uniform(x.count);
+    }
+    return more;
+  };
+  bool more = advance(jobs);
+  if (more) {
+    if (!x.open(jobs, 0, 0) || !x.open(jobs, 1, 0)) return;
+  }
+  while (more) {
+    more = advance(next);
+    const uint32_t qn = x.qs ^ (jobs.lone ? 1u : 0u);
+    if (!(jobs.lone ? x.template run<true>(jobs, more, next, qn) : x.template run<false>(jobs, more, next, qn))) return;
+    x.qs = qn;
+    jobs = next;
   }
 }
 
 template <int HD>
-__device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, uint32_t tmem, TcMisc* m,
+__device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, uint8_t* smp, uint32_t tmem, TcMisc* m,
                                              PrefixSegs<kTiles, kKeys>& segs) {
   const int lane = threadIdx.x & 31, quad = (threadIdx.x >> 5) & 3, row = quad * 32 + lane;
   const uint32_t ts = tmem + ((uint32_t)(quad * 32) << 16) + 128u * t, to = ts + 256u;
   const int tok = row / p.rep;
   const float sl = p.scale * kLog2e;
-  uint32_t ns = 0, no = 0;
+  uint32_t ns = 0, no = 0, tiles = 0;            // jobs, segments; ring tiles of the segments before
   PrefixSeg g;
   while (segs.next(g)) {
     const Jobs jobs = seg_jobs(p, g);
@@ -340,17 +445,13 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
       ++ns;
       tc_fence_after();
       uint32_t r[128];
-      tmem_ld128(ts, r);
-      if (!__all_sync(0xffffffffu, left >= kKeys)) {
-#pragma unroll
-        for (int c = 0; c < 128; ++c)
-          if (c >= left) r[c] = 0xff800000u;     // -inf
-      }
-      float b = -INFINITY;
-#pragma unroll
-      for (int c = 0; c < 128; c += 4)
-        b = fmaxf(fmaxf(fmaxf(b, __uint_as_float(r[c])), fmaxf(__uint_as_float(r[c + 1]), __uint_as_float(r[c + 2]))),
-                  __uint_as_float(r[c + 3]));
+      tmem_ld64(ts, r);
+      tmem_wait_ld64(r);
+      tmem_ld64(ts + 64, r + 64);                // lands while the first half's maximum is taken
+      const bool edge = !__all_sync(0xffffffffu, left >= kKeys);
+      float b = row_max64(r, left, edge);
+      tmem_wait_ld64(r + 64);
+      b = fmaxf(b, row_max64(r + 64, left - 64, edge));
       if (n == 0) {
         mx = b;
       } else {
@@ -372,20 +473,37 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
         }
       }
       const float base = mx == -INFINITY ? 0.f : -mx * sl;
-      float2 acc = make_float2(0.f, 0.f);
+      float2 acc[4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t w[32];
+      for (int c = 0; c < 4; ++c) acc[c] = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int c = 0; c < 64; c += 2) {
-          const float2 x = fma2(__uint_as_float(r[64 * h + c]), __uint_as_float(r[64 * h + c + 1]), sl, base);
+      for (int h = 0; h < 4; ++h) {
+        uint32_t w[16];
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) {
+          const float2 x = fma2(__uint_as_float(r[32 * h + c]), __uint_as_float(r[32 * h + c + 1]), sl, base);
           const float2 e = make_float2(ex2a(x.x), ex2a(x.y));
-          acc = add2(acc, e);
+          acc[(c >> 1) & 3] = add2(acc[(c >> 1) & 3], e);
           w[c >> 1] = pack_bf16(e.x, e.y);
         }
-        tmem_st32(ts + 32 * h, w);
+        tmem_st16(ts + 16 * h, w);
       }
-      sum += acc.x + acc.y;
+      if (jobs.lone || t == 0) {
+        // slots of a page past the last key hold anything: their weights are 0, and 0 x V must be 0
+        const int keys = g.k_end - g.k0 - kb * kKeys;
+        if (keys < kKeys) {
+          const int upto = min(kKeys, (keys + p.page - 1) / p.page * p.page), i = kb - g.kb0;
+          const uint32_t at = tiles + (jobs.lone ? i + min(i + 2, jobs.count) : 2 * i + 1), st = at % TcShape<HD>::kStages;
+          if (!tc_wait(smem_u32(&m->full[st]), (at / TcShape<HD>::kStages) & 1, &m->abort, p.err)) return;
+          uint8_t* v = smp + TcShape<HD>::kRing + st * TcShape<HD>::kTile;
+          for (int c = keys * 8 + row; c < upto * 8; c += kRows)
+            for (int h = 0; h < TcShape<HD>::kHalves; ++h)
+              *reinterpret_cast<uint4*>(v + h * TcShape<HD>::kHalf + c * 16) = make_uint4(0, 0, 0, 0);
+          fence_proxy_async_smem();
+        }
+      }
+      acc[0] = add2(add2(acc[0], acc[1]), add2(acc[2], acc[3]));
+      sum += acc[0].x + acc[0].y;
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
@@ -413,6 +531,7 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
       }
     }
     if (valid) p.part_ml[at] = make_float2(mx == -INFINITY ? mx : mx * sl, sum);
+    tiles += 2 * (g.kb1 - g.kb0);
   }
 }
 
@@ -424,16 +543,16 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* smp = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tc_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   TcMisc* m = reinterpret_cast<TcMisc*>(smp + TcShape<HD>::kMisc);
   const uint32_t sm = smem_u32(smp);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, cta = blockIdx.x;
   if (threadIdx.x == 256) {
     for (int i = 0; i < 8; ++i) {
       mbar_init(smem_u32(&m->full[i]), 1);
       mbar_init(smem_u32(&m->empty[i]), 1);
     }
-    mbar_init(smem_u32(&m->q_full), 1);
-    mbar_init(smem_u32(&m->q_empty), 1);
     mbar_init(smem_u32(&m->drain), 1);
     for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&m->q_full[i]), 1);
+      mbar_init(smem_u32(&m->q_empty[i]), 1);
       mbar_init(smem_u32(&m->s_full[i]), 1);
       mbar_init(smem_u32(&m->p_full[i]), 4);
       mbar_init(smem_u32(&m->o_full[i]), 1);
@@ -457,13 +576,18 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = m->tmem;
   PrefixSegs<kTiles, kKeys> segs(p, m->sched, m->step_base, m->info, cta);
-  if (warp == 8)
-    load_role<HD>(p, &mq, &mk, &mv, sm, m, segs);
-  else if (warp == 9)
-    mma_role<HD>(p, sm, smp, tmem, m, segs);
-  else
-    softmax_role<HD>(p, warp >> 2, tmem, m, segs);
-  if (cta == 0) publish_sched(p, m->sched, m->step_base);
+  // registers: 384 threads x 168 at launch = 256 x 200 (softmax) + 128 x 96 and some left over
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    if (warp == 8)
+      load_role<HD>(p, &mq, &mk, &mv, sm, m, segs);
+    else if (warp == 9)
+      mma_role<HD>(p, sm, tmem, m, segs);
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    softmax_role<HD>(p, warp >> 2, smp, tmem, m, segs);
+  }
+  if (cta == 0) publish_sched(p, m->sched, m->step_base, m->info);
   tc_fence_before();
   __syncthreads();
   // Every load has been waited for by its product, unless a wait gave up: then

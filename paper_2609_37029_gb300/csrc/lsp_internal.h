@@ -310,6 +310,7 @@ struct PrefixAttnParams {
   int tok_tile;             // rows of q (tokens) in a tile: tile rows / rep
   int units;                // units of tiles that cover all rows
   int splits;               // key ranges of the shared pages
+  int num_sms;
   int grid;                 // CTAs of the main kernel
   int64_t part_rows;        // rows of partial results the workspace holds
   char* sched;              // the schedule, for the joining kernel

@@ -84,6 +84,9 @@ CASES = {
     "empty ones": dict(lens=[0, 40, 5, 33, 0], rows=[0, 0, 9, 2, 3], shared=0, nq=4, nkv=2, d=128, page=16),
     "heads not of eight": dict(lens=[270, 290], rows=[17, 11], shared=256, nq=35, nkv=5, d=128, page=256),
     "many heads a key head": dict(lens=[270, 290, 300], rows=[3, 1, 2], shared=260, nq=64, nkv=1, d=64, page=16),
+    # several segments of one to four key blocks for every CTA, shared ones of one and two row tiles among them
+    "more segments than CTAs": dict(lens=[270 + 7 * i % 391 for i in range(90)], rows=[1 + i % 2 for i in range(90)], shared=260, nq=8, nkv=8, d=64, page=16),
+    "uneven segments": dict(lens=[150 + 131 * i % 700 for i in range(60)], rows=[1 + 7 * i % 21 for i in range(60)], shared=140, nq=16, nkv=4, d=128, page=32),
     "many sequences": dict(lens=[120 + i for i in range(70)], rows=[i % 3 for i in range(70)], shared=112, nq=2, nkv=1, d=64, page=16),
 }
 
