@@ -175,7 +175,7 @@ __device__ void fma_segment(const PrefixAttnParams& p, FmaSmem<HD>& sm, const Pr
     const int64_t at = seg.part.row + r;
 #pragma unroll
     for (int c = 0; c < kCols; ++c)
-      *reinterpret_cast<float4*>(p.part_o + at * HD + 4 * tx + 64 * c) = make_float4(o[a][c][0], o[a][c][1], o[a][c][2], o[a][c][3]);
+      *part_chunk<HD>(p.part_o, at, tx + 16 * c) = make_float4(o[a][c][0], o[a][c][1], o[a][c][2], o[a][c][3]);
     if (tx == 0) p.part_ml[at] = make_float2(m[a], l[a]);
   }
 }
@@ -201,18 +201,19 @@ __global__ void __launch_bounds__(kFmaThreads) prefix_attn_fma_kernel(const Pref
 // Joins the segments of an output row (token, query head): kWarps warps a row
 // take its segments in turn, lane l holds dims [l HD/32, (l + 1) HD/32).  The
 // running maxima come first, one segment a lane, so that the sums themselves
-// are independent loads.  Four warps where the rows alone would leave most of
-// the GPU idle (few rows have many segments), one where they fill it.
-constexpr int kJoinThreads = 128;
+// are independent loads.  A CTA has four consecutive rows, whose sums share cache
+// lines.  Four warps a row where the rows alone would leave most of the GPU idle
+// (few rows have many segments), one where they fill it.
+constexpr int kJoinRows = 4;
 template <typename T, int HD, int kUnitTiles, int kBlock, int kWarps>
-__global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixAttnParams p) {
-  constexpr int kVec = HD / 32, kRowsCta = kJoinThreads / 32 / kWarps, kAhead = 8;
-  __shared__ float s_o[kWarps > 1 ? kJoinThreads / 32 : 1][HD], s_l[kJoinThreads / 32];
+__global__ void __launch_bounds__(32 * kJoinRows * kWarps) prefix_join_kernel(const PrefixAttnParams p) {
+  constexpr int kVec = HD / 32, kAhead = 8;
+  __shared__ float s_o[kWarps > 1 ? kJoinRows * kWarps : 1][HD], s_l[kJoinRows * kWarps];
   griddep_wait();
   griddep_launch();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % kWarps;
-  const int64_t w = (int64_t)blockIdx.x * kRowsCta + warp / kWarps;
-  if (w >= (int64_t)p.total * p.nq) return;      // kWarps > 1: one row a CTA, all of it leaves
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp / kJoinRows;
+  const int64_t rows = (int64_t)p.total * p.nq, mine = (int64_t)blockIdx.x * kJoinRows + warp % kJoinRows;
+  const int64_t w = mine < rows ? mine : rows - 1;   // a row past the last does the last's work, and stores nothing
   const int t = (int)(w / p.nq), h = (int)(w % p.nq), g = h / p.rep, hr = h % p.rep;
   const SchedView v = sched_view(p);
   const PrefixSched s = *v.s;
@@ -295,12 +296,11 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixA
 #pragma unroll
         for (int e = 0; e < kVec; ++e) y[k][e] = 0.f;
         if (on) {
-          const float* from = p.part_o + at * HD + lane * kVec;
           if constexpr (kVec == 4) {
-            const float4 z = *reinterpret_cast<const float4*>(from);
+            const float4 z = *part_chunk<HD>(p.part_o, at, lane);
             y[k][0] = z.x; y[k][1] = z.y; y[k][2] = z.z; y[k][3] = z.w;
           } else {
-            const float2 z = *reinterpret_cast<const float2*>(from);
+            const float2 z = reinterpret_cast<const float2*>(part_chunk<HD>(p.part_o, at, lane >> 1))[lane & 1];
             y[k][0] = z.x; y[k][1] = z.y;
           }
         }
@@ -317,15 +317,16 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixA
     for (int e = 0; e < kVec; ++e) s_o[warp][lane * kVec + e] = o[e];
     if (lane == 0) s_l[warp] = l;
     __syncthreads();
-    if (warp > 0) return;
+    if (part > 0) return;
     l = 0.f;
-    for (int k = 0; k < kWarps; ++k) l += s_l[k];
+    for (int k = 0; k < kWarps; ++k) l += s_l[k * kJoinRows + warp];
 #pragma unroll
     for (int e = 0; e < kVec; ++e) {
       o[e] = 0.f;
-      for (int k = 0; k < kWarps; ++k) o[e] += s_o[k][lane * kVec + e];
+      for (int k = 0; k < kWarps; ++k) o[e] += s_o[k * kJoinRows + warp][lane * kVec + e];
     }
   }
+  if (mine >= rows) return;
   const float inv = l > 0.f ? 1.f / l : 0.f;
   T* out = static_cast<T*>(p.out) + w * HD + lane * kVec;
   if constexpr (sizeof(T) == 2 && kVec == 4)
@@ -339,10 +340,11 @@ __global__ void __launch_bounds__(kJoinThreads) prefix_join_kernel(const PrefixA
 template <typename T, int HD, int kUnitTiles, int kBlock>
 int launch_join(const PrefixAttnParams& p, cudaStream_t s) {
   const int64_t rows = (int64_t)p.total * p.nq;
+  const dim3 grid((unsigned)((rows + kJoinRows - 1) / kJoinRows));
   const bool few = rows < 16 * (int64_t)p.num_sms;
   const cudaError_t e =
-      few ? launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 4>, dim3((unsigned)rows), dim3(kJoinThreads), 0, s, p)
-          : launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(kJoinThreads), 0, s, p);
+      few ? launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 4>, grid, dim3(128 * kJoinRows), 0, s, p)
+          : launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 1>, grid, dim3(32 * kJoinRows), 0, s, p);
   return e == cudaSuccess ? LSP_OK : LSP_ERR_CUDA;
 }
 
@@ -402,6 +404,7 @@ size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms) {
   const int64_t rows = (int64_t)p->tok_tile * p->rep * unit_tiles, groups = (int64_t)p->nkv * p->units;
   p->part_rows = std::max<int64_t>(groups, kMaxTurns * p->grid) * rows + (int64_t)unit_tiles * p->nkv * p->rep * p->total +
                  p->grid * rows;
+  p->part_rows = (p->part_rows + 3) / 4 * 4;
   return align256(sched_bytes(p->n, p->grid)) + align256((size_t)p->part_rows * sizeof(float2)) +
          (size_t)p->part_rows * p->d * sizeof(float);
 }

@@ -1,25 +1,35 @@
 // Shared-prefix attention on the tcgen05 tensor cores: bf16, head dim 64 or 128
 // (mathematics: k_prefix_attn.cu, work distribution: prefix_sched.cuh).
 //
-// A persistent CTA per SM works through its segments.  Two softmax warpgroups
-// ("streams") keep two score tiles of 128 rows x 128 keys in flight, so that
-// the tensor cores multiply for one while the other takes exponentials.  A
-// segment with two row tiles gives each stream one, both over every key block;
-// a segment with one (few rows: decoding) gives both streams the same rows and
-// alternate key blocks, and each leaves its own partial result.
+// A persistent CTA per SM works through its segments.  Two "streams" keep two
+// score tiles of 128 rows x 128 keys in flight, so that the tensor cores
+// multiply for one while the other takes exponentials.  A segment with two row
+// tiles gives each stream one, both over every key block; a segment with one
+// (few rows: decoding) gives both streams the same rows and alternate key
+// blocks, and each leaves its own partial result.
 //
 //   warps 0-3, 4-7  streams 0 and 1: thread = row; scores from TMEM, running
-//                   maximum and sum, weights rounded to bf16 back to TMEM
-//                   over the scores, at the end the sums to the workspace
+//                   maximum and sum, weights rounded to bf16 back to TMEM over
+//                   the scores, at the end the sums to the workspace
 //   warp 8          loads: query tiles, then key and value blocks, page by page
 //                   (TMA, 128-byte swizzle), into a ring of tiles
-//   warp 9          products: S = Q K^T (both from shared memory) and O += P V
-//                   (P from TMEM, V MN-major from shared memory)
+//   warps 9, 10     products of streams 0 and 1: S = Q K^T (both from shared
+//                   memory) and O += P V (P from TMEM, V MN-major from shared
+//                   memory), one lane issuing
 //
-// Job j of a segment is a (stream j & 1, key block); the order of the products
-// is S(0) S(1) [PV(j) S(j + 2)]...: S(j + 2) overwrites the weights PV(j) reads,
-// and products complete in order.  The ring's tiles follow the order of first
-// use.  TMEM: scores of stream t at columns 128 t, sums at 256 + 128 t.
+// A product of 128 x 128 x 16 takes 64 cycles, the tensor cores queue a handful,
+// and a commit waits in line behind them, so every wait of an issuing warp shows
+// unless another warp's products run meanwhile: hence a warp for each stream.
+// They take turns -- P V of a block and the scores of the next -- because left
+// alone the streams drift into step, and then multiply at the same time and take
+// exponentials at the same time (32 requests over 128K: one warp for both 0.88
+// ms, two without turns 1.08, with them 0.87).  What bounds a stream now is its
+// chain: scores, their maximum, exponentials, P V, the next scores; P V therefore
+// starts when half of the weights are there (0.82).
+//
+// A stream's order is S(0) PV(0) S(1) PV(1) ...: S(j + 1) overwrites the weights
+// that PV(j) reads, and the products of one thread complete in order.  TMEM:
+// scores of stream t at columns 128 t, sums at 256 + 128 t.
 //
 // The maximum is raised (and the sums rescaled) only when it would grow by more
 // than 2^8: weights stay below 2^8 and the sums, in fp32, lose nothing.
@@ -31,7 +41,9 @@ namespace lsp {
 namespace {
 
 constexpr int kRows = kPrefixTcRows, kKeys = kPrefixTcKeys, kTiles = kPrefixTcTiles;
-constexpr int kThreads = 384;                   // warps 10 and 11 only share their registers out
+constexpr int kThreads = 384;                   // warp 11 only shares its registers out
+constexpr int kLoadWarp = 8, kMmaWarp = 9;
+constexpr int kFirstKeys = 64;                  // keys whose weights are handed over before the rest's (32: 0.84 ms, 96: 0.87)
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRaise = 8.0f;                   // log2 of the most a weight may exceed 1
 
@@ -46,7 +58,7 @@ struct TcShape {
 };
 
 struct TcMisc {
-  uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], o_free[2], drain;
+  uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_first[2], p_full[2], o_full[2], o_free[2], turn[2], drain;
   uint32_t tmem;
   int abort;
   PrefixSched sched;
@@ -210,6 +222,11 @@ __device__ __forceinline__ Jobs seg_jobs(const PrefixAttnParams& p, const Prefix
   return {lone, lone ? blocks : 2 * blocks};
 }
 __device__ __forceinline__ int stream_jobs(const Jobs& j, int stream) { return (j.count + 1 - stream) >> 1; }
+// Places in the ring, from the segment's first tile on: keys and values of its
+// block i.  Two row tiles: K0 V0 K1 V1 ...; one: K0 K1 V0 K2 V1 K3 ..., the order
+// in which two streams of alternate blocks come to them.
+__device__ __forceinline__ uint32_t key_tile(const Jobs& j, int i) { return j.lone ? (i > 0 ? 2 * i - 1 : 0) : 2 * i; }
+__device__ __forceinline__ uint32_t value_tile(const Jobs& j, int i) { return j.lone ? i + min(i + 2, j.count) : 2 * i + 1; }
 
 template <int HD>
 __device__ __forceinline__ void load_role(const PrefixAttnParams& p, const CUtensorMap* mq, const CUtensorMap* mk,
@@ -280,147 +297,131 @@ __device__ __forceinline__ bool elect_one() {
 }
 __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 
-// The products.  The whole warp runs this, in step, and one lane issues: a job's
-// 16 products take the tensor cores only about 1000 cycles, so their operands
-// have to stay in uniform registers (one thread's own branch cost 2.7 times as
-// much).  Barrier addresses and descriptors are sums of 32-bit words; the two
-// kinds of segment have a loop each.
+// The products of stream t.  The whole warp runs this, in step, and one lane
+// issues, so that operands stay in uniform registers (from a single thread's own
+// branch a product took 2.7 times as long).  Both streams come to every tile of
+// the ring and every query tile in order, and each arrives at it once: when its
+// products are done with the tile, or at once where it has no use for it.  So
+// neither is ever more than a phase from the other.
 template <int HD>
-struct MmaWarp {
+__device__ __forceinline__ void mma_role(const PrefixAttnParams& p, int t, uint32_t sm, uint32_t tmem, TcMisc* m,
+                                         PrefixSegs<kTiles, kKeys>& segs) {
   using Sh = TcShape<HD>;
-  static constexpr uint32_t kIdescS = idesc_bf16(kKeys, false), kIdescO = idesc_bf16(HD, true);
-  uint32_t tmem, qd, rd;                         // descriptors of query tile 0 and ring tile 0, as K-major operands
-  uint32_t full, empty, q_full, q_empty, s_full, p_full, o_full, o_free;
-  uint32_t st = 0, par = 0;                      // ring place and its phase
-  uint32_t kst = 0, vst = 0;
-  uint32_t pp = 0, po = 3, pq = 0;               // phase bits by stream (p_full, o_free) and query tile
-  uint32_t qs = 0;                               // query tile of the segment's stream 0
-  volatile int* abort;
-  unsigned* err;
-
-  __device__ MmaWarp(uint32_t sm, uint32_t tm, TcMisc* m, unsigned* e) : tmem(tm), abort(&m->abort), err(e) {
-    qd = desc_lo(sm, 16);
-    rd = desc_lo(sm + Sh::kRing, 16);
-    full = smem_u32(m->full); empty = smem_u32(m->empty);
-    q_full = smem_u32(m->q_full); q_empty = smem_u32(m->q_empty);
-    s_full = smem_u32(m->s_full); p_full = smem_u32(m->p_full);
-    o_full = smem_u32(m->o_full); o_free = smem_u32(m->o_free);
-  }
-  __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
+  constexpr uint32_t kIdescS = idesc_bf16(kKeys, false), kIdescO = idesc_bf16(HD, true), kTileDesc = Sh::kTile >> 4;
+  const uint32_t qd = desc_lo(sm, 16), kd = desc_lo(sm + Sh::kRing, 16), vd = desc_lo(sm + Sh::kRing, Sh::kHalf);
+  const uint32_t full = smem_u32(m->full), empty = smem_u32(m->empty), q_full = smem_u32(m->q_full), q_empty = smem_u32(m->q_empty);
+  const uint32_t s_full = smem_u32(&m->s_full[t]), p_first = smem_u32(&m->p_first[t]), p_full = smem_u32(&m->p_full[t]);
+  const uint32_t o_full = smem_u32(&m->o_full[t]), o_free = smem_u32(&m->o_free[t]);
+  const uint32_t ds = tmem + 128u * t, od = ds + 256u;
+  uint32_t turns = 0;
+  const uint32_t turn = smem_u32(m->turn);
+  uint32_t tiles = 0, seen = 0, nq = 0, pp = 0, po = 1;   // ring and query tiles, places passed; phases
+  auto wait = [&](uint32_t bar, uint32_t parity) {
     if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    return __all_sync(0xffffffffu, tc_wait(bar, parity, abort, err));
-  }
-  __device__ __forceinline__ bool take(uint32_t& at) {
-    at = st;
-    const bool ok = wait(full + 8 * st, par);
-    if (++st == Sh::kStages) { st = 0; par ^= 1; }
-    return ok;
-  }
-  // S of stream t: query tile slot times ring tile kst
-  __device__ __forceinline__ void scores(int t, uint32_t slot, bool free_k, bool free_q) {
-    const uint32_t a = qd + slot * (Sh::kTile >> 4), b = rd + kst * (Sh::kTile >> 4), d = tmem + 128u * t;
-    tc_fence_after();
-    if (elect_one()) {
+    return (bool)__all_sync(0xffffffffu, tc_wait(bar, parity, &m->abort, p.err));
+  };
+  auto landed = [&](uint32_t tile) { return wait(full + 8 * (tile & (Sh::kStages - 1)), (tile / Sh::kStages) & 1); };
+  auto pass = [&](uint32_t upto) {               // the other stream's tiles
+    for (; seen < upto; ++seen) {
+      if (!landed(seen)) return false;
+      if (elect_one()) mbar_arrive(empty + 8 * (seen & (Sh::kStages - 1)));
+      __syncwarp();
+    }
+    return true;
+  };
+  PrefixSeg g;
+  while (uniform(segs.next(g))) {
+    Jobs jobs = seg_jobs(p, g);
+    jobs.lone = uniform(jobs.lone) != 0;
+    jobs.count = uniform(jobs.count);
+    const int mine = stream_jobs(jobs, t), tiles_q = jobs.lone ? 1 : 2;
+    const uint32_t slot = (nq + (jobs.lone ? 0 : t)) & 1;
+    for (int x = 0; x < tiles_q; ++x, ++nq) {
+      if (!wait(q_full + 8 * (nq & 1), (nq >> 1) & 1)) return;
+      if (mine == 0 || (nq & 1) != slot) {
+        if (elect_one()) mbar_arrive(q_empty + 8 * (nq & 1));
+        __syncwarp();
+      }
+    }
+    uint32_t kst = 0;
+    auto keys = [&](int n) {                     // the stream's n-th key tile is there
+      const uint32_t kt = tiles + key_tile(jobs, jobs.lone ? 2 * n + t : n);
+      kst = kt & (Sh::kStages - 1);
+      if (!pass(kt) || !landed(kt)) return false;
+      seen = kt + 1;
+      return true;
+    };
+    auto scores = [&]() {
+      const uint32_t a = qd + slot * kTileDesc, b = kd + kst * kTileDesc;
 #pragma unroll
       for (int s = 0; s < HD / 16; ++s) {
         const uint32_t at = ((uint32_t)(s >> 2) * Sh::kHalf + (uint32_t)(s & 3) * 32u) >> 4;
-        mma_ss(d, a + at, b + at, kIdescS, s > 0 ? 1u : 0u);
+        mma_ss(ds, a + at, b + at, kIdescS, s > 0 ? 1u : 0u);
       }
-      umma_commit(s_full + 8 * t);
-      if (free_k) umma_commit(empty + 8 * kst);
-      if (free_q) umma_commit(q_empty + 8 * slot);
+    };
+    if (mine > 0) {
+      if (!keys(0)) return;
+      tc_fence_after();
+      if (elect_one()) {
+        scores();
+        umma_commit(s_full);
+        umma_commit(empty + 8 * kst);
+        if (mine == 1) umma_commit(q_empty + 8 * slot);
+      }
+      __syncwarp();
     }
-    __syncwarp();
-  }
-  // O of stream t (+)= its weights times ring tile vst
-  __device__ __forceinline__ bool weighted(int t, bool first, bool free_v, bool last) {
-    if (first) {                                 // the stream's sums of the segment before are read
-      if (!wait(o_free + 8 * t, (po >> t) & 1)) return false;
-      po ^= 1u << t;
-    }
-    if (!wait(p_full + 8 * t, (pp >> t) & 1)) return false;
-    pp ^= 1u << t;
-    tc_fence_after();
-    // as an MN-major operand: the distance between its 64-column blocks in place of the K-major one's
-    const uint32_t b = rd + vst * (Sh::kTile >> 4) + (((Sh::kHalf - 16) >> 4) << 16), d = tmem + 256u + 128u * t;
-    if (elect_one()) {
-#pragma unroll
-      for (int s = 0; s < kKeys / 16; ++s) mma_ts(d, tmem + 128u * t + 8u * s, b + 128u * s, kIdescO, s > 0 || !first ? 1u : 0u);
-      if (free_v) umma_commit(empty + 8 * vst);
-      if (last) umma_commit(o_full + 8 * t);
-    }
-    __syncwarp();
-    return true;
-  }
-  __device__ __forceinline__ bool query(uint32_t slot) {
-    const bool ok = wait(q_full + 8 * slot, (pq >> slot) & 1);
-    pq ^= 1u << slot;
-    return ok;
-  }
-  // The first score product of stream t of a segment with `count` jobs (qn: its first query tile).
-  __device__ __forceinline__ bool open(const Jobs& jobs, int t, uint32_t qn) {
-    if (t >= jobs.count) return true;
-    const uint32_t slot = jobs.lone ? qn : qn ^ (uint32_t)t;
-    if ((!jobs.lone || t == 0) && !query(slot)) return false;
-    if ((jobs.lone || t == 0) && !take(kst)) return false;
-    scores(t, slot, jobs.lone || t == 1, jobs.count <= (jobs.lone ? t + 1 : 2));
-    return true;
-  }
-  // The rest of a segment, and the first score products of the next one.
-  template <bool kLone>
-  __device__ __forceinline__ bool run(const Jobs& jobs, bool more, const Jobs& next, uint32_t qn) {
-    const int pairs = (jobs.count + 1) >> 1;
-    uint32_t vlast = 0;
-    for (int i = 0; i < pairs; ++i) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int j = 2 * i + t;
-        if (!kLone || t == 0 || j < jobs.count) {
-          if (kLone && t == 1 && i + 1 == pairs)
-            vst = vlast;
-          else if ((kLone || t == 0) && !take(vst))
-            return false;
-          // the next segment's first keys lie behind this one's last values in the ring
-          if (kLone && t == 0 && i + 1 == pairs && j + 1 < jobs.count && !take(vlast)) return false;
-          if (!weighted(t, i == 0, kLone || t == 1, j + 2 >= jobs.count)) return false;
-        }
-        if (j + 2 < jobs.count) {
-          if ((kLone || t == 0) && !take(kst)) return false;
-          scores(t, kLone ? qs : qs ^ (uint32_t)t, kLone || t == 1, kLone ? j + 3 == jobs.count : j + 4 >= jobs.count);
-        } else if (i + 1 == pairs && more && !open(next, t, qn)) {
-          return false;
+    // Turns of P V and the next scores, the two streams' in alternation: what a
+    // turn waits for is waited for during the other stream's.
+    for (int n = 0; n < (jobs.count + 1) >> 1; ++n, ++turns) {
+      const bool on = n + 1 < mine;
+      uint32_t vst = 0;
+      if (n < mine) {
+        const uint32_t vt = tiles + value_tile(jobs, jobs.lone ? 2 * n + t : n);
+        vst = vt & (Sh::kStages - 1);
+        if (!pass(vt) || !landed(vt)) return;
+        seen = vt + 1;
+        if (on && !keys(n + 1)) return;
+        if (n == 0) {                            // the sums of the segment before are read
+          if (!wait(o_free, po)) return;
+          po ^= 1;
         }
       }
+      if (!wait(turn + 8 * t, (turns & 1) ^ (t == 0 ? 1u : 0u))) return;
+      if (n < mine && !wait(p_first, pp)) return;
+      tc_fence_after();
+      const uint32_t b = vd + vst * kTileDesc;
+      if (n < mine) {
+        if (elect_one()) {
+#pragma unroll
+          for (int s = 0; s < kFirstKeys / 16; ++s) mma_ts(od, ds + 8u * s, b + 128u * s, kIdescO, s > 0 || n > 0 ? 1u : 0u);
+        }
+        __syncwarp();
+        if (!wait(p_full, pp)) return;
+        pp ^= 1;
+        tc_fence_after();
+      }
+      if (elect_one()) {
+        if (n < mine) {
+#pragma unroll
+          for (int s = kFirstKeys / 16; s < kKeys / 16; ++s) mma_ts(od, ds + 8u * s, b + 128u * s, kIdescO, 1u);
+          if (on) scores();
+        }
+        mbar_arrive(turn + 8 * (t ^ 1));
+        if (n < mine) {
+          if (on) {
+            umma_commit(s_full);
+            umma_commit(empty + 8 * kst);
+            if (n + 2 == mine) umma_commit(q_empty + 8 * slot);
+          } else {
+            umma_commit(o_full);
+          }
+          umma_commit(empty + 8 * vst);
+        }
+      }
+      __syncwarp();
     }
-    return true;
-  }
-};
-
-template <int HD>
-__device__ __forceinline__ void mma_role(const PrefixAttnParams& p, uint32_t sm, uint32_t tmem, TcMisc* m,
-                                         PrefixSegs<kTiles, kKeys>& segs) {
-  MmaWarp<HD> x(sm, tmem, m, p.err);
-  PrefixSeg g;
-  Jobs jobs = {false, 0}, next = {false, 0};
-  auto advance = [&](Jobs& j) {
-    const bool more = uniform(segs.next(g)) != 0;
-    if (more) {
-      const Jobs x = seg_jobs(p, g);
-      j.lone = uniform(x.lone) != 0;
-      j.count = uniform(x.count);
-    }
-    return more;
-  };
-  bool more = advance(jobs);
-  if (more) {
-    if (!x.open(jobs, 0, 0) || !x.open(jobs, 1, 0)) return;
-  }
-  while (more) {
-    more = advance(next);
-    const uint32_t qn = x.qs ^ (jobs.lone ? 1u : 0u);
-    if (!(jobs.lone ? x.template run<true>(jobs, more, next, qn) : x.template run<false>(jobs, more, next, qn))) return;
-    x.qs = qn;
-    jobs = next;
+    tiles += 2 * (jobs.lone ? jobs.count : jobs.count >> 1);
+    if (!pass(tiles)) return;
   }
 }
 
@@ -455,7 +456,7 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
       if (n == 0) {
         mx = b;
       } else {
-        const bool raise = (b - mx) * sl > kRaise || (mx == -INFINITY && b > -INFINITY);
+        const bool raise = valid && ((b - mx) * sl > kRaise || (mx == -INFINITY && b > -INFINITY));
         if (__any_sync(0xffffffffu, raise)) {
           // PV of the job before is complete: its product was issued before this score's
           const float keep = !raise || mx == -INFINITY ? 1.f : ex2a((mx - b) * sl);
@@ -470,6 +471,22 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
           }
           sum *= keep;
           if (raise) mx = b;
+        }
+      }
+      if (jobs.lone || t == 0) {
+        // slots of a page past the last key hold anything: their weights are 0, and 0 x V must be 0
+        // (where both streams use the tile, stream 1's turn comes after stream 0's)
+        const int keys = g.k_end - g.k0 - kb * kKeys;
+        if (keys < kKeys) {
+          const int upto = min(kKeys, (keys + p.page - 1) / p.page * p.page);
+          const uint32_t at = tiles + value_tile(jobs, kb - g.kb0), st = at & (TcShape<HD>::kStages - 1);
+          // (the ring is past this place's use before: the products have come to this block's keys)
+          if (!tc_wait(smem_u32(&m->full[st]), (at / TcShape<HD>::kStages) & 1, &m->abort, p.err)) return;
+          uint8_t* v = smp + TcShape<HD>::kRing + st * TcShape<HD>::kTile;
+          for (int c = keys * 8 + row; c < upto * 8; c += kRows)
+            for (int h = 0; h < TcShape<HD>::kHalves; ++h)
+              *reinterpret_cast<uint4*>(v + h * TcShape<HD>::kHalf + c * 16) = make_uint4(0, 0, 0, 0);
+          fence_proxy_async_smem();
         }
       }
       const float base = mx == -INFINITY ? 0.f : -mx * sl;
@@ -487,19 +504,11 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
           w[c >> 1] = pack_bf16(e.x, e.y);
         }
         tmem_st16(ts + 16 * h, w);
-      }
-      if (jobs.lone || t == 0) {
-        // slots of a page past the last key hold anything: their weights are 0, and 0 x V must be 0
-        const int keys = g.k_end - g.k0 - kb * kKeys;
-        if (keys < kKeys) {
-          const int upto = min(kKeys, (keys + p.page - 1) / p.page * p.page), i = kb - g.kb0;
-          const uint32_t at = tiles + (jobs.lone ? i + min(i + 2, jobs.count) : 2 * i + 1), st = at % TcShape<HD>::kStages;
-          if (!tc_wait(smem_u32(&m->full[st]), (at / TcShape<HD>::kStages) & 1, &m->abort, p.err)) return;
-          uint8_t* v = smp + TcShape<HD>::kRing + st * TcShape<HD>::kTile;
-          for (int c = keys * 8 + row; c < upto * 8; c += kRows)
-            for (int h = 0; h < TcShape<HD>::kHalves; ++h)
-              *reinterpret_cast<uint4*>(v + h * TcShape<HD>::kHalf + c * 16) = make_uint4(0, 0, 0, 0);
-          fence_proxy_async_smem();
+        if (32 * (h + 1) == kFirstKeys) {
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&m->p_first[t]));
         }
       }
       acc[0] = add2(add2(acc[0], acc[1]), add2(acc[2], acc[3]));
@@ -526,7 +535,7 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
         if (valid) {
 #pragma unroll
           for (int e = 0; e < 32; e += 4)
-            *reinterpret_cast<float4*>(p.part_o + at * HD + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            *part_chunk<HD>(p.part_o, at, (c + e) / 4) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
         }
       }
     }
@@ -544,16 +553,18 @@ __global__ void __launch_bounds__(kThreads, 1)
   TcMisc* m = reinterpret_cast<TcMisc*>(smp + TcShape<HD>::kMisc);
   const uint32_t sm = smem_u32(smp);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, cta = blockIdx.x;
-  if (threadIdx.x == 256) {
+  if (threadIdx.x == kLoadWarp * 32) {
     for (int i = 0; i < 8; ++i) {
       mbar_init(smem_u32(&m->full[i]), 1);
-      mbar_init(smem_u32(&m->empty[i]), 1);
+      mbar_init(smem_u32(&m->empty[i]), 2);
     }
-    mbar_init(smem_u32(&m->drain), 1);
+    mbar_init(smem_u32(&m->drain), 2);
     for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&m->turn[i]), 1);
       mbar_init(smem_u32(&m->q_full[i]), 1);
-      mbar_init(smem_u32(&m->q_empty[i]), 1);
+      mbar_init(smem_u32(&m->q_empty[i]), 2);
       mbar_init(smem_u32(&m->s_full[i]), 1);
+      mbar_init(smem_u32(&m->p_first[i]), 4);
       mbar_init(smem_u32(&m->p_full[i]), 4);
       mbar_init(smem_u32(&m->o_full[i]), 1);
       mbar_init(smem_u32(&m->o_free[i]), 4);
@@ -564,7 +575,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     tma_prefetch_desc(&mk);
     tma_prefetch_desc(&mv);
   }
-  if (warp == 9) tmem_alloc(smem_u32(&m->tmem), 512);
+  if (warp == kMmaWarp) tmem_alloc(smem_u32(&m->tmem), 512);
   griddep_wait();
   griddep_launch();
   if (warp == 0) {
@@ -577,12 +588,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = m->tmem;
   PrefixSegs<kTiles, kKeys> segs(p, m->sched, m->step_base, m->info, cta);
   // registers: 384 threads x 168 at launch = 256 x 200 (softmax) + 128 x 96 and some left over
-  if (warp >= 8) {
+  if (warp >= kLoadWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-    if (warp == 8)
+    if (warp == kLoadWarp)
       load_role<HD>(p, &mq, &mk, &mv, sm, m, segs);
-    else if (warp == 9)
-      mma_role<HD>(p, sm, tmem, m, segs);
+    else if (warp < kMmaWarp + 2)
+      mma_role<HD>(p, warp - kMmaWarp, sm, tmem, m, segs);
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     softmax_role<HD>(p, warp >> 2, smp, tmem, m, segs);
@@ -596,14 +607,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint64_t t0 = global_ns();
     while (global_ns() - t0 < 1000000ull) {}
   }
-  if (warp == 9) {
-    tc_fence_after();
-    if (lane == 0) {
-      umma_commit(smem_u32(&m->drain));
-      mbar_wait(smem_u32(&m->drain), 0, p.err);
-    }
+  if (warp == kMmaWarp || warp == kMmaWarp + 1) {
+    if (elect_one()) umma_commit(smem_u32(&m->drain));
     __syncwarp();
-    tmem_dealloc(tmem, 512);
+    if (warp == kMmaWarp) {
+      if (lane == 0) mbar_wait(smem_u32(&m->drain), 0, p.err);
+      __syncwarp();
+      tc_fence_after();
+      tmem_dealloc(tmem, 512);
+    }
   }
   __syncthreads();
 }

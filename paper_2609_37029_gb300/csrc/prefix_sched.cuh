@@ -171,6 +171,14 @@ __device__ __forceinline__ PartRows own_rows(const PrefixAttnParams& p, const Pr
   return {own0 + kUnitTiles * (before * p.rep + (int64_t)cta * p.tok_tile * p.rep), min(tokens, p.tok_tile) * p.rep};
 }
 
+// Four dims (chunk c) of workspace row r.  Four rows are interleaved chunk by
+// chunk: a warp whose threads have a row each stores 64 contiguous bytes per four
+// lanes (16 in 32 places before: the stores of a segment took 6000 cycles).
+template <int HD>
+__device__ __forceinline__ float4* part_chunk(float* part_o, int64_t r, int c) {
+  return reinterpret_cast<float4*>(part_o) + ((r >> 2) * (HD / 4) + c) * 4 + (r & 3);
+}
+
 // What a CTA works on at a time: the rows of a unit and a range of key blocks.
 struct PrefixSeg {
   const int32_t* tab;   // row of the table
