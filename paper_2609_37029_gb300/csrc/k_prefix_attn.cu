@@ -172,7 +172,7 @@ __device__ void fma_segment(const PrefixAttnParams& p, FmaSmem<HD>& sm, const Pr
   for (int a = 0; a < 4; ++a) {
     const int r = 4 * ty + a;
     if (r >= rows) continue;
-    const int64_t at = seg.part.row + r;
+    const int64_t at = seg.part + r;
 #pragma unroll
     for (int c = 0; c < kCols; ++c)
       *part_chunk<HD>(p.part_o, at, tx + 16 * c) = make_float4(o[a][c][0], o[a][c][1], o[a][c][2], o[a][c][3]);
@@ -222,50 +222,42 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps) prefix_join_kernel(co
     lo += __popc(__ballot_sync(0xffffffffu, i0 + lane < p.n && p.start[i0 + lane] <= t));
   PrefixSeq r = {-1, 0, 0, 0};
   if (lo >= 0) r = v.info[lo];
-  // segments: the shared part's ranges, then the CTAs of the own item; two of each where a unit has one tile
-  int shared = 0, shared_f = 1, own = 0, own_f = 1, c0 = 0;
-  int64_t shared_row = 0, shared_step = 0, first = 0, last = 0;
-  int shared_second = 0, unit = 0, own_at = 0;
+  // segments: the shared part's ranges, then the CTAs of the own item
+  int shared = 0, own = 0, c0 = 0, unit = 0, own_at = 0;
+  int64_t shared_row = 0, shared_step = 0, first = 0;
   if (t >= r.first && t < r.first + r.rows) {
+    const int tile_rows = p.tok_tile * p.rep;
     if (s.items > 0) {
       const int tile = t / p.tok_tile, u = tile / kUnitTiles;
-      shared_f = kUnitTiles > 1 && (u * kUnitTiles + 1) * p.tok_tile >= p.total ? 2 : 1;
       shared = cdiv(s.blocks, s.per_split);
-      const PartRows at = shared_rows<kUnitTiles>(p, g, 0, u);
-      shared_second = at.second;
-      shared_row = at.row + (tile % kUnitTiles) * at.second + (t % p.tok_tile) * p.rep + hr;
-      shared_step = shared_rows<kUnitTiles>(p, g, 1, u).row - at.row;
+      shared_row = shared_rows<kUnitTiles>(p, g, 0, u) + (tile % kUnitTiles) * tile_rows + (t % p.tok_tile) * p.rep + hr;
+      shared_step = (int64_t)p.units * kUnitTiles * tile_rows;
     }
     const int i = t - r.first, tile = i / p.tok_tile;
     unit = tile / kUnitTiles;
-    own_f = kUnitTiles > 1 && (unit * kUnitTiles + 1) * p.tok_tile >= r.rows ? 2 : 1;
-    own_at = (i % p.tok_tile) * p.rep + hr;
-    const int tokens = min(r.rows - unit * kUnitTiles * p.tok_tile, kUnitTiles * p.tok_tile);
-    own_at += (tile % kUnitTiles) * min(tokens, p.tok_tile) * p.rep;
+    own_at = (tile % kUnitTiles) * tile_rows + (i % p.tok_tile) * p.rep + hr;
     first = v.step_base[lo];
     for (int u = 0; u < unit; ++u) first += (int64_t)own_blocks<kUnitTiles, kBlock>(p, r, s.base, u) * p.nkv;
     const int blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, unit);
     first += (int64_t)g * blocks;
-    last = first + blocks;
-    if (blocks > 0) {                            // CTAs [c0, c1): those that begin before `last`, from the one that has `first`
+    if (blocks > 0) {                            // CTAs [c0, c1): those that begin before the item's end, from the one that has `first`
       int c1 = 0;
       c0 = -1;
       for (int i0 = 0; i0 < p.grid; i0 += 32) {
         const int64_t b = i0 + lane < p.grid ? v.cta_begin[i0 + lane] : INT64_MAX;
         c0 += __popc(__ballot_sync(0xffffffffu, b <= first));
-        c1 += __popc(__ballot_sync(0xffffffffu, b < last));
+        c1 += __popc(__ballot_sync(0xffffffffu, b < first + blocks));
       }
       own = c1 - c0;
     }
   }
-  const int ns = shared * shared_f, all = ns + own * own_f;
+  const int all = shared + own;
   auto row_of = [&](int q) -> int64_t {          // -1: no such segment
     if (q >= all) return -1;
-    if (q < ns) return shared_row + (q / shared_f) * shared_step + (q % shared_f) * shared_second;
-    const int c = c0 + (q - ns) / own_f;
+    if (q < shared) return shared_row + q * shared_step;
+    const int c = c0 + q - shared;
     if (v.cta_begin[c + 1] <= (first > v.cta_begin[c] ? first : v.cta_begin[c])) return -1;   // a CTA without steps
-    const PartRows at = own_rows<kUnitTiles>(p, r, unit, g, c);
-    return at.row + own_at + ((q - ns) % own_f) * at.second;
+    return own_rows<kUnitTiles>(p, r, unit, g, c) + own_at;
   };
   float m = -INFINITY, l = 0.f, o[kVec];
   for (int q = lane; q < all; q += 32) {
@@ -402,8 +394,7 @@ size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms) {
   p->grid = num_sms * per_sm;
   p->splits = choose_splits(p->nkv * p->units, (p->shared_len + block - 1) / block, p->grid);
   const int64_t rows = (int64_t)p->tok_tile * p->rep * unit_tiles, groups = (int64_t)p->nkv * p->units;
-  p->part_rows = std::max<int64_t>(groups, kMaxTurns * p->grid) * rows + (int64_t)unit_tiles * p->nkv * p->rep * p->total +
-                 p->grid * rows;
+  p->part_rows = std::max<int64_t>(groups, kMaxTurns * p->grid) * rows + (int64_t)p->nkv * p->rep * p->total + p->grid * rows;
   p->part_rows = (p->part_rows + 3) / 4 * 4;
   return align256(sched_bytes(p->n, p->grid)) + align256((size_t)p->part_rows * sizeof(float2)) +
          (size_t)p->part_rows * p->d * sizeof(float);

@@ -6,11 +6,12 @@
 // multiply for one while the other takes exponentials.  A segment with two row
 // tiles gives each stream one, both over every key block; a segment with one
 // (few rows: decoding) gives both streams the same rows and alternate key
-// blocks, and each leaves its own partial result.
+// blocks, and stream 0 adds the two up at the end.
 //
 //   warps 0-3, 4-7  streams 0 and 1: thread = row; scores from TMEM, running
 //                   maximum and sum, weights rounded to bf16 back to TMEM over
 //                   the scores, at the end the sums to the workspace
+//   warp 11         plans: what the CTA's segments are, a few ahead of the others
 //   warp 8          loads: query tiles, then key and value blocks, page by page
 //                   (TMA, 128-byte swizzle), into a ring of tiles
 //   warps 9, 10     products of streams 0 and 1: S = Q K^T (both from shared
@@ -41,8 +42,9 @@ namespace lsp {
 namespace {
 
 constexpr int kRows = kPrefixTcRows, kKeys = kPrefixTcKeys, kTiles = kPrefixTcTiles;
-constexpr int kThreads = 384;                   // warp 11 only shares its registers out
-constexpr int kLoadWarp = 8, kMmaWarp = 9;
+constexpr int kThreads = 384;
+constexpr int kLoadWarp = 8, kMmaWarp = 9, kPlanWarp = 11;
+constexpr int kAhead = 4;                        // segments planned ahead
 constexpr int kFirstKeys = 64;                  // keys whose weights are handed over before the rest's (32: 0.84 ms, 96: 0.87)
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRaise = 8.0f;                   // log2 of the most a weight may exceed 1
@@ -58,9 +60,14 @@ struct TcShape {
 };
 
 struct TcMisc {
-  uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_first[2], p_full[2], o_full[2], o_free[2], turn[2], drain;
+  uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_first[2], p_full[2], o_full[2], o_free[2], turn[2], seg_full[kAhead], seg_empty[kAhead], lone_full[2], drain;
   uint32_t tmem;
   int abort;
+  struct Planned {
+    PrefixSeg g;
+    int more;
+  } planned[kAhead];
+  float2 lone_ml[2][kRows];                      // stream 1's maximum and sum of segments with one row tile, by turns
   PrefixSched sched;
   int64_t step_base[kPrefixMaxSeqs + 1];
   PrefixSeq info[kPrefixMaxSeqs];
@@ -228,9 +235,48 @@ __device__ __forceinline__ int stream_jobs(const Jobs& j, int stream) { return (
 __device__ __forceinline__ uint32_t key_tile(const Jobs& j, int i) { return j.lone ? (i > 0 ? 2 * i - 1 : 0) : 2 * i; }
 __device__ __forceinline__ uint32_t value_tile(const Jobs& j, int i) { return j.lone ? i + min(i + 2, j.count) : 2 * i + 1; }
 
+// The plan of the CTA's segments, handed on through shared memory: finding the
+// next one takes some 500 cycles, which nobody should spend between two segments.
+__device__ __forceinline__ void plan_role(const PrefixAttnParams& p, TcMisc* m) {
+  const int lane = threadIdx.x & 31;
+  PrefixSegs<kTiles, kKeys> segs(p, m->sched, m->step_base, m->info, blockIdx.x);
+  bool more = true;
+  for (uint32_t k = 0; more; ++k) {
+    PrefixSeg g;
+    more = segs.next(g);
+    if (!tc_wait(smem_u32(&m->seg_empty[k % kAhead]), ((k / kAhead) & 1) ^ 1, &m->abort, p.err)) return;
+    if (lane == 0) {
+      if (more) m->planned[k % kAhead].g = g;
+      m->planned[k % kAhead].more = more;
+      mbar_arrive(smem_u32(&m->seg_full[k % kAhead]));
+    }
+    // the table entries that the loads will ask for
+    if (more)
+      for (int at = (g.k0 + g.kb0 * kKeys) / p.page + lane * 32, end = cdiv(min(g.k_end, g.k0 + g.kb1 * kKeys), p.page); at < end; at += 32 * 32)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(g.tab + at));
+    __syncwarp();
+  }
+}
+// One reader of the plan: every warp of the other roles.
+struct SegReader {
+  TcMisc* m;
+  unsigned* err;
+  uint32_t k = 0;
+  __device__ __forceinline__ bool next(PrefixSeg& g) {
+    const uint32_t at = k % kAhead;
+    if (!tc_wait(smem_u32(&m->seg_full[at]), (k / kAhead) & 1, &m->abort, err)) return false;
+    const bool more = m->planned[at].more;
+    if (more) g = m->planned[at].g;
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&m->seg_empty[at]));
+    ++k;
+    return more;
+  }
+};
+
 template <int HD>
 __device__ __forceinline__ void load_role(const PrefixAttnParams& p, const CUtensorMap* mq, const CUtensorMap* mk,
-                                          const CUtensorMap* mv, uint32_t sm, TcMisc* m, PrefixSegs<kTiles, kKeys>& segs) {
+                                          const CUtensorMap* mv, uint32_t sm, TcMisc* m, SegReader segs) {
   using Sh = TcShape<HD>;
   const int lane = threadIdx.x & 31;
   const int box = min(p.page, kKeys), boxes = kKeys / box;
@@ -305,7 +351,7 @@ __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, 
 // neither is ever more than a phase from the other.
 template <int HD>
 __device__ __forceinline__ void mma_role(const PrefixAttnParams& p, int t, uint32_t sm, uint32_t tmem, TcMisc* m,
-                                         PrefixSegs<kTiles, kKeys>& segs) {
+                                         SegReader segs) {
   using Sh = TcShape<HD>;
   constexpr uint32_t kIdescS = idesc_bf16(kKeys, false), kIdescO = idesc_bf16(HD, true), kTileDesc = Sh::kTile >> 4;
   const uint32_t qd = desc_lo(sm, 16), kd = desc_lo(sm + Sh::kRing, 16), vd = desc_lo(sm + Sh::kRing, Sh::kHalf);
@@ -427,12 +473,13 @@ __device__ __forceinline__ void mma_role(const PrefixAttnParams& p, int t, uint3
 
 template <int HD>
 __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, uint8_t* smp, uint32_t tmem, TcMisc* m,
-                                             PrefixSegs<kTiles, kKeys>& segs) {
+                                             SegReader segs) {
   const int lane = threadIdx.x & 31, quad = (threadIdx.x >> 5) & 3, row = quad * 32 + lane;
   const uint32_t ts = tmem + ((uint32_t)(quad * 32) << 16) + 128u * t, to = ts + 256u;
   const int tok = row / p.rep;
   const float sl = p.scale * kLog2e;
-  uint32_t ns = 0, no = 0, tiles = 0;            // jobs, segments; ring tiles of the segments before
+  uint32_t ns = 0, no = 0, no1 = 0;              // jobs; segments of this stream, of stream 1 (as stream 0 sees them)
+  uint32_t lones = 0, tiles = 0;                 // segments that both streams add up; ring tiles of the segments before
   PrefixSeg g;
   while (segs.next(g)) {
     const Jobs jobs = seg_jobs(p, g);
@@ -518,29 +565,64 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&m->p_full[t]));
     }
-    const int64_t at = g.part.row + (t ? g.part.second : 0) + row;
-    if (mine > 0) {
-      if (!tc_wait(smem_u32(&m->o_full[t]), no & 1, &m->abort, p.err)) return;
-      ++no;
-      tc_fence_after();
+    tiles += 2 * (g.kb1 - g.kb0);
+    const bool pair = jobs.lone && jobs.count > 1;         // stream 1's part of the same rows is added here
+    if (pair) {
+      if (t == 1) {
+        m->lone_ml[lones & 1][row] = make_float2(mx, sum);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&m->lone_full[lones & 1]));
+        ++lones;                                 // (at most one segment ahead of stream 0: it frees the sums)
+        ++no;
+        continue;
+      }
+    } else if (mine == 0) {
+      continue;
+    }
+    if (!tc_wait(smem_u32(&m->o_full[t]), no & 1, &m->abort, p.err)) return;
+    ++no;
+    float w0 = 1.f, w1 = 0.f;
+    if (t == 0 && jobs.count > 1) {              // (two row tiles: stream 1 waits for its own)
+      if (pair) {
+        if (!tc_wait(smem_u32(&m->o_full[1]), no1 & 1, &m->abort, p.err)) return;
+        if (!tc_wait(smem_u32(&m->lone_full[lones & 1]), (lones >> 1) & 1, &m->abort, p.err)) return;
+        const float2 other = m->lone_ml[lones & 1][row];
+        ++lones;
+        const float top = fmaxf(mx, other.x);
+        w0 = mx == -INFINITY ? 0.f : ex2a((mx - top) * sl);
+        w1 = other.x == -INFINITY ? 0.f : ex2a((other.x - top) * sl);
+        mx = top;
+        sum = sum * w0 + other.y * w1;
+      }
+      ++no1;
+    }
+    tc_fence_after();
+    const int64_t at = g.part + (!jobs.lone && t ? p.tok_tile * p.rep : 0) + row;
 #pragma unroll 1
-      for (int c = 0; c < HD; c += 32) {
-        float o[32];
-        tmem_ld32(to + c, o);
-        if (c + 32 == HD) {                      // the sums are in registers: the next segment may start
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&m->o_free[t]));
-        }
-        if (valid) {
+    for (int c = 0; c < HD; c += 32) {
+      float o[32];
+      tmem_ld32(to + c, o);
+      if (pair) {
+        float x[32];
+        tmem_ld32(to + 128 + c, x);
 #pragma unroll
-          for (int e = 0; e < 32; e += 4)
-            *part_chunk<HD>(p.part_o, at, (c + e) / 4) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        for (int e = 0; e < 32; ++e) o[e] = o[e] * w0 + x[e] * w1;
+      }
+      if (c + 32 == HD) {                        // the sums are in registers: the next segment may start
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(smem_u32(&m->o_free[t]));
+          if (pair) mbar_arrive(smem_u32(&m->o_free[1]));
         }
+      }
+      if (valid) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 4)
+          *part_chunk<HD>(p.part_o, at, (c + e) / 4) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
       }
     }
     if (valid) p.part_ml[at] = make_float2(mx == -INFINITY ? mx : mx * sl, sum);
-    tiles += 2 * (g.kb1 - g.kb0);
   }
 }
 
@@ -558,6 +640,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(smem_u32(&m->full[i]), 1);
       mbar_init(smem_u32(&m->empty[i]), 2);
     }
+    for (int i = 0; i < kAhead; ++i) {
+      mbar_init(smem_u32(&m->seg_full[i]), 1);
+      mbar_init(smem_u32(&m->seg_empty[i]), 11);
+    }
+    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&m->lone_full[i]), 4);
     mbar_init(smem_u32(&m->drain), 2);
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&m->turn[i]), 1);
@@ -586,7 +673,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = m->tmem;
-  PrefixSegs<kTiles, kKeys> segs(p, m->sched, m->step_base, m->info, cta);
+  const SegReader segs{m, p.err};
   // registers: 384 threads x 168 at launch = 256 x 200 (softmax) + 128 x 96 and some left over
   if (warp >= kLoadWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
@@ -594,6 +681,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       load_role<HD>(p, &mq, &mk, &mv, sm, m, segs);
     else if (warp < kMmaWarp + 2)
       mma_role<HD>(p, warp - kMmaWarp, sm, tmem, m, segs);
+    else
+      plan_role(p, m);
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     softmax_role<HD>(p, warp >> 2, smp, tmem, m, segs);

@@ -20,10 +20,12 @@
 // Every segment (an item, or the part of an own item that one CTA has) leaves
 // unnormalised sums and the running maximum and sum of its rows in rows of the
 // workspace; a second kernel joins a row's segments.  Shared segments lie at
-// ((head, range), unit); an own segment at kUnit * (rows of the items before
-// it) + CTA * (rows of a unit), which no two share: along the line the item or
-// the CTA rises from segment to segment, each by at least the room of one.
+// ((head, range), unit); an own segment at (rows of the items before it) + CTA *
+// (rows of a unit), which no two share: along the line the item or the CTA rises
+// from segment to segment, each by at least the room of one.
 #pragma once
+
+#include <climits>
 
 #include "common.cuh"
 #include "lsp_internal.h"
@@ -144,31 +146,29 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
 // First own step of CTA c (c == grid: the end).  CTAs below items % grid have
 // one shared item more than the rest; the rest get per_split own steps before
 // the others get any.
+__device__ __forceinline__ int64_t part_of(int64_t steps, int k, int n) {     // steps * k / n
+  return steps < (1 << 21) ? (int64_t)((uint32_t)steps * (uint32_t)k / (uint32_t)n) : steps * k / n;   // k <= grid < 2^11
+}
 __device__ __forceinline__ int64_t own_begin(const PrefixSched& s, int grid, int c) {
   const int more = s.items % grid, less = grid - more;
   const int64_t fill = (int64_t)less * s.per_split;
-  if (more > 0 && s.own_steps <= fill) return c <= more ? 0 : s.own_steps * (c - more) / less;
+  if (more > 0 && s.own_steps <= fill) return c <= more ? 0 : part_of(s.own_steps, c - more, less);
   const int64_t even = more > 0 ? s.own_steps - fill : s.own_steps;
-  return even * c / grid + (more > 0 && c > more ? (int64_t)(c - more) * s.per_split : 0);
+  return part_of(even, c, grid) + (more > 0 && c > more ? (int64_t)(c - more) * s.per_split : 0);
 }
 
-// Workspace rows: the first row of a segment, and where its second tile (or the
-// second stream of a unit with one tile) starts.
-struct PartRows {
-  int64_t row;
-  int second;
-};
+// Workspace rows: the first row of a segment; its second tile's rows follow its
+// first's (tok_tile * rep of them).
 template <int kUnitTiles>
-__device__ __forceinline__ PartRows shared_rows(const PrefixAttnParams& p, int head, int split, int unit) {
-  const int tile = p.tok_tile * p.rep;
-  return {((int64_t)(head * p.splits + split) * p.units + unit) * kUnitTiles * tile, tile};
+__device__ __forceinline__ int64_t shared_rows(const PrefixAttnParams& p, int head, int split, int unit) {
+  return ((int64_t)(head * p.splits + split) * p.units + unit) * kUnitTiles * p.tok_tile * p.rep;
 }
 template <int kUnitTiles>
-__device__ __forceinline__ PartRows own_rows(const PrefixAttnParams& p, const PrefixSeq& r, int unit, int head, int cta) {
+__device__ __forceinline__ int64_t own_rows(const PrefixAttnParams& p, const PrefixSeq& r, int unit, int head, int cta) {
   const int t0 = unit * kUnitTiles * p.tok_tile, tokens = min(r.rows - t0, kUnitTiles * p.tok_tile);
   const int64_t before = (int64_t)p.nkv * (r.first + t0) + (int64_t)head * tokens;
   const int64_t own0 = (int64_t)p.nkv * p.splits * p.units * kUnitTiles * p.tok_tile * p.rep;
-  return {own0 + kUnitTiles * (before * p.rep + (int64_t)cta * p.tok_tile * p.rep), min(tokens, p.tok_tile) * p.rep};
+  return own0 + before * p.rep + (int64_t)cta * kUnitTiles * p.tok_tile * p.rep;
 }
 
 // Four dims (chunk c) of workspace row r.  Four rows are interleaved chunk by
@@ -187,7 +187,7 @@ struct PrefixSeg {
   int k0, k_end;        // keys: tokens [k0, k_end) of the sequence
   int kb0, kb1;         // blocks of them, from k0 on
   int see0;             // token i of the unit sees tokens below min(see0 + i, k_end)
-  PartRows part;
+  int64_t part;         // its first row of the workspace
 };
 
 // The segments of a CTA in order: its shared items, then its piece of the own line.
@@ -243,7 +243,7 @@ struct PrefixSegs {
       rel -= (int64_t)blocks * p.nkv;
       blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, ++u);
     }
-    g.head = (int)(rel / blocks);
+    g.head = rel < INT_MAX ? (int)rel / blocks : (int)(rel / blocks);
     g.kb0 = (int)(rel - (int64_t)g.head * blocks);
     g.kb1 = (int)min((int64_t)blocks, g.kb0 + (end - x));
     g.tab = p.table + (size_t)r.seq * p.max_pages;
