@@ -192,7 +192,6 @@ __global__ void __launch_bounds__(kFmaThreads) prefix_attn_fma_kernel(const Pref
     if (threadIdx.x == 0) sm.sched = s;
   }
   __syncthreads();
-  if (cta == 0) publish_sched(p, sm.sched, sm.step_base, sm.info);
   PrefixSegs<1, kFmaKeys> segs(p, sm.sched, sm.step_base, sm.info, cta);
   PrefixSeg seg;
   while (segs.next(seg)) fma_segment<HD>(p, sm, seg);
@@ -204,139 +203,167 @@ __global__ void __launch_bounds__(kFmaThreads) prefix_attn_fma_kernel(const Pref
 // are independent loads.  A CTA has four consecutive rows, whose sums share cache
 // lines.  Four warps a row where the rows alone would leave most of the GPU idle
 // (few rows have many segments), one where they fill it.
+//
+// Bound by the latency of its three dependent rounds of loads.  Where the
+// segments are follows from the lengths alone, so every CTA finds that out again
+// before it waits for the main kernel (which lets it start only after its own
+// wait: the lengths are final).
 constexpr int kJoinRows = 4;
 template <typename T, int HD, int kUnitTiles, int kBlock, int kWarps>
 __global__ void __launch_bounds__(32 * kJoinRows * kWarps) prefix_join_kernel(const PrefixAttnParams p) {
   constexpr int kVec = HD / 32, kAhead = 8;
+  extern __shared__ __align__(16) uint8_t join_raw[];
   __shared__ float s_o[kWarps > 1 ? kJoinRows * kWarps : 1][HD], s_l[kJoinRows * kWarps];
-  griddep_wait();
-  griddep_launch();
+  __shared__ PrefixSched s_sched;
+  PrefixSeq* info = reinterpret_cast<PrefixSeq*>(join_raw);
+  int64_t* step_base = reinterpret_cast<int64_t*>(info + p.n);
+  int64_t* cta_begin = step_base + p.n + 1;      // [grid + 1]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp / kJoinRows;
-  const int64_t rows = (int64_t)p.total * p.nq, mine = (int64_t)blockIdx.x * kJoinRows + warp % kJoinRows;
-  const int64_t w = mine < rows ? mine : rows - 1;   // a row past the last does the last's work, and stores nothing
-  const int t = (int)(w / p.nq), h = (int)(w % p.nq), g = h / p.rep, hr = h % p.rep;
-  const SchedView v = sched_view(p);
-  const PrefixSched s = *v.s;
-  int lo = -1;                                   // the last sequence that starts at or before t
-  for (int i0 = 0; i0 < p.n; i0 += 32)
-    lo += __popc(__ballot_sync(0xffffffffu, i0 + lane < p.n && p.start[i0 + lane] <= t));
-  PrefixSeq r = {-1, 0, 0, 0};
-  if (lo >= 0) r = v.info[lo];
-  // segments: the shared part's ranges, then the CTAs of the own item
-  int shared = 0, own = 0, c0 = 0, unit = 0, own_at = 0;
-  int64_t shared_row = 0, shared_step = 0, first = 0;
-  if (t >= r.first && t < r.first + r.rows) {
-    const int tile_rows = p.tok_tile * p.rep;
-    if (s.items > 0) {
-      const int tile = t / p.tok_tile, u = tile / kUnitTiles;
-      shared = cdiv(s.blocks, s.per_split);
-      shared_row = shared_rows<kUnitTiles>(p, g, 0, u) + (tile % kUnitTiles) * tile_rows + (t % p.tok_tile) * p.rep + hr;
-      shared_step = (int64_t)p.units * kUnitTiles * tile_rows;
-    }
-    const int i = t - r.first, tile = i / p.tok_tile;
-    unit = tile / kUnitTiles;
-    own_at = (tile % kUnitTiles) * tile_rows + (i % p.tok_tile) * p.rep + hr;
-    first = v.step_base[lo];
-    for (int u = 0; u < unit; ++u) first += (int64_t)own_blocks<kUnitTiles, kBlock>(p, r, s.base, u) * p.nkv;
-    const int blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, unit);
-    first += (int64_t)g * blocks;
-    if (blocks > 0) {                            // CTAs [c0, c1): those that begin before the item's end, from the one that has `first`
-      int c1 = 0;
-      c0 = -1;
-      for (int i0 = 0; i0 < p.grid; i0 += 32) {
-        const int64_t b = i0 + lane < p.grid ? v.cta_begin[i0 + lane] : INT64_MAX;
-        c0 += __popc(__ballot_sync(0xffffffffu, b <= first));
-        c1 += __popc(__ballot_sync(0xffffffffu, b < first + blocks));
+  if (warp == 0) {
+    const PrefixSched s = build_sched<kUnitTiles, kBlock>(p, step_base, info, false);
+    if (lane == 0) s_sched = s;
+  }
+  __syncthreads();
+  const PrefixSched s = s_sched;
+  for (int c = threadIdx.x; c <= p.grid; c += blockDim.x) cta_begin[c] = own_begin(s, p.grid, c);
+  __syncthreads();
+  const int64_t rows = (int64_t)p.total * p.nq;
+  bool waited = false;
+  for (int64_t w0 = (int64_t)blockIdx.x * kJoinRows; w0 < rows; w0 += (int64_t)gridDim.x * kJoinRows) {
+    const int64_t mine = w0 + warp % kJoinRows;
+    const int64_t w = mine < rows ? mine : rows - 1;   // a row past the last does the last's work, and stores nothing
+    const int t = (int)(w / p.nq), h = (int)(w % p.nq), g = h / p.rep, hr = h % p.rep;
+    int lo = -1;                                 // the last sequence that starts at or before t
+    for (int i0 = 0; i0 < p.n; i0 += 32)
+      lo += __popc(__ballot_sync(0xffffffffu, i0 + lane < p.n && info[i0 + lane].first <= t));
+    PrefixSeq r = {-1, 0, 0, 0};
+    if (lo >= 0) r = info[lo];
+    // segments: the shared part's ranges, then the CTAs of the own item
+    int shared = 0, own = 0, c0 = 0, unit = 0, own_at = 0;
+    int64_t shared_row = 0, shared_step = 0, first = 0;
+    if (t >= r.first && t < r.first + r.rows) {
+      const int tile_rows = p.tok_tile * p.rep;
+      if (s.items > 0) {
+        const int tile = t / p.tok_tile, u = tile / kUnitTiles;
+        shared = cdiv(s.blocks, s.per_split);
+        shared_row = shared_rows<kUnitTiles>(p, g, 0, u) + (tile % kUnitTiles) * tile_rows + (t % p.tok_tile) * p.rep + hr;
+        shared_step = (int64_t)p.units * kUnitTiles * tile_rows;
       }
-      own = c1 - c0;
+      const int i = t - r.first, tile = i / p.tok_tile;
+      unit = tile / kUnitTiles;
+      own_at = (tile % kUnitTiles) * tile_rows + (i % p.tok_tile) * p.rep + hr;
+      first = step_base[lo];
+      for (int u = 0; u < unit; ++u) first += (int64_t)own_blocks<kUnitTiles, kBlock>(p, r, s.base, u) * p.nkv;
+      const int blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, unit);
+      first += (int64_t)g * blocks;
+      if (blocks > 0) {                          // CTAs [c0, c1): those that begin before the item's end, from the one that has `first`
+        int c1 = 0;
+        c0 = -1;
+        for (int i0 = 0; i0 < p.grid; i0 += 32) {
+          const int64_t b = i0 + lane < p.grid ? cta_begin[i0 + lane] : INT64_MAX;
+          c0 += __popc(__ballot_sync(0xffffffffu, b <= first));
+          c1 += __popc(__ballot_sync(0xffffffffu, b < first + blocks));
+        }
+        own = c1 - c0;
+      }
     }
-  }
-  const int all = shared + own;
-  auto row_of = [&](int q) -> int64_t {          // -1: no such segment
-    if (q >= all) return -1;
-    if (q < shared) return shared_row + q * shared_step;
-    const int c = c0 + q - shared;
-    if (v.cta_begin[c + 1] <= (first > v.cta_begin[c] ? first : v.cta_begin[c])) return -1;   // a CTA without steps
-    return own_rows<kUnitTiles>(p, r, unit, g, c) + own_at;
-  };
-  float m = -INFINITY, l = 0.f, o[kVec];
-  for (int q = lane; q < all; q += 32) {
-    const int64_t row = row_of(q);
-    if (row >= 0) m = fmaxf(m, p.part_ml[row].x);
-  }
-  m = warp_max(m);
-#pragma unroll
-  for (int e = 0; e < kVec; ++e) o[e] = 0.f;
-  for (int q0 = 0; q0 < all && m > -INFINITY; q0 += 32 * kWarps) {
-    const int64_t row = row_of(q0 + lane * kWarps + part);
-    float x = 0.f;
-    if (row >= 0) {
-      const float2 ml = p.part_ml[row];
-      x = ml.x == -INFINITY ? 0.f : ex2a(ml.x - m);
-      l += x * ml.y;
+    const int all = shared + own;
+    auto row_of = [&](int q) -> int64_t {        // -1: no such segment
+      if (q >= all) return -1;
+      if (q < shared) return shared_row + q * shared_step;
+      const int c = c0 + q - shared;
+      if (cta_begin[c + 1] <= (first > cta_begin[c] ? first : cta_begin[c])) return -1;   // a CTA without steps
+      return own_rows<kUnitTiles>(p, r, unit, g, c) + own_at;
+    };
+    int64_t row0 = row_of(lane);
+    if (!waited) {
+      griddep_wait();
+      griddep_launch();
+      waited = true;
     }
-    const unsigned has = __ballot_sync(0xffffffffu, x > 0.f);
-    for (unsigned left = has; left;) {
-      float y[kAhead][kVec], f[kAhead];
+    float m = -INFINITY, l = 0.f, o[kVec];
+    for (int q = lane; q < all; q += 32) {
+      const int64_t row = q == lane ? row0 : row_of(q);
+      if (row >= 0) m = fmaxf(m, p.part_ml[row].x);
+    }
+    m = warp_max(m);
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int src = left ? __ffs(left) - 1 : 0;
-        const bool on = left != 0;
-        left &= left - 1;
-        const int64_t at = __shfl_sync(0xffffffffu, row, src);
-        f[k] = on ? __shfl_sync(0xffffffffu, x, src) : 0.f;
+    for (int e = 0; e < kVec; ++e) o[e] = 0.f;
+    for (int q0 = 0; q0 < all && m > -INFINITY; q0 += 32 * kWarps) {
+      const int64_t row = row_of(q0 + lane * kWarps + part);
+      float x = 0.f;
+      if (row >= 0) {
+        const float2 ml = p.part_ml[row];
+        x = ml.x == -INFINITY ? 0.f : ex2a(ml.x - m);
+        l += x * ml.y;
+      }
+      const unsigned has = __ballot_sync(0xffffffffu, x > 0.f);
+      for (unsigned left = has; left;) {
+        float y[kAhead][kVec], f[kAhead];
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) y[k][e] = 0.f;
-        if (on) {
-          if constexpr (kVec == 4) {
-            const float4 z = *part_chunk<HD>(p.part_o, at, lane);
-            y[k][0] = z.x; y[k][1] = z.y; y[k][2] = z.z; y[k][3] = z.w;
-          } else {
-            const float2 z = reinterpret_cast<const float2*>(part_chunk<HD>(p.part_o, at, lane >> 1))[lane & 1];
-            y[k][0] = z.x; y[k][1] = z.y;
+        for (int k = 0; k < kAhead; ++k) {
+          const int src = left ? __ffs(left) - 1 : 0;
+          const bool on = left != 0;
+          left &= left - 1;
+          const int64_t at = __shfl_sync(0xffffffffu, row, src);
+          f[k] = on ? __shfl_sync(0xffffffffu, x, src) : 0.f;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) y[k][e] = 0.f;
+          if (on) {
+            if constexpr (kVec == 4) {
+              const float4 z = *part_chunk<HD>(p.part_o, at, lane);
+              y[k][0] = z.x; y[k][1] = z.y; y[k][2] = z.z; y[k][3] = z.w;
+            } else {
+              const float2 z = reinterpret_cast<const float2*>(part_chunk<HD>(p.part_o, at, lane >> 1))[lane & 1];
+              y[k][0] = z.x; y[k][1] = z.y;
+            }
           }
         }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) o[e] = fmaf(y[k][e], f[k], o[e]);
       }
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) o[e] = fmaf(y[k][e], f[k], o[e]);
     }
-  }
-  l = warp_sum(l);
-  if constexpr (kWarps > 1) {
+    l = warp_sum(l);
+    if constexpr (kWarps > 1) {
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) s_o[warp][lane * kVec + e] = o[e];
-    if (lane == 0) s_l[warp] = l;
-    __syncthreads();
-    if (part > 0) return;
-    l = 0.f;
-    for (int k = 0; k < kWarps; ++k) l += s_l[k * kJoinRows + warp];
+      for (int e = 0; e < kVec; ++e) s_o[warp][lane * kVec + e] = o[e];
+      if (lane == 0) s_l[warp] = l;
+      __syncthreads();
+      if (part == 0) {
+        l = 0.f;
+        for (int k = 0; k < kWarps; ++k) l += s_l[k * kJoinRows + warp];
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) {
-      o[e] = 0.f;
-      for (int k = 0; k < kWarps; ++k) o[e] += s_o[k * kJoinRows + warp][lane * kVec + e];
+        for (int e = 0; e < kVec; ++e) {
+          o[e] = 0.f;
+          for (int k = 0; k < kWarps; ++k) o[e] += s_o[k * kJoinRows + warp][lane * kVec + e];
+        }
+      }
+      __syncthreads();
     }
-  }
-  if (mine >= rows) return;
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  T* out = static_cast<T*>(p.out) + w * HD + lane * kVec;
-  if constexpr (sizeof(T) == 2 && kVec == 4)
-    *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-  else
+    if (mine >= rows || part > 0) continue;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    T* out = static_cast<T*>(p.out) + w * HD + lane * kVec;
+    if constexpr (sizeof(T) == 2 && kVec == 4)
+      *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+    else
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) out[e] = from_f<T>(o[e] * inv);
-  if (p.lse && lane == 0) p.lse[w] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
+      for (int e = 0; e < kVec; ++e) out[e] = from_f<T>(o[e] * inv);
+    if (p.lse && lane == 0) p.lse[w] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * kLn2;
+  }
+  if (!waited) griddep_wait();
 }
 
 template <typename T, int HD, int kUnitTiles, int kBlock>
 int launch_join(const PrefixAttnParams& p, cudaStream_t s) {
-  const int64_t rows = (int64_t)p.total * p.nq;
-  const dim3 grid((unsigned)((rows + kJoinRows - 1) / kJoinRows));
+  const int64_t rows = (int64_t)p.total * p.nq, ctas = (rows + kJoinRows - 1) / kJoinRows;
+  const size_t smem = p.n * (sizeof(PrefixSeq) + sizeof(int64_t)) + (p.grid + 2) * sizeof(int64_t);
   const bool few = rows < 16 * (int64_t)p.num_sms;
   const cudaError_t e =
-      few ? launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 4>, grid, dim3(128 * kJoinRows), 0, s, p)
-          : launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 1>, grid, dim3(32 * kJoinRows), 0, s, p);
+      few ? launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 4>, dim3((unsigned)ctas), dim3(128 * kJoinRows), smem, s, p)
+          : launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 1>, dim3((unsigned)std::min<int64_t>(ctas, 8 * p.num_sms)),
+                       dim3(32 * kJoinRows), smem, s, p);
   return e == cudaSuccess ? LSP_OK : LSP_ERR_CUDA;
 }
 
@@ -396,14 +423,11 @@ size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms) {
   const int64_t rows = (int64_t)p->tok_tile * p->rep * unit_tiles, groups = (int64_t)p->nkv * p->units;
   p->part_rows = std::max<int64_t>(groups, kMaxTurns * p->grid) * rows + (int64_t)p->nkv * p->rep * p->total + p->grid * rows;
   p->part_rows = (p->part_rows + 3) / 4 * 4;
-  return align256(sched_bytes(p->n, p->grid)) + align256((size_t)p->part_rows * sizeof(float2)) +
-         (size_t)p->part_rows * p->d * sizeof(float);
+  return align256((size_t)p->part_rows * sizeof(float2)) + (size_t)p->part_rows * p->d * sizeof(float);
 }
 
 int launch_prefix_attention(PrefixAttnParams p, int dtype, void* ws, cudaStream_t s) {
   char* w = static_cast<char*>(ws);
-  p.sched = w;
-  w += align256(sched_bytes(p.n, p.grid));
   p.part_ml = reinterpret_cast<float2*>(w);
   w += align256((size_t)p.part_rows * sizeof(float2));
   p.part_o = reinterpret_cast<float*>(w);

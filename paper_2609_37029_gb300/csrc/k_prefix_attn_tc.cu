@@ -687,7 +687,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     softmax_role<HD>(p, warp >> 2, smp, tmem, m, segs);
   }
-  if (cta == 0) publish_sched(p, m->sched, m->step_base, m->info);
   tc_fence_before();
   __syncthreads();
   // Every load has been waited for by its product, unless a wait gave up: then

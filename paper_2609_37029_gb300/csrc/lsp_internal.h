@@ -313,7 +313,6 @@ struct PrefixAttnParams {
   int num_sms;
   int grid;                 // CTAs of the main kernel
   int64_t part_rows;        // rows of partial results the workspace holds
-  char* sched;              // the schedule, for the joining kernel
   float* part_o;            // [part_rows][d] unnormalised sums
   float2* part_ml;          // [part_rows] (running maximum of the base-2 scores, sum)
 };

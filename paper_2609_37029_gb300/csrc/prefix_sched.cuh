@@ -19,7 +19,8 @@
 //
 // Every segment (an item, or the part of an own item that one CTA has) leaves
 // unnormalised sums and the running maximum and sum of its rows in rows of the
-// workspace; a second kernel joins a row's segments.  Shared segments lie at
+// workspace; a second kernel joins a row's segments, which it finds by the same
+// arithmetic.  Shared segments lie at
 // ((head, range), unit); an own segment at (rows of the items before it) + CTA *
 // (rows of a unit), which no two share: along the line the item or the CTA rises
 // from segment to segment, each by at least the room of one.
@@ -39,31 +40,9 @@ struct PrefixSched {
   int items;            // shared items
   int64_t own_steps;    // key blocks of the own part
 };
-// The schedule in the workspace, for the joining kernel: PrefixSched, the first
-// own step of every sequence and of every CTA, the sequences.
-struct SchedView {
-  PrefixSched* s;
-  int64_t* step_base;   // [n + 1]
-  int64_t* cta_begin;   // [grid + 1]
-  struct PrefixSeq* info;   // [n]
-};
-
 struct __align__(16) PrefixSeq {
   int seq, first, rows, len;    // row of the table (-1: none), first row of q, rows, tokens
 };
-
-__host__ __device__ inline size_t sched_bytes(int n, int grid) {
-  return 32 + 8 * ((size_t)n + 1) + 8 * ((size_t)grid + 1) + sizeof(PrefixSeq) * ((size_t)n + 1);
-}
-__device__ __forceinline__ SchedView sched_view(const PrefixAttnParams& p) {
-  SchedView v;
-  v.s = reinterpret_cast<PrefixSched*>(p.sched);
-  v.step_base = reinterpret_cast<int64_t*>(p.sched + 32);
-  v.cta_begin = v.step_base + p.n + 1;
-  const size_t at = 32 + 8 * ((size_t)p.n + 1) + 8 * ((size_t)p.grid + 1);
-  v.info = reinterpret_cast<PrefixSeq*>(p.sched + (at + 15) / 16 * 16);
-  return v;
-}
 
 __device__ __forceinline__ int cdiv(int a, int b) { return (a + b - 1) / b; }
 
@@ -258,15 +237,5 @@ struct PrefixSegs {
     return true;
   }
 };
-
-// The schedule goes to the workspace for the joining kernel (every thread of CTA 0).
-__device__ __forceinline__ void publish_sched(const PrefixAttnParams& p, const PrefixSched& s, const int64_t* step_base,
-                                              const PrefixSeq* info) {
-  const SchedView v = sched_view(p);
-  if (threadIdx.x == 0) *v.s = s;
-  for (int i = threadIdx.x; i <= p.n; i += blockDim.x) v.step_base[i] = step_base[i];
-  for (int i = threadIdx.x; i < p.n; i += blockDim.x) v.info[i] = info[i];
-  for (int c = threadIdx.x; c <= p.grid; c += blockDim.x) v.cta_begin[c] = own_begin(s, p.grid, c);
-}
 
 }  // namespace lsp
