@@ -35,7 +35,7 @@ struct FmaSmem {
   float kv[kFmaKeys][HD + 4];
   float p[kFmaRows][kFmaKeys + 4];
   int64_t at[kFmaKeys];                          // element offset of each key of the block, -1: none
-  int64_t step_base[kPrefixMaxSeqs + 1];
+  int64_t line_base[kPrefixMaxSeqs + 1];
   PrefixSeq info[kPrefixMaxSeqs];
   PrefixSched sched;
 };
@@ -188,13 +188,14 @@ __global__ void __launch_bounds__(kFmaThreads) prefix_attn_fma_kernel(const Pref
   griddep_launch();
   const int cta = blockIdx.x;
   if (threadIdx.x < 32) {
-    const PrefixSched s = build_sched<1, kFmaKeys>(p, sm.step_base, sm.info, cta == 0);
+    const PrefixSched s = build_sched<1, kFmaKeys>(p, sm.line_base, sm.info, cta == 0);
     if (threadIdx.x == 0) sm.sched = s;
   }
   __syncthreads();
-  PrefixSegs<1, kFmaKeys> segs(p, sm.sched, sm.step_base, sm.info, cta);
+  PrefixSegs<1, kFmaKeys> segs(p, sm.sched, sm.line_base, sm.info, cta);
   PrefixSeg seg;
-  while (segs.next(seg)) fma_segment<HD>(p, sm, seg);
+  while (segs.next_shared(seg)) fma_segment<HD>(p, sm, seg);
+  while (segs.next_own(seg)) fma_segment<HD>(p, sm, seg);
 }
 
 // Joins the segments of an output row (token, query head): kWarps warps a row
@@ -216,11 +217,11 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps) prefix_join_kernel(co
   __shared__ float s_o[kWarps > 1 ? kJoinRows * kWarps : 1][HD], s_l[kJoinRows * kWarps];
   __shared__ PrefixSched s_sched;
   PrefixSeq* info = reinterpret_cast<PrefixSeq*>(join_raw);
-  int64_t* step_base = reinterpret_cast<int64_t*>(info + p.n);
-  int64_t* cta_begin = step_base + p.n + 1;      // [grid + 1]
+  int64_t* line_base = reinterpret_cast<int64_t*>(info + p.n);
+  int64_t* cta_begin = line_base + p.n + 1;      // [grid + 1]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp / kJoinRows;
   if (warp == 0) {
-    const PrefixSched s = build_sched<kUnitTiles, kBlock>(p, step_base, info, false);
+    const PrefixSched s = build_sched<kUnitTiles, kBlock>(p, line_base, info, false);
     if (lane == 0) s_sched = s;
   }
   __syncthreads();
@@ -239,7 +240,7 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps) prefix_join_kernel(co
     PrefixSeq r = {-1, 0, 0, 0};
     if (lo >= 0) r = info[lo];
     // segments: the shared part's ranges, then the CTAs of the own item
-    int shared = 0, own = 0, c0 = 0, unit = 0, own_at = 0;
+    int shared = 0, own = 0, c0 = 0, unit = 0, own_at = 0, blocks = 0, cost = 1;
     int64_t shared_row = 0, shared_step = 0, first = 0;
     if (t >= r.first && t < r.first + r.rows) {
       const int tile_rows = p.tok_tile * p.rep;
@@ -252,17 +253,20 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps) prefix_join_kernel(co
       const int i = t - r.first, tile = i / p.tok_tile;
       unit = tile / kUnitTiles;
       own_at = (tile % kUnitTiles) * tile_rows + (i % p.tok_tile) * p.rep + hr;
-      first = step_base[lo];
-      for (int u = 0; u < unit; ++u) first += (int64_t)own_blocks<kUnitTiles, kBlock>(p, r, s.base, u) * p.nkv;
-      const int blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, unit);
-      first += (int64_t)g * blocks;
+      first = line_base[lo];
+      for (int u = 0; u < unit; ++u)
+        first += (int64_t)item_length<kUnitTiles>(p, r, u, own_blocks<kUnitTiles, kBlock>(p, r, s.base, u)) * p.nkv;
+      blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, unit);
+      cost = block_cost<kUnitTiles>(p, r.rows - unit * kUnitTiles * p.tok_tile);
+      const int len = item_length<kUnitTiles>(p, r, unit, blocks);
+      first += (int64_t)g * len;
       if (blocks > 0) {                          // CTAs [c0, c1): those that begin before the item's end, from the one that has `first`
         int c1 = 0;
         c0 = -1;
         for (int i0 = 0; i0 < p.grid; i0 += 32) {
           const int64_t b = i0 + lane < p.grid ? cta_begin[i0 + lane] : INT64_MAX;
           c0 += __popc(__ballot_sync(0xffffffffu, b <= first));
-          c1 += __popc(__ballot_sync(0xffffffffu, b < first + blocks));
+          c1 += __popc(__ballot_sync(0xffffffffu, b < first + len));
         }
         own = c1 - c0;
       }
@@ -272,7 +276,8 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps) prefix_join_kernel(co
       if (q >= all) return -1;
       if (q < shared) return shared_row + q * shared_step;
       const int c = c0 + q - shared;
-      if (cta_begin[c + 1] <= (first > cta_begin[c] ? first : cta_begin[c])) return -1;   // a CTA without steps
+      // a CTA may have a piece of the item without any of its blocks
+      if (blocks_before<kUnitTiles>(cta_begin[c + 1] - first, blocks, cost) <= blocks_before<kUnitTiles>(cta_begin[c] - first, blocks, cost)) return -1;
       return own_rows<kUnitTiles>(p, r, unit, g, c) + own_at;
     };
     int64_t row0 = row_of(lane);
@@ -418,7 +423,7 @@ size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms) {
   p->tok_tile = tile / p->rep;
   p->units = (p->total + p->tok_tile * unit_tiles - 1) / (p->tok_tile * unit_tiles);
   p->num_sms = num_sms;
-  p->grid = num_sms * per_sm;
+  p->grid = std::min(num_sms * per_sm, kPrefixMaxGrid);
   p->splits = choose_splits(p->nkv * p->units, (p->shared_len + block - 1) / block, p->grid);
   const int64_t rows = (int64_t)p->tok_tile * p->rep * unit_tiles, groups = (int64_t)p->nkv * p->units;
   p->part_rows = std::max<int64_t>(groups, kMaxTurns * p->grid) * rows + (int64_t)p->nkv * p->rep * p->total + p->grid * rows;

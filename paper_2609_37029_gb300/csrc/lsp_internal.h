@@ -318,6 +318,7 @@ struct PrefixAttnParams {
 };
 constexpr int kPrefixMaxSeqs = 1024;
 constexpr int kPrefixMaxRep = 64;
+constexpr int kPrefixMaxGrid = 1024;  // CTAs of the main kernel
 // Fills the plan fields; returns the workspace bytes.
 size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms);
 // bf16 on the tensor cores; the joining kernel is the caller's.

@@ -11,11 +11,10 @@
 // the unit fastest, dealt to the CTAs in turn, so that units of the same keys
 // run at the same time and find each other's loads in L2.
 //
-// Own part: tokens [base, len) of each sequence, its own rows only, causal.
-// Its key blocks, in the order (sequence, unit, head, block), form one line of
-// `own_steps` steps that is cut into contiguous pieces so that every CTA's
-// blocks, shared and own, add up to about the same number.  A piece may start
-// and end inside an item.
+// Own part: tokens [base, len) of each sequence, its own rows only, causal.  Its
+// items, in the order (sequence, unit, head), form one line, each as long as it
+// costs, that is cut into contiguous pieces so that every CTA's work, shared and
+// own, adds up to about the same.  A piece may start and end inside an item.
 //
 // Every segment (an item, or the part of an own item that one CTA has) leaves
 // unnormalised sums and the running maximum and sum of its rows in rows of the
@@ -38,8 +37,18 @@ struct PrefixSched {
   int blocks;           // its key blocks
   int per_split;        // key blocks of a range
   int items;            // shared items
-  int64_t own_steps;    // key blocks of the own part
+  int item_cost;        // of one, on average over the units
+  int64_t own_line;     // length of the own line
 };
+
+// What work costs a CTA, for dealing it out: a key block against one and against
+// two row tiles (1.1 and 1.55 us measured at 16 requests over 32K), and what a
+// segment takes besides (some 2 us).
+constexpr int kCostOne = 2, kCostTwo = 3, kCostSegment = 4;
+template <int kUnitTiles>
+__device__ __forceinline__ int block_cost(const PrefixAttnParams& p, int tokens) {
+  return kUnitTiles == 1 || tokens > p.tok_tile ? kCostTwo : kCostOne;
+}
 struct __align__(16) PrefixSeq {
   int seq, first, rows, len;    // row of the table (-1: none), first row of q, rows, tokens
 };
@@ -78,9 +87,16 @@ __device__ __forceinline__ int own_units(const PrefixAttnParams& p, const Prefix
   return cdiv(r.rows, unit_tiles * p.tok_tile);
 }
 
-// Built by one warp of every CTA; step_base [n + 1], info [n] in shared memory.
+// The own line: items of every sequence in the order (unit, head), each as long
+// as it costs.  Length of an item of a unit with `blocks` key blocks:
+template <int kUnitTiles>
+__device__ __forceinline__ int item_length(const PrefixAttnParams& p, const PrefixSeq& r, int u, int blocks) {
+  return blocks > 0 ? kCostSegment + blocks * block_cost<kUnitTiles>(p, r.rows - u * kUnitTiles * p.tok_tile) : 0;
+}
+
+// Built by one warp of every CTA; line_base [n + 1], info [n] in shared memory.
 template <int kUnitTiles, int kBlock>
-__device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, int64_t* step_base, PrefixSeq* info, bool report) {
+__device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, int64_t* line_base, PrefixSeq* info, bool report) {
   const int lane = threadIdx.x & 31;
   PrefixSched s;
   int base = p.shared_len;
@@ -98,14 +114,16 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
   s.blocks = cdiv(s.base, kBlock);
   s.per_split = cdiv(s.blocks, p.splits);
   s.items = s.blocks > 0 ? p.nkv * p.splits * p.units : 0;
-  int64_t steps = 0;
+  const int last = block_cost<kUnitTiles>(p, p.total - (p.units - 1) * kUnitTiles * p.tok_tile);
+  s.item_cost = kCostSegment + (int)((int64_t)s.per_split * ((p.units - 1) * kCostTwo + last) / p.units);
+  int64_t line = 0;
   for (int i0 = 0; i0 < p.n; i0 += 32) {
     const int i = i0 + lane;
     int64_t mine = 0;
     if (i < p.n) {
       const PrefixSeq r = info[i];               // this lane's own store
       for (int u = 0, units = own_units(p, r, kUnitTiles); u < units; ++u)
-        mine += own_blocks<kUnitTiles, kBlock>(p, r, s.base, u);
+        mine += item_length<kUnitTiles>(p, r, u, own_blocks<kUnitTiles, kBlock>(p, r, s.base, u));
       mine *= p.nkv;
     }
     int64_t x = mine;
@@ -114,26 +132,28 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
       const int64_t a = __shfl_up_sync(0xffffffffu, x, o);
       if (lane >= o) x += a;
     }
-    if (i < p.n) step_base[i] = steps + x - mine;
-    steps += __shfl_sync(0xffffffffu, x, 31);
+    if (i < p.n) line_base[i] = line + x - mine;
+    line += __shfl_sync(0xffffffffu, x, 31);
   }
-  if (lane == 0) step_base[p.n] = steps;
-  s.own_steps = steps;
+  if (lane == 0) line_base[p.n] = line;
+  s.own_line = line;
   return s;
 }
 
-// First own step of CTA c (c == grid: the end).  CTAs below items % grid have
-// one shared item more than the rest; the rest get per_split own steps before
-// the others get any.
-__device__ __forceinline__ int64_t part_of(int64_t steps, int k, int n) {     // steps * k / n
-  return steps < (1 << 21) ? (int64_t)((uint32_t)steps * (uint32_t)k / (uint32_t)n) : steps * k / n;   // k <= grid < 2^11
+// Where CTA c's piece of the own line begins (c == grid: the line's end).  CTAs
+// below items % grid have one shared item more than the rest; the rest get as
+// much of the line as a shared item costs before the others get any.  (Filling
+// every CTA up by its own items' cost balances 16 requests over 32K by a few us
+// more, but to find that level takes 2.4 us before anything starts.)
+__device__ __forceinline__ int64_t part_of(int64_t line, int k, int n) {      // line * k / n
+  return line < (1 << 21) ? (int64_t)((uint32_t)line * (uint32_t)k / (uint32_t)n) : line * k / n;   // k <= grid < 2^11
 }
 __device__ __forceinline__ int64_t own_begin(const PrefixSched& s, int grid, int c) {
   const int more = s.items % grid, less = grid - more;
-  const int64_t fill = (int64_t)less * s.per_split;
-  if (more > 0 && s.own_steps <= fill) return c <= more ? 0 : part_of(s.own_steps, c - more, less);
-  const int64_t even = more > 0 ? s.own_steps - fill : s.own_steps;
-  return part_of(even, c, grid) + (more > 0 && c > more ? (int64_t)(c - more) * s.per_split : 0);
+  const int64_t fill = (int64_t)less * s.item_cost;
+  if (more > 0 && s.own_line <= fill) return c <= more ? 0 : part_of(s.own_line, c - more, less);
+  const int64_t even = more > 0 ? s.own_line - fill : s.own_line;
+  return part_of(even, c, grid) + (more > 0 && c > more ? (int64_t)(c - more) * s.item_cost : 0);
 }
 
 // Workspace rows: the first row of a segment; its second tile's rows follow its
@@ -169,12 +189,25 @@ struct PrefixSeg {
   int64_t part;         // its first row of the workspace
 };
 
-// The segments of a CTA in order: its shared items, then its piece of the own line.
+// Key blocks of an own item (of `blocks`, each of `cost`) that belong to the
+// places before `at` of it: groups of blocks, the first with the segment's cost,
+// go to where they begin.  An item cut in two is two segments, and each costs its
+// CTA what a segment costs: on the tensor cores as much as two blocks, so four
+// stay together; a block of the fp32 kernel takes longer than what comes with it.
+template <int kUnitTiles>
+__device__ __forceinline__ int blocks_before(int64_t at, int blocks, int cost) {
+  constexpr int kTogether = kUnitTiles == 1 ? 1 : 4;
+  if (at <= 0) return 0;
+  const int64_t groups = at <= kCostSegment ? 1 : max((at - kCostSegment + kTogether * cost - 1) / (kTogether * cost), (int64_t)1);
+  return (int)min(groups * kTogether, (int64_t)blocks);
+}
+
+// The segments of a CTA: its shared items, and its piece [x, end) of the own line.
 template <int kUnitTiles, int kBlock>
 struct PrefixSegs {
   const PrefixAttnParams& p;
   const PrefixSched s;
-  const int64_t* step_base;
+  const int64_t* line_base;
   const PrefixSeq* info;
   const int cta;
   const int32_t* shared_tab;
@@ -182,7 +215,7 @@ struct PrefixSegs {
   int64_t x, end;
 
   __device__ PrefixSegs(const PrefixAttnParams& p_, const PrefixSched& s_, const int64_t* base, const PrefixSeq* info_, int cta_)
-      : p(p_), s(s_), step_base(base), info(info_), cta(cta_), shared_tab(nullptr), j(cta_) {
+      : p(p_), s(s_), line_base(base), info(info_), cta(cta_), shared_tab(nullptr), j(cta_) {
     x = own_begin(s, p.grid, cta);
     end = own_begin(s, p.grid, cta + 1);
     if (s.items > 0) {                           // base > 0: some sequence has rows
@@ -192,7 +225,7 @@ struct PrefixSegs {
     }
   }
 
-  __device__ bool next(PrefixSeg& g) {
+  __device__ bool next_shared(PrefixSeg& g) {
     for (; j < s.items; j += p.grid) {
       const int u = j % p.units, gs = j / p.units, split = gs % p.splits;
       g.kb0 = split * s.per_split;
@@ -208,33 +241,44 @@ struct PrefixSegs {
       j += p.grid;
       return true;
     }
-    if (x >= end) return false;
-    int lo = 0, hi = p.n;                        // the last sequence that starts at or before step x
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (step_base[mid] <= x) lo = mid; else hi = mid;
+    return false;
+  }
+
+  __device__ bool next_own(PrefixSeg& g) {
+    while (x < end) {
+      int lo = 0, hi = p.n;                      // the last sequence that starts at or before x
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (line_base[mid] <= x) lo = mid; else hi = mid;
+      }
+      const PrefixSeq r = info[lo];
+      const int units = own_units(p, r, kUnitTiles);
+      int64_t rel = x - line_base[lo];
+      int u = 0, blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, 0);
+      int64_t len = item_length<kUnitTiles>(p, r, 0, blocks);
+      while (rel >= len * p.nkv && u + 1 < units) {
+        rel -= len * p.nkv;
+        blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, ++u);
+        len = item_length<kUnitTiles>(p, r, u, blocks);
+      }
+      if (len <= 0) break;                       // (the line is made of items that have a length)
+      g.head = rel < INT_MAX && len < INT_MAX ? (int)rel / (int)len : (int)(rel / len);
+      const int64_t from = rel - g.head * len, to = min(len, from + (end - x));
+      x += to - from;
+      const int i0 = u * kUnitTiles * p.tok_tile, cost = block_cost<kUnitTiles>(p, r.rows - i0);
+      g.kb0 = blocks_before<kUnitTiles>(from, blocks, cost);
+      g.kb1 = blocks_before<kUnitTiles>(to, blocks, cost);
+      if (g.kb0 >= g.kb1) continue;
+      g.tab = p.table + (size_t)r.seq * p.max_pages;
+      g.t0 = r.first + i0;
+      g.tokens = min(kUnitTiles * p.tok_tile, r.rows - i0);
+      g.k0 = s.base;
+      g.k_end = r.len;
+      g.see0 = r.len - r.rows + i0 + 1;
+      g.part = own_rows<kUnitTiles>(p, r, u, g.head, cta);
+      return true;
     }
-    const PrefixSeq r = info[lo];
-    const int units = own_units(p, r, kUnitTiles);
-    int64_t rel = x - step_base[lo];
-    int u = 0, blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, 0);
-    while (rel >= (int64_t)blocks * p.nkv && u + 1 < units) {
-      rel -= (int64_t)blocks * p.nkv;
-      blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, ++u);
-    }
-    g.head = rel < INT_MAX ? (int)rel / blocks : (int)(rel / blocks);
-    g.kb0 = (int)(rel - (int64_t)g.head * blocks);
-    g.kb1 = (int)min((int64_t)blocks, g.kb0 + (end - x));
-    g.tab = p.table + (size_t)r.seq * p.max_pages;
-    const int i0 = u * kUnitTiles * p.tok_tile;
-    g.t0 = r.first + i0;
-    g.tokens = min(kUnitTiles * p.tok_tile, r.rows - i0);
-    g.k0 = s.base;
-    g.k_end = r.len;
-    g.see0 = r.len - r.rows + i0 + 1;
-    g.part = own_rows<kUnitTiles>(p, r, u, g.head, cta);
-    x += g.kb1 - g.kb0;
-    return true;
+    return false;
   }
 };
 
