@@ -211,8 +211,8 @@ __global__ void __launch_bounds__(kFmaThreads) prefix_attn_fma_kernel(const Pref
 // wait: the lengths are final).
 constexpr int kJoinRows = 4;
 template <typename T, int HD, int kUnitTiles, int kBlock, int kWarps>
-__global__ void __launch_bounds__(32 * kJoinRows * kWarps) prefix_join_kernel(const PrefixAttnParams p) {
-  constexpr int kVec = HD / 32, kAhead = 8;
+__global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : 8) prefix_join_kernel(const PrefixAttnParams p) {
+  constexpr int kVec = HD / 32, kAhead = kWarps > 1 ? 6 : 8;
   extern __shared__ __align__(16) uint8_t join_raw[];
   __shared__ float s_o[kWarps > 1 ? kJoinRows * kWarps : 1][HD], s_l[kJoinRows * kWarps];
   __shared__ PrefixSched s_sched;

@@ -45,7 +45,6 @@ constexpr int kRows = kPrefixTcRows, kKeys = kPrefixTcKeys, kTiles = kPrefixTcTi
 constexpr int kThreads = 384;
 constexpr int kLoadWarp = 8, kMmaWarp = 9, kPlanWarp = 11;
 constexpr int kAhead = 4;                        // segments planned ahead
-constexpr int kHintBlocks = 4;                   // key blocks of a segment that L2 is asked for ahead
 constexpr int kFirstKeys = 64;                  // keys whose weights are handed over before the rest's (32: 0.84 ms, 96: 0.87)
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRaise = 8.0f;                   // log2 of the most a weight may exceed 1
@@ -68,6 +67,7 @@ struct TcMisc {
     PrefixSeg g;
     int more;
   } planned[kAhead];
+  PrefixSched sched;
   float2 lone_ml[2][kRows];                      // stream 1's maximum and sum of segments with one row tile, by turns
   int64_t line_base[kPrefixMaxSeqs + 1];
   PrefixSeq info[kPrefixMaxSeqs];
@@ -235,51 +235,11 @@ __device__ __forceinline__ int stream_jobs(const Jobs& j, int stream) { return (
 __device__ __forceinline__ uint32_t key_tile(const Jobs& j, int i) { return j.lone ? (i > 0 ? 2 * i - 1 : 0) : 2 * i; }
 __device__ __forceinline__ uint32_t value_tile(const Jobs& j, int i) { return j.lone ? i + min(i + 2, j.count) : 2 * i + 1; }
 
-__device__ __forceinline__ void tma_prefetch_4d(const void* map, int x, int y, int z, int w) {
-  asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(reinterpret_cast<uint64_t>(map)),
-               "r"(x), "r"(y), "r"(z), "r"(w)
-               : "memory");
-}
-
-// Asks L2 for the pages of key blocks [kb0, kb1) of a segment, a lane a page.
-template <int HD>
-__device__ __forceinline__ void prefetch_pages(const PrefixAttnParams& p, const CUtensorMap* mk, const CUtensorMap* mv, const int32_t* tab,
-                                               int head, int k0, int k_end, int kb0, int kb1) {
-  const int box = min(p.page, kKeys), boxes = kKeys / box;
-  for (int i = threadIdx.x & 31; i < (kb1 - kb0) * boxes; i += 32) {
-    const int pos = k0 + kb0 * kKeys + i * box;
-    if (pos >= k_end) break;
-    const int pg = __ldg(tab + pos / p.page);
-    if (pg < 0 || pg >= p.pages) continue;       // (reported when it is loaded)
-#pragma unroll
-    for (int h = 0; h < HD / 64; ++h) {
-      tma_prefetch_4d(mk, 64 * h, pos & (p.page - 1), head, pg);
-      tma_prefetch_4d(mv, 64 * h, pos & (p.page - 1), head, pg);
-    }
-  }
-}
-
-// While the schedule is being found: the first key blocks of the CTA's first
-// shared item, as far as the call's own arguments tell where they are.  A guess
-// that is wrong costs a few reads.
-template <int HD>
-__device__ __forceinline__ void prefetch_first(const PrefixAttnParams& p, const CUtensorMap* mk, const CUtensorMap* mv) {
-  const int base = p.shared_len / p.page * p.page, blocks = cdiv(base, kKeys), per_split = cdiv(blocks, p.splits);
-  const int gs = (int)blockIdx.x / p.units, kb0 = gs % p.splits * per_split, head = gs / p.splits;
-  if (head >= p.nkv || kb0 >= blocks) return;
-  const int seq = p.seqs[0];
-  if (seq < 0 || seq >= p.n_seqs) return;
-  prefetch_pages<HD>(p, mk, mv, p.table + (size_t)seq * p.max_pages, head, 0, base, kb0, min(min(kb0 + per_split, blocks), kb0 + kHintBlocks));
-}
-
 // The plan of the CTA's segments, handed on through shared memory: finding the
 // next one takes some 500 cycles, which nobody should spend between two segments.
-template <int HD>
-__device__ __forceinline__ void plan_role(const PrefixAttnParams& p, const CUtensorMap* mk, const CUtensorMap* mv, TcMisc* m) {
+__device__ __forceinline__ void plan_role(const PrefixAttnParams& p, TcMisc* m) {
   const int lane = threadIdx.x & 31;
-  const PrefixSched sched = build_sched<kTiles, kKeys>(p, m->line_base, m->info, blockIdx.x == 0);
-  __syncwarp();
-  PrefixSegs<kTiles, kKeys> segs(p, sched, m->line_base, m->info, blockIdx.x);
+  PrefixSegs<kTiles, kKeys> segs(p, m->sched, m->line_base, m->info, blockIdx.x);
   PrefixSeg g;
   uint32_t k = 0;
   auto publish = [&](bool more) {
@@ -295,11 +255,8 @@ __device__ __forceinline__ void plan_role(const PrefixAttnParams& p, const CUten
   };
   while (segs.next_shared(g))
     if (!publish(true)) return;
-  while (segs.next_own(g)) {
-    // nobody else asks for these: a sequence's own pages come from HBM
-    prefetch_pages<HD>(p, mk, mv, g.tab, g.head, g.k0, g.k_end, g.kb0, min(g.kb1, g.kb0 + kHintBlocks));
+  while (segs.next_own(g))
     if (!publish(true)) return;
-  }
   publish(false);
 }
 // One reader of the plan: every warp of the other roles.
@@ -710,6 +667,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == kMmaWarp) tmem_alloc(smem_u32(&m->tmem), 512);
   griddep_wait();
   griddep_launch();
+  if (warp == 0) {
+    const PrefixSched sc = build_sched<kTiles, kKeys>(p, m->line_base, m->info, cta == 0);
+    if (lane == 0) m->sched = sc;
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -719,14 +680,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp >= kLoadWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     if (warp == kLoadWarp)
-    {
-      prefetch_first<HD>(p, &mk, &mv);
       load_role<HD>(p, &mq, &mk, &mv, sm, m, segs);
-    }
     else if (warp < kMmaWarp + 2)
       mma_role<HD>(p, warp - kMmaWarp, sm, tmem, m, segs);
     else
-      plan_role<HD>(p, &mk, &mv, m);
+      plan_role(p, m);
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     softmax_role<HD>(p, warp >> 2, smp, tmem, m, segs);

@@ -53,6 +53,9 @@ struct __align__(16) PrefixSeq {
   int seq, first, rows, len;    // row of the table (-1: none), first row of q, rows, tokens
 };
 
+// Division of what outgrows 32 bits only in the longest batches, kept out of line:
+// the schedule runs once, and costs what its code takes to be fetched.
+static __device__ __noinline__ int64_t long_div(int64_t a, int64_t b) { return a / b; }
 __device__ __forceinline__ int cdiv(int a, int b) { return (a + b - 1) / b; }
 
 // Sequence i of the batch; rows = 0 for one the call cannot use.
@@ -115,7 +118,8 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
   s.per_split = cdiv(s.blocks, p.splits);
   s.items = s.blocks > 0 ? p.nkv * p.splits * p.units : 0;
   const int last = block_cost<kUnitTiles>(p, p.total - (p.units - 1) * kUnitTiles * p.tok_tile);
-  s.item_cost = kCostSegment + (int)((int64_t)s.per_split * ((p.units - 1) * kCostTwo + last) / p.units);
+  const int64_t cost = (int64_t)s.per_split * ((p.units - 1) * kCostTwo + last);
+  s.item_cost = kCostSegment + (int)(cost < INT_MAX ? (int)cost / p.units : long_div(cost, p.units));
   int64_t line = 0;
   for (int i0 = 0; i0 < p.n; i0 += 32) {
     const int i = i0 + lane;
@@ -146,7 +150,7 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
 // every CTA up by its own items' cost balances 16 requests over 32K by a few us
 // more, but to find that level takes 2.4 us before anything starts.)
 __device__ __forceinline__ int64_t part_of(int64_t line, int k, int n) {      // line * k / n
-  return line < (1 << 21) ? (int64_t)((uint32_t)line * (uint32_t)k / (uint32_t)n) : line * k / n;   // k <= grid < 2^11
+  return line < (1 << 21) ? (int64_t)((uint32_t)line * (uint32_t)k / (uint32_t)n) : long_div(line * k, n);   // k <= grid < 2^11
 }
 __device__ __forceinline__ int64_t own_begin(const PrefixSched& s, int grid, int c) {
   const int more = s.items % grid, less = grid - more;
@@ -198,7 +202,9 @@ template <int kUnitTiles>
 __device__ __forceinline__ int blocks_before(int64_t at, int blocks, int cost) {
   constexpr int kTogether = kUnitTiles == 1 ? 1 : 4;
   if (at <= 0) return 0;
-  const int64_t groups = at <= kCostSegment ? 1 : max((at - kCostSegment + kTogether * cost - 1) / (kTogether * cost), (int64_t)1);
+  const int group = kTogether * cost;
+  const int64_t past = at - kCostSegment + group - 1;
+  const int64_t groups = at <= kCostSegment ? 1 : max(past < INT_MAX ? (int64_t)((int)past / group) : long_div(past, group), (int64_t)1);
   return (int)min(groups * kTogether, (int64_t)blocks);
 }
 
@@ -262,7 +268,7 @@ struct PrefixSegs {
         len = item_length<kUnitTiles>(p, r, u, blocks);
       }
       if (len <= 0) break;                       // (the line is made of items that have a length)
-      g.head = rel < INT_MAX && len < INT_MAX ? (int)rel / (int)len : (int)(rel / len);
+      g.head = rel < INT_MAX && len < INT_MAX ? (int)rel / (int)len : (int)long_div(rel, len);
       const int64_t from = rel - g.head * len, to = min(len, from + (end - x));
       x += to - from;
       const int i0 = u * kUnitTiles * p.tok_tile, cost = block_cost<kUnitTiles>(p, r.rows - i0);

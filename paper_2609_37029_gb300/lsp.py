@@ -132,6 +132,13 @@ _f = {
 }
 
 
+_pages_workspace_bytes, _pages_fork, _pages_reserve = (
+    _f[n] for n in ("lsp_pages_workspace_bytes", "lsp_pages_fork", "lsp_pages_reserve"))
+_pages_write, _pages_trim, _pages_compact = (_f[n] for n in ("lsp_pages_write", "lsp_pages_trim", "lsp_pages_compact"))
+_prefix_attention_workspace_bytes, _prefix_attention, _verify_probs = (
+    _f[n] for n in ("lsp_prefix_attention_workspace_bytes", "lsp_prefix_attention", "lsp_verify_probs"))
+
+
 def _ptr(x):
     """Device/host address of a tensor (or an int address, or None)."""
     if x is None:
@@ -141,12 +148,18 @@ def _ptr(x):
     return x.data_ptr()
 
 
+_raw_stream = None
+
+
 def _stream(stream):
+    global _raw_stream
     if stream is None:
-        import torch
-        if not torch.cuda.is_initialized():
-            return torch.cuda.current_stream().cuda_stream
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())   # the same, without a Stream object
+        if _raw_stream is None:
+            import torch
+            torch.cuda.current_stream()                 # initialises CUDA where nothing has yet
+            get, dev = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+            _raw_stream = lambda: get(dev())            # current_stream().cuda_stream without a Stream object
+        return _raw_stream()
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -189,8 +202,6 @@ def make_kv_cache(k, v, table, lens, refs) -> lsp_kv_cache:
     import torch
     if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.dim() != 5 or k.stride(4) != 1:
         raise ValueError("k and v: the same 5-D shape, type and strides, the last axis dense")
-    if k.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError("k and v: bfloat16 or float32")
     for t in (table, lens, refs):
         if t.dtype != torch.int32 or not t.is_contiguous():
             raise ValueError("table, lens and refs: contiguous int32")
@@ -200,7 +211,7 @@ def make_kv_cache(k, v, table, lens, refs) -> lsp_kv_cache:
     c.k, c.v, c.table, c.len, c.refs = (t.data_ptr() for t in (k, v, table, lens, refs))
     c.s_layer, c.s_page, c.s_head, c.s_slot = k.stride()[:4]
     c.layers, c.pages, c.nkv, c.page, c.d = k.shape
-    c.dtype = LSP_DTYPE_BF16 if k.dtype == torch.bfloat16 else LSP_DTYPE_F32
+    c.dtype = _dtype_code(k.dtype)
     c.seqs, c.max_pages = table.shape
     return c
 
@@ -343,80 +354,100 @@ def lsp_state_import(st, host_buf, stream=None) -> None:
                                   _stream(stream)), "lsp_state_import")
 
 
+# The calls below are made once a layer or a round, with kernels of a few microseconds behind them: their
+# tensors' addresses are taken in place, and what does not change from call to call is looked up once.
+_codes: dict = {}
+
+
+def _dtype_code(dtype) -> int:
+    """LSP_DTYPE_* of a torch type (ValueError for any but bfloat16 and float32)."""
+    if not _codes:
+        import torch
+        _codes.update({torch.bfloat16: LSP_DTYPE_BF16, torch.float32: LSP_DTYPE_F32})
+    if dtype not in _codes:
+        raise ValueError("bfloat16 or float32 tensors")
+    return _codes[dtype]
+
+
+def _opt(x):
+    return None if x is None else x.data_ptr()
+
+
 def lsp_pages_workspace_bytes(cache: lsp_kv_cache) -> int:
-    return _f["lsp_pages_workspace_bytes"](cache)
+    return _pages_workspace_bytes(cache)
 
 
 def lsp_pages_fork(cache: lsp_kv_cache, src, dst, dev_error=None, stream=None) -> None:
-    _check(_f["lsp_pages_fork"](cache, _ptr(src), _ptr(dst), dst.numel(), _ptr(dev_error), _stream(stream)),
+    _check(_pages_fork(cache, src.data_ptr(), dst.data_ptr(), dst.numel(), _opt(dev_error), _stream(stream)),
            "lsp_pages_fork")
 
 
 def lsp_pages_reserve(cache: lsp_kv_cache, seqs, add, workspace, dev_error=None, stream=None) -> None:
-    _check(_f["lsp_pages_reserve"](cache, _ptr(seqs), _ptr(add), seqs.numel(), _ptr(workspace),
-                                   workspace.nbytes, _ptr(dev_error),
-                                   _stream(stream)), "lsp_pages_reserve")
+    _check(_pages_reserve(cache, seqs.data_ptr(), add.data_ptr(), seqs.numel(), workspace.data_ptr(),
+                          workspace.nbytes, _opt(dev_error), _stream(stream)), "lsp_pages_reserve")
 
 
 def lsp_pages_write(cache: lsp_kv_cache, layer, seqs, start, k_new, v_new, dev_error=None, stream=None) -> None:
     """k_new, v_new: [total][nkv][d], dense within a row, the same stride between rows."""
-    if k_new.stride() != v_new.stride() or k_new.stride()[1:] != (cache.d, 1) or k_new.shape[1:] != (cache.nkv, cache.d):
+    shape, stride, d = k_new.shape, k_new.stride(), cache.d
+    if stride != v_new.stride() or stride[1] != d or stride[2] != 1 or shape[1] != cache.nkv or shape[2] != d:
         raise ValueError("k_new and v_new: [total][nkv][d] of the same strides, dense within a row")
-    _check(_f["lsp_pages_write"](cache, int(layer), _ptr(seqs), _ptr(start), seqs.numel(), _ptr(k_new),
-                                 _ptr(v_new), k_new.stride(0), k_new.shape[0], _ptr(dev_error),
-                                 _stream(stream)), "lsp_pages_write")
+    _check(_pages_write(cache, layer, seqs.data_ptr(), start.data_ptr(), seqs.numel(), k_new.data_ptr(),
+                        v_new.data_ptr(), stride[0], shape[0], _opt(dev_error), _stream(stream)), "lsp_pages_write")
 
 
 def lsp_pages_trim(cache: lsp_kv_cache, seqs, new_len, dev_error=None, stream=None) -> None:
-    _check(_f["lsp_pages_trim"](cache, _ptr(seqs), _ptr(new_len), seqs.numel(), _ptr(dev_error),
-                                _stream(stream)), "lsp_pages_trim")
+    _check(_pages_trim(cache, seqs.data_ptr(), new_len.data_ptr(), seqs.numel(), _opt(dev_error), _stream(stream)),
+           "lsp_pages_trim")
 
 
 def lsp_pages_compact(cache: lsp_kv_cache, live, workspace, stream=None) -> None:
     """live: int32 [1] that receives the number of live pages, or None."""
-    _check(_f["lsp_pages_compact"](cache, _ptr(live), _ptr(workspace),
-                                   workspace.nbytes, _stream(stream)),
+    _check(_pages_compact(cache, _opt(live), workspace.data_ptr(), workspace.nbytes, _stream(stream)),
            "lsp_pages_compact")
 
 
 def lsp_prefix_attention_workspace_bytes(cache: lsp_kv_cache, nq: int, n: int, total: int) -> int:
-    return _f["lsp_prefix_attention_workspace_bytes"](cache, nq, n, total)
+    return _prefix_attention_workspace_bytes(cache, nq, n, total)
 
 
 def lsp_prefix_attention(cache: lsp_kv_cache, layer, q, seqs, start, out, lse=None, *, shared_len, scale,
                          workspace, dev_error=None, stream=None) -> None:
     """q: [total][nq][d], dense within a row (a slice of a fused q/k/v row will do); out: dense."""
-    if q.stride()[1:] != (cache.d, 1) or q.shape[2] != cache.d or out.shape != q.shape or not out.is_contiguous():
+    shape, stride, d = q.shape, q.stride(), cache.d
+    if stride[1] != d or stride[2] != 1 or shape[2] != d or out.shape != shape or not out.is_contiguous():
         raise ValueError("q: [total][nq][d], dense within a row; out: the same shape, contiguous")
-    _check(_f["lsp_prefix_attention"](cache, int(layer), _ptr(q), q.stride(0), q.shape[1], _ptr(seqs),
-                                      _ptr(start), seqs.numel(), q.shape[0], int(shared_len), float(scale),
-                                      _ptr(out), _ptr(lse), _ptr(workspace),
-                                      workspace.nbytes, _ptr(dev_error),
-                                      _stream(stream)), "lsp_prefix_attention")
+    _check(_prefix_attention(cache, layer, q.data_ptr(), stride[0], shape[1], seqs.data_ptr(), start.data_ptr(),
+                             seqs.numel(), shape[0], shared_len, scale, out.data_ptr(), _opt(lse),
+                             workspace.data_ptr(), workspace.nbytes, _opt(dev_error), _stream(stream)),
+           "lsp_prefix_attention")
+
+
+def _row_stride(t, C, rows, V):
+    """Elements between the rows of t [C][rows][V], evenly spaced."""
+    stride = t.stride()
+    ld = stride[1] if rows > 1 else stride[0] if C > 1 else max(V, stride[1])
+    if t.shape != (C, rows, V) or (V > 1 and stride[2] != 1) or (C > 1 and stride[0] != rows * ld):
+        raise ValueError("target_probs [C][B+1][V] and draft_probs [C][B][V], rows evenly spaced")
+    return ld
 
 
 def lsp_verify_probs(target_probs, draft_probs, draft_tokens, u, e, accepted_len, next_token, n_draft=None,
                      out_tokens=None, dev_error=None, stream=None) -> None:
     """target_probs [C][B+1][V], draft_probs [C][B][V] (or None) of one type, bfloat16 or float32; the
     stride between their rows may exceed V."""
-    import torch
     C, B = draft_tokens.shape
-    V = target_probs.shape[2]
-    ld = [0, 0]
-    for i, (t, rows) in enumerate(((target_probs, B + 1), (draft_probs, B))):
-        if t is None or t.numel() == 0:
-            continue
-        ld[i] = t.stride(1) if rows > 1 else t.stride(0) if C > 1 else max(V, t.stride(1))
-        if t.dtype != target_probs.dtype or t.shape != (C, rows, V) or (V > 1 and t.stride(2) != 1) or (
-                C > 1 and t.stride(0) != rows * ld[i]):
-            raise ValueError("target_probs [C][B+1][V] and draft_probs [C][B][V]: one type, rows evenly spaced")
-    if target_probs.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError("target_probs: bfloat16 or float32")
-    dtype = LSP_DTYPE_BF16 if target_probs.dtype == torch.bfloat16 else LSP_DTYPE_F32
-    _check(_f["lsp_verify_probs"](_ptr(target_probs), _ptr(draft_probs), dtype, _ptr(draft_tokens),
-                                  _ptr(n_draft), _ptr(u), _ptr(e), C, B, V, ld[0], ld[1],
-                                  _ptr(accepted_len), _ptr(next_token), _ptr(out_tokens),
-                                  _ptr(dev_error), _stream(stream)), "lsp_verify_probs")
+    V, dtype = target_probs.shape[2], target_probs.dtype
+    code, ld_q, drafted = _dtype_code(dtype), 0, None
+    ld_t = _row_stride(target_probs, C, B + 1, V)
+    if draft_probs is not None and B > 0:
+        if draft_probs.dtype != dtype:
+            raise ValueError("target_probs and draft_probs: one type")
+        ld_q, drafted = _row_stride(draft_probs, C, B, V), draft_probs.data_ptr()
+    _check(_verify_probs(target_probs.data_ptr(), drafted, code, draft_tokens.data_ptr(), _opt(n_draft),
+                         u.data_ptr(), e.data_ptr(), C, B, V, ld_t, ld_q, accepted_len.data_ptr(),
+                         next_token.data_ptr(), _opt(out_tokens), _opt(dev_error), _stream(stream)),
+           "lsp_verify_probs")
 
 
 EXPORTED = sorted(_f)
