@@ -12,8 +12,11 @@
 // acceptance tests itself (lane i of warp 0 tests candidate i), scans its slice
 // of the one row that decides (p, q, e), and the CTAs exchange their best
 // (score, index) through distributed shared memory.  No workspace, no atomics.
-// Bound by HBM at many requests (3 V values a request), by the chain
-// token -> p, q -> row -> exchange at few.
+//
+// 4 requests of 32001 entries take 5.6 us: launch, and the chain token -> p, q ->
+// row -> exchange.  16 of 151936 entries: 10.4 us for 29 MB, 64 with 16-bit
+// probabilities and drafts without a distribution: 17.9 us for 58 MB (3.3 TB/s);
+// the rounds of loads of a slice bound it, two CTAs of 512 threads on an SM.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -29,7 +32,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kVpThreads = 512;
-constexpr int kVpCluster = 8;                    // CTAs per request (the portable maximum)
+constexpr int kVpMaxCluster = 8;                 // CTAs per request at most (16 requests: 10.4 us with 8, 15.9 with 16)
 constexpr unsigned kAll = 0xffffffffu;
 
 __device__ __forceinline__ bool better(float v, int i, float bv, int bi) { return v > bv || (v == bv && i < bi); }
@@ -58,15 +61,25 @@ __device__ __forceinline__ void load_floats(const float* p, float* x) {
   }
 }
 
-// kQ: subtract the row q (res), or drop the one token `skip` (a point mass; -1: none).
+__device__ __noinline__ float quotient(float w, float e) { return __fdiv_rn(w, e); }
+
+// kQ: subtract the row q, or drop the one token `skip` (a point mass; -1: none).
+// Few entries can still win once some have been seen, and a correctly rounded
+// division takes longer than all the rest: an entry is only divided if w >= e
+// times the warp's best so far, less 2^-19 of it for the roundings (and always
+// where the best or the product is tiny or no number).
 template <typename T, int VEC, bool kQ>
 __device__ __forceinline__ void scan_row(const T* p, const T* q, const float* e, int skip, int g0, int g1, float& bv, int& bi) {
   constexpr int kBatch = VEC == 1 ? 8 : 2;
-  for (int base = g0 + threadIdx.x; base < g1; base += kBatch * kVpThreads) {
+  float bound = -1.f;
+  for (int first = g0; first < g1; first += kBatch * kVpThreads) {     // the same count for the whole CTA
+    const int base = first + threadIdx.x;
     float a[kBatch][VEC], b[kBatch][VEC], x[kBatch][VEC];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       const int g = base + k * kVpThreads;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) a[k][j] = b[k][j] = x[k][j] = 0.f;
       if (g < g1) {
         load_probs<T, VEC>(p + (size_t)g * VEC, a[k]);
         if (kQ) load_probs<T, VEC>(q + (size_t)g * VEC, b[k]);
@@ -75,23 +88,34 @@ __device__ __forceinline__ void scan_row(const T* p, const T* q, const float* e,
     }
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
-      const int g = base + k * kVpThreads;
-      if (g >= g1) break;
+      const int v0 = (base + k * kVpThreads) * VEC;
+      bool any = false;
+      float w[VEC];
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        const int v = g * VEC + j;
-        const float w = kQ ? a[k][j] - b[k][j] : a[k][j];
-        if (w > 0.f && (kQ || v != skip)) {
-          const float sc = __fdiv_rn(w, x[k][j]);
-          // indices rise within a thread: a strict > keeps the lowest on ties
-          if (sc > bv) { bv = sc; bi = v; }
-        }
+        w[j] = kQ ? a[k][j] - b[k][j] : a[k][j];
+        if (!kQ && v0 + j == skip) w[j] = 0.f;
+        const float least = bound * x[k][j];
+        any |= w[j] > 0.f && (!(w[j] < least) || !(least > 1e-36f));
+      }
+      if (any) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j)
+          if (w[j] > 0.f) {
+            const float sc = quotient(w[j], x[k][j]);
+            // indices rise within a thread: a strict > keeps the lowest on ties
+            if (sc > bv) { bv = sc; bi = v0 + j; }
+          }
       }
     }
+    float top = bv;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kAll, top, o));
+    bound = top > 1e-30f ? top * (1.f - 1.9073486328125e-06f) : -1.f;
   }
 }
 
-// Best of the cluster; every CTA gets it.  s_val, s_idx: kVpCluster slots.
+// Best of the cluster; every CTA gets it.  s_val, s_idx: a slot for each of its CTAs.
 __device__ __forceinline__ void cluster_best(cg::cluster_group cl, float& v, int& i, float* s_val, int* s_idx, float* w_val,
                                              int* w_idx) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -113,7 +137,7 @@ __device__ __forceinline__ void cluster_best(cg::cluster_group cl, float& v, int
       if (better(ov, oi, v, i)) { v = ov; i = oi; }
     }
     const int me = (int)cl.block_rank();
-    if (lane < kVpCluster) {
+    if (lane < (int)cl.num_blocks()) {
       cl.map_shared_rank(s_val, lane)[me] = v;
       cl.map_shared_rank(s_idx, lane)[me] = i;
     }
@@ -121,21 +145,20 @@ __device__ __forceinline__ void cluster_best(cg::cluster_group cl, float& v, int
   cl.sync();
   v = s_val[0];
   i = s_idx[0];
-#pragma unroll
-  for (int k = 1; k < kVpCluster; ++k)
+  for (int k = 1; k < (int)cl.num_blocks(); ++k)
     if (better(s_val[k], s_idx[k], v, i)) { v = s_val[k]; i = s_idx[k]; }
 }
 
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kVpThreads) verify_probs_kernel(const VerifyProbsParams p) {
-  __shared__ float s_val[2][kVpCluster], w_val[32];
-  __shared__ int s_idx[2][kVpCluster], w_idx[32];
+__global__ void __launch_bounds__(kVpThreads, 2) verify_probs_kernel(const VerifyProbsParams p) {
+  __shared__ float s_val[2][kVpMaxCluster], w_val[32];
+  __shared__ int s_idx[2][kVpMaxCluster], w_idx[32];
   __shared__ int s_r;
   cg::cluster_group cl = cg::this_cluster();
   cg::cluster_group::arrival_token started = cl.barrier_arrive();
   griddep_wait();
   griddep_launch();
-  const int b = blockIdx.x / kVpCluster, ch = (int)cl.block_rank(), B = p.B, V = p.V;
+  const int parts = (int)cl.num_blocks(), b = blockIdx.x / parts, ch = (int)cl.block_rank(), B = p.B, V = p.V;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const T* pt = static_cast<const T*>(p.pt) + (int64_t)b * (B + 1) * p.ld_t;
   const T* pq = p.pq ? static_cast<const T*>(p.pq) + (int64_t)b * B * p.ld_q : nullptr;
@@ -174,7 +197,7 @@ __global__ void __launch_bounds__(kVpThreads) verify_probs_kernel(const VerifyPr
   const T* row = pt + (int64_t)r * p.ld_t;
   const float* e = p.e + (size_t)b * V;
   const int ng = V / VEC;                        // VEC > 1 only where V % VEC == 0
-  const int g0 = (int)((int64_t)ch * ng / kVpCluster), g1 = (int)((int64_t)(ch + 1) * ng / kVpCluster);
+  const int g0 = (int)((int64_t)ch * ng / parts), g1 = (int)((int64_t)(ch + 1) * ng / parts);
   float bv = -1.f;
   int bi = INT_MAX;
   if (r < n && pq)
@@ -200,16 +223,16 @@ __global__ void __launch_bounds__(kVpThreads) verify_probs_kernel(const VerifyPr
 }
 
 template <typename T, int VEC>
-cudaError_t launch(const VerifyProbsParams& p, cudaStream_t s) {
+cudaError_t launch(const VerifyProbsParams& p, int parts, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(p.C * kVpCluster);
+  cfg.gridDim = dim3(p.C * parts);
   cfg.blockDim = dim3(kVpThreads);
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = kVpCluster;
+  attr[1].val.clusterDim.x = parts;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
@@ -218,17 +241,21 @@ cudaError_t launch(const VerifyProbsParams& p, cudaStream_t s) {
 
 }  // namespace
 
-int launch_verify_probs(const VerifyProbsParams& p, int dtype, cudaStream_t s) {
+int launch_verify_probs(const VerifyProbsParams& p, int dtype, int num_sms, cudaStream_t s) {
   const int es = dtype == LSP_DTYPE_BF16 ? 2 : 4;
-  // four values a load where every row starts on a load's boundary
+  // four values a load where every row starts on a load's boundary (64 requests of 16-bit
+  // probabilities: 17.9 us, one value a load 22.0)
   const uintptr_t at = reinterpret_cast<uintptr_t>(p.pt) | reinterpret_cast<uintptr_t>(p.pq);
   const bool vec = p.V % 4 == 0 && p.ld_t % 4 == 0 && (!p.pq || p.ld_q % 4 == 0) && at % (4 * es) == 0 &&
                    reinterpret_cast<uintptr_t>(p.e) % 16 == 0;
+  // as many CTAs a request as are resident at once, two on an SM (64 requests: 17.9 us with 4, 23 with 8)
+  int parts = kVpMaxCluster;
+  while (parts > 1 && (int64_t)p.C * parts > 2 * num_sms) parts /= 2;
   cudaError_t e;
   if (dtype == LSP_DTYPE_BF16)
-    e = vec ? launch<bf16, 4>(p, s) : launch<bf16, 1>(p, s);
+    e = vec ? launch<bf16, 4>(p, parts, s) : launch<bf16, 1>(p, parts, s);
   else
-    e = vec ? launch<float, 4>(p, s) : launch<float, 1>(p, s);
+    e = vec ? launch<float, 4>(p, parts, s) : launch<float, 1>(p, parts, s);
   return e == cudaSuccess ? LSP_OK : LSP_ERR_CUDA;
 }
 

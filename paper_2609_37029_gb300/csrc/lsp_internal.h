@@ -342,6 +342,6 @@ struct VerifyProbsParams {
   int C, B, V;
   int64_t ld_t, ld_q;
 };
-int launch_verify_probs(const VerifyProbsParams& p, int dtype, cudaStream_t s);
+int launch_verify_probs(const VerifyProbsParams& p, int dtype, int num_sms, cudaStream_t s);
 
 }  // namespace lsp

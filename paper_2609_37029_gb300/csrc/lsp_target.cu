@@ -190,7 +190,9 @@ int lsp_verify_probs(const void* target_probs, const void* draft_probs, int dtyp
   p.pt = target_probs; p.pq = B > 0 ? draft_probs : nullptr; p.y = draft_tokens; p.n = n_draft; p.u = u; p.e = e;
   p.accepted = accepted_len; p.next_token = next_token; p.out_tokens = out_tokens; p.err = dev_error;
   p.C = C; p.B = B; p.V = V; p.ld_t = ld_target; p.ld_q = ld_draft;
-  return launch_verify_probs(p, dtype, S(stream));
+  int sms = 0;
+  const int rc = num_sms(&sms);
+  return rc == LSP_OK ? launch_verify_probs(p, dtype, sms, S(stream)) : rc;
 }
 
 }  // extern "C"
