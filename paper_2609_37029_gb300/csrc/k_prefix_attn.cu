@@ -218,7 +218,6 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : 8) p
   __shared__ PrefixSched s_sched;
   PrefixSeq* info = reinterpret_cast<PrefixSeq*>(join_raw);
   int64_t* line_base = reinterpret_cast<int64_t*>(info + p.n);
-  int64_t* cta_begin = line_base + p.n + 1;      // [grid + 1]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp / kJoinRows;
   if (warp == 0) {
     const PrefixSched s = build_sched<kUnitTiles, kBlock>(p, line_base, info, false);
@@ -226,8 +225,6 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : 8) p
   }
   __syncthreads();
   const PrefixSched s = s_sched;
-  for (int c = threadIdx.x; c <= p.grid; c += blockDim.x) cta_begin[c] = own_begin(s, p.grid, c);
-  __syncthreads();
   const int64_t rows = (int64_t)p.total * p.nq;
   bool waited = false;
   for (int64_t w0 = (int64_t)blockIdx.x * kJoinRows; w0 < rows; w0 += (int64_t)gridDim.x * kJoinRows) {
@@ -239,63 +236,78 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : 8) p
       lo += __popc(__ballot_sync(0xffffffffu, i0 + lane < p.n && info[i0 + lane].first <= t));
     PrefixSeq r = {-1, 0, 0, 0};
     if (lo >= 0) r = info[lo];
-    // segments: the shared part's ranges, then the CTAs of the own item
-    int shared = 0, own = 0, c0 = 0, unit = 0, own_at = 0, blocks = 0, cost = 1;
-    int64_t shared_row = 0, shared_step = 0, first = 0;
+    // segments: of each range of the shared part the (at most `pieces`) CTAs that
+    // have part of its item, then those of the own item
+    int shared = 0, pieces = 1, own = 0, c0 = 0, u = 0, unit = 0, shared_at = 0, own_at = 0, blocks = 0, cost = 1, shared_cost = 1;
+    int64_t first = 0;
     if (t >= r.first && t < r.first + r.rows) {
       const int tile_rows = p.tok_tile * p.rep;
       if (s.items > 0) {
-        const int tile = t / p.tok_tile, u = tile / kUnitTiles;
-        shared = cdiv(s.blocks, s.per_split);
-        shared_row = shared_rows<kUnitTiles>(p, g, 0, u) + (tile % kUnitTiles) * tile_rows + (t % p.tok_tile) * p.rep + hr;
-        shared_step = (int64_t)p.units * kUnitTiles * tile_rows;
+        const int tile = t / p.tok_tile;
+        u = tile / kUnitTiles;
+        shared_at = (tile % kUnitTiles) * tile_rows + (t % p.tok_tile) * p.rep + hr;
+        const bool last = u + 1 == p.units;
+        shared_cost = last ? block_cost<kUnitTiles>(p, p.total - u * kUnitTiles * p.tok_tile) : kCostTwo;
+        if (s.whole < s.items) pieces = (int)div_floor((int64_t)(last ? s.len_last : s.len_two) * s.ctas, s.line) + 2;
+        shared = p.splits * pieces;
       }
       const int i = t - r.first, tile = i / p.tok_tile;
       unit = tile / kUnitTiles;
       own_at = (tile % kUnitTiles) * tile_rows + (i % p.tok_tile) * p.rep + hr;
-      first = line_base[lo];
+      first = s.shared_line + line_base[lo];
       for (int u = 0; u < unit; ++u)
         first += (int64_t)item_length<kUnitTiles>(p, r, u, own_blocks<kUnitTiles, kBlock>(p, r, s.base, u)) * p.nkv;
       blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, unit);
       cost = block_cost<kUnitTiles>(p, r.rows - unit * kUnitTiles * p.tok_tile);
       const int len = item_length<kUnitTiles>(p, r, unit, blocks);
       first += (int64_t)g * len;
-      if (blocks > 0) {                          // CTAs [c0, c1): those that begin before the item's end, from the one that has `first`
-        int c1 = 0;
-        c0 = -1;
-        for (int i0 = 0; i0 < p.grid; i0 += 32) {
-          const int64_t b = i0 + lane < p.grid ? cta_begin[i0 + lane] : INT64_MAX;
-          c0 += __popc(__ballot_sync(0xffffffffu, b <= first));
-          c1 += __popc(__ballot_sync(0xffffffffu, b < first + len));
-        }
-        own = c1 - c0;
+      if (blocks > 0) {
+        c0 = piece_at(s, first);
+        own = piece_at(s, first + len - 1) + 1 - c0;
       }
     }
     const int all = shared + own;
     auto row_of = [&](int q) -> int64_t {        // -1: no such segment
       if (q >= all) return -1;
-      if (q < shared) return shared_row + q * shared_step;
-      const int c = c0 + q - shared;
+      const bool sh = q < shared;
+      const int range = sh ? q / pieces : 0, k = sh ? q - range * pieces : q - shared;
+      const int head_range = g * p.splits + range, item = head_range * p.units + u;
+      const int nb = sh ? range_blocks(s, range) : blocks;
+      if (sh && item < s.whole) return k == 0 && nb > 0 ? shared_rows<kUnitTiles>(p, s, item, 0) + shared_at : -1;
+      const int64_t place = sh ? shared_place(s, head_range, u) - s.whole_line : first;
+      const int c = (sh ? piece_at(s, place) : c0) + k;
+      if (c >= s.ctas) return -1;
       // a CTA may have a piece of the item without any of its blocks
-      if (blocks_before<kUnitTiles>(cta_begin[c + 1] - first, blocks, cost) <= blocks_before<kUnitTiles>(cta_begin[c] - first, blocks, cost)) return -1;
-      return own_rows<kUnitTiles>(p, r, unit, g, c) + own_at;
+      const int price = sh ? shared_cost : cost;
+      if (blocks_before(s, piece_begin(s, c + 1) - place, nb, price) <=
+          blocks_before(s, piece_begin(s, c) - place, nb, price))
+        return -1;
+      return sh ? shared_rows<kUnitTiles>(p, s, item, c) + shared_at : own_rows<kUnitTiles>(p, r, unit, g, c) + own_at;
     };
-    int64_t row0 = row_of(lane);
+    // the first segment of this lane for the maxima, and for the sums
+    int64_t row_m = -1, row_s = -1;
+#pragma unroll 1
+    for (int k = 0; k < (kWarps > 1 ? 2 : 1); ++k) {
+      const int64_t x = row_of(k == 0 ? lane : lane * kWarps + part);
+      if (k == 0) row_m = x;
+      row_s = x;
+    }
     if (!waited) {
       griddep_wait();
       griddep_launch();
       waited = true;
     }
     float m = -INFINITY, l = 0.f, o[kVec];
-    for (int q = lane; q < all; q += 32) {
-      const int64_t row = q == lane ? row0 : row_of(q);
-      if (row >= 0) m = fmaxf(m, p.part_ml[row].x);
+    for (int q = lane;;) {
+      if (row_m >= 0) m = fmaxf(m, p.part_ml[row_m].x);
+      if ((q += 32) >= all) break;
+      row_m = row_of(q);
     }
     m = warp_max(m);
 #pragma unroll
     for (int e = 0; e < kVec; ++e) o[e] = 0.f;
     for (int q0 = 0; q0 < all && m > -INFINITY; q0 += 32 * kWarps) {
-      const int64_t row = row_of(q0 + lane * kWarps + part);
+      const int64_t row = q0 == 0 ? row_s : row_of(q0 + lane * kWarps + part);
       float x = 0.f;
       if (row >= 0) {
         const float2 ml = p.part_ml[row];
@@ -363,7 +375,7 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : 8) p
 template <typename T, int HD, int kUnitTiles, int kBlock>
 int launch_join(const PrefixAttnParams& p, cudaStream_t s) {
   const int64_t rows = (int64_t)p.total * p.nq, ctas = (rows + kJoinRows - 1) / kJoinRows;
-  const size_t smem = p.n * (sizeof(PrefixSeq) + sizeof(int64_t)) + (p.grid + 2) * sizeof(int64_t);
+  const size_t smem = p.n * (sizeof(PrefixSeq) + sizeof(int64_t)) + sizeof(int64_t);
   const bool few = rows < 16 * (int64_t)p.num_sms;
   const cudaError_t e =
       few ? launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 4>, dim3((unsigned)ctas), dim3(128 * kJoinRows), smem, s, p)
@@ -396,22 +408,11 @@ int launch_tc(const PrefixAttnParams& p, cudaStream_t s) {
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Key ranges of the shared part.  Items (heads x units x ranges) of equal size
-// run in turns of `grid`: for each number of turns the most ranges that fit,
-// and of those the fewest key blocks on the longest CTA, each item counted
-// kItemBlocks more for its query loads and partial sums.
-constexpr int kMaxTurns = 4;
-int choose_splits(int groups, int blocks, int grid) {
-  constexpr double kItemBlocks = 3.0;
-  int best = 1;
-  double cost = 0.0;
-  for (int t = 0; t <= kMaxTurns; ++t) {
-    const int s = std::max(1, std::min(t * grid / groups, blocks));
-    const int turns = (groups * s + grid - 1) / grid, per = (blocks + s - 1) / s;
-    const double c = turns * (per + kItemBlocks);
-    if (t == 0 || c < cost) { best = s; cost = c; }
-  }
-  return best;
+// Key ranges of the shared part.  The line cuts the keys among the CTAs by
+// itself, in the fewest segments; ranges only keep the units of a head close to
+// each other in the keys: as many as there are CTAs for, if it has several units.
+int choose_splits(int heads, int units, int blocks, int grid) {
+  return units == 1 ? 1 : std::max(1, std::min(grid / (heads * units), blocks));
 }
 
 }  // namespace
@@ -424,9 +425,10 @@ size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms) {
   p->units = (p->total + p->tok_tile * unit_tiles - 1) / (p->tok_tile * unit_tiles);
   p->num_sms = num_sms;
   p->grid = std::min(num_sms * per_sm, kPrefixMaxGrid);
-  p->splits = choose_splits(p->nkv * p->units, (p->shared_len + block - 1) / block, p->grid);
-  const int64_t rows = (int64_t)p->tok_tile * p->rep * unit_tiles, groups = (int64_t)p->nkv * p->units;
-  p->part_rows = std::max<int64_t>(groups, kMaxTurns * p->grid) * rows + (int64_t)p->nkv * p->rep * p->total + p->grid * rows;
+  p->splits = choose_splits(p->nkv, p->units, (p->shared_len + block - 1) / block, p->grid);
+  // (not of `splits`: the workspace of one shared_len is enough for any)
+  const int64_t rows = (int64_t)p->tok_tile * p->rep * unit_tiles, items = std::max<int64_t>((int64_t)p->nkv * p->units, p->grid);
+  p->part_rows = (items + 2 * p->grid) * rows + (int64_t)p->nkv * p->rep * p->total;
   p->part_rows = (p->part_rows + 3) / 4 * 4;
   return align256((size_t)p->part_rows * sizeof(float2)) + (size_t)p->part_rows * p->d * sizeof(float);
 }

@@ -7,22 +7,27 @@
 // Shared part: the whole pages before every row's position that all sequences
 // hold, `base` tokens.  All `total` tokens of the batch are stacked into units
 // against them, without regard to whose they are (nothing is masked), and the
-// keys are cut into `splits` ranges of equal size: items (head, range, unit),
-// the unit fastest, dealt to the CTAs in turn, so that units of the same keys
-// run at the same time and find each other's loads in L2.
+// keys are cut into `splits` ranges: items (head, range, unit), the unit fastest.
 //
-// Own part: tokens [base, len) of each sequence, its own rows only, causal.  Its
-// items, in the order (sequence, unit, head), form one line, each as long as it
-// costs, that is cut into contiguous pieces so that every CTA's work, shared and
-// own, adds up to about the same.  A piece may start and end inside an item.
+// Own part: tokens [base, len) of each sequence, its own rows only, causal: items
+// (sequence, unit, head).
 //
-// Every segment (an item, or the part of an own item that one CTA has) leaves
-// unnormalised sums and the running maximum and sum of its rows in rows of the
-// workspace; a second kernel joins a row's segments, which it finds by the same
-// arithmetic.  Shared segments lie at
-// ((head, range), unit); an own segment at (rows of the items before it) + CTA *
-// (rows of a unit), which no two share: along the line the item or the CTA rises
-// from segment to segment, each by at least the room of one.
+// As many shared items as go round evenly are dealt to the CTAs whole, in turn,
+// so that units of the same keys run at the same time and find each other's
+// loads in L2.  The rest of them and the own items form one line, each as long
+// as it costs, that is cut into a piece of the same length for every CTA.  A
+// piece may start and end inside an item.  A CTA goes through the shared segments
+// of its piece from the last to the first: with pieces somewhat shorter than
+// items, it then comes to the first keys of one item and the last of the item
+// before when the others do (forwards, every unit read the keys from memory:
+// 4.7 GB for 0.5 at 32 requests over 128K).
+//
+// Every segment (the part of an item that one CTA has) leaves unnormalised sums
+// and the running maximum and sum of its rows in rows of the workspace; a second
+// kernel joins a row's segments, which it finds by the same arithmetic.  A
+// segment of the line lies at (rows of the items before it) + CTA * (rows of a
+// unit), which no two share: along the line the item or the CTA rises from
+// segment to segment, each by at least the room of one.
 #pragma once
 
 #include <climits>
@@ -34,17 +39,26 @@ namespace lsp {
 
 struct PrefixSched {
   int base;             // tokens of the shared part
-  int blocks;           // its key blocks
-  int per_split;        // key blocks of a range
-  int items;            // shared items
-  int item_cost;        // of one, on average over the units
-  int64_t own_line;     // length of the own line
+  int blocks;           // its key blocks,
+  int range, longer;    // of a key range; the first `longer` ranges have one more
+  int items, whole;     // shared items; those dealt whole, the first ones
+  int len_two, len_last;    // lengths of the shared items of a range's units: all but the last, the last
+  int64_t len_range;    // of a range's items together
+  int64_t whole_line;   // of the items dealt whole
+  int64_t shared_line;  // of the other shared items: where own items begin on the line
+  int64_t line;         // length of the line
+  int ctas;             // pieces it is cut into: CTAs [0, ctas) have one
+  int together;         // key blocks that a cut keeps together in a short item
 };
 
-// What work costs a CTA, for dealing it out: a key block against one and against
-// two row tiles (1.1 and 1.55 us measured at 16 requests over 32K), and what a
-// segment takes besides (some 2 us).
-constexpr int kCostOne = 2, kCostTwo = 3, kCostSegment = 4;
+// What work costs a CTA, for dealing it out, in units of 0.37 us: a key block
+// against one and against two row tiles (1.1 and 1.46 us measured at 16 requests
+// over 32K), and what a segment takes besides (1.9 us).
+constexpr int kCostOne = 3, kCostTwo = 4, kCostSegment = 5;
+// A segment of the tensor cores costs as much as two blocks, so a cut leaves four
+// together in a short item (of up to kShort), unless there is less work than CTAs;
+// a block of the fp32 kernel takes longer than what comes with it.
+constexpr int kTogether = 4, kShort = 8;
 template <int kUnitTiles>
 __device__ __forceinline__ int block_cost(const PrefixAttnParams& p, int tokens) {
   return kUnitTiles == 1 || tokens > p.tok_tile ? kCostTwo : kCostOne;
@@ -90,8 +104,7 @@ __device__ __forceinline__ int own_units(const PrefixAttnParams& p, const Prefix
   return cdiv(r.rows, unit_tiles * p.tok_tile);
 }
 
-// The own line: items of every sequence in the order (unit, head), each as long
-// as it costs.  Length of an item of a unit with `blocks` key blocks:
+// Length on the line of an own item of a unit with `blocks` key blocks:
 template <int kUnitTiles>
 __device__ __forceinline__ int item_length(const PrefixAttnParams& p, const PrefixSeq& r, int u, int blocks) {
   return blocks > 0 ? kCostSegment + blocks * block_cost<kUnitTiles>(p, r.rows - u * kUnitTiles * p.tok_tile) : 0;
@@ -115,11 +128,16 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
   for (int o = 16; o > 0; o >>= 1) base = min(base, __shfl_xor_sync(0xffffffffu, base, o));
   s.base = max(base, 0) / p.page * p.page;
   s.blocks = cdiv(s.base, kBlock);
-  s.per_split = cdiv(s.blocks, p.splits);
+  s.range = s.blocks / p.splits;
+  s.longer = s.blocks - s.range * p.splits;
   s.items = s.blocks > 0 ? p.nkv * p.splits * p.units : 0;
-  const int last = block_cost<kUnitTiles>(p, p.total - (p.units - 1) * kUnitTiles * p.tok_tile);
-  const int64_t cost = (int64_t)s.per_split * ((p.units - 1) * kCostTwo + last);
-  s.item_cost = kCostSegment + (int)(cost < INT_MAX ? (int)cost / p.units : long_div(cost, p.units));
+  s.whole = s.items / p.grid * p.grid;
+  const int most = s.range + (s.longer > 0);
+  s.len_two = kCostSegment + most * kCostTwo;
+  s.len_last = kCostSegment + most * block_cost<kUnitTiles>(p, p.total - (p.units - 1) * kUnitTiles * p.tok_tile);
+  s.len_range = (int64_t)(p.units - 1) * s.len_two + s.len_last;
+  s.whole_line = (int64_t)(s.whole / p.units) * s.len_range + (int64_t)(s.whole % p.units) * s.len_two;
+  s.shared_line = (int64_t)(s.items / p.units) * s.len_range - s.whole_line;
   int64_t line = 0;
   for (int i0 = 0; i0 < p.n; i0 += 32) {
     const int i = i0 + lane;
@@ -140,38 +158,48 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
     line += __shfl_sync(0xffffffffu, x, 31);
   }
   if (lane == 0) line_base[p.n] = line;
-  s.own_line = line;
+  s.line = s.shared_line + line;
+  const int least = kUnitTiles == 1 ? kCostTwo : kCostOne;
+  const bool small = s.line < (int64_t)p.grid * (kCostSegment + kTogether * least);
+  s.together = kUnitTiles == 1 || small ? 1 : kTogether;
+  s.ctas = small ? max(min((int)s.line / least, p.grid), 1) : p.grid;
   return s;
 }
 
-// Where CTA c's piece of the own line begins (c == grid: the line's end).  CTAs
-// below items % grid have one shared item more than the rest; the rest get as
-// much of the line as a shared item costs before the others get any.  (Filling
-// every CTA up by its own items' cost balances 16 requests over 32K by a few us
-// more, but to find that level takes 2.4 us before anything starts.)
-__device__ __forceinline__ int64_t part_of(int64_t line, int k, int n) {      // line * k / n
-  return line < (1 << 21) ? (int64_t)((uint32_t)line * (uint32_t)k / (uint32_t)n) : long_div(line * k, n);   // k <= grid < 2^11
+// Where CTA c's piece of the line begins (from c == ctas on: the line's end), and
+// the last CTA whose piece begins at or before place x of it.
+__device__ __forceinline__ int64_t piece_begin(const PrefixSched& s, int c) {
+  if (c >= s.ctas) return s.line;
+  return s.line < (1 << 21) ? (int64_t)((uint32_t)s.line * (uint32_t)c / (uint32_t)s.ctas) : long_div(s.line * c, s.ctas);   // c < 2^11
 }
-__device__ __forceinline__ int64_t own_begin(const PrefixSched& s, int grid, int c) {
-  const int more = s.items % grid, less = grid - more;
-  const int64_t fill = (int64_t)less * s.item_cost;
-  if (more > 0 && s.own_line <= fill) return c <= more ? 0 : part_of(s.own_line, c - more, less);
-  const int64_t even = more > 0 ? s.own_line - fill : s.own_line;
-  return part_of(even, c, grid) + (more > 0 && c > more ? (int64_t)(c - more) * s.item_cost : 0);
+__device__ __forceinline__ int piece_at(const PrefixSched& s, int64_t x) {
+  return s.line < (1 << 21) ? (int)((((uint32_t)x + 1) * (uint32_t)s.ctas - 1) / (uint32_t)s.line)
+                            : (int)long_div((x + 1) * s.ctas - 1, s.line);
+}
+__device__ __forceinline__ int64_t div_floor(int64_t a, int64_t b) {           // a >= 0, b > 0
+  return a <= INT_MAX && b <= INT_MAX ? (int64_t)((int)a / (int)b) : long_div(a, b);
+}
+
+// Shared items: the first key block of a range and their number, and the place
+// of an item counted from the first of all.
+__device__ __forceinline__ int range_begin(const PrefixSched& s, int range) { return range * s.range + min(range, s.longer); }
+__device__ __forceinline__ int range_blocks(const PrefixSched& s, int range) { return s.range + (range < s.longer); }
+__device__ __forceinline__ int64_t shared_place(const PrefixSched& s, int head_range, int unit) {
+  return head_range * s.len_range + (int64_t)unit * s.len_two;
 }
 
 // Workspace rows: the first row of a segment; its second tile's rows follow its
-// first's (tok_tile * rep of them).
+// first's (tok_tile * rep of them).  Shared items come before own ones.
 template <int kUnitTiles>
-__device__ __forceinline__ int64_t shared_rows(const PrefixAttnParams& p, int head, int split, int unit) {
-  return ((int64_t)(head * p.splits + split) * p.units + unit) * kUnitTiles * p.tok_tile * p.rep;
+__device__ __forceinline__ int64_t shared_rows(const PrefixAttnParams& p, const PrefixSched& s, int item, int cta) {
+  return ((int64_t)item + (item >= s.whole ? cta : 0)) * kUnitTiles * p.tok_tile * p.rep;
 }
 template <int kUnitTiles>
 __device__ __forceinline__ int64_t own_rows(const PrefixAttnParams& p, const PrefixSeq& r, int unit, int head, int cta) {
   const int t0 = unit * kUnitTiles * p.tok_tile, tokens = min(r.rows - t0, kUnitTiles * p.tok_tile);
   const int64_t before = (int64_t)p.nkv * (r.first + t0) + (int64_t)head * tokens;
-  const int64_t own0 = (int64_t)p.nkv * p.splits * p.units * kUnitTiles * p.tok_tile * p.rep;
-  return own0 + before * p.rep + (int64_t)cta * kUnitTiles * p.tok_tile * p.rep;
+  const int64_t units = (int64_t)p.nkv * p.splits * p.units + p.grid + cta;
+  return units * kUnitTiles * p.tok_tile * p.rep + before * p.rep;
 }
 
 // Four dims (chunk c) of workspace row r.  Four rows are interleaved chunk by
@@ -193,22 +221,17 @@ struct PrefixSeg {
   int64_t part;         // its first row of the workspace
 };
 
-// Key blocks of an own item (of `blocks`, each of `cost`) that belong to the
-// places before `at` of it: groups of blocks, the first with the segment's cost,
-// go to where they begin.  An item cut in two is two segments, and each costs its
-// CTA what a segment costs: on the tensor cores as much as two blocks, so four
-// stay together; a block of the fp32 kernel takes longer than what comes with it.
-template <int kUnitTiles>
-__device__ __forceinline__ int blocks_before(int64_t at, int blocks, int cost) {
-  constexpr int kTogether = kUnitTiles == 1 ? 1 : 4;
+// Key blocks of an item of the line (of `blocks`, each of `cost`) that belong to
+// the places before `at` of it: single ones or groups, the first with the
+// segment's cost, go to where they begin.
+__device__ __forceinline__ int blocks_before(const PrefixSched& s, int64_t at, int blocks, int cost) {
   if (at <= 0) return 0;
-  const int group = kTogether * cost;
-  const int64_t past = at - kCostSegment + group - 1;
-  const int64_t groups = at <= kCostSegment ? 1 : max(past < INT_MAX ? (int64_t)((int)past / group) : long_div(past, group), (int64_t)1);
-  return (int)min(groups * kTogether, (int64_t)blocks);
+  const int together = blocks <= kShort ? s.together : 1, group = together * cost;
+  const int64_t groups = at <= kCostSegment ? 1 : max(div_floor(at - kCostSegment + group - 1, group), (int64_t)1);
+  return (int)min(groups * together, (int64_t)blocks);
 }
 
-// The segments of a CTA: its shared items, and its piece [x, end) of the own line.
+// The segments of a CTA: its whole items, and its piece [x, end) of the line.
 template <int kUnitTiles, int kBlock>
 struct PrefixSegs {
   const PrefixAttnParams& p;
@@ -218,12 +241,13 @@ struct PrefixSegs {
   const int cta;
   const int32_t* shared_tab;
   int j;
-  int64_t x, end;
+  int64_t x, mid, end;                           // own segments [x, end); shared ones from mid down
 
   __device__ PrefixSegs(const PrefixAttnParams& p_, const PrefixSched& s_, const int64_t* base, const PrefixSeq* info_, int cta_)
       : p(p_), s(s_), line_base(base), info(info_), cta(cta_), shared_tab(nullptr), j(cta_) {
-    x = own_begin(s, p.grid, cta);
-    end = own_begin(s, p.grid, cta + 1);
+    x = piece_begin(s, cta);
+    end = piece_begin(s, cta + 1);
+    mid = min(end, s.shared_line);
     if (s.items > 0) {                           // base > 0: some sequence has rows
       int i = 0;
       while (i + 1 < p.n && info[i].rows == 0) ++i;
@@ -232,34 +256,56 @@ struct PrefixSegs {
   }
 
   __device__ bool next_shared(PrefixSeg& g) {
-    for (; j < s.items; j += p.grid) {
-      const int u = j % p.units, gs = j / p.units, split = gs % p.splits;
-      g.kb0 = split * s.per_split;
-      g.kb1 = min(g.kb0 + s.per_split, s.blocks);
-      if (g.kb0 >= g.kb1) continue;
+    for (;;) {
+      int gs, u, split, c0, c1;
+      if (j < s.whole) {
+        gs = j / p.units;
+        u = j - gs * p.units;
+        j += p.grid;
+        split = gs % p.splits;
+        c0 = 0;
+        c1 = range_blocks(s, split);
+      } else if (x < mid) {                      // the item of the place before mid
+        const int64_t place = s.whole_line + mid - 1;
+        gs = (int)div_floor(place, s.len_range);
+        const int64_t rel = place - gs * s.len_range;
+        u = (int)min(div_floor(rel, s.len_two), (int64_t)(p.units - 1));
+        const int cost = u + 1 < p.units ? kCostTwo : block_cost<kUnitTiles>(p, p.total - u * kUnitTiles * p.tok_tile);
+        const int64_t to = rel - (int64_t)u * s.len_two + 1, from = max(to - (mid - x), (int64_t)0);
+        mid -= to - from;
+        split = gs % p.splits;
+        const int blocks = range_blocks(s, split);
+        c0 = blocks_before(s, from, blocks, cost);
+        c1 = blocks_before(s, to, blocks, cost);
+      } else {
+        x = max(x, min(end, s.shared_line));
+        return false;
+      }
+      if (c0 >= c1) continue;
+      g.kb0 = range_begin(s, split) + c0;
+      g.kb1 = range_begin(s, split) + c1;
       g.tab = shared_tab;
       g.head = gs / p.splits;
       g.t0 = u * kUnitTiles * p.tok_tile;
       g.tokens = min(kUnitTiles * p.tok_tile, p.total - g.t0);
       g.k0 = 0;
       g.k_end = g.see0 = s.base;
-      g.part = shared_rows<kUnitTiles>(p, g.head, split, u);
-      j += p.grid;
+      g.part = shared_rows<kUnitTiles>(p, s, gs * p.units + u, cta);
       return true;
     }
-    return false;
   }
 
   __device__ bool next_own(PrefixSeg& g) {
     while (x < end) {
-      int lo = 0, hi = p.n;                      // the last sequence that starts at or before x
+      const int64_t place = x - s.shared_line;
+      int lo = 0, hi = p.n;                      // the last sequence that starts at or before it
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (line_base[mid] <= x) lo = mid; else hi = mid;
+        if (line_base[mid] <= place) lo = mid; else hi = mid;
       }
       const PrefixSeq r = info[lo];
       const int units = own_units(p, r, kUnitTiles);
-      int64_t rel = x - line_base[lo];
+      int64_t rel = place - line_base[lo];
       int u = 0, blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, 0);
       int64_t len = item_length<kUnitTiles>(p, r, 0, blocks);
       while (rel >= len * p.nkv && u + 1 < units) {
@@ -268,12 +314,12 @@ struct PrefixSegs {
         len = item_length<kUnitTiles>(p, r, u, blocks);
       }
       if (len <= 0) break;                       // (the line is made of items that have a length)
-      g.head = rel < INT_MAX && len < INT_MAX ? (int)rel / (int)len : (int)long_div(rel, len);
+      g.head = (int)div_floor(rel, len);
       const int64_t from = rel - g.head * len, to = min(len, from + (end - x));
       x += to - from;
       const int i0 = u * kUnitTiles * p.tok_tile, cost = block_cost<kUnitTiles>(p, r.rows - i0);
-      g.kb0 = blocks_before<kUnitTiles>(from, blocks, cost);
-      g.kb1 = blocks_before<kUnitTiles>(to, blocks, cost);
+      g.kb0 = blocks_before(s, from, blocks, cost);
+      g.kb1 = blocks_before(s, to, blocks, cost);
       if (g.kb0 >= g.kb1) continue;
       g.tab = p.table + (size_t)r.seq * p.max_pages;
       g.t0 = r.first + i0;
