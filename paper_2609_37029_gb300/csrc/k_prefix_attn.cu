@@ -28,13 +28,16 @@ __device__ __forceinline__ float ex2a(float x) {
 }
 
 constexpr int kFmaRows = 64, kFmaKeys = 64, kFmaThreads = 256;
+// CTAs of an SM: what is on its way in registers (HD / 16 float4) takes too many of them for two where HD = 128
+template <int HD>
+constexpr int kFmaPerSm = HD == 64 ? 2 : 1;
 
 template <int HD>
 struct FmaSmem {
   float q[kFmaRows][HD + 4];
   float kv[kFmaKeys][HD + 4];
   float p[kFmaRows][kFmaKeys + 4];
-  int64_t at[kFmaKeys];                          // element offset of each key of the block, -1: none
+  int64_t at[2][kFmaKeys];                       // element offset of each key of a block, -1: none
   int64_t line_base[kPrefixMaxSeqs + 1];
   PrefixSeq info[kPrefixMaxSeqs];
   PrefixSched sched;
@@ -45,6 +48,7 @@ __device__ void fma_segment(const PrefixAttnParams& p, FmaSmem<HD>& sm, const Pr
   constexpr int kD4 = HD / 4, kCols = HD / 64;   // float4 of a row; float4 output columns of a thread
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   const int rows = seg.tokens * p.rep, g = seg.head;
+  const bool live = 8 * (tid >> 5) < rows;       // the warp has rows (8 of the tile are its)
   const float* q = static_cast<const float*>(p.q);
   __syncthreads();
   for (int i = tid; i < kFmaRows * kD4; i += kFmaThreads) {
@@ -67,105 +71,127 @@ __device__ void fma_segment(const PrefixAttnParams& p, FmaSmem<HD>& sm, const Pr
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[a][c][e] = 0.f;
   }
+  // Keys, then values of a block go through one tile; the next ones are on their
+  // way in registers meanwhile.
+  float4 ahead[kFmaKeys * kD4 / kFmaThreads];
+  auto fetch = [&](const char* pool, int kb) {
+#pragma unroll
+    for (int i = 0; i < kFmaKeys * kD4 / kFmaThreads; ++i) {
+      const int x = tid + i * kFmaThreads;
+      const int64_t at = sm.at[kb & 1][x / kD4];
+      ahead[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (at >= 0) ahead[i] = *reinterpret_cast<const float4*>(pool + 4 * (at + 4 * (x % kD4)));
+    }
+  };
+  auto store = [&]() {
+#pragma unroll
+    for (int i = 0; i < kFmaKeys * kD4 / kFmaThreads; ++i) {
+      const int x = tid + i * kFmaThreads;
+      *reinterpret_cast<float4*>(&sm.kv[x / kD4][4 * (x % kD4)]) = ahead[i];
+    }
+  };
+  auto page_of = [&](int kb) {                   // of this thread's key of block kb; -1: none
+    const int pos = seg.k0 + kb * kFmaKeys + tid;
+    return tid < kFmaKeys && kb < seg.kb1 && pos < seg.k_end ? seg.tab[pos / p.page] : -1;
+  };
+  auto put_at = [&](int kb, int pg) {
+    if (tid >= kFmaKeys) return;
+    const int pos = seg.k0 + kb * kFmaKeys + tid;
+    int64_t at = -1;
+    if (pg >= 0 && pg < p.pages)
+      at = (int64_t)pg * p.s_page + (int64_t)(pos % p.page) * p.s_slot + (int64_t)g * p.s_head;
+    else if (kb < seg.kb1 && pos < seg.k_end)
+      set_err(p.err, LSP_DEV_BAD_SEQ);
+    sm.at[kb & 1][tid] = at;
+  };
+  put_at(seg.kb0, page_of(seg.kb0));
+  __syncthreads();                               // (and q is stored)
+  fetch(p.k, seg.kb0);
   for (int kb = seg.kb0; kb < seg.kb1; ++kb) {
     const int key0 = seg.k0 + kb * kFmaKeys;
-    __syncthreads();                             // q is stored; kv and p of the block before are read
-    if (tid < kFmaKeys) {
-      const int pos = key0 + tid;
-      int64_t at = -1;
-      if (pos < seg.k_end) {
-        const int pg = seg.tab[pos / p.page];
-        if (pg >= 0 && pg < p.pages)
-          at = (int64_t)pg * p.s_page + (int64_t)(pos % p.page) * p.s_slot + (int64_t)g * p.s_head;
-        else
-          set_err(p.err, LSP_DEV_BAD_SEQ);
-      }
-      sm.at[tid] = at;
-    }
+    const int next = page_of(kb + 1);
+    if (kb > seg.kb0) __syncthreads();           // the block before's values are read
+    store();
     __syncthreads();
-    auto load_kv = [&](const char* pool) {
-      for (int i = tid; i < kFmaKeys * kD4; i += kFmaThreads) {
-        const int r = i / kD4, c = i % kD4;
-        const int64_t at = sm.at[r];
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (at >= 0) x = *reinterpret_cast<const float4*>(pool + 4 * (at + 4 * c));
-        *reinterpret_cast<float4*>(&sm.kv[r][4 * c]) = x;
-      }
-    };
-    load_kv(p.k);
-    __syncthreads();
-    float s[4][4];
-#pragma unroll
-    for (int a = 0; a < 4; ++a)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) s[a][c] = 0.f;
-#pragma unroll 4
-    for (int d = 0; d < HD; d += 4) {
-      float4 x[4], y[4];
-#pragma unroll
-      for (int a = 0; a < 4; ++a) x[a] = *reinterpret_cast<const float4*>(&sm.q[4 * ty + a][d]);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) y[c] = *reinterpret_cast<const float4*>(&sm.kv[tx + 16 * c][d]);
+    fetch(p.v, kb);
+    if (live) {
+      float s[4][4];
 #pragma unroll
       for (int a = 0; a < 4; ++a)
 #pragma unroll
+        for (int c = 0; c < 4; ++c) s[a][c] = 0.f;
+#pragma unroll 2
+      for (int d = 0; d < HD; d += 4) {
+        float4 x[4], y[4];
+#pragma unroll
+        for (int a = 0; a < 4; ++a) x[a] = *reinterpret_cast<const float4*>(&sm.q[4 * ty + a][d]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[c] = *reinterpret_cast<const float4*>(&sm.kv[tx + 16 * c][d]);
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            s[a][c] = fmaf(x[a].x, y[c].x, s[a][c]);
+            s[a][c] = fmaf(x[a].y, y[c].y, s[a][c]);
+            s[a][c] = fmaf(x[a].z, y[c].z, s[a][c]);
+            s[a][c] = fmaf(x[a].w, y[c].w, s[a][c]);
+          }
+      }
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        float mx = -INFINITY;
+#pragma unroll
         for (int c = 0; c < 4; ++c) {
-          s[a][c] = fmaf(x[a].x, y[c].x, s[a][c]);
-          s[a][c] = fmaf(x[a].y, y[c].y, s[a][c]);
-          s[a][c] = fmaf(x[a].z, y[c].z, s[a][c]);
-          s[a][c] = fmaf(x[a].w, y[c].w, s[a][c]);
+          s[a][c] = key0 + tx + 16 * c < lim[a] ? s[a][c] * sl : -INFINITY;
+          mx = fmaxf(mx, s[a][c]);
         }
-    }
 #pragma unroll
-    for (int a = 0; a < 4; ++a) {
-      float mx = -INFINITY;
+        for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
+        const float nm = fmaxf(m[a], mx), mb = nm == -INFINITY ? 0.f : nm;
+        const float keep = ex2a(m[a] - mb);
+        float sum = 0.f;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        s[a][c] = key0 + tx + 16 * c < lim[a] ? s[a][c] * sl : -INFINITY;
-        mx = fmaxf(mx, s[a][c]);
+        for (int c = 0; c < 4; ++c) {
+          const float w = ex2a(s[a][c] - mb);
+          sum += w;
+          sm.p[4 * ty + a][tx + 16 * c] = w;
+        }
+#pragma unroll
+        for (int w = 8; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+        l[a] = l[a] * keep + sum;
+        m[a] = nm;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[a][c][e] *= keep;
       }
-#pragma unroll
-      for (int w = 8; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-      const float nm = fmaxf(m[a], mx), mb = nm == -INFINITY ? 0.f : nm;
-      const float keep = ex2a(m[a] - mb);
-      float sum = 0.f;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const float w = ex2a(s[a][c] - mb);
-        sum += w;
-        sm.p[4 * ty + a][tx + 16 * c] = w;
-      }
-#pragma unroll
-      for (int w = 8; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
-      l[a] = l[a] * keep + sum;
-      m[a] = nm;
-#pragma unroll
-      for (int c = 0; c < kCols; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[a][c][e] *= keep;
     }
     __syncthreads();                             // p is stored, k is read
-    load_kv(p.v);
+    store();
+    if (kb + 1 < seg.kb1) put_at(kb + 1, next);
     __syncthreads();
+    if (kb + 1 < seg.kb1) fetch(p.k, kb + 1);
+    if (live) {
 #pragma unroll 2
-    for (int j = 0; j < kFmaKeys; j += 4) {
-      float4 w[4];
+      for (int j = 0; j < kFmaKeys; j += 4) {
+        float4 w[4];
 #pragma unroll
-      for (int a = 0; a < 4; ++a) w[a] = *reinterpret_cast<const float4*>(&sm.p[4 * ty + a][j]);
+        for (int a = 0; a < 4; ++a) w[a] = *reinterpret_cast<const float4*>(&sm.p[4 * ty + a][j]);
 #pragma unroll
-      for (int jj = 0; jj < 4; ++jj)
+        for (int jj = 0; jj < 4; ++jj)
 #pragma unroll
-        for (int c = 0; c < kCols; ++c) {
-          const float4 y = *reinterpret_cast<const float4*>(&sm.kv[j + jj][4 * tx + 64 * c]);
+          for (int c = 0; c < kCols; ++c) {
+            const float4 y = *reinterpret_cast<const float4*>(&sm.kv[j + jj][4 * tx + 64 * c]);
 #pragma unroll
-          for (int a = 0; a < 4; ++a) {
-            const float x = jj == 0 ? w[a].x : jj == 1 ? w[a].y : jj == 2 ? w[a].z : w[a].w;
-            o[a][c][0] = fmaf(x, y.x, o[a][c][0]);
-            o[a][c][1] = fmaf(x, y.y, o[a][c][1]);
-            o[a][c][2] = fmaf(x, y.z, o[a][c][2]);
-            o[a][c][3] = fmaf(x, y.w, o[a][c][3]);
+            for (int a = 0; a < 4; ++a) {
+              const float x = jj == 0 ? w[a].x : jj == 1 ? w[a].y : jj == 2 ? w[a].z : w[a].w;
+              o[a][c][0] = fmaf(x, y.x, o[a][c][0]);
+              o[a][c][1] = fmaf(x, y.y, o[a][c][1]);
+              o[a][c][2] = fmaf(x, y.z, o[a][c][2]);
+              o[a][c][3] = fmaf(x, y.w, o[a][c][3]);
+            }
           }
-        }
+      }
     }
   }
 #pragma unroll
@@ -181,7 +207,7 @@ __device__ void fma_segment(const PrefixAttnParams& p, FmaSmem<HD>& sm, const Pr
 }
 
 template <int HD>
-__global__ void __launch_bounds__(kFmaThreads) prefix_attn_fma_kernel(const PrefixAttnParams p) {
+__global__ void __launch_bounds__(kFmaThreads, kFmaPerSm<HD>) prefix_attn_fma_kernel(const PrefixAttnParams p) {
   extern __shared__ __align__(16) uint8_t fma_raw[];
   FmaSmem<HD>& sm = *reinterpret_cast<FmaSmem<HD>*>(fma_raw);
   griddep_wait();
@@ -452,7 +478,7 @@ int choose_splits(int heads, int units, int blocks, int grid) {
 size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms) {
   const bool tc = dtype == LSP_DTYPE_BF16;
   const int tile = tc ? kPrefixTcRows : kFmaRows, unit_tiles = tc ? kPrefixTcTiles : 1;
-  const int block = tc ? kPrefixTcKeys : kFmaKeys, per_sm = tc ? 1 : 2;
+  const int block = tc ? kPrefixTcKeys : kFmaKeys, per_sm = tc ? 1 : p->d == 64 ? kFmaPerSm<64> : kFmaPerSm<128>;
   p->tok_tile = tile / p->rep;
   p->units = (p->total + p->tok_tile * unit_tiles - 1) / (p->tok_tile * unit_tiles);
   p->num_sms = num_sms;

@@ -282,6 +282,7 @@ __device__ __forceinline__ void load_role(const PrefixAttnParams& p, const CUten
   using Sh = TcShape<HD>;
   const int lane = threadIdx.x & 31;
   const int box = min(p.page, kKeys), boxes = kKeys / box;
+  const int page_bits = 31 - __clz(p.page);      // (a power of two)
   uint32_t fill = 0, nq = 0;
   PrefixSeg g;
   while (segs.next(g)) {
@@ -301,7 +302,7 @@ __device__ __forceinline__ void load_role(const PrefixAttnParams& p, const CUten
       const int pos = g.k0 + kb * kKeys + lane * box;
       int pg = p.pages;
       if (lane < boxes && kb < g.kb1 && pos < g.k_end) {
-        pg = __ldg(g.tab + pos / p.page);
+        pg = __ldg(g.tab + (pos >> page_bits));
         if (pg < 0 || pg >= p.pages) {
           set_err(p.err, LSP_DEV_BAD_SEQ);
           pg = p.pages;
@@ -316,7 +317,7 @@ __device__ __forceinline__ void load_role(const PrefixAttnParams& p, const CUten
       __syncwarp();
       if (lane < boxes) {
         const uint32_t dst = sm + Sh::kRing + st * Sh::kTile + (uint32_t)(lane * box) * 128u;
-        const int slot = (g.k0 + kb * kKeys + lane * box) % p.page;
+        const int slot = (g.k0 + kb * kKeys + lane * box) & (p.page - 1);
         for (int h = 0; h < Sh::kHalves; ++h) tma_load_4d(dst + h * Sh::kHalf, map, bar, 64 * h, slot, g.head, pg);
       }
       ++fill;

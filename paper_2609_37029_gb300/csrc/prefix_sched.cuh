@@ -53,15 +53,17 @@ struct PrefixSched {
 
 // What work costs a CTA, for dealing it out, in units of 0.37 us: a key block
 // against one and against two row tiles (1.1 and 1.46 us measured at 16 requests
-// over 32K), and what a segment takes besides (1.9 us).
-constexpr int kCostOne = 3, kCostTwo = 4, kCostSegment = 5;
+// over 32K), and what a segment takes besides (1.9 us).  The fp32 kernel's warps
+// have eight rows each, and those without rows leave the block to the others.
+constexpr int kCostFew = 2, kCostOne = 3, kCostTwo = 4, kCostSegment = 5;
 // A segment of the tensor cores costs as much as two blocks, so a cut leaves four
 // together in a short item (of up to kShort), unless there is less work than CTAs;
 // a block of the fp32 kernel takes longer than what comes with it.
 constexpr int kTogether = 4, kShort = 8;
 template <int kUnitTiles>
 __device__ __forceinline__ int block_cost(const PrefixAttnParams& p, int tokens) {
-  return kUnitTiles == 1 || tokens > p.tok_tile ? kCostTwo : kCostOne;
+  if (kUnitTiles == 1) return tokens * p.rep > 32 ? kCostTwo : tokens * p.rep > 8 ? kCostOne : kCostFew;
+  return tokens > p.tok_tile ? kCostTwo : kCostOne;
 }
 struct __align__(16) PrefixSeq {
   int seq, first, rows, len;    // row of the table (-1: none), first row of q, rows, tokens
