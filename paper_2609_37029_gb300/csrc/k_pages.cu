@@ -13,6 +13,13 @@
 //                list of pages to copy), then pages_copy_kernel
 //   compact      pages_compact_plan_kernel (one CTA: ranks, the list of moves),
 //                then pages_copy_kernel, which also rewrites the table
+//
+// branch (fork, reserve 17 tokens, write, trim) of 4 continuations of each of 16
+// prompts of 1000-4000 tokens, 32 layers: 76 us for 521 MB copied and written (6.9
+// TB/s, the rate of a plain copy).  compact of 2000 live pages of 3000, 8 layers:
+// 430 us for 2.8 GB (6.5 TB/s).  Both are bound by memory; small calls by their
+// launches (17 us from the host, 13 us and 10 us on the device for the four calls
+// and for the one).
 #include <algorithm>
 
 #include "common.cuh"
@@ -121,7 +128,8 @@ __global__ void __launch_bounds__(kSmallThreads) pages_write_kernel(const KvCach
   griddep_wait();
   griddep_launch();
   const int lane = threadIdx.x & 31;
-  const int w = (blockIdx.x * kSmallThreads + threadIdx.x) >> 5, t = w >> 1;
+  const int w = blockIdx.x * (kSmallThreads / 32) + (threadIdx.x >> 5);
+  const int t = (int)((unsigned)w >> 1);         // (two warps a row: w may pass 2^31)
   if (t >= total) return;
   int lo = 0, hi = n;                            // the last entry that starts at or before t
   while (hi - lo > 1) {

@@ -23,10 +23,17 @@
 // unless another warp's products run meanwhile: hence a warp for each stream.
 // They take turns -- P V of a block and the scores of the next -- because left
 // alone the streams drift into step, and then multiply at the same time and take
-// exponentials at the same time (32 requests over 128K: one warp for both 0.88
-// ms, two without turns 1.08, with them 0.87).  What bounds a stream now is its
-// chain: scores, their maximum, exponentials, P V, the next scores; P V therefore
-// starts when half of the weights are there (0.82).
+// exponentials at the same time (32 requests over 128K, when this was chosen: one
+// warp for both 0.88 ms, two without turns 1.08, with them 0.87).  P V starts when
+// half of the weights are there, for a stream is bound by its chain: scores, their
+// maximum, exponentials, P V, the next scores.
+//
+// Measured: 32 requests of 9 to 17 rows over 128K 750 us in all (1.47 PFLOP/s), 16
+// of 17 over 32K 131 us (1.14 PFLOP/s), 16 of one over 32K 46 us (3.2 TB/s, of
+// which 26 us at 5.7 TB/s; the rest is finding the work, the first loads and the
+// join).  In the long ones a block of two tiles takes 1.46 us, some 2800 cycles:
+// 2048 of products, and as many of shared memory, which the scores (both operands
+// from there) read at its full rate while the next keys and values are written.
 //
 // A stream's order is S(0) PV(0) S(1) PV(1) ...: S(j + 1) overwrites the weights
 // that PV(j) reads, and the products of one thread complete in order.  TMEM:
@@ -43,9 +50,9 @@ namespace {
 
 constexpr int kRows = kPrefixTcRows, kKeys = kPrefixTcKeys, kTiles = kPrefixTcTiles;
 constexpr int kThreads = 384;
-constexpr int kLoadWarp = 8, kMmaWarp = 9, kPlanWarp = 11;
+constexpr int kLoadWarp = 8, kMmaWarp = 9;       // the second products' warp and the plan's follow
 constexpr int kAhead = 4;                        // segments planned ahead
-constexpr int kFirstKeys = 64;                  // keys whose weights are handed over before the rest's (32: 0.84 ms, 96: 0.87)
+constexpr int kFirstKeys = 64;                   // keys whose weights are handed over before the rest's (0.75 ms over 128K; 32: 0.79, 96: 0.81)
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRaise = 8.0f;                   // log2 of the most a weight may exceed 1
 
@@ -60,7 +67,8 @@ struct TcShape {
 };
 
 struct TcMisc {
-  uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_first[2], p_full[2], o_full[2], o_free[2], turn[2], seg_full[kAhead], seg_empty[kAhead], lone_full[2], drain;
+  uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_first[2], p_full[2], o_full[2], o_free[2], turn[2];
+  uint64_t seg_full[kAhead], seg_empty[kAhead], lone_full[2], drain;
   uint32_t tmem;
   int abort;
   struct Planned {

@@ -1,0 +1,66 @@
+"""lsp_prefix_attention where its distribution of work is at an edge: more shared items than CTAs (some dealt
+whole, the rest cut), key ranges of several units cut in the middle, and so much work that places on the line of
+what is cut take more than 32-bit arithmetic.
+
+Tolerances: those of the other tests of this call, and for sums over some 2^11 key blocks in turn 8 sqrt(2^11)
+2^-24 = 2e-5 of sum_j w_j |v_j| more (fp32 rounding errors of either sign).
+"""
+import pytest
+import torch
+
+from tests.gpu_common import lsp_lib
+from tests.target_common import DT, make_cache, make_pool, oracle_cache
+from tests.test_gpu_prefix_attn import attend, case, compare
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lsp():
+    return lsp_lib()
+
+
+CASES = {
+    "more items than CTAs": dict(lens=[434 + 3 * i for i in range(40)], rows=[33] * 40, shared=400, nq=32, nkv=4, d=64, page=16),
+    "more items than CTAs, d 128": dict(lens=[300 + 5 * i for i in range(24)], rows=[20 + i for i in range(24)], shared=256, nq=32, nkv=8, d=128, page=64),
+    "ranges of several units": dict(lens=[2100 + 40 * i for i in range(12)], rows=[30 + i for i in range(12)], shared=2050, nq=8, nkv=2, d=128, page=32),
+    "a last unit of one tile": dict(lens=[1500 + i for i in range(9)], rows=[15] * 9, shared=1400, nq=16, nkv=2, d=64, page=128),
+}
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("name", list(CASES))
+def test_dealt_and_cut_items(lsp, name, dtype):
+    kw = dict(CASES[name], dtype=dtype)
+    pool, t, q = case(**kw)
+    out, z = attend(lsp, pool, t, q, list(range(len(kw["lens"]))), kw["rows"], kw["shared"])
+    compare(oracle_cache(*pool, *t), q, list(range(len(kw["lens"]))), kw["rows"], out, z)
+    again, z2 = attend(lsp, pool, t, q, list(range(len(kw["lens"]))), kw["rows"], kw["shared"], fill=0)
+    assert torch.equal(out, again) and torch.equal(z, z2)
+
+
+# rows and keys so that every shared item is on the line, and the line is longer than 2^21
+@pytest.mark.parametrize("dtype,rows,shared", [("bf16", [900, 1500], 460800), ("f32", [1200, 1100], 131072)])
+def test_a_line_beyond_32_bit_products(lsp, dtype, rows, shared):
+    page, nkv, rep, d = 256, 8, 2 if dtype == "bf16" else 1, 64
+    lens = [shared + r + 300 for r in rows]
+    g = torch.Generator(device="cuda").manual_seed(3)
+    need = shared // page + sum(-(-(n - shared) // page) for n in lens)
+    k, v = torch.randn(2, 1, need, nkv, page, d, generator=g, device="cuda").to(DT[dtype])
+    t = [x.cuda() for x in make_cache(lens, shared, page, (k, v))]
+    q = (torch.randn(sum(rows), nkv * rep, d, generator=g, device="cuda") * 1.5).to(DT[dtype])
+    out, z = attend(lsp, (k, v), t, q, [0, 1], rows, shared)
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(z).all())
+    at = [0, 1, 127, 128, 500, rows[0] - 1, rows[0], rows[0] + 513, sum(rows) - 130, sum(rows) - 1]
+    for i, row in enumerate(at):
+        b = int(row >= rows[0])
+        n = lens[b] - rows[b] + (row - b * rows[0]) + 1
+        pages = t[0][b, :-(-n // page)].long()
+        for h in {(3 * i) % (nkv * rep), nkv * rep - 1}:
+            kk, vv = (x[0, pages, h // rep].reshape(-1, d)[:n].double() for x in (k, v))
+            s = kk @ q[row, h].double() * d ** -0.5
+            w = torch.softmax(s, 0)
+            want, size, lse = w @ vv, w @ vv.abs(), float(torch.logsumexp(s, 0))
+            tol = (2 ** -8 + 2 ** -10) * (size + want.abs()) if dtype == "bf16" else (4e-5 + 2e-5) * size
+            assert bool(((out[row, h].double() - want).abs() <= tol).all()), (row, h)
+            assert abs(float(z[row, h]) - lse) <= 2e-5 + 2e-6 * abs(lse)
