@@ -437,7 +437,9 @@ int launch_join(const PrefixAttnParams& p, cudaStream_t s) {
   const int64_t rows = (int64_t)p.total * p.nq;
   auto ctas = [&](int heads) { return ((int64_t)p.total * p.nkv * ((p.rep + heads - 1) / heads) + kJoinRows - 1) / kJoinRows; };
   const size_t smem = p.n * (sizeof(PrefixSeq) + sizeof(int64_t)) + sizeof(int64_t);
-  const bool few = rows < 16 * (int64_t)p.num_sms;
+  // four warps a row while all their CTAs are resident at once, two on an SM (over 8K, 1024 rows: 32.4 us, with
+  // one warp for several 33.2; 512 rows 27.6 and 30.5; 2048 rows 53 and 42)
+  const bool few = rows <= 2 * kJoinRows * (int64_t)p.num_sms;
   const cudaError_t e =
       few ? launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 4, 1>, dim3((unsigned)ctas(1)), dim3(128 * kJoinRows), smem, s, p)
           : launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 1, kJoinHeads>, dim3((unsigned)std::min<int64_t>(ctas(kJoinHeads), kJoinPerSm * p.num_sms)),
