@@ -14,8 +14,8 @@
 // (score, index) through distributed shared memory.  No workspace, no atomics.
 //
 // 4 requests of 32001 entries take 5.6 us: launch, and the chain token -> p, q ->
-// row -> exchange.  16 of 151936 entries: 10.4 us for 29 MB, 64 with 16-bit
-// probabilities and drafts without a distribution: 17.9 us for 58 MB (3.3 TB/s);
+// row -> exchange.  16 of 151936 entries: 10.6 us for 29 MB, 64 with 16-bit
+// probabilities and drafts without a distribution: 17.4 us for 58 MB (3.4 TB/s);
 // the rounds of loads of a slice bound it, two CTAs of 512 threads on an SM.
 #include <cooperative_groups.h>
 
@@ -32,34 +32,36 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kVpThreads = 512;
-constexpr int kVpMaxCluster = 8;                 // CTAs per request at most (16 requests: 10.4 us with 8, 15.9 with 16)
+constexpr int kVpMaxCluster = 8;                 // CTAs per request at most (16 requests: 10.6 us with 8, 15.9 with 16)
 constexpr unsigned kAll = 0xffffffffu;
 
 __device__ __forceinline__ bool better(float v, int i, float bv, int bi) { return v > bv || (v == bv && i < bi); }
 
-// VEC consecutive probabilities as fp32 (one 16-byte load where VEC > 1)
+// VEC consecutive values as they lie in memory (one load), and as fp32
 template <typename T, int VEC>
-__device__ __forceinline__ void load_probs(const T* p, float* x) {
-  if constexpr (VEC == 1) {
-    x[0] = to_f(__ldg(p));
-  } else if constexpr (sizeof(T) == 4) {
-    const float4 v = __ldg(reinterpret_cast<const float4*>(p));
-    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-  } else {
-    const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
-    const __nv_bfloat162 a = *reinterpret_cast<const __nv_bfloat162*>(&v.x), b = *reinterpret_cast<const __nv_bfloat162*>(&v.y);
-    x[0] = __low2float(a); x[1] = __high2float(a); x[2] = __low2float(b); x[3] = __high2float(b);
+struct Vals {
+  static constexpr int kRegs = sizeof(T) * VEC < 4 ? 1 : (int)sizeof(T) * VEC / 4;
+  uint32_t w[kRegs];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (VEC == 1) {
+      w[0] = sizeof(T) == 4 ? __ldg(reinterpret_cast<const uint32_t*>(p)) : (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p));
+    } else if constexpr (sizeof(T) == 4) {
+      const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
+      w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    } else {
+      const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+      w[0] = v.x; w[1] = v.y;
+    }
   }
-}
-template <int VEC>
-__device__ __forceinline__ void load_floats(const float* p, float* x) {
-  if constexpr (VEC == 1) {
-    x[0] = __ldg(p);
-  } else {
-    const float4 v = __ldg(reinterpret_cast<const float4*>(p));
-    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int k = 0; k < kRegs; ++k) w[k] = 0;
   }
-}
+  __device__ __forceinline__ float get(int j) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[j]);
+    return __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+  }
+};
 
 __device__ __noinline__ float quotient(float w, float e) { return __fdiv_rn(w, e); }
 
@@ -70,20 +72,23 @@ __device__ __noinline__ float quotient(float w, float e) { return __fdiv_rn(w, e
 // where the best or the product is tiny or no number).
 template <typename T, int VEC, bool kQ>
 __device__ __forceinline__ void scan_row(const T* p, const T* q, const float* e, int skip, int g0, int g1, float& bv, int& bi) {
-  constexpr int kBatch = VEC == 1 ? 8 : 2;
+  // loads in flight: what some 32 registers hold
+  constexpr int kBatch = VEC == 1 ? 8 : 32 / ((kQ ? 2 : 1) * Vals<T, VEC>::kRegs + VEC);
   float bound = -1.f;
   for (int first = g0; first < g1; first += kBatch * kVpThreads) {     // the same count for the whole CTA
     const int base = first + threadIdx.x;
-    float a[kBatch][VEC], b[kBatch][VEC], x[kBatch][VEC];
+    Vals<T, VEC> a[kBatch], b[kBatch];
+    Vals<float, VEC> x[kBatch];
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       const int g = base + k * kVpThreads;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) a[k][j] = b[k][j] = x[k][j] = 0.f;
+      a[k].zero();
+      if (kQ) b[k].zero();
+      x[k].zero();
       if (g < g1) {
-        load_probs<T, VEC>(p + (size_t)g * VEC, a[k]);
-        if (kQ) load_probs<T, VEC>(q + (size_t)g * VEC, b[k]);
-        load_floats<VEC>(e + (size_t)g * VEC, x[k]);
+        a[k].load(p + (size_t)g * VEC);
+        if (kQ) b[k].load(q + (size_t)g * VEC);
+        x[k].load(e + (size_t)g * VEC);
       }
     }
 #pragma unroll
@@ -93,16 +98,16 @@ __device__ __forceinline__ void scan_row(const T* p, const T* q, const float* e,
       float w[VEC];
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        w[j] = kQ ? a[k][j] - b[k][j] : a[k][j];
+        w[j] = kQ ? a[k].get(j) - b[k].get(j) : a[k].get(j);
         if (!kQ && v0 + j == skip) w[j] = 0.f;
-        const float least = bound * x[k][j];
+        const float least = bound * x[k].get(j);
         any |= w[j] > 0.f && (!(w[j] < least) || !(least > 1e-36f));
       }
       if (any) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j)
           if (w[j] > 0.f) {
-            const float sc = quotient(w[j], x[k][j]);
+            const float sc = quotient(w[j], x[k].get(j));
             // indices rise within a thread: a strict > keeps the lowest on ties
             if (sc > bv) { bv = sc; bi = v0 + j; }
           }
@@ -171,6 +176,9 @@ __global__ void __launch_bounds__(kVpThreads, 2) verify_probs_kernel(const Verif
       n = n < 0 ? 0 : B;
     }
   }
+  const float* e = p.e + (size_t)b * V;
+  const int ng = V / VEC;                        // VEC > 1 only where V % VEC == 0
+  const int g0 = (int)((int64_t)ch * ng / parts), g1 = (int)((int64_t)(ch + 1) * ng / parts);
   if (warp == 0) {
     int r = n;
     for (int i0 = 0; i0 < n; i0 += 32) {
@@ -195,9 +203,6 @@ __global__ void __launch_bounds__(kVpThreads, 2) verify_probs_kernel(const Verif
   __syncthreads();
   const int r = s_r;
   const T* row = pt + (int64_t)r * p.ld_t;
-  const float* e = p.e + (size_t)b * V;
-  const int ng = V / VEC;                        // VEC > 1 only where V % VEC == 0
-  const int g0 = (int)((int64_t)ch * ng / parts), g1 = (int)((int64_t)(ch + 1) * ng / parts);
   float bv = -1.f;
   int bi = INT_MAX;
   if (r < n && pq)
@@ -244,11 +249,11 @@ cudaError_t launch(const VerifyProbsParams& p, int parts, cudaStream_t s) {
 int launch_verify_probs(const VerifyProbsParams& p, int dtype, int num_sms, cudaStream_t s) {
   const int es = dtype == LSP_DTYPE_BF16 ? 2 : 4;
   // four values a load where every row starts on a load's boundary (64 requests of 16-bit
-  // probabilities: 17.9 us, one value a load 22.0)
+  // probabilities: 17.4 us, one value a load 21.6)
   const uintptr_t at = reinterpret_cast<uintptr_t>(p.pt) | reinterpret_cast<uintptr_t>(p.pq);
   const bool vec = p.V % 4 == 0 && p.ld_t % 4 == 0 && (!p.pq || p.ld_q % 4 == 0) && at % (4 * es) == 0 &&
                    reinterpret_cast<uintptr_t>(p.e) % 16 == 0;
-  // as many CTAs a request as are resident at once, two on an SM (64 requests: 17.9 us with 4, 23 with 8)
+  // as many CTAs a request as are resident at once, two on an SM (64 requests: 17.4 us with 4, 23 with 8)
   int parts = kVpMaxCluster;
   while (parts > 1 && (int64_t)p.C * parts > 2 * num_sms) parts /= 2;
   cudaError_t e;
