@@ -11,7 +11,7 @@
 // prefix_attn_fma_kernel: f32 storage, fp32 multiply-adds, 64 rows x 64 keys a
 // step, 4 x 4 scores and 4 x (HD / 16) sums a thread.  Bound by the multiply-adds
 // where rows fill the tiles (16 requests of 1 to 17 rows, 32 heads of 128, over 8K:
-// 635 us), by the latency of its rounds of loads in small calls (5 over 2K: 21 us).
+// 637 us), by the latency of its rounds of loads in small calls (5 over 2K: 18 us).
 // bf16 storage: k_prefix_attn_tc.cu.
 #include <algorithm>
 #include <cstdint>

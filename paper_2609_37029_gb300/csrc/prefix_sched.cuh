@@ -55,14 +55,14 @@ struct PrefixSched {
 // against one and against two row tiles (1.1 and 1.46 us measured at 16 requests
 // over 32K), and what a segment takes besides (1.9 us).  The fp32 kernel's warps
 // have eight rows each, and those without rows leave the block to the others.
-constexpr int kCostFew = 2, kCostOne = 3, kCostTwo = 4, kCostSegment = 5;
+constexpr int kCostOne = 3, kCostTwo = 4, kCostSegment = 5;
 // A segment of the tensor cores costs as much as two blocks, so a cut leaves four
 // together in a short item (of up to kShort), unless there is less work than CTAs;
 // a block of the fp32 kernel takes longer than what comes with it.
 constexpr int kTogether = 4, kShort = 8;
 template <int kUnitTiles>
 __device__ __forceinline__ int block_cost(const PrefixAttnParams& p, int tokens) {
-  if (kUnitTiles == 1) return tokens * p.rep > 32 ? kCostTwo : tokens * p.rep > 8 ? kCostOne : kCostFew;
+  if (kUnitTiles == 1) return tokens * p.rep > 32 ? kCostTwo : kCostOne;
   return tokens > p.tok_tile ? kCostTwo : kCostOne;
 }
 struct __align__(16) PrefixSeq {
@@ -161,7 +161,7 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
   }
   if (lane == 0) line_base[p.n] = line;
   s.line = s.shared_line + line;
-  const int least = kUnitTiles == 1 ? kCostTwo : kCostOne;
+  const int least = kCostOne;
   const bool small = s.line < (int64_t)p.grid * (kCostSegment + kTogether * least);
   s.together = kUnitTiles == 1 || small ? 1 : kTogether;
   s.ctas = small ? max(min((int)s.line / least, p.grid), 1) : p.grid;

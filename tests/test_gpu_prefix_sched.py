@@ -64,3 +64,25 @@ def test_a_line_beyond_32_bit_products(lsp, dtype, rows, shared):
             tol = (2 ** -8 + 2 ** -10) * (size + want.abs()) if dtype == "bf16" else (4e-5 + 2e-5) * size
             assert bool(((out[row, h].double() - want).abs() <= tol).all()), (row, h)
             assert abs(float(z[row, h]) - lse) <= 2e-5 + 2e-6 * abs(lse)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_rows_of_no_sequence_beside_a_shared_prefix(lsp, dtype):
+    """They are stacked with the others against the shared pages, and give 0 all the same; so does an entry
+    outside the cache, and the others are not disturbed."""
+    lens, rows, shared = [310, 333, 340], [5, 9, 17], 300
+    pool, t, _ = case(lens, rows, shared, nq=4, nkv=2, d=64, dtype=dtype, page=16)
+    total, before = 44, 6
+    q = torch.randn(total, 4, 64, device="cuda").to(DT[dtype])
+    c = lsp.make_kv_cache(*pool, *t)
+    start = torch.tensor([6, 11, 20, 37, 40], dtype=torch.int32, device="cuda")
+    ids = torch.tensor([0, 1, 2, 99], dtype=torch.int32, device="cuda")      # the last one does not exist
+    ws = torch.empty(lsp.lsp_prefix_attention_workspace_bytes(c, 4, 4, total), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    out, z = torch.full_like(q, 7), torch.full((total, 4), 7.0, device="cuda")
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    lsp.lsp_prefix_attention(c, 0, q, ids, start, out, z, shared_len=shared, scale=0.125, workspace=ws, dev_error=err)
+    torch.cuda.synchronize()
+    assert int(err) == lsp.LSP_DEV_BAD_SEQ
+    none = list(range(before)) + list(range(37, total))
+    assert not out[none].any() and torch.isneginf(z[none]).all()
+    compare(oracle_cache(*pool, *t), q[6:37], [0, 1, 2], rows, out[6:37], z[6:37], scale=0.125)
