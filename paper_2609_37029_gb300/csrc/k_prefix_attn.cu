@@ -247,8 +247,10 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
   extern __shared__ __align__(16) uint8_t join_raw[];
   __shared__ float s_o[kWarps > 1 ? kJoinRows * kWarps : 1][HD], s_l[kJoinRows * kWarps];
   __shared__ PrefixSched s_sched;
+  __shared__ int s_pieces[2];
   PrefixSeq* info = reinterpret_cast<PrefixSeq*>(join_raw);
   int64_t* line_base = reinterpret_cast<int64_t*>(info + p.n);
+  int64_t* begin = line_base + p.n + 1;          // [grid + 1]: piece_begin
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp / kJoinRows;
   if (warp == 0) {
     const PrefixSched s = build_sched<kUnitTiles, kBlock>(p, line_base, info, false);
@@ -256,6 +258,19 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
   }
   __syncthreads();
   const PrefixSched s = s_sched;
+  for (int c = threadIdx.x; c <= p.grid; c += blockDim.x) begin[c] = piece_begin(s, c);
+  // the most pieces that have part of a shared item of a unit but the last, of the last
+  if (threadIdx.x < 2)
+    s_pieces[threadIdx.x] = s.whole < s.items ? (int)div_floor((int64_t)(threadIdx.x ? s.len_last : s.len_two) * s.ctas, s.line) + 2 : 1;
+  __syncthreads();
+  // the last CTA whose piece begins at or before place x of the line: an estimate, and what rounding leaves
+  const float per_place = __fdividef((float)s.ctas, (float)s.line);
+  auto piece_at = [&](int64_t x) {
+    int c = min((int)((float)x * per_place), s.ctas - 1);
+    while (c + 1 < s.ctas && begin[c + 1] <= x) ++c;
+    while (begin[c] > x) --c;
+    return c;
+  };
   const int parts = cdiv(p.rep, kHeads), per = cdiv(p.rep, parts);   // of a KV head's query heads, and heads of one
   const int64_t rows = (int64_t)p.total * p.nkv * parts;
   bool waited = false;
@@ -272,21 +287,22 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
     // segments: of each range of the shared part the (at most `pieces`) CTAs that
     // have part of its item, then those of the own item
     int shared = 0, pieces = 1, own = 0, c0 = 0, u = 0, unit = 0, shared_at = 0, own_at = 0, blocks = 0, cost = 1, shared_cost = 1;
-    int64_t first = 0;
+    int64_t first = 0, shared_first = 0;         // places of the own item, and of the first range's
     if (t >= r.first && t < r.first + r.rows) {
       const int tile_rows = p.tok_tile * p.rep;
       if (s.items > 0) {
         const int tile = t / p.tok_tile;
         u = tile / kUnitTiles;
-        shared_at = (tile % kUnitTiles) * tile_rows + (t % p.tok_tile) * p.rep + hr;
+        shared_at = (tile % kUnitTiles) * tile_rows + (t - tile * p.tok_tile) * p.rep + hr;
         const bool last = u + 1 == p.units;
         shared_cost = last ? block_cost<kUnitTiles>(p, p.total - u * kUnitTiles * p.tok_tile) : kCostTwo;
-        if (s.whole < s.items) pieces = (int)div_floor((int64_t)(last ? s.len_last : s.len_two) * s.ctas, s.line) + 2;
+        pieces = s_pieces[last];
         shared = p.splits * pieces;
+        shared_first = shared_place(s, g * p.splits, u) - s.whole_line;
       }
       const int i = t - r.first, tile = i / p.tok_tile;
       unit = tile / kUnitTiles;
-      own_at = (tile % kUnitTiles) * tile_rows + (i % p.tok_tile) * p.rep + hr;
+      own_at = (tile % kUnitTiles) * tile_rows + (i - tile * p.tok_tile) * p.rep + hr;
       first = s.shared_line + line_base[lo];
       for (int u = 0; u < unit; ++u)
         first += (int64_t)item_length<kUnitTiles>(p, r, u, own_blocks<kUnitTiles, kBlock>(p, r, s.base, u)) * p.nkv;
@@ -295,35 +311,31 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
       const int len = item_length<kUnitTiles>(p, r, unit, blocks);
       first += (int64_t)g * len;
       if (blocks > 0) {
-        c0 = piece_at(s, first);
-        own = piece_at(s, first + len - 1) + 1 - c0;
+        c0 = piece_at(first);
+        own = piece_at(first + len - 1) + 1 - c0;
       }
     }
     const int all = shared + own;
     auto row_of = [&](int q) -> int64_t {        // -1: no such segment
       if (q >= all) return -1;
       const bool sh = q < shared;
-      const int range = sh ? q / pieces : 0, k = sh ? q - range * pieces : q - shared;
-      const int head_range = g * p.splits + range, item = head_range * p.units + u;
-      const int nb = sh ? range_blocks(s, range) : blocks;
+      const int range = sh && q >= pieces ? q / pieces : 0, k = sh ? q - range * pieces : q - shared;
+      const int item = (g * p.splits + range) * p.units + u, nb = sh ? range_blocks(s, range) : blocks;
       if (sh && item < s.whole) return k == 0 && nb > 0 ? shared_rows<kUnitTiles>(p, s, item, 0) + shared_at : -1;
-      const int64_t place = sh ? shared_place(s, head_range, u) - s.whole_line : first;
-      const int c = (sh ? piece_at(s, place) : c0) + k;
+      const int64_t place = sh ? shared_first + range * s.len_range : first;
+      const int c = (sh ? piece_at(place) : c0) + k;
       if (c >= s.ctas) return -1;
       // a CTA may have a piece of the item without any of its blocks
       const int price = sh ? shared_cost : cost;
-      if (blocks_before(s, piece_begin(s, c + 1) - place, nb, price) <=
-          blocks_before(s, piece_begin(s, c) - place, nb, price))
-        return -1;
+      if (blocks_before(s, begin[c + 1] - place, nb, price) <= blocks_before(s, begin[c] - place, nb, price)) return -1;
       return sh ? shared_rows<kUnitTiles>(p, s, item, c) + shared_at : own_rows<kUnitTiles>(p, r, unit, g, c) + own_at;
     };
     // the first segment of this lane for the maxima, and for the sums
-    int64_t row_m = -1, row_s = -1;
-#pragma unroll 1
-    for (int k = 0; k < (kWarps > 1 ? 2 : 1); ++k) {
-      const int64_t x = row_of(k == 0 ? lane : lane * kWarps + part);
-      if (k == 0) row_m = x;
-      row_s = x;
+    int64_t row_m = row_of(lane), row_s = row_m;
+    if (kWarps > 1) {
+      const int src = lane * kWarps + part;
+      row_s = __shfl_sync(0xffffffffu, row_m, src & 31);
+      if (src >= 32) row_s = row_of(src);
     }
     if (!waited) {
       griddep_wait();
@@ -436,7 +448,7 @@ template <typename T, int HD, int kUnitTiles, int kBlock>
 int launch_join(const PrefixAttnParams& p, cudaStream_t s) {
   const int64_t rows = (int64_t)p.total * p.nq;
   auto ctas = [&](int heads) { return ((int64_t)p.total * p.nkv * ((p.rep + heads - 1) / heads) + kJoinRows - 1) / kJoinRows; };
-  const size_t smem = p.n * (sizeof(PrefixSeq) + sizeof(int64_t)) + sizeof(int64_t);
+  const size_t smem = p.n * (sizeof(PrefixSeq) + sizeof(int64_t)) + (p.grid + 2) * sizeof(int64_t);
   // four warps a row while all their CTAs are resident at once, two on an SM (over 8K, 1024 rows: 32.4 us, with
   // one warp for several 33.2; 512 rows 27.6 and 30.5; 2048 rows 53 and 42)
   const bool few = rows <= 2 * kJoinRows * (int64_t)p.num_sms;

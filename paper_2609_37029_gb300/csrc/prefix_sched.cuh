@@ -168,15 +168,10 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
   return s;
 }
 
-// Where CTA c's piece of the line begins (from c == ctas on: the line's end), and
-// the last CTA whose piece begins at or before place x of it.
+// Where CTA c's piece of the line begins (from c == ctas on: the line's end).
 __device__ __forceinline__ int64_t piece_begin(const PrefixSched& s, int c) {
   if (c >= s.ctas) return s.line;
   return s.line < (1 << 21) ? (int64_t)((uint32_t)s.line * (uint32_t)c / (uint32_t)s.ctas) : long_div(s.line * c, s.ctas);   // c < 2^11
-}
-__device__ __forceinline__ int piece_at(const PrefixSched& s, int64_t x) {
-  return s.line < (1 << 21) ? (int)((((uint32_t)x + 1) * (uint32_t)s.ctas - 1) / (uint32_t)s.line)
-                            : (int)long_div((x + 1) * s.ctas - 1, s.line);
 }
 __device__ __forceinline__ int64_t div_floor(int64_t a, int64_t b) {           // a >= 0, b > 0
   return a <= INT_MAX && b <= INT_MAX ? (int64_t)((int)a / (int)b) : long_div(a, b);
@@ -227,9 +222,13 @@ struct PrefixSeg {
 // the places before `at` of it: single ones or groups, the first with the
 // segment's cost, go to where they begin.
 __device__ __forceinline__ int blocks_before(const PrefixSched& s, int64_t at, int blocks, int cost) {
-  if (at <= 0) return 0;
+  if (at <= kCostSegment) return at > 0 ? min(blocks <= kShort ? s.together : 1, blocks) : 0;
   const int together = blocks <= kShort ? s.together : 1, group = together * cost;
-  const int64_t groups = at <= kCostSegment ? 1 : max(div_floor(at - kCostSegment + group - 1, group), (int64_t)1);
+  const int64_t n = at - kCostSegment + group - 1;
+  // n / group, by ceil(2^32 / group): exact below 2^32 / group
+  static_assert(kCostOne == 3 && kCostTwo == 4 && kTogether == 4, "the groups' inverses");
+  const uint32_t inverse = cost == kCostOne ? (together == 1 ? 1431655766u : 357913942u) : (together == 1 ? 1u << 30 : 1u << 28);
+  const int64_t groups = n < (1 << 28) ? (int64_t)__umulhi((uint32_t)n, inverse) : long_div(n, group);
   return (int)min(groups * together, (int64_t)blocks);
 }
 
