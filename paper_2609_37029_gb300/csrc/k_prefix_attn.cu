@@ -235,8 +235,8 @@ __global__ void __launch_bounds__(kFmaThreads, kFmaPerSm<HD>) prefix_attn_fma_ke
 // once, and their sums lie side by side (16 requests over 32K, a round: 132 us in
 // all with four heads a warp, 139 with one).
 //
-// Bound by the latency of its three dependent rounds of loads.  Where the
-// segments are follows from the lengths alone, so every CTA finds that out again
+// Bound by latency: 5 us to find a row's segments in code that is not cached yet,
+// and three dependent rounds of loads of some 3 us.  Where the segments are follows from the lengths alone, so every CTA finds that out again
 // before it waits for the main kernel (which lets it start only after its own
 // wait: the lengths are final).
 constexpr int kJoinRows = 4, kJoinHeads = 4, kJoinPerSm = 4;

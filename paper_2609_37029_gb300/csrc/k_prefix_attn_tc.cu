@@ -29,7 +29,7 @@
 // maximum, exponentials, P V, the next scores.
 //
 // Measured: 32 requests of 9 to 17 rows over 128K 750 us in all (1.47 PFLOP/s), 16
-// of 17 over 32K 131 us (1.14 PFLOP/s), 16 of one over 32K 46 us (3.2 TB/s, of
+// of 17 over 32K 130 us (1.15 PFLOP/s), 16 of one over 32K 44 us (3.4 TB/s, of
 // which 26 us at 5.7 TB/s; the rest is finding the work, the first loads and the
 // join).  In the long ones a block of two tiles takes 1.46 us, some 2800 cycles:
 // 2048 of products, and as many of shared memory, which the scores (both operands
