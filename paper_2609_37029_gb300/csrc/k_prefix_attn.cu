@@ -236,9 +236,10 @@ __global__ void __launch_bounds__(kFmaThreads, kFmaPerSm<HD>) prefix_attn_fma_ke
 // all with four heads a warp, 139 with one).
 //
 // Bound by latency: 5 us to find a row's segments in code that is not cached yet,
-// and three dependent rounds of loads of some 3 us.  Where the segments are follows from the lengths alone, so every CTA finds that out again
-// before it waits for the main kernel (which lets it start only after its own
-// wait: the lengths are final).
+// and three dependent rounds of loads of some 3 us.  Where the segments are
+// follows from the lengths alone, so every CTA finds that out again before it
+// waits for the main kernel (which lets it start only after its own wait: the
+// lengths are final).
 constexpr int kJoinRows = 4, kJoinHeads = 4, kJoinPerSm = 4;
 template <typename T, int HD, int kUnitTiles, int kBlock, int kWarps, int kHeads>
 __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoinPerSm) prefix_join_kernel(const PrefixAttnParams p) {

@@ -86,3 +86,22 @@ def test_rows_of_no_sequence_beside_a_shared_prefix(lsp, dtype):
     none = list(range(before)) + list(range(37, total))
     assert not out[none].any() and torch.isneginf(z[none]).all()
     compare(oracle_cache(*pool, *t), q[6:37], [0, 1, 2], rows, out[6:37], z[6:37], scale=0.125)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("rise", [20.0, 45.0, 300.0, 5000.0])
+@pytest.mark.parametrize("spots", [(130,), (200,), (140, 220, 400), (1, 300, 390, 511, 640, 1000)])
+def test_maxima_that_rise_late(lsp, dtype, rise, spots):
+    """Scores that jump by `rise` at each of `spots`, in either half of a key block, for some of the rows: weights
+    relative to the maximum so far would pass every range."""
+    n, d = 1100, 64
+    pool, t, q = case([n, n], [3, 2], 1024, nq=4, nkv=2, d=d, dtype=dtype, page=64, seed=11)
+    k = pool[0]
+    q[:, :, 0] = torch.tensor([4.0, 0.0, 2.0, 0.5], device="cuda").to(q.dtype)       # which heads see the jumps, and how
+    k[..., 0] = 0
+    for i, pos in enumerate(spots):
+        pages, slot = t[0][:, pos // 64].long(), pos % 64
+        for pg in pages.tolist():
+            k[0, pg, :, slot, 0] = (i + 1) * rise * 2                                # head 0: (i + 1) rise at scale 1 / 8
+    out, z = attend(lsp, pool, t, q, [0, 1], [3, 2], 1024)
+    compare(oracle_cache(*pool, *t), q, [0, 1], [3, 2], out, z)
