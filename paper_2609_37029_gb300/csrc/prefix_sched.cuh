@@ -19,8 +19,8 @@
 // piece may start and end inside an item.  A CTA goes through the shared segments
 // of its piece from the last to the first: with pieces somewhat shorter than
 // items, it then comes to the first keys of one item and the last of the item
-// before when the others do (forwards, every unit read the keys from memory:
-// 4.7 GB for 0.5 at 32 requests over 128K).
+// before when the others do (forwards, nearly every unit read the keys from
+// memory: 4.7 GB instead of 1.1 at 32 requests over 128K, 0.92 ms instead of 0.80).
 //
 // Every segment (the part of an item that one CTA has) leaves unnormalised sums
 // and the running maximum and sum of its rows in rows of the workspace; a second
