@@ -595,8 +595,10 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
     float w0 = 1.f, w1 = 0.f;
     if (t == 0 && jobs.count > 1) {              // (two row tiles: stream 1 waits for its own)
       if (pair) {
-        if (!tc_wait(smem_u32(&m->o_full[1]), no1 & 1, &m->abort, p.err)) return;
+        // lone_full first: stream 1 has then waited for its sums of a segment with two row tiles, which stream 0
+        // does not, so that o_full[1] is at most one phase behind and its parity tells this segment's from the last
         if (!tc_wait(smem_u32(&m->lone_full[lones & 1]), (lones >> 1) & 1, &m->abort, p.err)) return;
+        if (!tc_wait(smem_u32(&m->o_full[1]), no1 & 1, &m->abort, p.err)) return;
         const float2 other = m->lone_ml[lones & 1][row];
         ++lones;
         const float top = fmaxf(mx, other.x);
