@@ -44,6 +44,7 @@
 #include <algorithm>
 
 #include "prefix_sched.cuh"
+#include "warp_wait.cuh"
 
 namespace lsp {
 namespace {
@@ -84,21 +85,23 @@ struct TcMisc {
 template <int HD>
 constexpr size_t tc_smem() { return TcShape<HD>::kMisc + sizeof(TcMisc) + 1024; }
 
-// Bounded wait that also gives up when another role has.
-__device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity, volatile int* abort, unsigned* err) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const uint64_t t0 = global_ns();
-  for (uint32_t i = 1;; ++i) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if ((i & 31u) == 0) {
-      if (*abort) return false;
-      if (global_ns() - t0 > kWaitLimitNs) {
-        *abort = 1;
-        set_err(err, LSP_DEV_TIMEOUT);
-        return false;
-      }
-    }
+// Bounded wait that also gives up when another role has; for whole warps, the same answer in every lane.
+struct BarrierWait {
+  uint32_t bar, parity;
+  volatile int* abort;
+  unsigned* err;
+  __device__ __forceinline__ bool ready() const { return mbar_try_wait(bar, parity); }
+  __device__ __forceinline__ bool all(bool x) const { return __all_sync(0xffffffffu, x); }
+  __device__ __forceinline__ bool any(bool x) const { return __any_sync(0xffffffffu, x); }
+  __device__ __forceinline__ bool gone() const { return *abort != 0; }
+  __device__ __forceinline__ uint64_t now() const { return global_ns(); }
+  __device__ __forceinline__ void give_up(bool late) const {
+    if (late) set_err(err, LSP_DEV_TIMEOUT);
+    *abort = 1;
   }
+};
+__device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity, volatile int* abort, unsigned* err) {
+  return warp_wait(BarrierWait{bar, parity, abort, err}, kWaitLimitNs);
 }
 
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
@@ -373,10 +376,7 @@ __device__ __forceinline__ void mma_role(const PrefixAttnParams& p, int t, uint3
   uint32_t turns = 0;
   const uint32_t turn = smem_u32(m->turn);
   uint32_t tiles = 0, seen = 0, nq = 0, pp = 0, po = 1;   // ring and query tiles, places passed; phases
-  auto wait = [&](uint32_t bar, uint32_t parity) {
-    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    return (bool)__all_sync(0xffffffffu, tc_wait(bar, parity, &m->abort, p.err));
-  };
+  auto wait = [&](uint32_t bar, uint32_t parity) { return tc_wait(bar, parity, &m->abort, p.err); };
   auto landed = [&](uint32_t tile) { return wait(full + 8 * (tile & (Sh::kStages - 1)), (tile / Sh::kStages) & 1); };
   auto pass = [&](uint32_t upto) {               // the other stream's tiles
     for (; seen < upto; ++seen) {
