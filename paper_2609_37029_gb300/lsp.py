@@ -357,13 +357,20 @@ def lsp_state_import(st, host_buf, stream=None) -> None:
 # The calls below are made once a layer or a round, with kernels of a few microseconds behind them: their
 # tensors' addresses are taken in place, and what does not change from call to call is looked up once.
 _codes: dict = {}
+_int32 = _float32 = None
+
+
+def _types() -> None:
+    global _int32, _float32
+    import torch
+    _int32, _float32 = torch.int32, torch.float32
+    _codes.update({torch.bfloat16: LSP_DTYPE_BF16, torch.float32: LSP_DTYPE_F32})
 
 
 def _dtype_code(dtype) -> int:
     """LSP_DTYPE_* of a torch type (ValueError for any but bfloat16 and float32)."""
     if not _codes:
-        import torch
-        _codes.update({torch.bfloat16: LSP_DTYPE_BF16, torch.float32: LSP_DTYPE_F32})
+        _types()
     if dtype not in _codes:
         raise ValueError("bfloat16 or float32 tensors")
     return _codes[dtype]
@@ -371,6 +378,26 @@ def _dtype_code(dtype) -> int:
 
 def _opt(x):
     return None if x is None else x.data_ptr()
+
+
+def _dense(t, dtype, n) -> bool:
+    """n elements of this type, without gaps: what a bare address stands for."""
+    return t.dtype == dtype and t.numel() == n and t.is_contiguous()
+
+
+def _word(dev_error):
+    if dev_error is None:
+        return None
+    if dev_error.element_size() != 4 or dev_error.numel() < 1:
+        raise ValueError("dev_error: a 32-bit word")
+    return dev_error.data_ptr()
+
+
+def _room(workspace):
+    """(address, bytes) of a workspace."""
+    if not workspace.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor")
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def lsp_pages_workspace_bytes(cache: lsp_kv_cache) -> int:
@@ -413,14 +440,20 @@ def lsp_prefix_attention_workspace_bytes(cache: lsp_kv_cache, nq: int, n: int, t
 
 def lsp_prefix_attention(cache: lsp_kv_cache, layer, q, seqs, start, out, lse=None, *, shared_len, scale,
                          workspace, dev_error=None, stream=None) -> None:
-    """q: [total][nq][d], dense within a row (a slice of a fused q/k/v row will do); out: dense."""
-    shape, stride, d = q.shape, q.stride(), cache.d
+    """q: [total][nq][d] of the cache's type, dense within a row (a slice of a fused q/k/v row will do); out:
+    the same, dense; seqs [n], start [n + 1] int32; lse: float32 [total][nq] or None."""
+    shape, stride, d, n = q.shape, q.stride(), cache.d, seqs.numel()
     if stride[1] != d or stride[2] != 1 or shape[2] != d or out.shape != shape or not out.is_contiguous():
         raise ValueError("q: [total][nq][d], dense within a row; out: the same shape, contiguous")
+    if _dtype_code(q.dtype) != cache.dtype or out.dtype != q.dtype:
+        raise ValueError("q and out: the cache's type")
+    if not _dense(seqs, _int32, n) or not _dense(start, _int32, n + 1):
+        raise ValueError("seqs [n] and start [n + 1]: contiguous int32")
+    if lse is not None and not _dense(lse, _float32, shape[0] * shape[1]):
+        raise ValueError("lse: contiguous float32 [total][nq]")
     _check(_prefix_attention(cache, layer, q.data_ptr(), stride[0], shape[1], seqs.data_ptr(), start.data_ptr(),
-                             seqs.numel(), shape[0], shared_len, scale, out.data_ptr(), _opt(lse),
-                             workspace.data_ptr(), workspace.nbytes, _opt(dev_error), _stream(stream)),
-           "lsp_prefix_attention")
+                             n, shape[0], shared_len, scale, out.data_ptr(), _opt(lse), *_room(workspace),
+                             _word(dev_error), _stream(stream)), "lsp_prefix_attention")
 
 
 def _row_stride(t, C, rows, V):

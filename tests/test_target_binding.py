@@ -1,0 +1,66 @@
+"""What the Python binding of the target-side calls refuses: the library gets bare addresses, so a tensor of another
+type, length or layout than it takes would be read, or written, past its end.  Nothing is launched (no GPU): a call
+that is in order gets as far as the library, which has no device here, or refuses it for a reason of its own."""
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def lsp():
+    from paper_2609_37029_gb300 import build
+    build.build()
+    from paper_2609_37029_gb300 import lsp as mod
+    return mod
+
+
+def ints(*shape):
+    return torch.zeros(*shape, dtype=torch.int32)
+
+
+def cache(lsp, dtype):
+    k = torch.zeros(2, 5, 2, 16, 64, dtype=dtype)
+    held = [k, torch.zeros_like(k), ints(4, 7), ints(4), ints(5)]
+    c = lsp.make_kv_cache(*held)
+    c.held = held
+    return c
+
+
+def refused(lsp, call, base, changes):
+    """Every change of `base` raises ValueError with its own text; `base` itself gets to the library."""
+    with pytest.raises(lsp.LspError):                # (no device)
+        call(**base)
+    for text, kw in changes:
+        with pytest.raises(ValueError, match=text):
+            call(**{**base, **kw})
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the calls that are in order would run")
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_attention(lsp, dtype):
+    other = torch.float32 if dtype == torch.bfloat16 else torch.bfloat16
+    c = cache(lsp, dtype)
+    q = torch.zeros(6, 4, 64, dtype=dtype)
+    base = dict(cache=c, layer=0, q=q, seqs=ints(3), start=ints(4), out=torch.zeros_like(q), lse=torch.zeros(6, 4), shared_len=0,
+                scale=1.0, workspace=torch.zeros(1 << 10, dtype=torch.uint8), dev_error=ints(1), stream=0)
+    refused(lsp, lsp.lsp_prefix_attention, base, [
+        ("cache's type", dict(q=q.to(other), out=q.to(other))),
+        ("cache's type", dict(out=q.to(other))),
+        ("bfloat16 or float32", dict(q=q.half(), out=q.half())),
+        ("dense within", dict(q=q[..., :32], out=q[..., :32])),
+        ("dense within", dict(out=q[:5])),
+        ("seqs", dict(seqs=ints(3).long())),
+        ("seqs", dict(seqs=ints(6)[::2])),
+        ("seqs", dict(start=ints(4).long())),
+        ("seqs", dict(start=ints(3))),
+        ("seqs", dict(start=ints(8)[::2])),
+        ("lse", dict(lse=torch.zeros(6, 4, dtype=torch.float64))),
+        ("lse", dict(lse=torch.zeros(6, 4, dtype=torch.bfloat16))),
+        ("lse", dict(lse=torch.zeros(5, 4))),
+        ("lse", dict(lse=torch.zeros(4, 6).T)),
+        ("workspace", dict(workspace=torch.zeros(1 << 11, dtype=torch.uint8)[::2])),
+        ("dev_error", dict(dev_error=torch.zeros(1, dtype=torch.uint8))),
+        ("dev_error", dict(dev_error=ints(0))),
+    ])
+    # rows of a fused projection, no sums of exponentials, no error word: in order too
+    wide = torch.zeros(6, 8, 64, dtype=dtype)
+    refused(lsp, lsp.lsp_prefix_attention, {**base, "q": wide[:, 2:6], "lse": None, "dev_error": None}, [])
