@@ -404,34 +404,55 @@ def lsp_pages_workspace_bytes(cache: lsp_kv_cache) -> int:
     return _pages_workspace_bytes(cache)
 
 
+def _entries(a, b) -> int:
+    """The entries of a page call: two int32 lists of one length."""
+    if not _codes:
+        _types()
+    n = a.numel()
+    if not _dense(a, _int32, n) or not _dense(b, _int32, n):
+        raise ValueError("an entry's lists: contiguous int32 of one length")
+    return n
+
+
 def lsp_pages_fork(cache: lsp_kv_cache, src, dst, dev_error=None, stream=None) -> None:
-    _check(_pages_fork(cache, src.data_ptr(), dst.data_ptr(), dst.numel(), _opt(dev_error), _stream(stream)),
-           "lsp_pages_fork")
+    n = _entries(src, dst)
+    _check(_pages_fork(cache, src.data_ptr(), dst.data_ptr(), n, _word(dev_error), _stream(stream)), "lsp_pages_fork")
 
 
 def lsp_pages_reserve(cache: lsp_kv_cache, seqs, add, workspace, dev_error=None, stream=None) -> None:
-    _check(_pages_reserve(cache, seqs.data_ptr(), add.data_ptr(), seqs.numel(), workspace.data_ptr(),
-                          workspace.nbytes, _opt(dev_error), _stream(stream)), "lsp_pages_reserve")
+    n = _entries(seqs, add)
+    _check(_pages_reserve(cache, seqs.data_ptr(), add.data_ptr(), n, *_room(workspace), _word(dev_error),
+                          _stream(stream)), "lsp_pages_reserve")
 
 
 def lsp_pages_write(cache: lsp_kv_cache, layer, seqs, start, k_new, v_new, dev_error=None, stream=None) -> None:
-    """k_new, v_new: [total][nkv][d], dense within a row, the same stride between rows."""
-    shape, stride, d = k_new.shape, k_new.stride(), cache.d
-    if stride != v_new.stride() or stride[1] != d or stride[2] != 1 or shape[1] != cache.nkv or shape[2] != d:
+    """k_new, v_new: [total][nkv][d] of the cache's type, dense within a row, the same stride between rows; seqs
+    [n], start [n + 1] int32."""
+    shape, stride, d, n = k_new.shape, k_new.stride(), cache.d, seqs.numel()
+    if (shape != v_new.shape or stride != v_new.stride() or stride[1] != d or stride[2] != 1 or shape[1] != cache.nkv
+            or shape[2] != d):
         raise ValueError("k_new and v_new: [total][nkv][d] of the same strides, dense within a row")
-    _check(_pages_write(cache, layer, seqs.data_ptr(), start.data_ptr(), seqs.numel(), k_new.data_ptr(),
-                        v_new.data_ptr(), stride[0], shape[0], _opt(dev_error), _stream(stream)), "lsp_pages_write")
+    if _dtype_code(k_new.dtype) != cache.dtype or v_new.dtype != k_new.dtype:
+        raise ValueError("k_new and v_new: the cache's type")
+    if not _dense(seqs, _int32, n) or not _dense(start, _int32, n + 1):
+        raise ValueError("seqs [n] and start [n + 1]: contiguous int32")
+    _check(_pages_write(cache, layer, seqs.data_ptr(), start.data_ptr(), n, k_new.data_ptr(), v_new.data_ptr(),
+                        stride[0], shape[0], _word(dev_error), _stream(stream)), "lsp_pages_write")
 
 
 def lsp_pages_trim(cache: lsp_kv_cache, seqs, new_len, dev_error=None, stream=None) -> None:
-    _check(_pages_trim(cache, seqs.data_ptr(), new_len.data_ptr(), seqs.numel(), _opt(dev_error), _stream(stream)),
+    n = _entries(seqs, new_len)
+    _check(_pages_trim(cache, seqs.data_ptr(), new_len.data_ptr(), n, _word(dev_error), _stream(stream)),
            "lsp_pages_trim")
 
 
 def lsp_pages_compact(cache: lsp_kv_cache, live, workspace, stream=None) -> None:
     """live: int32 [1] that receives the number of live pages, or None."""
-    _check(_pages_compact(cache, _opt(live), workspace.data_ptr(), workspace.nbytes, _stream(stream)),
-           "lsp_pages_compact")
+    if not _codes:
+        _types()
+    if live is not None and not _dense(live, _int32, 1):
+        raise ValueError("live: one int32")
+    _check(_pages_compact(cache, _opt(live), *_room(workspace), _stream(stream)), "lsp_pages_compact")
 
 
 def lsp_prefix_attention_workspace_bytes(cache: lsp_kv_cache, nq: int, n: int, total: int) -> int:

@@ -64,3 +64,52 @@ def test_attention(lsp, dtype):
     # rows of a fused projection, no sums of exponentials, no error word: in order too
     wide = torch.zeros(6, 8, 64, dtype=dtype)
     refused(lsp, lsp.lsp_prefix_attention, {**base, "q": wide[:, 2:6], "lse": None, "dev_error": None}, [])
+
+
+no_gpu = pytest.mark.skipif(torch.cuda.is_available(), reason="the calls that are in order would run")
+
+
+@no_gpu
+@pytest.mark.parametrize("name", ["lsp_pages_fork", "lsp_pages_trim", "lsp_pages_reserve"])
+def test_page_lists(lsp, name):
+    a, b = ("src", "dst") if name == "lsp_pages_fork" else ("seqs", "new_len" if name == "lsp_pages_trim" else "add")
+    base = {"cache": cache(lsp, torch.float32), a: ints(3), b: ints(3), "dev_error": ints(1), "stream": 0}
+    changes = [(None, {b: ints(2)}), (None, {b: ints(4)}), (None, {a: ints(2)}), (None, {a: ints(3).long()}),
+               (None, {b: ints(3).long()}), (None, {b: torch.zeros(3)}), (None, {a: ints(6)[::2]}), (None, {b: ints(6)[::2]})]
+    changes = [("lists", kw) for _, kw in changes] + [("dev_error", dict(dev_error=torch.zeros(3, dtype=torch.uint8)))]
+    if name == "lsp_pages_reserve":
+        base["workspace"] = torch.zeros(1 << 16, dtype=torch.uint8)
+        changes.append(("workspace", dict(workspace=torch.zeros(1 << 17, dtype=torch.uint8)[::2])))
+    refused(lsp, getattr(lsp, name), base, changes)
+
+
+@no_gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_page_writes(lsp, dtype):
+    other = torch.float32 if dtype == torch.bfloat16 else torch.bfloat16
+    rows = torch.zeros(6, 2, 64, dtype=dtype)
+    base = dict(cache=cache(lsp, dtype), layer=5, seqs=ints(3), start=ints(4), k_new=rows, v_new=rows.clone(), dev_error=ints(1),
+                stream=0)                            # (there is no layer 5: the library refuses it)
+    refused(lsp, lsp.lsp_pages_write, base, [
+        ("cache's type", dict(k_new=rows.to(other), v_new=rows.to(other))),
+        ("cache's type", dict(v_new=rows.to(other))),
+        ("bfloat16 or float32", dict(k_new=rows.half(), v_new=rows.half())),
+        ("same strides", dict(v_new=rows[:4])),
+        ("same strides", dict(k_new=rows[..., :32], v_new=rows[..., :32])),
+        ("seqs", dict(seqs=ints(3).long())),
+        ("seqs", dict(start=ints(3))),
+        ("seqs", dict(start=ints(5))),
+        ("seqs", dict(start=ints(4).long())),
+        ("dev_error", dict(dev_error=ints(0))),
+    ])
+
+
+@no_gpu
+def test_compaction(lsp):
+    base = dict(cache=cache(lsp, torch.float32), live=ints(1), workspace=torch.zeros(1 << 16, dtype=torch.uint8), stream=0)
+    refused(lsp, lsp.lsp_pages_compact, base, [
+        ("live", dict(live=ints(0))),
+        ("live", dict(live=torch.zeros(1, dtype=torch.uint8))),
+        ("live", dict(live=torch.zeros(1))),
+        ("workspace", dict(workspace=torch.zeros(1 << 17, dtype=torch.uint8)[::2])),
+    ])
