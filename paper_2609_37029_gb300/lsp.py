@@ -489,7 +489,8 @@ def _row_stride(t, C, rows, V):
 def lsp_verify_probs(target_probs, draft_probs, draft_tokens, u, e, accepted_len, next_token, n_draft=None,
                      out_tokens=None, dev_error=None, stream=None) -> None:
     """target_probs [C][B+1][V], draft_probs [C][B][V] (or None) of one type, bfloat16 or float32; the
-    stride between their rows may exceed V."""
+    stride between their rows may exceed V.  Contiguous: int32 draft_tokens [C][B], n_draft [C], accepted_len
+    [C], next_token [C] and out_tokens [C][B+1], float32 u [C][B] and e [C][V]."""
     C, B = draft_tokens.shape
     V, dtype = target_probs.shape[2], target_probs.dtype
     code, ld_q, drafted = _dtype_code(dtype), 0, None
@@ -498,9 +499,15 @@ def lsp_verify_probs(target_probs, draft_probs, draft_tokens, u, e, accepted_len
         if draft_probs.dtype != dtype:
             raise ValueError("target_probs and draft_probs: one type")
         ld_q, drafted = _row_stride(draft_probs, C, B, V), draft_probs.data_ptr()
+    if not _dense(u, _float32, C * B) or not _dense(e, _float32, C * V):
+        raise ValueError("u [C][B] and e [C][V]: contiguous float32")
+    if (not _dense(draft_tokens, _int32, C * B) or not _dense(accepted_len, _int32, C) or not _dense(next_token, _int32, C)
+            or n_draft is not None and not _dense(n_draft, _int32, C)
+            or out_tokens is not None and not _dense(out_tokens, _int32, C * (B + 1))):
+        raise ValueError("draft_tokens, n_draft, accepted_len, next_token and out_tokens: contiguous int32 of their sizes")
     _check(_verify_probs(target_probs.data_ptr(), drafted, code, draft_tokens.data_ptr(), _opt(n_draft),
                          u.data_ptr(), e.data_ptr(), C, B, V, ld_t, ld_q, accepted_len.data_ptr(),
-                         next_token.data_ptr(), _opt(out_tokens), _opt(dev_error), _stream(stream)),
+                         next_token.data_ptr(), _opt(out_tokens), _word(dev_error), _stream(stream)),
            "lsp_verify_probs")
 
 

@@ -113,3 +113,30 @@ def test_compaction(lsp):
         ("live", dict(live=torch.zeros(1))),
         ("workspace", dict(workspace=torch.zeros(1 << 17, dtype=torch.uint8)[::2])),
     ])
+
+
+@no_gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_verification(lsp, dtype):
+    C, B, V = 3, 4, 10
+    f32 = lambda *x: torch.zeros(*x)
+    base = dict(target_probs=torch.zeros(C, B + 1, V, dtype=dtype), draft_probs=torch.zeros(C, B, V, dtype=dtype), draft_tokens=ints(C, B),
+                u=f32(C, B), e=f32(C, V), accepted_len=ints(C), next_token=ints(C), n_draft=ints(C), out_tokens=ints(C, B + 1),
+                dev_error=ints(1), stream=0)
+    changes = [("one type", dict(draft_probs=torch.zeros(C, B, V, dtype=torch.float16))),
+               ("evenly spaced", dict(draft_probs=torch.zeros(C, B - 1, V, dtype=dtype)))]
+    changes += [("contiguous float32", kw) for kw in (
+        dict(u=f32(C, B).double()), dict(u=f32(C, B).half()), dict(u=f32(C, B - 1)), dict(u=f32(C, B + 1)[:, :B]), dict(u=f32(B, C).T),
+        dict(e=f32(C, V).bfloat16()), dict(e=f32(V)), dict(e=f32(C, 2 * V)[:, :V]), dict(e=f32(V).expand(C, V)))]
+    changes += [("contiguous int32", kw) for kw in (
+        dict(draft_tokens=ints(C, B).long()), dict(draft_tokens=ints(C, B + 1)[:, :B]), dict(accepted_len=ints(C).long()),
+        dict(accepted_len=ints(C - 1)), dict(next_token=ints(C).long()), dict(next_token=ints(2 * C)[::2]), dict(n_draft=ints(C + 1)),
+        dict(n_draft=f32(C)), dict(out_tokens=ints(C, B)), dict(out_tokens=ints(C, B + 1).long()))]
+    changes += [("dev_error", dict(dev_error=torch.zeros(4, dtype=torch.uint8)))]
+    refused(lsp, lsp.lsp_verify_probs, base, changes)
+    for kw in (dict(draft_probs=None), dict(n_draft=None, out_tokens=None, dev_error=None),
+               dict(target_probs=torch.zeros(C, B + 1, V + 6, dtype=dtype)[..., :V])):
+        refused(lsp, lsp.lsp_verify_probs, {**base, **kw}, [])
+    # no candidates at all
+    none = dict(target_probs=torch.zeros(C, 1, V, dtype=dtype), draft_probs=None, draft_tokens=ints(C, 0), u=f32(C, 0), out_tokens=ints(C, 1))
+    refused(lsp, lsp.lsp_verify_probs, {**base, **none}, [])
