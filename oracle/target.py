@@ -21,11 +21,15 @@ class PagedCache:
     def held(self, s):
         return -(-int(self.len[s]) // self.page)
 
+    def usable(self, s):
+        """A sequence of the cache, of a length that its row of the table can hold."""
+        return 0 <= s < len(self.len) and 0 <= self.len[s] <= self.table.shape[1] * self.page
+
     def fork(self, src, dst):
         """-> indices of the pairs that were refused."""
         bad = []
         for i, (s, d) in enumerate(zip(src, dst)):
-            if not (0 <= s < len(self.len) and 0 <= d < len(self.len)) or d in dst[:i] or d in src:
+            if not (self.usable(s) and self.usable(d)) or d in dst[:i] or d in src:
                 bad.append(i)
                 continue
             self._cut(d, 0)
@@ -45,7 +49,7 @@ class PagedCache:
     def trim(self, seqs, new_len):
         bad = []
         for i, (s, n) in enumerate(zip(seqs, new_len)):
-            if not 0 <= s < len(self.len) or n < 0 or s in seqs[:i]:
+            if not self.usable(s) or n < 0 or s in seqs[:i]:
                 bad.append(i)
             elif n < self.len[s]:
                 self._cut(s, n)
@@ -57,7 +61,7 @@ class PagedCache:
         free = [int(x) for x in np.flatnonzero(self.refs == 0)]
         refs0, copies, used = self.refs.copy(), {}, 0
         for i, (s, a) in enumerate(zip(seqs, add)):
-            if not 0 <= s < len(self.len) or a < 0 or s in seqs[:i] or self.len[s] + a > self.table.shape[1] * self.page:
+            if not self.usable(s) or a < 0 or s in seqs[:i] or self.len[s] + a > self.table.shape[1] * self.page:
                 bad.append(i)
                 continue
             n = int(self.len[s])
@@ -89,6 +93,8 @@ class PagedCache:
 
     def write(self, layer, seqs, start, k_new, v_new):
         for i, s in enumerate(seqs):
+            if not self.usable(s):
+                continue
             for r in range(start[i], start[i + 1]):
                 pos = int(self.len[s]) - int(start[i + 1]) + r
                 pg, slot = self.table[s, pos // self.page], pos % self.page
@@ -127,7 +133,7 @@ def cache_attention(cache, layer, q, seqs, start, scale):
     out, size = np.zeros((total, nq, d)), np.zeros((total, nq, d))
     lse = np.full((total, nq), -np.inf)
     for i, s in enumerate(seqs):
-        if not 0 <= s < len(cache.len):
+        if not cache.usable(s):
             continue
         k, v = cache.tokens(layer, s)
         rep = nq // k.shape[1]

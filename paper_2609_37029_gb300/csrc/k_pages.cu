@@ -55,14 +55,10 @@ PagesWs ws_split(void* p, int pages) {
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
-// A sequence's length as the table can hold it (a damaged one is cut, and reported).
-__device__ __forceinline__ int seq_len(const KvCache& c, int s, unsigned* err) {
-  const int l = c.len[s], most = c.max_pages * c.page;
-  if (l < 0 || l > most) {
-    set_err(err, LSP_DEV_BAD_SEQ);
-    return l < 0 ? 0 : most;
-  }
-  return l;
+// A sequence's length; -1 where the table cannot hold it: an entry with such a sequence is left as it is.
+__device__ __forceinline__ int seq_len(const KvCache& c, int s) {
+  const int l = c.len[s];
+  return l < 0 || l > c.max_pages * c.page ? -1 : l;
 }
 
 __device__ __forceinline__ void add_ref(const KvCache& c, int pg, int by, unsigned* err) {
@@ -79,12 +75,13 @@ __global__ void __launch_bounds__(kSmallThreads) pages_fork_kernel(const KvCache
   const int i = blockIdx.x, tid = threadIdx.x;
   const int s = src[i], d = dst[i];
   bool bad = s < 0 || s >= c.seqs || d < 0 || d >= c.seqs;
+  const int ls = bad ? -1 : seq_len(c, s), ld = bad ? -1 : seq_len(c, d);
+  bad = ls < 0 || ld < 0;
   for (int j = tid; j < n; j += kSmallThreads) bad |= src[j] == d || (j < i && dst[j] == d);
   if (__syncthreads_or(bad)) {
     if (tid == 0) set_err(err, LSP_DEV_BAD_SEQ);
     return;
   }
-  const int ls = seq_len(c, s, err), ld = seq_len(c, d, err);
   const int ns = ceil_div(ls, c.page), nd = ceil_div(ld, c.page);
   const int* from = c.table + (size_t)s * c.max_pages;
   int* to = c.table + (size_t)d * c.max_pages;
@@ -105,13 +102,13 @@ __global__ void __launch_bounds__(kSmallThreads) pages_trim_kernel(const KvCache
   const int i = blockIdx.x, tid = threadIdx.x;
   const int s = seqs[i], want = new_len[i];
   bool bad = s < 0 || s >= c.seqs || want < 0;
+  const int l = bad ? -1 : seq_len(c, s);
+  bad = l < 0;
   for (int j = tid; j < i; j += kSmallThreads) bad |= seqs[j] == s;
-  if (__syncthreads_or(bad)) {
+  if (__syncthreads_or(bad)) {                   // (and every thread has read the length)
     if (tid == 0) set_err(err, LSP_DEV_BAD_SEQ);
     return;
   }
-  const int l = seq_len(c, s, err);
-  __syncthreads();
   if (want >= l) return;
   int* row = c.table + (size_t)s * c.max_pages;
   for (int k = ceil_div(want, c.page) + tid; k < ceil_div(l, c.page); k += kSmallThreads) {
@@ -141,8 +138,9 @@ __global__ void __launch_bounds__(kSmallThreads) pages_write_kernel(const KvCach
   int pg = -1;
   int pos = -1;
   if (s >= 0 && s < c.seqs && e <= total && b >= 0) {
-    pos = seq_len(c, s, err) - e + t;
-    if (pos >= 0) pg = c.table[(size_t)s * c.max_pages + pos / c.page];
+    const int l = seq_len(c, s);
+    pos = l - e + t;
+    if (l >= 0 && pos >= 0) pg = c.table[(size_t)s * c.max_pages + pos / c.page];
   }
   if (pg < 0 || pg >= c.pages) {
     if (lane == 0) set_err(err, LSP_DEV_BAD_SEQ);
@@ -213,11 +211,11 @@ __global__ void __launch_bounds__(kPlanThreads) pages_plan_kernel(const KvCache 
   for (int j = 0; ok && j < i; ++j) ok = s_seq[j] != s;
   int before = 0, after = 0, last = -1, holders = 0;
   if (ok) {
-    l = seq_len(c, s, err);
-    before = ceil_div(l, c.page);
-    ok = (int64_t)l + a <= (int64_t)c.max_pages * c.page;
+    l = seq_len(c, s);
+    ok = l >= 0 && (int64_t)l + a <= (int64_t)c.max_pages * c.page;
   }
   if (ok) {
+    before = ceil_div(l, c.page);
     after = ceil_div(l + a, c.page);
     if (a > 0 && l % c.page) {
       last = c.table[(size_t)s * c.max_pages + before - 1];
