@@ -405,7 +405,9 @@ int lsp_state_import(lsp_state* st, const void* host_buf, size_t bytes, lsp_stre
  *   refs   [pages] how many sequences hold each page; 0 = free
  * An empty cache has table = -1, len = 0, refs = 0.  A sequence whose len is
  * outside [0, max_pages * page] counts as one outside the cache: every call
- * leaves an entry with it as it was (LSP_DEV_BAD_SEQ).
+ * leaves an entry with it as it was (LSP_DEV_BAD_SEQ).  So do lsp_pages_fork,
+ * trim and reserve where a page they would let go of, hand on or grow is none of
+ * the pool.
  * Supported: page 16, 32, 64, 128 or 256; d 64 or 128; dtype BF16 or F32;
  * pages <= 2^20; seqs * max_pages <= 2^30; max_pages * page <= 2^30.
  */

@@ -25,11 +25,15 @@ class PagedCache:
         """A sequence of the cache, of a length that its row of the table can hold."""
         return 0 <= s < len(self.len) and 0 <= self.len[s] <= self.table.shape[1] * self.page
 
+    def stray(self, s, first=0):
+        """Whether one of the sequence's pages, from column `first` on, is none of the pool."""
+        return any(not 0 <= pg < len(self.refs) for pg in self.table[s, first:self.held(s)])
+
     def fork(self, src, dst):
         """-> indices of the pairs that were refused."""
         bad = []
         for i, (s, d) in enumerate(zip(src, dst)):
-            if not (self.usable(s) and self.usable(d)) or d in dst[:i] or d in src:
+            if not (self.usable(s) and self.usable(d)) or d in dst[:i] or d in src or self.stray(s) or self.stray(d):
                 bad.append(i)
                 continue
             self._cut(d, 0)
@@ -49,7 +53,7 @@ class PagedCache:
     def trim(self, seqs, new_len):
         bad = []
         for i, (s, n) in enumerate(zip(seqs, new_len)):
-            if not self.usable(s) or n < 0 or s in seqs[:i]:
+            if not self.usable(s) or n < 0 or s in seqs[:i] or self.stray(s, -(-n // self.page)):
                 bad.append(i)
             elif n < self.len[s]:
                 self._cut(s, n)
@@ -67,6 +71,9 @@ class PagedCache:
             n = int(self.len[s])
             part = n % self.page
             last = int(self.table[s, self.held(s) - 1]) if part and a else -1
+            if part and a and not 0 <= last < len(self.refs):
+                bad.append(i)
+                continue
             copy = last >= 0 and copies.get(last, 0) < refs0[last] - 1
             if last >= 0:
                 copies[last] = copies.get(last, 0) + 1
@@ -97,6 +104,8 @@ class PagedCache:
                 continue
             for r in range(start[i], start[i + 1]):
                 pos = int(self.len[s]) - int(start[i + 1]) + r
+                if pos < 0 or not 0 <= self.table[s, pos // self.page] < len(self.refs):
+                    continue
                 pg, slot = self.table[s, pos // self.page], pos % self.page
                 self.k[layer, pg, :, slot], self.v[layer, pg, :, slot] = k_new[r], v_new[r]
 

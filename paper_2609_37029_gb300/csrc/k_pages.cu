@@ -61,12 +61,7 @@ __device__ __forceinline__ int seq_len(const KvCache& c, int s) {
   return l < 0 || l > c.max_pages * c.page ? -1 : l;
 }
 
-__device__ __forceinline__ void add_ref(const KvCache& c, int pg, int by, unsigned* err) {
-  if (pg >= 0 && pg < c.pages)
-    atomicAdd(c.refs + pg, by);
-  else
-    set_err(err, LSP_DEV_BAD_SEQ);
-}
+__device__ __forceinline__ bool in_pool(const KvCache& c, int pg) { return pg >= 0 && pg < c.pages; }
 
 __global__ void __launch_bounds__(kSmallThreads) pages_fork_kernel(const KvCache c, const int* src, const int* dst, int n,
                                                                    unsigned* err) {
@@ -85,14 +80,20 @@ __global__ void __launch_bounds__(kSmallThreads) pages_fork_kernel(const KvCache
   const int ns = ceil_div(ls, c.page), nd = ceil_div(ld, c.page);
   const int* from = c.table + (size_t)s * c.max_pages;
   int* to = c.table + (size_t)d * c.max_pages;
+  bool stray = false;
+  for (int k = tid; k < max(ns, nd); k += kSmallThreads)
+    stray |= (k < nd && !in_pool(c, to[k])) || (k < ns && !in_pool(c, from[k]));
+  if (__syncthreads_or(stray)) {
+    if (tid == 0) set_err(err, LSP_DEV_BAD_SEQ);
+    return;
+  }
   for (int k = tid; k < max(ns, nd); k += kSmallThreads) {
-    const int old = k < nd ? to[k] : -1, pg = k < ns ? from[k] : -1;
-    if (k < nd) add_ref(c, old, -1, err);
-    if (k < ns) add_ref(c, pg, 1, err);
+    const int pg = k < ns ? from[k] : -1;
+    if (k < nd) atomicSub(c.refs + to[k], 1);
+    if (k < ns) atomicAdd(c.refs + pg, 1);
     to[k] = pg;
   }
-  __syncthreads();                               // every thread has read len[d]
-  if (tid == 0) c.len[d] = ls;
+  if (tid == 0) c.len[d] = ls;                   // (every thread has read it)
 }
 
 __global__ void __launch_bounds__(kSmallThreads) pages_trim_kernel(const KvCache c, const int* seqs, const int* new_len,
@@ -111,8 +112,15 @@ __global__ void __launch_bounds__(kSmallThreads) pages_trim_kernel(const KvCache
   }
   if (want >= l) return;
   int* row = c.table + (size_t)s * c.max_pages;
-  for (int k = ceil_div(want, c.page) + tid; k < ceil_div(l, c.page); k += kSmallThreads) {
-    add_ref(c, row[k], -1, err);
+  const int end = ceil_div(l, c.page), begin = ceil_div(want, c.page) + tid;
+  bool stray = false;
+  for (int k = begin; k < end; k += kSmallThreads) stray |= !in_pool(c, row[k]);
+  if (__syncthreads_or(stray)) {
+    if (tid == 0) set_err(err, LSP_DEV_BAD_SEQ);
+    return;
+  }
+  for (int k = begin; k < end; k += kSmallThreads) {
+    atomicSub(c.refs + row[k], 1);
     row[k] = -1;
   }
   if (tid == 0) c.len[s] = want;
@@ -142,7 +150,7 @@ __global__ void __launch_bounds__(kSmallThreads) pages_write_kernel(const KvCach
     pos = l - e + t;
     if (l >= 0 && pos >= 0) pg = c.table[(size_t)s * c.max_pages + pos / c.page];
   }
-  if (pg < 0 || pg >= c.pages) {
+  if (!in_pool(c, pg)) {
     if (lane == 0) set_err(err, LSP_DEV_BAD_SEQ);
     return;
   }
@@ -219,7 +227,7 @@ __global__ void __launch_bounds__(kPlanThreads) pages_plan_kernel(const KvCache 
     after = ceil_div(l + a, c.page);
     if (a > 0 && l % c.page) {
       last = c.table[(size_t)s * c.max_pages + before - 1];
-      ok = last >= 0 && last < c.pages;
+      ok = in_pool(c, last);
       if (ok) holders = c.refs[last];
     }
   }

@@ -95,3 +95,49 @@ def test_the_longest_length_that_fits_is_in_order(lsp):
     b.reserve([1], [1])
     b.check()
     assert int(b.t[1][1]) == WIDTH * PAGE
+
+
+STRAYS = [-1, -7, 24, 10 ** 6, -2 ** 31]             # the pool has 24 pages
+
+
+@pytest.mark.parametrize("pg", STRAYS)
+def test_fork_and_trim_leave_sequences_with_a_page_of_no_pool(lsp, pg):
+    b = damaged(lsp, [50, 40, 20, 33, 0])
+    b.set_page(0, 1, pg)
+    b.fork([0, 1], [4, 2])                           # a damaged source, and a pair in order
+    b.check()
+    b.fork([1, 3], [0, 4])                           # a damaged destination
+    b.check()
+    b.trim([0, 1], [3, 3])                           # it would let go of the stray page
+    b.check()
+    b.trim([0], [32])                                # only of a later one
+    b.check()
+    b.trim([0], [0])
+    b.check()
+
+
+@pytest.mark.parametrize("pg", STRAYS)
+def test_reserve_and_write_leave_a_last_page_of_no_pool(lsp, pg):
+    b = damaged(lsp, [50, 40, 20])
+    b.set_page(1, 2, pg)                             # tokens 32 to 39
+    bad, _ = b.reserve([0, 1, 2], [1, 1, 30])
+    assert bad == [1]
+    b.check()
+    b.write_rows([0, 1, 2], [0, 1, 13, 15], gen(4), lsp.LSP_DEV_BAD_SEQ)     # rows of tokens 28 to 39: the first four have a place
+    b.check()
+
+
+def test_many_columns(lsp):
+    """A sequence of more pages than a block has threads, the stray one among the last."""
+    pool = make_pool(1, 700, 1, PAGE, 64, "bf16", gen(3), device="cuda")
+    b = Damaged(lsp, pool, *make_cache([600 * PAGE, 20, 0], 0, PAGE, pool, spare=0))
+    keep = b.t[0][0, 590].item()
+    b.set_page(0, 590, 700)
+    b.fork([0, 1], [2, 0])
+    b.check()
+    b.trim([0], [400 * PAGE])
+    b.check()
+    b.set_page(0, 590, keep)
+    b.fork([0], [2])
+    b.trim([0], [100 * PAGE - 3])
+    b.check()
