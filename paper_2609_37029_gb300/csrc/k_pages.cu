@@ -321,7 +321,12 @@ __global__ void __launch_bounds__(kPlanThreads) pages_compact_plan_kernel(const 
     for (int k = 0; k < kScanBatch; ++k) {
       const bool in = at + k < c.pages;
       if (in && at + k < live && r[k] <= 0) w.dst[hr++] = at + k;
-      if (in && at + k >= live && r[k] > 0) w.src[mr++] = at + k;
+      if (in && at + k >= live) {
+        if (r[k] > 0)
+          w.src[mr++] = at + k;
+        else
+          w.map[at + k] = at + k;                // a table entry that names a free page stays
+      }
     }
     holes += all & 0xffff;
     movers += all >> 16;

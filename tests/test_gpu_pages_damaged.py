@@ -141,3 +141,20 @@ def test_many_columns(lsp):
     b.fork([0], [2])
     b.trim([0], [100 * PAGE - 3])
     b.check()
+
+
+@pytest.mark.parametrize("fill", [0, 0xAB, 0xFF])
+def test_compaction_leaves_entries_that_name_free_pages(lsp, fill):
+    """Whatever the workspace holds: free pages at, past and before the live count, and pages of no pool."""
+    b = damaged(lsp, [50, 40, 20, 33], pages=40)
+    live = int((b.t[2] > 0).sum())
+    free = [pg for pg in range(40) if int(b.t[2][pg]) == 0]
+    assert any(pg >= live for pg in free) and any(pg < live for pg in free)
+    b.set_page(0, 1, free[-1])
+    b.set_page(1, 0, next(pg for pg in free if pg >= live))
+    b.set_page(1, 2, next(pg for pg in free if pg < live))
+    b.set_page(2, 0, 40)
+    b.set_page(3, 2, -5)
+    b.ws.fill_(fill)
+    b.compact()
+    b.check()
