@@ -466,9 +466,9 @@ int lsp_pages_trim(const lsp_kv_cache* cache, const int32_t* seqs, const int32_t
 
 /* Move the live pages (refs > 0) to the front of the pool, every layer: with
  * `live` of them, the k-th live page at an index >= live goes to the k-th free
- * index < live; table and refs follow.  A table entry that names a free page
- * stays.  live: device int32, receives the count, or NULL.  workspace as for
- * lsp_pages_reserve. */
+ * index < live; table and refs follow, whatever a sequence's length.  A table
+ * entry that names a free page stays.  live: device int32, receives the count,
+ * or NULL.  workspace as for lsp_pages_reserve. */
 int lsp_pages_compact(const lsp_kv_cache* cache, int32_t* live, void* workspace,
                       size_t workspace_bytes, lsp_stream_t stream);
 

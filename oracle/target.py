@@ -117,9 +117,8 @@ class PagedCache:
         for a, b in to.items():
             self.k[:, b], self.v[:, b] = self.k[:, a], self.v[:, a]
             self.refs[b], self.refs[a] = self.refs[a], 0
-        for s in range(len(self.len)):
-            for col in range(self.held(s)):
-                self.table[s, col] = to.get(int(self.table[s, col]), self.table[s, col])
+        for row in self.table:
+            row[:] = [to.get(int(pg), pg) for pg in row]
         return live
 
     def tokens(self, layer, s):

@@ -388,9 +388,7 @@ __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const KvCache 
   const int64_t entries = (int64_t)c.seqs * c.max_pages;
   for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < entries; i += (int64_t)gridDim.x * kCopyThreads) {
     const int pg = c.table[i];
-    if (pg < live || pg >= c.pages) continue;
-    const int s = (int)(i / c.max_pages), col = (int)(i - (int64_t)s * c.max_pages);
-    if ((int64_t)col * c.page < c.len[s]) c.table[i] = w.map[pg];
+    if (pg >= live && pg < c.pages) c.table[i] = w.map[pg];
   }
 }
 

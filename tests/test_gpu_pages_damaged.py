@@ -158,3 +158,18 @@ def test_compaction_leaves_entries_that_name_free_pages(lsp, fill):
     b.ws.fill_(fill)
     b.compact()
     b.check()
+
+
+@pytest.mark.parametrize("n", LENGTHS)
+def test_compaction_keeps_the_pages_of_a_sequence_of_no_length(lsp, n):
+    """Its pages are moved like the others; its table follows, so that a length that is put right finds them."""
+    b = damaged(lsp, [50, 40, 20, 33], pages=40)
+    want = [[x.copy() for x in b.o.tokens(layer, 1)] for layer in range(2)]
+    b.set_len(1, n)
+    b.compact()
+    b.check()
+    b.set_len(1, 40)
+    for layer in range(2):
+        for pool, x in zip((b.k, b.v), want[layer]):
+            got = up(pool[layer, b.t[0][1, :3].long()].transpose(1, 2).flatten(0, 1)[:40])
+            assert (got == x).all()
