@@ -238,8 +238,11 @@ __global__ void __launch_bounds__(kFmaThreads, kFmaPerSm<HD>) prefix_attn_fma_ke
 // Bound by latency: 5 us to find a row's segments in code that is not cached yet,
 // and three dependent rounds of loads of some 3 us.  Where the segments are
 // follows from the lengths alone, so every CTA finds that out again before it
-// waits for the main kernel (which lets it start only after its own wait: the
-// lengths are final).
+// waits for the main kernel.  That kernel lets it start only after its own wait, so
+// the lengths are final by then; but what a grid reads before it has waited itself
+// need not be what the calls before wrote, so the lengths are read once more after
+// the wait, and the work is laid out again should they differ.  (16 x 1 row over
+// 32K: 45.6 us; 43.7 without reading again, 49.5 with all of it after the wait.)
 constexpr int kJoinRows = 4, kJoinHeads = 4, kJoinPerSm = 4;
 template <typename T, int HD, int kUnitTiles, int kBlock, int kWarps, int kHeads>
 __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoinPerSm) prefix_join_kernel(const PrefixAttnParams p) {
@@ -253,193 +256,200 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
   int64_t* line_base = reinterpret_cast<int64_t*>(info + p.n);
   int64_t* begin = line_base + p.n + 1;          // [grid + 1]: piece_begin
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp / kJoinRows;
-  if (warp == 0) {
-    const PrefixSched s = build_sched<kUnitTiles, kBlock>(p, line_base, info, false);
-    if (lane == 0) s_sched = s;
-  }
-  __syncthreads();
-  const PrefixSched s = s_sched;
-  for (int c = threadIdx.x; c <= p.grid; c += blockDim.x) begin[c] = piece_begin(s, c);
-  // the most pieces that have part of a shared item of a unit but the last, of the last
-  if (threadIdx.x < 2)
-    s_pieces[threadIdx.x] = s.whole < s.items ? (int)div_floor((int64_t)(threadIdx.x ? s.len_last : s.len_two) * s.ctas, s.line) + 2 : 1;
-  __syncthreads();
-  // the last CTA whose piece begins at or before place x of the line: an estimate, and what rounding leaves
-  const float per_place = __fdividef((float)s.ctas, (float)s.line);
-  auto piece_at = [&](int64_t x) {
-    int c = min((int)((float)x * per_place), s.ctas - 1);
-    while (c + 1 < s.ctas && begin[c + 1] <= x) ++c;
-    while (begin[c] > x) --c;
-    return c;
-  };
-  const int parts = cdiv(p.rep, kHeads), per = cdiv(p.rep, parts);   // of a KV head's query heads, and heads of one
-  const int64_t rows = (int64_t)p.total * p.nkv * parts;
-  bool waited = false;
-  for (int64_t w0 = (int64_t)blockIdx.x * kJoinRows; w0 < rows; w0 += (int64_t)gridDim.x * kJoinRows) {
-    const int64_t mine = w0 + warp % kJoinRows;
-    const int64_t w = mine < rows ? mine : rows - 1;   // a row past the last does the last's work, and stores nothing
-    const int t = (int)div_floor(w, p.nkv * parts), h = (int)(w - (int64_t)t * p.nkv * parts), g = h / parts;
-    const int hr = (h - g * parts) * per, heads = min(per, p.rep - hr);
-    int lo = -1;                                 // the last sequence that starts at or before t
-    for (int i0 = 0; i0 < p.n; i0 += 32)
-      lo += __popc(__ballot_sync(0xffffffffu, i0 + lane < p.n && info[i0 + lane].first <= t));
-    PrefixSeq r = {-1, 0, 0, 0};
-    if (lo >= 0) r = info[lo];
-    // segments: of each range of the shared part the (at most `pieces`) CTAs that
-    // have part of its item, then those of the own item
-    int shared = 0, pieces = 1, own = 0, c0 = 0, u = 0, unit = 0, shared_at = 0, own_at = 0, blocks = 0, cost = 1, shared_cost = 1;
-    int64_t first = 0, shared_first = 0;         // places of the own item, and of the first range's
-    if (t >= r.first && t < r.first + r.rows) {
-      const int tile_rows = p.tok_tile * p.rep;
-      if (s.items > 0) {
-        const int tile = t / p.tok_tile;
-        u = tile / kUnitTiles;
-        shared_at = (tile % kUnitTiles) * tile_rows + (t - tile * p.tok_tile) * p.rep + hr;
-        const bool last = u + 1 == p.units;
-        shared_cost = last ? block_cost<kUnitTiles>(p, p.total - u * kUnitTiles * p.tok_tile) : kCostTwo;
-        pieces = s_pieces[last];
-        shared = p.splits * pieces;
-        shared_first = shared_place(s, g * p.splits, u) - s.whole_line;
-      }
-      const int i = t - r.first, tile = i / p.tok_tile;
-      unit = tile / kUnitTiles;
-      own_at = (tile % kUnitTiles) * tile_rows + (i - tile * p.tok_tile) * p.rep + hr;
-      first = s.shared_line + line_base[lo];
-      for (int u = 0; u < unit; ++u)
-        first += (int64_t)item_length<kUnitTiles>(p, r, u, own_blocks<kUnitTiles, kBlock>(p, r, s.base, u)) * p.nkv;
-      blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, unit);
-      cost = block_cost<kUnitTiles>(p, r.rows - unit * kUnitTiles * p.tok_tile);
-      const int len = item_length<kUnitTiles>(p, r, unit, blocks);
-      first += (int64_t)g * len;
-      if (blocks > 0) {
-        c0 = piece_at(first);
-        own = piece_at(first + len - 1) + 1 - c0;
-      }
+  bool waited = false, again = true;
+  while (again) {
+    if (warp == 0) {
+      const PrefixSched s = build_sched<kUnitTiles, kBlock>(p, line_base, info, false);
+      if (lane == 0) s_sched = s;
     }
-    const int all = shared + own;
-    auto row_of = [&](int q) -> int64_t {        // -1: no such segment
-      if (q >= all) return -1;
-      const bool sh = q < shared;
-      const int range = sh && q >= pieces ? q / pieces : 0, k = sh ? q - range * pieces : q - shared;
-      const int item = (g * p.splits + range) * p.units + u, nb = sh ? range_blocks(s, range) : blocks;
-      if (sh && item < s.whole) return k == 0 && nb > 0 ? shared_rows<kUnitTiles>(p, s, item, 0) + shared_at : -1;
-      const int64_t place = sh ? shared_first + range * s.len_range : first;
-      const int c = (sh ? piece_at(place) : c0) + k;
-      if (c >= s.ctas) return -1;
-      // a CTA may have a piece of the item without any of its blocks
-      const int price = sh ? shared_cost : cost;
-      if (blocks_before(s, begin[c + 1] - place, nb, price) <= blocks_before(s, begin[c] - place, nb, price)) return -1;
-      return sh ? shared_rows<kUnitTiles>(p, s, item, c) + shared_at : own_rows<kUnitTiles>(p, r, unit, g, c) + own_at;
+    __syncthreads();
+    const PrefixSched s = s_sched;
+    for (int c = threadIdx.x; c <= p.grid; c += blockDim.x) begin[c] = piece_begin(s, c);
+    // the most pieces that have part of a shared item of a unit but the last, of the last
+    if (threadIdx.x < 2)
+      s_pieces[threadIdx.x] = s.whole < s.items ? (int)div_floor((int64_t)(threadIdx.x ? s.len_last : s.len_two) * s.ctas, s.line) + 2 : 1;
+    __syncthreads();
+    // the last CTA whose piece begins at or before place x of the line: an estimate, and what rounding leaves
+    const float per_place = __fdividef((float)s.ctas, (float)s.line);
+    auto piece_at = [&](int64_t x) {
+      int c = min((int)((float)x * per_place), s.ctas - 1);
+      while (c + 1 < s.ctas && begin[c + 1] <= x) ++c;
+      while (begin[c] > x) --c;
+      return c;
     };
-    // the first segment of this lane for the maxima, and for the sums
-    int64_t row_m = row_of(lane), row_s = row_m;
-    if (kWarps > 1) {
-      const int src = lane * kWarps + part;
-      row_s = __shfl_sync(0xffffffffu, row_m, src & 31);
-      if (src >= 32) row_s = row_of(src);
-    }
-    if (!waited) {
-      griddep_wait();
-      griddep_launch();
-      waited = true;
-    }
-    float m[kHeads], l[kHeads], o[kHeads][kVec];
-#pragma unroll
-    for (int k = 0; k < kHeads; ++k) m[k] = -INFINITY, l[k] = 0.f;
-    for (int q = lane;;) {
-      if (row_m >= 0) {
-#pragma unroll
-        for (int k = 0; k < kHeads; ++k)
-          if (k < heads) m[k] = fmaxf(m[k], p.part_ml[row_m + k].x);
+    const int parts = cdiv(p.rep, kHeads), per = cdiv(p.rep, parts);   // of a KV head's query heads, and heads of one
+    const int64_t rows = (int64_t)p.total * p.nkv * parts;
+    again = false;
+    for (int64_t w0 = (int64_t)blockIdx.x * kJoinRows; w0 < rows; w0 += (int64_t)gridDim.x * kJoinRows) {
+      const int64_t mine = w0 + warp % kJoinRows;
+      const int64_t w = mine < rows ? mine : rows - 1;   // a row past the last does the last's work, and stores nothing
+      const int t = (int)div_floor(w, p.nkv * parts), h = (int)(w - (int64_t)t * p.nkv * parts), g = h / parts;
+      const int hr = (h - g * parts) * per, heads = min(per, p.rep - hr);
+      int lo = -1;                                 // the last sequence that starts at or before t
+      for (int i0 = 0; i0 < p.n; i0 += 32)
+        lo += __popc(__ballot_sync(0xffffffffu, i0 + lane < p.n && info[i0 + lane].first <= t));
+      PrefixSeq r = {-1, 0, 0, 0};
+      if (lo >= 0) r = info[lo];
+      // segments: of each range of the shared part the (at most `pieces`) CTAs that
+      // have part of its item, then those of the own item
+      int shared = 0, pieces = 1, own = 0, c0 = 0, u = 0, unit = 0, shared_at = 0, own_at = 0, blocks = 0, cost = 1, shared_cost = 1;
+      int64_t first = 0, shared_first = 0;         // places of the own item, and of the first range's
+      if (t >= r.first && t < r.first + r.rows) {
+        const int tile_rows = p.tok_tile * p.rep;
+        if (s.items > 0) {
+          const int tile = t / p.tok_tile;
+          u = tile / kUnitTiles;
+          shared_at = (tile % kUnitTiles) * tile_rows + (t - tile * p.tok_tile) * p.rep + hr;
+          const bool last = u + 1 == p.units;
+          shared_cost = last ? block_cost<kUnitTiles>(p, p.total - u * kUnitTiles * p.tok_tile) : kCostTwo;
+          pieces = s_pieces[last];
+          shared = p.splits * pieces;
+          shared_first = shared_place(s, g * p.splits, u) - s.whole_line;
+        }
+        const int i = t - r.first, tile = i / p.tok_tile;
+        unit = tile / kUnitTiles;
+        own_at = (tile % kUnitTiles) * tile_rows + (i - tile * p.tok_tile) * p.rep + hr;
+        first = s.shared_line + line_base[lo];
+        for (int u = 0; u < unit; ++u)
+          first += (int64_t)item_length<kUnitTiles>(p, r, u, own_blocks<kUnitTiles, kBlock>(p, r, s.base, u)) * p.nkv;
+        blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, unit);
+        cost = block_cost<kUnitTiles>(p, r.rows - unit * kUnitTiles * p.tok_tile);
+        const int len = item_length<kUnitTiles>(p, r, unit, blocks);
+        first += (int64_t)g * len;
+        if (blocks > 0) {
+          c0 = piece_at(first);
+          own = piece_at(first + len - 1) + 1 - c0;
+        }
       }
-      if ((q += 32) >= all) break;
-      row_m = row_of(q);
-    }
-    bool some = false;
+      const int all = shared + own;
+      auto row_of = [&](int q) -> int64_t {        // -1: no such segment
+        if (q >= all) return -1;
+        const bool sh = q < shared;
+        const int range = sh && q >= pieces ? q / pieces : 0, k = sh ? q - range * pieces : q - shared;
+        const int item = (g * p.splits + range) * p.units + u, nb = sh ? range_blocks(s, range) : blocks;
+        if (sh && item < s.whole) return k == 0 && nb > 0 ? shared_rows<kUnitTiles>(p, s, item, 0) + shared_at : -1;
+        const int64_t place = sh ? shared_first + range * s.len_range : first;
+        const int c = (sh ? piece_at(place) : c0) + k;
+        if (c >= s.ctas) return -1;
+        // a CTA may have a piece of the item without any of its blocks
+        const int price = sh ? shared_cost : cost;
+        if (blocks_before(s, begin[c + 1] - place, nb, price) <= blocks_before(s, begin[c] - place, nb, price)) return -1;
+        return sh ? shared_rows<kUnitTiles>(p, s, item, c) + shared_at : own_rows<kUnitTiles>(p, r, unit, g, c) + own_at;
+      };
+      // the first segment of this lane for the maxima, and for the sums
+      int64_t row_m = row_of(lane), row_s = row_m;
+      if (kWarps > 1) {
+        const int src = lane * kWarps + part;
+        row_s = __shfl_sync(0xffffffffu, row_m, src & 31);
+        if (src >= 32) row_s = row_of(src);
+      }
+      if (!waited) {
+        griddep_wait();
+        griddep_launch();
+        waited = true;
+        bool changed = false;
+        for (int i = threadIdx.x; i < p.n; i += blockDim.x) changed |= !same_seq(p, i, info[i]);
+        again = __syncthreads_or(changed);
+        if (again) break;
+      }
+      float m[kHeads], l[kHeads], o[kHeads][kVec];
 #pragma unroll
-    for (int k = 0; k < kHeads; ++k) {
-      m[k] = warp_max(m[k]);
-      some |= m[k] > -INFINITY;
+      for (int k = 0; k < kHeads; ++k) m[k] = -INFINITY, l[k] = 0.f;
+      for (int q = lane;;) {
+        if (row_m >= 0) {
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) o[k][e] = 0.f;
-    }
-    for (int q0 = 0; q0 < all && some; q0 += 32 * kWarps) {
-      const int64_t row = q0 == 0 ? row_s : row_of(q0 + lane * kWarps + part);
-      float x[kHeads];
-      bool any = false;
+          for (int k = 0; k < kHeads; ++k)
+            if (k < heads) m[k] = fmaxf(m[k], p.part_ml[row_m + k].x);
+        }
+        if ((q += 32) >= all) break;
+        row_m = row_of(q);
+      }
+      bool some = false;
 #pragma unroll
       for (int k = 0; k < kHeads; ++k) {
-        x[k] = 0.f;
-        if (row >= 0 && k < heads) {
-          const float2 ml = p.part_ml[row + k];
-          x[k] = ml.x == -INFINITY ? 0.f : ex2a(ml.x - m[k]);
-          l[k] += x[k] * ml.y;
-        }
-        any |= x[k] > 0.f;
+        m[k] = warp_max(m[k]);
+        some |= m[k] > -INFINITY;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) o[k][e] = 0.f;
       }
-      for (unsigned left = __ballot_sync(0xffffffffu, any); left;) {
-        float y[kAhead][kHeads][kVec], f[kAhead][kHeads];
+      for (int q0 = 0; q0 < all && some; q0 += 32 * kWarps) {
+        const int64_t row = q0 == 0 ? row_s : row_of(q0 + lane * kWarps + part);
+        float x[kHeads];
+        bool any = false;
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-          const int src = left ? __ffs(left) - 1 : 0;
-          const bool on = left != 0;
-          left &= left - 1;
-          const int64_t at = __shfl_sync(0xffffffffu, row, src);
+        for (int k = 0; k < kHeads; ++k) {
+          x[k] = 0.f;
+          if (row >= 0 && k < heads) {
+            const float2 ml = p.part_ml[row + k];
+            x[k] = ml.x == -INFINITY ? 0.f : ex2a(ml.x - m[k]);
+            l[k] += x[k] * ml.y;
+          }
+          any |= x[k] > 0.f;
+        }
+        for (unsigned left = __ballot_sync(0xffffffffu, any); left;) {
+          float y[kAhead][kHeads][kVec], f[kAhead][kHeads];
 #pragma unroll
-          for (int k = 0; k < kHeads; ++k) {
-            f[a][k] = on ? __shfl_sync(0xffffffffu, x[k], src) : 0.f;
+          for (int a = 0; a < kAhead; ++a) {
+            const int src = left ? __ffs(left) - 1 : 0;
+            const bool on = left != 0;
+            left &= left - 1;
+            const int64_t at = __shfl_sync(0xffffffffu, row, src);
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) y[a][k][e] = 0.f;
-            if (f[a][k] > 0.f) {
-              if constexpr (kVec == 4) {
-                const float4 z = *part_chunk<HD>(p.part_o, at + k, lane);
-                y[a][k][0] = z.x; y[a][k][1] = z.y; y[a][k][2] = z.z; y[a][k][3] = z.w;
-              } else {
-                const float2 z = reinterpret_cast<const float2*>(part_chunk<HD>(p.part_o, at + k, lane >> 1))[lane & 1];
-                y[a][k][0] = z.x; y[a][k][1] = z.y;
+            for (int k = 0; k < kHeads; ++k) {
+              f[a][k] = on ? __shfl_sync(0xffffffffu, x[k], src) : 0.f;
+#pragma unroll
+              for (int e = 0; e < kVec; ++e) y[a][k][e] = 0.f;
+              if (f[a][k] > 0.f) {
+                if constexpr (kVec == 4) {
+                  const float4 z = *part_chunk<HD>(p.part_o, at + k, lane);
+                  y[a][k][0] = z.x; y[a][k][1] = z.y; y[a][k][2] = z.z; y[a][k][3] = z.w;
+                } else {
+                  const float2 z = reinterpret_cast<const float2*>(part_chunk<HD>(p.part_o, at + k, lane >> 1))[lane & 1];
+                  y[a][k][0] = z.x; y[a][k][1] = z.y;
+                }
               }
             }
           }
-        }
 #pragma unroll
-        for (int a = 0; a < kAhead; ++a)
+          for (int a = 0; a < kAhead; ++a)
 #pragma unroll
-          for (int k = 0; k < kHeads; ++k)
+            for (int k = 0; k < kHeads; ++k)
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) o[k][e] = fmaf(y[a][k][e], f[a][k], o[k][e]);
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < kHeads; ++k) l[k] = warp_sum(l[k]);
-    if constexpr (kWarps > 1) {
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) s_o[warp][lane * kVec + e] = o[0][e];
-      if (lane == 0) s_l[warp] = l[0];
-      __syncthreads();
-      if (part == 0) {
-        l[0] = 0.f;
-        for (int k = 0; k < kWarps; ++k) l[0] += s_l[k * kJoinRows + warp];
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          o[0][e] = 0.f;
-          for (int k = 0; k < kWarps; ++k) o[0][e] += s_o[k * kJoinRows + warp][lane * kVec + e];
+              for (int e = 0; e < kVec; ++e) o[k][e] = fmaf(y[a][k][e], f[a][k], o[k][e]);
         }
       }
-      __syncthreads();
-    }
-    if (mine >= rows || part > 0) continue;
 #pragma unroll
-    for (int k = 0; k < kHeads; ++k) {
-      if (k >= heads) break;
-      const float inv = l[k] > 0.f ? 1.f / l[k] : 0.f;
-      const int64_t to = (int64_t)t * p.nq + g * p.rep + hr + k;
-      T* out = static_cast<T*>(p.out) + to * HD + lane * kVec;
-      if constexpr (sizeof(T) == 2 && kVec == 4)
-        *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(o[k][0] * inv, o[k][1] * inv), pack_bf16(o[k][2] * inv, o[k][3] * inv));
-      else
+      for (int k = 0; k < kHeads; ++k) l[k] = warp_sum(l[k]);
+      if constexpr (kWarps > 1) {
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) out[e] = from_f<T>(o[k][e] * inv);
-      if (p.lse && lane == 0) p.lse[to] = m[k] == -INFINITY ? -INFINITY : (m[k] + log2f(l[k])) * kLn2;
+        for (int e = 0; e < kVec; ++e) s_o[warp][lane * kVec + e] = o[0][e];
+        if (lane == 0) s_l[warp] = l[0];
+        __syncthreads();
+        if (part == 0) {
+          l[0] = 0.f;
+          for (int k = 0; k < kWarps; ++k) l[0] += s_l[k * kJoinRows + warp];
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            o[0][e] = 0.f;
+            for (int k = 0; k < kWarps; ++k) o[0][e] += s_o[k * kJoinRows + warp][lane * kVec + e];
+          }
+        }
+        __syncthreads();
+      }
+      if (mine >= rows || part > 0) continue;
+#pragma unroll
+      for (int k = 0; k < kHeads; ++k) {
+        if (k >= heads) break;
+        const float inv = l[k] > 0.f ? 1.f / l[k] : 0.f;
+        const int64_t to = (int64_t)t * p.nq + g * p.rep + hr + k;
+        T* out = static_cast<T*>(p.out) + to * HD + lane * kVec;
+        if constexpr (sizeof(T) == 2 && kVec == 4)
+          *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(o[k][0] * inv, o[k][1] * inv), pack_bf16(o[k][2] * inv, o[k][3] * inv));
+        else
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) out[e] = from_f<T>(o[k][e] * inv);
+        if (p.lse && lane == 0) p.lse[to] = m[k] == -INFINITY ? -INFINITY : (m[k] + log2f(l[k])) * kLn2;
+      }
     }
   }
   if (!waited) griddep_wait();

@@ -74,17 +74,23 @@ struct __align__(16) PrefixSeq {
 static __device__ __noinline__ int64_t long_div(int64_t a, int64_t b) { return a / b; }
 __device__ __forceinline__ int cdiv(int a, int b) { return (a + b - 1) / b; }
 
-// Sequence i of the batch; rows = 0 for one the call cannot use.
+// Sequence i of the batch; rows = 0 for one the call cannot use.  kFresh: read from
+// memory whatever this grid has read there before.
+template <bool kFresh>
+__device__ __forceinline__ int seq_word(const int32_t* p) {
+  return kFresh ? *reinterpret_cast<const volatile int32_t*>(p) : *p;
+}
+template <bool kFresh = false>
 __device__ __forceinline__ PrefixSeq prefix_seq(const PrefixAttnParams& p, int i, bool report) {
   PrefixSeq r;
-  r.seq = p.seqs[i];
-  r.first = p.start[i];
-  r.rows = p.start[i + 1] - r.first;
+  r.seq = seq_word<kFresh>(p.seqs + i);
+  r.first = seq_word<kFresh>(p.start + i);
+  r.rows = seq_word<kFresh>(p.start + i + 1) - r.first;
   r.len = 0;
   const int most = p.max_pages * p.page;
   bool bad = r.first < 0 || r.rows < 0 || r.first > p.total - r.rows || r.seq < 0 || r.seq >= p.n_seqs;
   if (!bad) {
-    r.len = p.len[r.seq];
+    r.len = seq_word<kFresh>(p.len + r.seq);
     bad = r.len < 0 || r.len > most;
   }
   if (bad) {
@@ -93,6 +99,16 @@ __device__ __forceinline__ PrefixSeq prefix_seq(const PrefixAttnParams& p, int i
     r.rows = r.len = 0;
   }
   return r;
+}
+
+// Whether memory still says what r was made of (one round of loads where the call can use the sequence).
+__device__ __forceinline__ bool same_seq(const PrefixAttnParams& p, int i, const PrefixSeq& r) {
+  if (r.seq >= 0) {
+    const int seq = seq_word<true>(p.seqs + i), first = seq_word<true>(p.start + i), next = seq_word<true>(p.start + i + 1);
+    return (seq == r.seq) & (first == r.first) & (next - first == r.rows) & (seq_word<true>(p.len + r.seq) == r.len);
+  }
+  const PrefixSeq x = prefix_seq<true>(p, i, false);
+  return x.seq < 0 && x.first == r.first;
 }
 
 // Own key blocks that unit u of a sequence has to see.
