@@ -13,6 +13,9 @@ namespace {
 inline int esize(int dtype) { return dtype == LSP_DTYPE_BF16 ? 2 : 4; }
 inline cudaStream_t S(lsp_stream_t s) { return static_cast<cudaStream_t>(s); }
 inline bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+// Lists of 32-bit words (or none): a kernel that read one at another address would fault.
+template <typename... P>
+inline bool words(P... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & 3) == 0; }
 
 int num_sms(int* sms) {
   int dev = 0;
@@ -44,7 +47,7 @@ int view(const lsp_kv_cache* c, KvCache* out) {
   const int rc = check_shape(c);
   if (rc != LSP_OK) return rc;
   if (!c->k || !c->v || !c->table || !c->len || !c->refs || !aligned(c->k, 16) || !aligned(c->v, 16) ||
-      !aligned(c->table, 4) || !aligned(c->len, 4) || !aligned(c->refs, 4))
+      !words(c->table, c->len, c->refs))
     return LSP_ERR_ARG;
   out->k = static_cast<char*>(c->k);
   out->v = static_cast<char*>(c->v);
@@ -61,8 +64,8 @@ int view(const lsp_kv_cache* c, KvCache* out) {
   return LSP_OK;
 }
 
-int entries(const int32_t* a, const int32_t* b, int n) {
-  if (n < 0 || (n > 0 && (!a || !b))) return LSP_ERR_ARG;
+int entries(const int32_t* a, const int32_t* b, int n, const uint32_t* dev_error) {
+  if (n < 0 || (n > 0 && (!a || !b)) || !words(a, b, dev_error)) return LSP_ERR_ARG;
   return n > kPagesMaxSeqs ? LSP_ERR_SHAPE : LSP_OK;
 }
 
@@ -87,7 +90,7 @@ int lsp_pages_fork(const lsp_kv_cache* cache, const int32_t* src, const int32_t*
                    lsp_stream_t stream) {
   KvCache c;
   int rc = view(cache, &c);
-  if (rc == LSP_OK) rc = entries(src, dst, n);
+  if (rc == LSP_OK) rc = entries(src, dst, n, dev_error);
   if (rc != LSP_OK || n == 0) return rc;
   return launch_pages_fork(c, src, dst, n, dev_error, S(stream));
 }
@@ -96,7 +99,7 @@ int lsp_pages_trim(const lsp_kv_cache* cache, const int32_t* seqs, const int32_t
                    lsp_stream_t stream) {
   KvCache c;
   int rc = view(cache, &c);
-  if (rc == LSP_OK) rc = entries(seqs, new_len, n);
+  if (rc == LSP_OK) rc = entries(seqs, new_len, n, dev_error);
   if (rc != LSP_OK || n == 0) return rc;
   return launch_pages_trim(c, seqs, new_len, n, dev_error, S(stream));
 }
@@ -105,7 +108,7 @@ int lsp_pages_reserve(const lsp_kv_cache* cache, const int32_t* seqs, const int3
                       size_t workspace_bytes, uint32_t* dev_error, lsp_stream_t stream) {
   KvCache c;
   int rc = view(cache, &c), sms = 0;
-  if (rc == LSP_OK) rc = entries(seqs, add, n);
+  if (rc == LSP_OK) rc = entries(seqs, add, n, dev_error);
   if (rc != LSP_OK || n == 0) return rc;
   if (!workspace || !aligned(workspace, 16) || workspace_bytes < pages_ws_bytes(c.pages)) return LSP_ERR_ARG;
   if ((rc = num_sms(&sms)) != LSP_OK) return rc;
@@ -117,7 +120,7 @@ int lsp_pages_compact(const lsp_kv_cache* cache, int32_t* live, void* workspace,
   KvCache c;
   int rc = view(cache, &c), sms = 0;
   if (rc != LSP_OK) return rc;
-  if (!workspace || !aligned(workspace, 16) || workspace_bytes < pages_ws_bytes(c.pages)) return LSP_ERR_ARG;
+  if (!workspace || !aligned(workspace, 16) || workspace_bytes < pages_ws_bytes(c.pages) || !words(live)) return LSP_ERR_ARG;
   if ((rc = num_sms(&sms)) != LSP_OK) return rc;
   return launch_pages_compact(c, live, workspace, esize(cache->dtype), sms, S(stream));
 }
@@ -130,7 +133,7 @@ int lsp_pages_write(const lsp_kv_cache* cache, int layer, const int32_t* seqs, c
   if (rc != LSP_OK) return rc;
   if (layer < 0 || layer >= c.layers || n < 0 || total < 0) return LSP_ERR_ARG;
   if (n == 0 || total == 0) return LSP_OK;
-  if (!seqs || !start) return LSP_ERR_ARG;
+  if (!seqs || !start || !words(seqs, start, dev_error)) return LSP_ERR_ARG;
   const int es = esize(cache->dtype);
   if (!k_new || !v_new || !aligned(k_new, 16) || !aligned(v_new, 16)) return LSP_ERR_ARG;
   if (total > (1 << 28) || (total > 1 && (row_stride < (int64_t)c.nkv * c.d || row_stride * es % 16))) return LSP_ERR_SHAPE;
@@ -155,7 +158,8 @@ int lsp_prefix_attention(const lsp_kv_cache* cache, int layer, const void* q, in
   int rc = view(cache, &c), sms = 0;
   if (rc == LSP_OK) rc = attn_shape(cache, nq, n, total, &p);
   if (rc != LSP_OK) return rc;
-  if (layer < 0 || layer >= c.layers || shared_len < 0 || !(scale > 0.f) || !std::isfinite(scale) || !seqs || !start)
+  if (layer < 0 || layer >= c.layers || shared_len < 0 || !(scale > 0.f) || !std::isfinite(scale) || !seqs || !start ||
+      !words(seqs, start, lse, dev_error))
     return LSP_ERR_ARG;
   if (total == 0) return LSP_OK;
   const int es = esize(cache->dtype);
@@ -185,7 +189,9 @@ int lsp_verify_probs(const void* target_probs, const void* draft_probs, int dtyp
   if (C < 1 || C > (1 << 20) || B < 0 || B > 1024 || V < 1 || V > (1 << 30)) return LSP_ERR_SHAPE;
   if (ld_target < V || (draft_probs && B > 0 && ld_draft < V)) return LSP_ERR_SHAPE;
   const size_t es = esize(dtype);
-  if (!aligned(target_probs, es) || !aligned(draft_probs, es) || !aligned(e, 4)) return LSP_ERR_ARG;
+  if (!aligned(target_probs, es) || !aligned(draft_probs, es) ||
+      !words(draft_tokens, n_draft, u, e, accepted_len, next_token, out_tokens, dev_error))
+    return LSP_ERR_ARG;
   VerifyProbsParams p;
   p.pt = target_probs; p.pq = B > 0 ? draft_probs : nullptr; p.y = draft_tokens; p.n = n_draft; p.u = u; p.e = e;
   p.accepted = accepted_len; p.next_token = next_token; p.out_tokens = out_tokens; p.err = dev_error;
