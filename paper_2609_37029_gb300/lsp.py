@@ -200,7 +200,8 @@ def make_kv_cache(k, v, table, lens, refs) -> lsp_kv_cache:
     four axes (their strides are taken), int32 table [seqs][max_pages], lens [seqs], refs [pages].
     The struct holds addresses only: the caller keeps the tensors."""
     import torch
-    if k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.dim() != 5 or k.stride(4) != 1:
+    apart = any(a != b for a, b, n in zip(k.stride(), v.stride(), k.shape) if n > 1)
+    if k.shape != v.shape or apart or k.dtype != v.dtype or k.dim() != 5 or k.stride(4) != 1:
         raise ValueError("k and v: the same 5-D shape, type and strides, the last axis dense")
     for t in (table, lens, refs):
         if t.dtype != torch.int32 or not t.is_contiguous():
@@ -428,9 +429,10 @@ def lsp_pages_reserve(cache: lsp_kv_cache, seqs, add, workspace, dev_error=None,
 def lsp_pages_write(cache: lsp_kv_cache, layer, seqs, start, k_new, v_new, dev_error=None, stream=None) -> None:
     """k_new, v_new: [total][nkv][d] of the cache's type, dense within a row, the same stride between rows; seqs
     [n], start [n + 1] int32."""
-    shape, stride, d, n = k_new.shape, k_new.stride(), cache.d, seqs.numel()
-    if (shape != v_new.shape or stride != v_new.stride() or stride[1] != d or stride[2] != 1 or shape[1] != cache.nkv
-            or shape[2] != d):
+    shape, stride, other, d, n = k_new.shape, k_new.stride(), v_new.stride(), cache.d, seqs.numel()
+    # (the stride along an axis of one is never used, and may be anything)
+    if (shape != v_new.shape or shape[1] != cache.nkv or shape[2] != d or stride[2] != 1 or other[2] != 1
+            or shape[1] > 1 and (stride[1] != d or other[1] != d) or shape[0] > 1 and stride[0] != other[0]):
         raise ValueError("k_new and v_new: [total][nkv][d] of the same strides, dense within a row")
     if _dtype_code(k_new.dtype) != cache.dtype or v_new.dtype != k_new.dtype:
         raise ValueError("k_new and v_new: the cache's type")
@@ -464,7 +466,8 @@ def lsp_prefix_attention(cache: lsp_kv_cache, layer, q, seqs, start, out, lse=No
     """q: [total][nq][d] of the cache's type, dense within a row (a slice of a fused q/k/v row will do); out:
     the same, dense; seqs [n], start [n + 1] int32; lse: float32 [total][nq] or None."""
     shape, stride, d, n = q.shape, q.stride(), cache.d, seqs.numel()
-    if stride[1] != d or stride[2] != 1 or shape[2] != d or out.shape != shape or not out.is_contiguous():
+    if (stride[1] != d and shape[1] > 1 or stride[2] != 1 or shape[2] != d or out.shape != shape
+            or not out.is_contiguous()):
         raise ValueError("q: [total][nq][d], dense within a row; out: the same shape, contiguous")
     if _dtype_code(q.dtype) != cache.dtype or out.dtype != q.dtype:
         raise ValueError("q and out: the cache's type")

@@ -140,3 +140,31 @@ def test_verification(lsp, dtype):
     # no candidates at all
     none = dict(target_probs=torch.zeros(C, 1, V, dtype=dtype), draft_probs=None, draft_tokens=ints(C, 0), u=f32(C, 0), out_tokens=ints(C, 1))
     refused(lsp, lsp.lsp_verify_probs, {**base, **none}, [])
+
+
+@no_gpu
+def test_the_stride_of_an_axis_of_one_may_be_anything(lsp):
+    """One head, one row, one layer, one page: dense however torch counts the steps along them."""
+    def odd(t, **steps):
+        stride = list(t.stride())
+        for axis, step in steps.items():
+            assert t.shape[int(axis[1:])] == 1
+            stride[int(axis[1:])] = step
+        return t.as_strided(t.shape, stride)
+    k = torch.zeros(1, 1, 1, 16, 64)
+    c = lsp.make_kv_cache(odd(k, a0=7), odd(k, a1=3, a2=1), ints(4, 7), ints(4), ints(1))
+    q = torch.zeros(6, 1, 64)
+    lists = dict(seqs=ints(3), start=ints(4), stream=0)
+    for x in (odd(q, a1=1), odd(q, a1=12345), q.transpose(0, 1).contiguous().transpose(0, 1)):
+        refused(lsp, lsp.lsp_prefix_attention, dict(cache=c, layer=0, q=x, out=torch.zeros_like(q), shared_len=0, scale=1.0,
+                                                    workspace=torch.zeros(64, dtype=torch.uint8), **lists), [])
+        refused(lsp, lsp.lsp_pages_write, dict(cache=c, layer=5, k_new=x, v_new=q, **lists), [])
+    one = torch.zeros(1, 1, 64)
+    refused(lsp, lsp.lsp_pages_write, dict(cache=c, layer=5, k_new=odd(one, a0=1), v_new=odd(one, a0=500, a1=9), **lists), [])
+    # but not of any other
+    two = torch.zeros(1, 2, 1, 16, 64)
+    with pytest.raises(ValueError):
+        lsp.make_kv_cache(two, torch.zeros(1, 4, 1, 16, 64)[:, ::2], ints(4, 7), ints(4), ints(2))
+    wide = torch.zeros(6, 1, 128)[..., :64]
+    refused(lsp, lsp.lsp_pages_write, dict(cache=c, layer=5, k_new=wide, v_new=wide, **lists), [
+        ("same strides", dict(v_new=q)), ("same strides", dict(v_new=torch.zeros(6, 1, 128)[..., ::2]))])
