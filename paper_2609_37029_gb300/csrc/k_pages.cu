@@ -17,9 +17,9 @@
 // branch (fork, reserve 17 tokens, write, trim) of 4 continuations of each of 16
 // prompts of 1000-4000 tokens, 32 layers: 76 us for 521 MB copied and written (6.9
 // TB/s, the rate of a plain copy).  compact of 2000 live pages of 3000, 8 layers:
-// 430 us for 2.8 GB (6.5 TB/s).  Both are bound by memory; small calls by their
-// launches (17 us from the host, 13 us and 10 us on the device for the four calls
-// and for the one).
+// 421 to 432 us for 2.8 GB (6.5 to 6.6 TB/s).  Both are bound by memory; small calls
+// by their launches (18 to 21 us from the host, 13 us and 9 us on the device for the
+// four calls and for the one).
 #include <algorithm>
 
 #include "common.cuh"
@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(kSmallThreads) pages_write_kernel(const KvCach
   griddep_launch();
   const int lane = threadIdx.x & 31;
   const int w = blockIdx.x * (kSmallThreads / 32) + (threadIdx.x >> 5);
-  const int t = (int)((unsigned)w >> 1);         // (two warps a row: w may pass 2^31)
+  const int t = w >> 1;                          // (total <= 2^28: w stays below 2^30)
   if (t >= total) return;
   int lo = 0, hi = n;                            // the last entry that starts at or before t
   while (hi - lo > 1) {

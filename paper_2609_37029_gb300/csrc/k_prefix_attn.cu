@@ -9,9 +9,12 @@
 // weights 2^(m2_seg - max m2).
 //
 // prefix_attn_fma_kernel: f32 storage, fp32 multiply-adds, 64 rows x 64 keys a
-// step, 4 x 4 scores and 4 x (HD / 16) sums a thread.  Bound by the multiply-adds
-// where rows fill the tiles (16 requests of 1 to 17 rows, 32 heads of 128, over 8K:
-// 637 us), by the latency of its rounds of loads in small calls (5 over 2K: 18 us).
+// step, 4 x 4 scores and 4 x (HD / 16) sums a thread.  Where rows fill the tiles (16
+// requests of 1 to 16 rows, 32 heads of 128, over 8K: 634 us) it runs at 34 of some 80
+// TFLOP/s: 8 shared loads of 16 bytes for 64 multiply-adds keep shared memory's port
+// busy 12 cycles of 16, a block of keys has four barriers, and registers and tiles
+// leave one CTA of 8 warps on an SM.  Small calls are bound by the latency of their
+// rounds of loads (5 over 2K: 18 us).
 // bf16 storage: k_prefix_attn_tc.cu.
 #include <algorithm>
 #include <cstdint>
@@ -232,8 +235,8 @@ __global__ void __launch_bounds__(kFmaThreads, kFmaPerSm<HD>) prefix_attn_fma_ke
 // that the sums themselves are independent loads.  Where rows are few (they have
 // many segments each), four warps take a row's segments in turn.  Where they fill
 // the GPU, a warp has up to four heads of one KV head: their segments are found
-// once, and their sums lie side by side (16 requests over 32K, a round: 132 us in
-// all with four heads a warp, 139 with one).
+// once, and their sums lie side by side (16 requests over 32K, a round, when this was
+// chosen: 132 us in all with four heads a warp, 139 with one).
 //
 // Bound by latency: 5 us to find a row's segments in code that is not cached yet,
 // and three dependent rounds of loads of some 3 us.  Where the segments are

@@ -28,19 +28,22 @@
 // half of the weights are there, for a stream is bound by its chain: scores, their
 // maximum, exponentials, P V, the next scores.
 //
-// Measured: 32 requests of 9 to 17 rows over 128K 750 us in all (1.47 PFLOP/s), 16
-// of 17 over 32K 130 us (1.15 PFLOP/s), 16 of one over 32K 44 us (3.4 TB/s, of
-// which 26 us at 5.7 TB/s; the rest is finding the work, the first loads and the
-// join).  In the long ones a block of two tiles takes 1.46 us, some 2800 cycles:
-// 2048 of products, and as many of shared memory, which the scores (both operands
-// from there) read at its full rate while the next keys and values are written.
+// Measured: 32 requests of 9 to 17 rows over 128K 757 to 826 us in all (1.46 to 1.33
+// PFLOP/s: the clock falls in long runs), 16 of 17 over 32K 133 to 136 us (1.1
+// PFLOP/s), 16 of one over 32K 45 us (3.3 TB/s, of which 26 us at 5.7 TB/s; the rest
+// is finding the work, the first loads and the join); 4 prompt chunks of 232 to 591
+// rows over 2K to 7K tokens in pages of 16 133 us (0.75 PFLOP/s).  In the long ones a
+// block of two tiles takes 1.46 us, some 2800 cycles: 2048 of products, and as many
+// of shared memory, which the scores (both operands from there) read at its full
+// rate while the next keys and values are written.
 //
 // A stream's order is S(0) PV(0) S(1) PV(1) ...: S(j + 1) overwrites the weights
 // that PV(j) reads, and the products of one thread complete in order.  TMEM:
 // scores of stream t at columns 128 t, sums at 256 + 128 t.
 //
 // The maximum is raised (and the sums rescaled) only when it would grow by more
-// than 2^8: weights stay below 2^8 and the sums, in fp32, lose nothing.
+// than 2^8, as attention kernels in the literature do: weights stay below 2^8 and
+// the sums, in fp32, lose nothing.
 #include <algorithm>
 
 #include "prefix_sched.cuh"
@@ -53,7 +56,7 @@ constexpr int kRows = kPrefixTcRows, kKeys = kPrefixTcKeys, kTiles = kPrefixTcTi
 constexpr int kThreads = 384;
 constexpr int kLoadWarp = 8, kMmaWarp = 9;       // the second products' warp and the plan's follow
 constexpr int kAhead = 4;                        // segments planned ahead
-constexpr int kFirstKeys = 64;                   // keys whose weights are handed over before the rest's (0.75 ms over 128K; 32: 0.79, 96: 0.81)
+constexpr int kFirstKeys = 64;                   // keys whose weights are handed over before the rest's (when chosen 0.75 ms over 128K; 32: 0.79, 96: 0.81)
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRaise = 8.0f;                   // log2 of the most a weight may exceed 1
 
@@ -561,6 +564,9 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
           acc[(c >> 1) & 3] = add2(acc[(c >> 1) & 3], e);
           w[c >> 1] = pack_bf16(e.x, e.y);
         }
+        // (for the product with V the weights are rounded to the storage type, 2^-9 of each; their sum is not.
+        // The other operand is bf16, and an output's own rounding outweighs it: off by 0.0017 of 64 bits in all, 0.0016
+        // with fp32 weights, over 32K)
         tmem_st16(ts + 16 * h, w);
         if (32 * (h + 1) == kFirstKeys) {
           tmem_wait_st();
