@@ -67,6 +67,7 @@ extern "C" {
 
 #define LSP_DTYPE_BF16 0
 #define LSP_DTYPE_F32 1
+#define LSP_DTYPE_Q4 2            /* lsp_kv_cache only: a cache held in 4 bits */
 
 /* lsp_config.flags.  LSP_NO_BOUNDARY: the "w/o boundary state" variant of the
  * ablation (Sec. 3.4, Fig. 5): the state keeps no boundary hidden state, the
@@ -390,7 +391,12 @@ int lsp_state_import(lsp_state* st, const void* host_buf, size_t bytes, lsp_stre
  *                      only partly filled and shared is copied first
  *   per target layer:  lsp_pages_write, lsp_prefix_attention
  *   lsp_verify_probs   (or lsp_verify) accepts r of the drafted tokens
+ *   lsp_logprobs       what a server answers beside them: log probabilities,
+ *                      entropies, the likeliest alternatives
  *   lsp_pages_trim     gives back the rejected rows' pages
+ * A cache held in 4 bits takes lsp_pages_write_q4 and lsp_prefix_attention_q4
+ * instead of the two calls per layer.  lsp_pages_read gives the rows of any cache
+ * back in the layout that lsp_prefill and lsp_view_update take.
  */
 
 /*
@@ -408,8 +414,23 @@ int lsp_state_import(lsp_state* st, const void* host_buf, size_t bytes, lsp_stre
  * leaves an entry with it as it was (LSP_DEV_BAD_SEQ).  So do lsp_pages_fork,
  * trim and reserve where a page they would let go of, hand on or grow is none of
  * the pool.
- * Supported: page 16, 32, 64, 128 or 256; d 64 or 128; dtype BF16 or F32;
+ * Supported: page 16, 32, 64, 128 or 256; d 64 or 128; dtype BF16, F32 or Q4;
  * pages <= 2^20; seqs * max_pages <= 2^30; max_pages * page <= 2^30.
+ *
+ * dtype Q4: keys and values in 4 bits, 4.5 with their scales.  Each 32 dims of a
+ * token's head are a group: with a = max |x| of its values, s, its scale, is the
+ * least number of five significant bits with 7 s >= a (below 2^-126: the least
+ * multiple of 2^-130; 0 if a = 0), and x is held as the whole number c in -7..7
+ * nearest x / s, ties to even.  It stands for c s: of eight significant bits, so
+ * bfloat16 has it exactly (where it passes bfloat16's largest number: infinity).
+ * A group with a value that is not finite is held as NaN throughout.
+ * The slots of a (layer, page, head) lie in one block of page * d * 9/16 bytes:
+ * codes c + 8 [page][d/2 bytes], then scales [page][d/32] in bfloat16.  Element
+ * 8 w + 2 k + h (k < 4, h < 2) of a group is at bits 16 h + 4 k of its 32-bit word
+ * w.  Strides are in bytes, multiples of 16, s_slot = d * 9/16 (of s_layer, s_page
+ * and s_head in any order, each at least the block).  lsp_pages_fork, reserve, trim
+ * and compact take such a cache as any other; lsp_pages_write and
+ * lsp_prefix_attention refuse it (LSP_ERR_ARG).
  */
 typedef struct lsp_kv_cache {
   void* k;
@@ -456,6 +477,26 @@ int lsp_pages_reserve(const lsp_kv_cache* cache, const int32_t* seqs, const int3
 int lsp_pages_write(const lsp_kv_cache* cache, int layer, const int32_t* seqs, const int32_t* start,
                     int n, const void* k_new, const void* v_new, int64_t row_stride, int total,
                     uint32_t* dev_error, lsp_stream_t stream);
+
+/* lsp_pages_write into a cache of dtype Q4: the rows are quantised as they are
+ * stored.  k_new, v_new: device, `dtype` BF16 or F32, else as there.  (Of rows
+ * that one call stores in the same slot, a sequence listed twice, nothing is
+ * promised, in either call.) */
+int lsp_pages_write_q4(const lsp_kv_cache* cache, int layer, const int32_t* seqs, const int32_t* start,
+                       int n, const void* k_new, const void* v_new, int dtype, int64_t row_stride,
+                       int total, uint32_t* dev_error, lsp_stream_t stream);
+
+/* Read keys and values of one layer back into dense rows: the last start[i+1] -
+ * start[i] tokens of sequence seqs[i] become rows [start[i], start[i+1]) (device
+ * int32 [n+1]).  k_out, v_out: device, `dtype` -- the cache's, or BF16 or F32 for
+ * a cache of dtype Q4, both exact -- row r at r * row_stride elements, [nkv][d]
+ * dense within (row_stride and the pointers multiples of 16 bytes); total: rows in
+ * all.  Rows of no entry, and of an entry whose sequence or range is outside the
+ * cache (LSP_DEV_BAD_SEQ), are left as they were; tokens of a page outside the
+ * pool are zero (LSP_DEV_BAD_SEQ).  The cache is only read. */
+int lsp_pages_read(const lsp_kv_cache* cache, int layer, const int32_t* seqs, const int32_t* start,
+                   int n, void* k_out, void* v_out, int dtype, int64_t row_stride, int total,
+                   uint32_t* dev_error, lsp_stream_t stream);
 
 /* Cut sequence seqs[i] down to its first new_len[i] tokens (i < n <= 1024;
  * device int32; 0 frees it, more than it has changes nothing): the pages past
@@ -506,6 +547,23 @@ int lsp_prefix_attention(const lsp_kv_cache* cache, int layer, const void* q, in
                          int shared_len, float scale, void* out, float* lse, void* workspace,
                          size_t workspace_bytes, uint32_t* dev_error, lsp_stream_t stream);
 
+/* The same for lsp_prefix_attention_q4 with rows of `dtype`. */
+size_t lsp_prefix_attention_q4_workspace_bytes(const lsp_kv_cache* cache, int dtype, int nq, int n,
+                                               int total);
+
+/* lsp_prefix_attention over a cache of dtype Q4, whose keys and values enter as
+ * the numbers they stand for: the same rows, shared pages and results, for q and
+ * out of `dtype` BF16 or F32.  Nothing is unpacked to memory.  bf16: scores and
+ * sums in fp32, weights rounded to bf16 for the product with V.  f32: q and the
+ * weights enter the tensor cores as sums of three bf16 numbers each (24 bits), the
+ * products are exact and summed in fp32.  workspace: at least
+ * lsp_prefix_attention_q4_workspace_bytes, 256-byte aligned, not initialised. */
+int lsp_prefix_attention_q4(const lsp_kv_cache* cache, int layer, const void* q, int dtype,
+                            int64_t q_stride, int nq, const int32_t* seqs, const int32_t* start, int n,
+                            int total, int shared_len, float scale, void* out, float* lse,
+                            void* workspace, size_t workspace_bytes, uint32_t* dev_error,
+                            lsp_stream_t stream);
+
 /* Acceptance of drafted tokens (Eq. acceptance, Eq. residual) from
  * probabilities and random numbers that the caller gives: lsp_verify for
  * programs that shape their distributions (top-k, top-p, ...) or draw their
@@ -531,6 +589,30 @@ int lsp_verify_probs(const void* target_probs, const void* draft_probs, int dtyp
                      const float* e, int C, int B, int V, int64_t ld_target, int64_t ld_draft,
                      int32_t* accepted_len, int32_t* next_token, int32_t* out_tokens,
                      uint32_t* dev_error, lsp_stream_t stream);
+
+/* Log probabilities of given tokens (what lsp_verify_probs leaves in out_tokens,
+ * or any others), with the entropy and the likeliest alternatives of each row of
+ * logits.  With x_v = z_v / T and lse = log sum_v exp(x_v), per row:
+ *   logprob = x_token - lse,  entropy = lse - sum_v exp(x_v - lse) x_v  (nats; a
+ *   term of x_v = -inf is 0),  and the k largest z_v in order, ties to the lowest
+ *   index: top = their v, top_logprob = x_v - lse.
+ *   logits  device dtype BF16 or F32, row r at r * ld elements, V within, no
+ *           alignment beyond the type's
+ *   tokens  device int32 [rows]; -1: no token, the row is not read and gives
+ *           logprob -inf, entropy 0, top -1 and top_logprob -inf.  One outside
+ *           [-1, V) is taken as -1 (LSP_DEV_BAD_TOKEN)
+ *   logprob, entropy  device float [rows];  entropy may be NULL
+ *   top     device int32 [rows][k], top_logprob device float [rows][k]; either may
+ *           be NULL, and both are not written with k = 0
+ * A row whose largest logit is not finite (all -inf, a +inf) or that has a NaN has
+ * no distribution: NaN in logprob, entropy and top_logprob; top still holds k
+ * tokens (+inf first, -inf after the finite ones, NaN last).
+ * T > 0; rows >= 0, V in [1, 2^30], ld >= V, k in [0, min(V, 32)].  One launch;
+ * each row is read once (the parts of it with its largest logits twice).  In fp32;
+ * the result does not depend on the other rows. */
+int lsp_logprobs(const void* logits, int dtype, const int32_t* tokens, int rows, int V, int64_t ld,
+                 float temperature, int k, float* logprob, float* entropy, int32_t* top,
+                 float* top_logprob, uint32_t* dev_error, lsp_stream_t stream);
 
 #ifdef __cplusplus
 }

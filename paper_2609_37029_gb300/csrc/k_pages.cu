@@ -350,12 +350,15 @@ __global__ void __launch_bounds__(kPlanThreads) pages_compact_plan_kernel(const 
 // a unit is one head of one page, a warp takes units in turn.  Sources and
 // destinations never meet (new pages are free ones; moves go from behind the
 // live count to before it).  remap: also rewrite the table by w.map (compact).
+// kQ4: a unit is two runs, the codes of the filled slots and their scales (to the
+// next 16 bytes, which are the block's too).
+template <bool kQ4>
 __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const KvCache c, const PagesWs w, int es, int remap) {
   griddep_wait();
   griddep_launch();
   const int lane = threadIdx.x & 31;
   const int64_t n = w.hdr[0], units = n * c.layers * 2 * c.nkv;
-  const int per_slot = c.d * es / 16;            // 16-byte pieces of a slot: 8, 16 or 32
+  const int per_slot = kQ4 ? c.d / 32 : c.d * es / 16;   // 16-byte pieces of a slot (its codes): 2, 4, 8, 16 or 32
   const int shift = 31 - __clz(per_slot);
   const int64_t step = (int64_t)gridDim.x * (kCopyThreads / 32);
   for (int64_t u = (int64_t)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); u < units; u += step) {
@@ -367,19 +370,21 @@ __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const KvCache 
     char* base = (kv ? c.v : c.k) + ((int64_t)layer * c.s_layer + (int64_t)g * c.s_head) * es;
     const char* from = base + (int64_t)w.src[k] * c.s_page * es;
     char* to = base + (int64_t)w.dst[k] * c.s_page * es;
-    const int vecs = w.used[k] << shift;
-    const int64_t slot_bytes = c.s_slot * es;
+    const int codes = w.used[k] << shift, vecs = kQ4 ? codes + (w.used[k] * (c.d / 16) + 15) / 16 : codes;
+    const int64_t slot_bytes = kQ4 ? per_slot * 16 : c.s_slot * es;
+    const int gap = kQ4 ? ((c.page - w.used[k]) << shift) * 16 : 0;     // from the filled slots' codes to the scales
+    auto at = [&](int i) { return (i >> shift) * slot_bytes + (i & (per_slot - 1)) * 16 + (kQ4 && i >= codes ? gap : 0); };
     for (int i0 = lane; i0 < vecs; i0 += 32 * kCopyBatch) {
       uint4 x[kCopyBatch];
 #pragma unroll
       for (int q = 0; q < kCopyBatch; ++q) {
         const int i = i0 + 32 * q;
-        if (i < vecs) x[q] = __ldcs(reinterpret_cast<const uint4*>(from + (i >> shift) * slot_bytes) + (i & (per_slot - 1)));
+        if (i < vecs) x[q] = __ldcs(reinterpret_cast<const uint4*>(from + at(i)));
       }
 #pragma unroll
       for (int q = 0; q < kCopyBatch; ++q) {
         const int i = i0 + 32 * q;
-        if (i < vecs) __stcs(reinterpret_cast<uint4*>(to + (i >> shift) * slot_bytes) + (i & (per_slot - 1)), x[q]);
+        if (i < vecs) __stcs(reinterpret_cast<uint4*>(to + at(i)), x[q]);
       }
     }
   }
@@ -394,7 +399,12 @@ __global__ void __launch_bounds__(kCopyThreads) pages_copy_kernel(const KvCache 
 
 int status(cudaError_t e) { return e == cudaSuccess ? LSP_OK : LSP_ERR_CUDA; }
 
-int copy_grid(int num_sms) { return num_sms * 8; }
+// es: bytes of an element, 0 for a cache in 4 bits (its strides are in bytes)
+cudaError_t launch_copy(const KvCache& c, const PagesWs& w, int es, int remap, int num_sms, cudaStream_t s) {
+  const dim3 grid(num_sms * 8), block(kCopyThreads);
+  return es ? launch_pdl(pages_copy_kernel<false>, grid, block, 0, s, c, w, es, remap)
+            : launch_pdl(pages_copy_kernel<true>, grid, block, 0, s, c, w, 1, remap);
+}
 
 }  // namespace
 
@@ -423,7 +433,7 @@ int launch_pages_reserve(const KvCache& c, const int* seqs, const int* add, int 
   const PagesWs w = ws_split(ws, c.pages);
   cudaError_t e = launch_pdl(pages_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, seqs, add, n, w, err);
   if (e == cudaSuccess)
-    e = launch_pdl(pages_copy_kernel, dim3(copy_grid(num_sms)), dim3(kCopyThreads), 0, s, c, w, es, 0);
+    e = launch_copy(c, w, es, 0, num_sms, s);
   return status(e);
 }
 
@@ -431,7 +441,7 @@ int launch_pages_compact(const KvCache& c, int* live, void* ws, int es, int num_
   const PagesWs w = ws_split(ws, c.pages);
   cudaError_t e = launch_pdl(pages_compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, c, w, live);
   if (e == cudaSuccess)
-    e = launch_pdl(pages_copy_kernel, dim3(copy_grid(num_sms)), dim3(kCopyThreads), 0, s, c, w, es, 1);
+    e = launch_copy(c, w, es, 1, num_sms, s);
   return status(e);
 }
 

@@ -495,6 +495,13 @@ int launch_tc(const PrefixAttnParams& p, cudaStream_t s) {
   return rc == LSP_OK ? launch_join<bf16, HD, kPrefixTcTiles, kPrefixTcKeys>(p, s) : rc;
 }
 
+template <int HD>
+int launch_q4(const PrefixAttnParams& p, int dtype, cudaStream_t s) {
+  const int rc = launch_prefix_attn_q4(p, dtype, s);
+  if (rc != LSP_OK) return rc;
+  return dtype == LSP_DTYPE_BF16 ? launch_join<bf16, HD, 1, kPrefixQ4Keys>(p, s) : launch_join<float, HD, 1, kPrefixQ4Keys>(p, s);
+}
+
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Key ranges of the shared part.  The line cuts the keys among the CTAs by
@@ -504,19 +511,27 @@ int choose_splits(int heads, int units, int blocks, int grid) {
   return units == 1 ? 1 : std::max(1, std::min(grid / (heads * units), blocks));
 }
 
+// Tiles of the kernels: rows of one, tiles of a unit, key block, CTAs of an SM.
+struct Shape {
+  int tile, unit_tiles, block, per_sm;
+};
+Shape attn_shape(const PrefixAttnParams& p, int dtype) {
+  if (p.q4) return {kPrefixQ4Rows, 1, kPrefixQ4Keys, prefix_q4_per_sm(dtype, p.d)};
+  if (dtype == LSP_DTYPE_BF16) return {kPrefixTcRows, kPrefixTcTiles, kPrefixTcKeys, 1};
+  return {kFmaRows, 1, kFmaKeys, p.d == 64 ? kFmaPerSm<64> : kFmaPerSm<128>};
+}
+
 }  // namespace
 
 size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms) {
-  const bool tc = dtype == LSP_DTYPE_BF16;
-  const int tile = tc ? kPrefixTcRows : kFmaRows, unit_tiles = tc ? kPrefixTcTiles : 1;
-  const int block = tc ? kPrefixTcKeys : kFmaKeys, per_sm = tc ? 1 : p->d == 64 ? kFmaPerSm<64> : kFmaPerSm<128>;
-  p->tok_tile = tile / p->rep;
-  p->units = (p->total + p->tok_tile * unit_tiles - 1) / (p->tok_tile * unit_tiles);
+  const Shape sh = attn_shape(*p, dtype);
+  p->tok_tile = sh.tile / p->rep;
+  p->units = (p->total + p->tok_tile * sh.unit_tiles - 1) / (p->tok_tile * sh.unit_tiles);
   p->num_sms = num_sms;
-  p->grid = std::min(num_sms * per_sm, kPrefixMaxGrid);
-  p->splits = choose_splits(p->nkv, p->units, (p->shared_len + block - 1) / block, p->grid);
+  p->grid = std::min(num_sms * sh.per_sm, kPrefixMaxGrid);
+  p->splits = choose_splits(p->nkv, p->units, (p->shared_len + sh.block - 1) / sh.block, p->grid);
   // (not of `splits`: the workspace of one shared_len is enough for any)
-  const int64_t rows = (int64_t)p->tok_tile * p->rep * unit_tiles, items = std::max<int64_t>((int64_t)p->nkv * p->units, p->grid);
+  const int64_t rows = (int64_t)p->tok_tile * p->rep * sh.unit_tiles, items = std::max<int64_t>((int64_t)p->nkv * p->units, p->grid);
   p->part_rows = (items + 2 * p->grid) * rows + (int64_t)p->nkv * p->rep * p->total;
   p->part_rows = (p->part_rows + 3) / 4 * 4;
   return align256((size_t)p->part_rows * sizeof(float2)) + (size_t)p->part_rows * p->d * sizeof(float);
@@ -527,6 +542,7 @@ int launch_prefix_attention(PrefixAttnParams p, int dtype, void* ws, cudaStream_
   p.part_ml = reinterpret_cast<float2*>(w);
   w += align256((size_t)p.part_rows * sizeof(float2));
   p.part_o = reinterpret_cast<float*>(w);
+  if (p.q4) return p.d == 128 ? launch_q4<128>(p, dtype, s) : launch_q4<64>(p, dtype, s);
   if (dtype == LSP_DTYPE_BF16) return p.d == 128 ? launch_tc<128>(p, s) : launch_tc<64>(p, s);
   return p.d == 128 ? launch_fma<128>(p, s) : launch_fma<64>(p, s);
 }

@@ -46,8 +46,8 @@
 // the sums, in fp32, lose nothing.
 #include <algorithm>
 
+#include "barrier_wait.cuh"
 #include "prefix_sched.cuh"
-#include "warp_wait.cuh"
 
 namespace lsp {
 namespace {
@@ -87,29 +87,6 @@ struct TcMisc {
 
 template <int HD>
 constexpr size_t tc_smem() { return TcShape<HD>::kMisc + sizeof(TcMisc) + 1024; }
-
-// Bounded wait that also gives up when another role has; for whole warps, the same answer in every lane.
-struct BarrierWait {
-  uint32_t bar, parity;
-  volatile int* abort;
-  unsigned* err;
-  __device__ __forceinline__ bool ready() const { return mbar_try_wait(bar, parity); }
-  __device__ __forceinline__ bool all(bool x) const { return __all_sync(0xffffffffu, x); }
-  __device__ __forceinline__ bool any(bool x) const { return __any_sync(0xffffffffu, x); }
-  __device__ __forceinline__ bool gone() const { return *abort != 0; }
-  __device__ __forceinline__ uint64_t now() const { return global_ns(); }
-  __device__ __forceinline__ void give_up(bool late) const {
-    if (late) set_err(err, LSP_DEV_TIMEOUT);
-    *abort = 1;
-  }
-};
-__device__ __forceinline__ bool tc_wait(uint32_t bar, uint32_t parity, volatile int* abort, unsigned* err) {
-  return warp_wait(BarrierWait{bar, parity, abort, err}, kWaitLimitNs);
-}
-
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* map, uint32_t bar, int x, int y, int z) {
   asm volatile(

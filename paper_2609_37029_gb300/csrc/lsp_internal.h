@@ -269,7 +269,7 @@ int launch_philox_words(uint64_t seed, uint32_t round, uint32_t b, uint32_t i, u
                         int count, cudaStream_t s);
 
 // ------------------------------------------------------------------ paged cache (target side)
-// lsp_kv_cache with byte-addressed pools; strides in elements.
+// lsp_kv_cache with byte-addressed pools; strides in elements (a cache in 4 bits: bytes).
 struct KvCache {
   char* k;
   char* v;
@@ -285,9 +285,16 @@ int launch_pages_fork(const KvCache& c, const int* src, const int* dst, int n, u
 int launch_pages_trim(const KvCache& c, const int* seqs, const int* new_len, int n, unsigned* err, cudaStream_t s);
 int launch_pages_write(const KvCache& c, const int* seqs, const int* start, int n, const void* k_new, const void* v_new,
                        int64_t row_bytes, int total, int es, unsigned* err, cudaStream_t s);
+// es: bytes of an element, 0 for a cache in 4 bits.
 int launch_pages_reserve(const KvCache& c, const int* seqs, const int* add, int n, void* ws, int es, int num_sms,
                          unsigned* err, cudaStream_t s);
 int launch_pages_compact(const KvCache& c, int* live, void* ws, int es, int num_sms, cudaStream_t s);
+// es: bytes of an element of the rows.
+int launch_pages_write_q4(const KvCache& c, const int* seqs, const int* start, int n, const void* k_new, const void* v_new,
+                          int64_t row_bytes, int total, int es, unsigned* err, cudaStream_t s);
+// q4: the cache is in 4 bits, else it holds elements of es bytes too.
+int launch_pages_read(const KvCache& c, const int* seqs, const int* start, int n, void* k_out, void* v_out, int64_t row_bytes,
+                      int total, int es, bool q4, unsigned* err, cudaStream_t s);
 
 // ------------------------------------------------------------------ shared-prefix attention
 struct PrefixAttnParams {
@@ -304,6 +311,7 @@ struct PrefixAttnParams {
   int n, total, nq, nkv, rep, d;
   int page, pages, max_pages, n_seqs;
   int shared_len;
+  bool q4;                  // k, v in 4 bits (strides in bytes)
   float scale;
   unsigned* err;
   // plan (prefix_attn_plan) and workspace
@@ -324,6 +332,10 @@ size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms);
 // bf16 on the tensor cores; the joining kernel is the caller's.
 int launch_prefix_attn_tc(const PrefixAttnParams& p, cudaStream_t s);
 constexpr int kPrefixTcRows = 128, kPrefixTcKeys = 128, kPrefixTcTiles = 2;   // tile rows, key block, tiles of a unit
+// rows of bf16 or f32 over a cache in 4 bits
+int launch_prefix_attn_q4(const PrefixAttnParams& p, int dtype, cudaStream_t s);
+int prefix_q4_per_sm(int dtype, int d);
+constexpr int kPrefixQ4Rows = 64, kPrefixQ4Keys = 128;
 // ws: prefix_attn_plan's bytes, 256-byte aligned.
 int launch_prefix_attention(PrefixAttnParams p, int dtype, void* ws, cudaStream_t s);
 
@@ -343,5 +355,21 @@ struct VerifyProbsParams {
   int64_t ld_t, ld_q;
 };
 int launch_verify_probs(const VerifyProbsParams& p, int dtype, int num_sms, cudaStream_t s);
+
+// ------------------------------------------------------------------ log probabilities
+struct LogprobsParams {
+  const void* z;            // [rows][V], ld apart
+  const int32_t* tokens;    // [rows]
+  float* logprob;           // [rows]
+  float* entropy;           // [rows] or null
+  int32_t* top;             // [rows][k] or null
+  float* top_logprob;       // [rows][k] or null
+  unsigned* err;
+  int rows, V, k;
+  int64_t ld;
+  float temperature;
+};
+constexpr int kLogprobsMaxK = 32;
+int launch_logprobs(const LogprobsParams& p, int dtype, int num_sms, cudaStream_t s);
 
 }  // namespace lsp

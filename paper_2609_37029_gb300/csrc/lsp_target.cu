@@ -1,5 +1,6 @@
 // C ABI of the target side of a round: host-side validation of the paged-cache,
-// attention and verification calls (declarations and contracts: include/lsp.h).
+// attention, verification and log-probability calls (declarations and contracts:
+// include/lsp.h).
 #include <cuda_runtime.h>
 
 #include <cmath>
@@ -11,6 +12,10 @@ using namespace lsp;
 namespace {
 
 inline int esize(int dtype) { return dtype == LSP_DTYPE_BF16 ? 2 : 4; }
+inline bool is_float(int dtype) { return dtype == LSP_DTYPE_BF16 || dtype == LSP_DTYPE_F32; }
+// Bytes of an element of a cache's strides; of what its copies take a slot to be made of (0: 4 bits).
+inline int unit(const lsp_kv_cache* c) { return c->dtype == LSP_DTYPE_Q4 ? 1 : esize(c->dtype); }
+inline int slot_size(const lsp_kv_cache* c) { return c->dtype == LSP_DTYPE_Q4 ? 0 : esize(c->dtype); }
 inline cudaStream_t S(lsp_stream_t s) { return static_cast<cudaStream_t>(s); }
 inline bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 // Lists of 32-bit words (or none): a kernel that read one at another address would fault.
@@ -28,7 +33,8 @@ int num_sms(int* sms) {
 // Sizes, type and strides (no pointers).
 int check_shape(const lsp_kv_cache* c) {
   if (!c) return LSP_ERR_ARG;
-  if (c->dtype != LSP_DTYPE_BF16 && c->dtype != LSP_DTYPE_F32) return LSP_ERR_ARG;
+  const bool q4 = c->dtype == LSP_DTYPE_Q4;
+  if (!is_float(c->dtype) && !q4) return LSP_ERR_ARG;
   if (c->layers < 1 || c->pages < 1 || c->pages > (1 << 20) || c->nkv < 1 || c->nkv > 65535 || c->seqs < 1 ||
       c->max_pages < 1 || (int64_t)c->seqs * c->max_pages > (1 << 30))
     return LSP_ERR_SHAPE;
@@ -36,10 +42,10 @@ int check_shape(const lsp_kv_cache* c) {
   if ((int64_t)c->max_pages * c->page > (1 << 30)) return LSP_ERR_SHAPE;
   const int64_t stride[4] = {c->s_layer, c->s_page, c->s_head, c->s_slot};
   const int extent[4] = {c->layers, c->pages, c->nkv, c->page};
-  for (int i = 0; i < 4; ++i)
-    if (extent[i] > 1 && (stride[i] < c->d || stride[i] * esize(c->dtype) % 16 ||
-                          stride[i] * esize(c->dtype) >= ((int64_t)1 << 40)))
-      return LSP_ERR_SHAPE;
+  const int64_t es = unit(c), held = c->d * 9 / 16, least = q4 ? c->page * held : c->d;
+  if (q4 && c->s_slot != held) return LSP_ERR_SHAPE;
+  for (int i = 0; i < (q4 ? 3 : 4); ++i)
+    if (extent[i] > 1 && (stride[i] < least || stride[i] >= ((int64_t)1 << 40) / es || stride[i] * es % 16)) return LSP_ERR_SHAPE;
   return LSP_OK;
 }
 
@@ -69,13 +75,71 @@ int entries(const int32_t* a, const int32_t* b, int n, const uint32_t* dev_error
   return n > kPagesMaxSeqs ? LSP_ERR_SHAPE : LSP_OK;
 }
 
+// A call that moves rows of `dtype` between one layer of a cache and its sequences: LSP_OK with *out the layer's
+// view, or with total = 0 (nothing to do).
+int rows_call(const lsp_kv_cache* cache, int layer, const int32_t* seqs, const int32_t* start, int n, const void* k,
+              const void* v, int dtype, int64_t row_stride, int total, const uint32_t* dev_error, KvCache* out) {
+  const int rc = view(cache, out);
+  if (rc != LSP_OK) return rc;
+  if (layer < 0 || layer >= out->layers || n < 0 || total < 0) return LSP_ERR_ARG;
+  if (n == 0 || total == 0) return LSP_OK;
+  if (!seqs || !start || !words(seqs, start, dev_error)) return LSP_ERR_ARG;
+  const int es = esize(dtype);
+  if (!k || !v || !aligned(k, 16) || !aligned(v, 16)) return LSP_ERR_ARG;
+  if (total > (1 << 28) || (total > 1 && (row_stride < (int64_t)out->nkv * out->d || row_stride >= ((int64_t)1 << 40) / es ||
+                                          row_stride * es % 16)))
+    return LSP_ERR_SHAPE;
+  out->k += (int64_t)layer * out->s_layer * unit(cache);
+  out->v += (int64_t)layer * out->s_layer * unit(cache);
+  return LSP_OK;
+}
+
 // The sizes of an attention call that its plan depends on.
 int attn_shape(const lsp_kv_cache* c, int nq, int n, int total, PrefixAttnParams* p) {
   if (nq < 1 || n < 1 || total < 0) return LSP_ERR_ARG;
   if (nq % c->nkv || nq / c->nkv > kPrefixMaxRep || n > kPrefixMaxSeqs || (int64_t)total * nq > (1 << 30)) return LSP_ERR_SHAPE;
   p->nq = nq; p->nkv = c->nkv; p->rep = nq / c->nkv; p->d = c->d;
   p->n = n; p->total = total;
+  p->q4 = c->dtype == LSP_DTYPE_Q4;
   return LSP_OK;
+}
+
+// dtype: of the rows.
+size_t attn_workspace(const lsp_kv_cache* cache, int dtype, int nq, int n, int total) {
+  PrefixAttnParams p = {};
+  int sms = 0;
+  if (check_shape(cache) != LSP_OK || attn_shape(cache, nq, n, total, &p) != LSP_OK || num_sms(&sms) != LSP_OK) return 0;
+  return total == 0 ? 0 : prefix_attn_plan(&p, dtype, sms);
+}
+
+int attention(const lsp_kv_cache* cache, int layer, const void* q, int dtype, int64_t q_stride, int nq, const int32_t* seqs,
+              const int32_t* start, int n, int total, int shared_len, float scale, void* out, float* lse, void* workspace,
+              size_t workspace_bytes, uint32_t* dev_error, lsp_stream_t stream) {
+  KvCache c;
+  PrefixAttnParams p = {};
+  int rc = view(cache, &c), sms = 0;
+  if (rc == LSP_OK) rc = attn_shape(cache, nq, n, total, &p);
+  if (rc != LSP_OK) return rc;
+  if (layer < 0 || layer >= c.layers || shared_len < 0 || !(scale > 0.f) || !std::isfinite(scale) || !seqs || !start ||
+      !words(seqs, start, lse, dev_error))
+    return LSP_ERR_ARG;
+  if (total == 0) return LSP_OK;
+  const int es = esize(dtype);
+  if (!q || !out || !aligned(q, 16) || !aligned(out, 16) || !workspace || !aligned(workspace, 256)) return LSP_ERR_ARG;
+  if (total > 1 && (q_stride < (int64_t)nq * c.d || q_stride * es % 16 || q_stride * es >= ((int64_t)1 << 40)))
+    return LSP_ERR_SHAPE;
+  if ((rc = num_sms(&sms)) != LSP_OK) return rc;
+  p.k = c.k + (int64_t)layer * c.s_layer * unit(cache);
+  p.v = c.v + (int64_t)layer * c.s_layer * unit(cache);
+  p.q = q; p.out = out; p.lse = lse;
+  p.table = c.table; p.len = c.len; p.seqs = seqs; p.start = start;
+  p.q_stride = total > 1 ? q_stride : (int64_t)nq * c.d;
+  p.s_page = c.s_page; p.s_head = c.s_head; p.s_slot = c.s_slot;
+  p.page = c.page; p.pages = c.pages; p.max_pages = c.max_pages; p.n_seqs = c.seqs;
+  p.shared_len = shared_len < c.max_pages * c.page ? shared_len : c.max_pages * c.page;
+  p.scale = scale; p.err = dev_error;
+  if (workspace_bytes < prefix_attn_plan(&p, dtype, sms)) return LSP_ERR_ARG;
+  return launch_prefix_attention(p, dtype, workspace, S(stream));
 }
 
 }  // namespace
@@ -112,7 +176,7 @@ int lsp_pages_reserve(const lsp_kv_cache* cache, const int32_t* seqs, const int3
   if (rc != LSP_OK || n == 0) return rc;
   if (!workspace || !aligned(workspace, 16) || workspace_bytes < pages_ws_bytes(c.pages)) return LSP_ERR_ARG;
   if ((rc = num_sms(&sms)) != LSP_OK) return rc;
-  return launch_pages_reserve(c, seqs, add, n, workspace, esize(cache->dtype), sms, dev_error, S(stream));
+  return launch_pages_reserve(c, seqs, add, n, workspace, slot_size(cache), sms, dev_error, S(stream));
 }
 
 int lsp_pages_compact(const lsp_kv_cache* cache, int32_t* live, void* workspace, size_t workspace_bytes,
@@ -122,62 +186,66 @@ int lsp_pages_compact(const lsp_kv_cache* cache, int32_t* live, void* workspace,
   if (rc != LSP_OK) return rc;
   if (!workspace || !aligned(workspace, 16) || workspace_bytes < pages_ws_bytes(c.pages) || !words(live)) return LSP_ERR_ARG;
   if ((rc = num_sms(&sms)) != LSP_OK) return rc;
-  return launch_pages_compact(c, live, workspace, esize(cache->dtype), sms, S(stream));
+  return launch_pages_compact(c, live, workspace, slot_size(cache), sms, S(stream));
 }
 
 int lsp_pages_write(const lsp_kv_cache* cache, int layer, const int32_t* seqs, const int32_t* start, int n,
                     const void* k_new, const void* v_new, int64_t row_stride, int total, uint32_t* dev_error,
                     lsp_stream_t stream) {
   KvCache c;
-  const int rc = view(cache, &c);
-  if (rc != LSP_OK) return rc;
-  if (layer < 0 || layer >= c.layers || n < 0 || total < 0) return LSP_ERR_ARG;
-  if (n == 0 || total == 0) return LSP_OK;
-  if (!seqs || !start || !words(seqs, start, dev_error)) return LSP_ERR_ARG;
+  if (!cache || cache->dtype == LSP_DTYPE_Q4) return LSP_ERR_ARG;
+  const int rc = rows_call(cache, layer, seqs, start, n, k_new, v_new, cache->dtype, row_stride, total, dev_error, &c);
+  if (rc != LSP_OK || n == 0 || total == 0) return rc;
   const int es = esize(cache->dtype);
-  if (!k_new || !v_new || !aligned(k_new, 16) || !aligned(v_new, 16)) return LSP_ERR_ARG;
-  if (total > (1 << 28) || (total > 1 && (row_stride < (int64_t)c.nkv * c.d || row_stride * es % 16))) return LSP_ERR_SHAPE;
-  c.k += (int64_t)layer * c.s_layer * es;
-  c.v += (int64_t)layer * c.s_layer * es;
   return launch_pages_write(c, seqs, start, n, k_new, v_new, row_stride * es, total, es, dev_error, S(stream));
 }
 
+int lsp_pages_write_q4(const lsp_kv_cache* cache, int layer, const int32_t* seqs, const int32_t* start, int n,
+                       const void* k_new, const void* v_new, int dtype, int64_t row_stride, int total, uint32_t* dev_error,
+                       lsp_stream_t stream) {
+  KvCache c;
+  if (!cache || cache->dtype != LSP_DTYPE_Q4 || !is_float(dtype)) return LSP_ERR_ARG;
+  const int rc = rows_call(cache, layer, seqs, start, n, k_new, v_new, dtype, row_stride, total, dev_error, &c);
+  if (rc != LSP_OK || n == 0 || total == 0) return rc;
+  const int es = esize(dtype);
+  return launch_pages_write_q4(c, seqs, start, n, k_new, v_new, row_stride * es, total, es, dev_error, S(stream));
+}
+
+int lsp_pages_read(const lsp_kv_cache* cache, int layer, const int32_t* seqs, const int32_t* start, int n, void* k_out,
+                   void* v_out, int dtype, int64_t row_stride, int total, uint32_t* dev_error, lsp_stream_t stream) {
+  KvCache c;
+  if (!cache || !is_float(dtype) || (cache->dtype != LSP_DTYPE_Q4 && cache->dtype != dtype)) return LSP_ERR_ARG;
+  const int rc = rows_call(cache, layer, seqs, start, n, k_out, v_out, dtype, row_stride, total, dev_error, &c);
+  if (rc != LSP_OK || n == 0 || total == 0) return rc;
+  const int es = esize(dtype);
+  return launch_pages_read(c, seqs, start, n, k_out, v_out, row_stride * es, total, es, cache->dtype == LSP_DTYPE_Q4, dev_error,
+                           S(stream));
+}
+
 size_t lsp_prefix_attention_workspace_bytes(const lsp_kv_cache* cache, int nq, int n, int total) {
-  PrefixAttnParams p = {};
-  int sms = 0;
-  if (check_shape(cache) != LSP_OK || attn_shape(cache, nq, n, total, &p) != LSP_OK || num_sms(&sms) != LSP_OK) return 0;
-  return total == 0 ? 0 : prefix_attn_plan(&p, cache->dtype, sms);
+  return cache && cache->dtype != LSP_DTYPE_Q4 ? attn_workspace(cache, cache->dtype, nq, n, total) : 0;
+}
+
+size_t lsp_prefix_attention_q4_workspace_bytes(const lsp_kv_cache* cache, int dtype, int nq, int n, int total) {
+  return cache && cache->dtype == LSP_DTYPE_Q4 && is_float(dtype) ? attn_workspace(cache, dtype, nq, n, total) : 0;
 }
 
 int lsp_prefix_attention(const lsp_kv_cache* cache, int layer, const void* q, int64_t q_stride, int nq,
                          const int32_t* seqs, const int32_t* start, int n, int total, int shared_len, float scale,
                          void* out, float* lse, void* workspace, size_t workspace_bytes, uint32_t* dev_error,
                          lsp_stream_t stream) {
-  KvCache c;
-  PrefixAttnParams p = {};
-  int rc = view(cache, &c), sms = 0;
-  if (rc == LSP_OK) rc = attn_shape(cache, nq, n, total, &p);
-  if (rc != LSP_OK) return rc;
-  if (layer < 0 || layer >= c.layers || shared_len < 0 || !(scale > 0.f) || !std::isfinite(scale) || !seqs || !start ||
-      !words(seqs, start, lse, dev_error))
-    return LSP_ERR_ARG;
-  if (total == 0) return LSP_OK;
-  const int es = esize(cache->dtype);
-  if (!q || !out || !aligned(q, 16) || !aligned(out, 16) || !workspace || !aligned(workspace, 256)) return LSP_ERR_ARG;
-  if (total > 1 && (q_stride < (int64_t)nq * c.d || q_stride * es % 16 || q_stride * es >= ((int64_t)1 << 40)))
-    return LSP_ERR_SHAPE;
-  if ((rc = num_sms(&sms)) != LSP_OK) return rc;
-  p.k = c.k + (int64_t)layer * c.s_layer * es;
-  p.v = c.v + (int64_t)layer * c.s_layer * es;
-  p.q = q; p.out = out; p.lse = lse;
-  p.table = c.table; p.len = c.len; p.seqs = seqs; p.start = start;
-  p.q_stride = total > 1 ? q_stride : (int64_t)nq * c.d;
-  p.s_page = c.s_page; p.s_head = c.s_head; p.s_slot = c.s_slot;
-  p.page = c.page; p.pages = c.pages; p.max_pages = c.max_pages; p.n_seqs = c.seqs;
-  p.shared_len = shared_len < c.max_pages * c.page ? shared_len : c.max_pages * c.page;
-  p.scale = scale; p.err = dev_error;
-  if (workspace_bytes < prefix_attn_plan(&p, cache->dtype, sms)) return LSP_ERR_ARG;
-  return launch_prefix_attention(p, cache->dtype, workspace, S(stream));
+  if (!cache || cache->dtype == LSP_DTYPE_Q4) return LSP_ERR_ARG;
+  return attention(cache, layer, q, cache->dtype, q_stride, nq, seqs, start, n, total, shared_len, scale, out, lse, workspace,
+                   workspace_bytes, dev_error, stream);
+}
+
+int lsp_prefix_attention_q4(const lsp_kv_cache* cache, int layer, const void* q, int dtype, int64_t q_stride, int nq,
+                            const int32_t* seqs, const int32_t* start, int n, int total, int shared_len, float scale,
+                            void* out, float* lse, void* workspace, size_t workspace_bytes, uint32_t* dev_error,
+                            lsp_stream_t stream) {
+  if (!cache || cache->dtype != LSP_DTYPE_Q4 || !is_float(dtype)) return LSP_ERR_ARG;
+  return attention(cache, layer, q, dtype, q_stride, nq, seqs, start, n, total, shared_len, scale, out, lse, workspace,
+                   workspace_bytes, dev_error, stream);
 }
 
 int lsp_verify_probs(const void* target_probs, const void* draft_probs, int dtype, const int32_t* draft_tokens,
@@ -199,6 +267,23 @@ int lsp_verify_probs(const void* target_probs, const void* draft_probs, int dtyp
   int sms = 0;
   const int rc = num_sms(&sms);
   return rc == LSP_OK ? launch_verify_probs(p, dtype, sms, S(stream)) : rc;
+}
+
+int lsp_logprobs(const void* logits, int dtype, const int32_t* tokens, int rows, int V, int64_t ld, float temperature, int k,
+                 float* logprob, float* entropy, int32_t* top, float* top_logprob, uint32_t* dev_error, lsp_stream_t stream) {
+  if (!is_float(dtype) || rows < 0 || k < 0 || !(temperature > 0.f) || !std::isfinite(temperature)) return LSP_ERR_ARG;
+  if (V < 1 || V > (1 << 30) || ld < V || ld >= ((int64_t)1 << 40) || k > kLogprobsMaxK || k > V) return LSP_ERR_SHAPE;
+  if (rows == 0) return LSP_OK;
+  if (!logits || !tokens || !logprob || !aligned(logits, esize(dtype)) ||
+      !words(tokens, logprob, entropy, top, top_logprob, dev_error))
+    return LSP_ERR_ARG;
+  LogprobsParams p;
+  p.z = logits; p.tokens = tokens; p.logprob = logprob; p.entropy = entropy; p.err = dev_error;
+  p.top = k > 0 ? top : nullptr; p.top_logprob = k > 0 ? top_logprob : nullptr;
+  p.rows = rows; p.V = V; p.k = p.top || p.top_logprob ? k : 0; p.ld = ld; p.temperature = temperature;
+  int sms = 0;
+  const int rc = num_sms(&sms);
+  return rc == LSP_OK ? launch_logprobs(p, dtype, sms, S(stream)) : rc;
 }
 
 }  // extern "C"

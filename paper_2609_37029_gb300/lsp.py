@@ -22,7 +22,7 @@ LSP_ERR_TIMEOUT, LSP_ERR_STATE, LSP_ERR_NOMEM, LSP_ERR_UNSUPPORTED = -4, -5, -6,
 LSP_DEV_TIMEOUT, LSP_DEV_BAD_TOKEN, LSP_DEV_BAD_DELTA = 1, 2, 4
 LSP_DEV_BAD_SEQ, LSP_DEV_NO_PAGE = 8, 16
 LSP_NO_BOUNDARY = 1
-LSP_DTYPE_BF16, LSP_DTYPE_F32 = 0, 1
+LSP_DTYPE_BF16, LSP_DTYPE_F32, LSP_DTYPE_Q4 = 0, 1, 2
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2609_37029_gb300.build`"
@@ -126,6 +126,17 @@ _f = {
     "lsp_prefix_attention": _sig("lsp_prefix_attention", c_int, POINTER(lsp_kv_cache), c_int, c_void_p,
                                  c_int64, c_int, c_void_p, c_void_p, c_int, c_int, c_int, c_float,
                                  c_void_p, c_void_p, c_void_p, c_size_t, c_void_p, c_void_p),
+    "lsp_pages_write_q4": _sig("lsp_pages_write_q4", c_int, POINTER(lsp_kv_cache), c_int, c_void_p, c_void_p,
+                               c_int, c_void_p, c_void_p, c_int, c_int64, c_int, c_void_p, c_void_p),
+    "lsp_pages_read": _sig("lsp_pages_read", c_int, POINTER(lsp_kv_cache), c_int, c_void_p, c_void_p,
+                           c_int, c_void_p, c_void_p, c_int, c_int64, c_int, c_void_p, c_void_p),
+    "lsp_prefix_attention_q4_workspace_bytes": _sig("lsp_prefix_attention_q4_workspace_bytes", c_size_t,
+                                                    POINTER(lsp_kv_cache), c_int, c_int, c_int, c_int),
+    "lsp_prefix_attention_q4": _sig("lsp_prefix_attention_q4", c_int, POINTER(lsp_kv_cache), c_int, c_void_p,
+                                    c_int, c_int64, c_int, c_void_p, c_void_p, c_int, c_int, c_int, c_float,
+                                    c_void_p, c_void_p, c_void_p, c_size_t, c_void_p, c_void_p),
+    "lsp_logprobs": _sig("lsp_logprobs", c_int, c_void_p, c_int, c_void_p, c_int, c_int, c_int64, c_float,
+                         c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p),
     "lsp_verify_probs": _sig("lsp_verify_probs", c_int, c_void_p, c_void_p, c_int, c_void_p, c_void_p,
                              c_void_p, c_void_p, c_int, c_int, c_int, c_int64, c_int64, c_void_p,
                              c_void_p, c_void_p, c_void_p, c_void_p),
@@ -137,6 +148,9 @@ _pages_workspace_bytes, _pages_fork, _pages_reserve = (
 _pages_write, _pages_trim, _pages_compact = (_f[n] for n in ("lsp_pages_write", "lsp_pages_trim", "lsp_pages_compact"))
 _prefix_attention_workspace_bytes, _prefix_attention, _verify_probs = (
     _f[n] for n in ("lsp_prefix_attention_workspace_bytes", "lsp_prefix_attention", "lsp_verify_probs"))
+_pages_write_q4, _pages_read, _prefix_attention_q4_workspace_bytes, _prefix_attention_q4, _logprobs = (
+    _f[n] for n in ("lsp_pages_write_q4", "lsp_pages_read", "lsp_prefix_attention_q4_workspace_bytes",
+                    "lsp_prefix_attention_q4", "lsp_logprobs"))
 
 
 def _ptr(x):
@@ -198,6 +212,8 @@ def make_weights(w: dict) -> lsp_weights:
 def make_kv_cache(k, v, table, lens, refs) -> lsp_kv_cache:
     """lsp_kv_cache of device pointers: k, v [layers][pages][nkv][page][d] in any order of the first
     four axes (their strides are taken), int32 table [seqs][max_pages], lens [seqs], refs [pages].
+    A cache held in 4 bits: uint8 k, v [layers][pages][nkv][page][9 d / 16], the last two axes dense (a
+    head's block of codes and scales, see LSP_DTYPE_Q4 in the header) and the others in any order.
     The struct holds addresses only: the caller keeps the tensors."""
     import torch
     apart = any(a != b for a, b, n in zip(k.stride(), v.stride(), k.shape) if n > 1)
@@ -212,7 +228,12 @@ def make_kv_cache(k, v, table, lens, refs) -> lsp_kv_cache:
     c.k, c.v, c.table, c.len, c.refs = (t.data_ptr() for t in (k, v, table, lens, refs))
     c.s_layer, c.s_page, c.s_head, c.s_slot = k.stride()[:4]
     c.layers, c.pages, c.nkv, c.page, c.d = k.shape
-    c.dtype = _dtype_code(k.dtype)
+    if k.dtype == torch.uint8:
+        if k.stride(3) != k.shape[4] or k.shape[4] % 9:
+            raise ValueError("k and v of a cache in 4 bits: [page][9 d / 16] dense")
+        c.d, c.dtype = k.shape[4] // 9 * 16, LSP_DTYPE_Q4
+    else:
+        c.dtype = _dtype_code(k.dtype)
     c.seqs, c.max_pages = table.shape
     return c
 
@@ -426,20 +447,48 @@ def lsp_pages_reserve(cache: lsp_kv_cache, seqs, add, workspace, dev_error=None,
                           _stream(stream)), "lsp_pages_reserve")
 
 
+def _rows(cache, k, v, seqs, start):
+    """Keys and values of rows that a call moves into or out of a cache: (type, elements between rows, rows, entries)."""
+    shape, stride, other, d, n = k.shape, k.stride(), v.stride(), cache.d, seqs.numel()
+    # (the stride along an axis of one is never used, and may be anything)
+    if (len(shape) != 3 or shape != v.shape or shape[1] != cache.nkv or shape[2] != d or stride[2] != 1 or other[2] != 1
+            or shape[1] > 1 and (stride[1] != d or other[1] != d) or shape[0] > 1 and stride[0] != other[0]):
+        raise ValueError("keys and values: [total][nkv][d] of the same strides, dense within a row")
+    code = _dtype_code(k.dtype)
+    if v.dtype != k.dtype:
+        raise ValueError("keys and values: one type, the cache's type")
+    if not _dense(seqs, _int32, n) or not _dense(start, _int32, n + 1):
+        raise ValueError("seqs [n] and start [n + 1]: contiguous int32")
+    return code, stride[0], shape[0], n
+
+
+def lsp_pages_write_q4(cache: lsp_kv_cache, layer, seqs, start, k_new, v_new, dev_error=None, stream=None) -> None:
+    """lsp_pages_write into a cache held in 4 bits: bfloat16 or float32 k_new, v_new [total][nkv][d]."""
+    code, step, total, n = _rows(cache, k_new, v_new, seqs, start)
+    if cache.dtype != LSP_DTYPE_Q4:
+        raise ValueError("a cache held in 4 bits")
+    _check(_pages_write_q4(cache, layer, seqs.data_ptr(), start.data_ptr(), n, k_new.data_ptr(), v_new.data_ptr(), code,
+                           step, total, _word(dev_error), _stream(stream)), "lsp_pages_write_q4")
+
+
+def lsp_pages_read(cache: lsp_kv_cache, layer, seqs, start, k_out, v_out, dev_error=None, stream=None) -> None:
+    """k_out, v_out: [total][nkv][d] of the cache's type (bfloat16 or float32 for a cache held in 4 bits), dense
+    within a row, the same stride between rows; rows [start[i], start[i + 1]) get the last tokens of sequence seqs[i]."""
+    code, step, total, n = _rows(cache, k_out, v_out, seqs, start)
+    if cache.dtype != code and cache.dtype != LSP_DTYPE_Q4:
+        raise ValueError("k_out and v_out: the cache's type")
+    _check(_pages_read(cache, layer, seqs.data_ptr(), start.data_ptr(), n, k_out.data_ptr(), v_out.data_ptr(), code, step,
+                       total, _word(dev_error), _stream(stream)), "lsp_pages_read")
+
+
 def lsp_pages_write(cache: lsp_kv_cache, layer, seqs, start, k_new, v_new, dev_error=None, stream=None) -> None:
     """k_new, v_new: [total][nkv][d] of the cache's type, dense within a row, the same stride between rows; seqs
     [n], start [n + 1] int32."""
-    shape, stride, other, d, n = k_new.shape, k_new.stride(), v_new.stride(), cache.d, seqs.numel()
-    # (the stride along an axis of one is never used, and may be anything)
-    if (shape != v_new.shape or shape[1] != cache.nkv or shape[2] != d or stride[2] != 1 or other[2] != 1
-            or shape[1] > 1 and (stride[1] != d or other[1] != d) or shape[0] > 1 and stride[0] != other[0]):
-        raise ValueError("k_new and v_new: [total][nkv][d] of the same strides, dense within a row")
-    if _dtype_code(k_new.dtype) != cache.dtype or v_new.dtype != k_new.dtype:
+    code, step, total, n = _rows(cache, k_new, v_new, seqs, start)
+    if cache.dtype != code:
         raise ValueError("k_new and v_new: the cache's type")
-    if not _dense(seqs, _int32, n) or not _dense(start, _int32, n + 1):
-        raise ValueError("seqs [n] and start [n + 1]: contiguous int32")
     _check(_pages_write(cache, layer, seqs.data_ptr(), start.data_ptr(), n, k_new.data_ptr(), v_new.data_ptr(),
-                        stride[0], shape[0], _word(dev_error), _stream(stream)), "lsp_pages_write")
+                        step, total, _word(dev_error), _stream(stream)), "lsp_pages_write")
 
 
 def lsp_pages_trim(cache: lsp_kv_cache, seqs, new_len, dev_error=None, stream=None) -> None:
@@ -461,23 +510,48 @@ def lsp_prefix_attention_workspace_bytes(cache: lsp_kv_cache, nq: int, n: int, t
     return _prefix_attention_workspace_bytes(cache, nq, n, total)
 
 
-def lsp_prefix_attention(cache: lsp_kv_cache, layer, q, seqs, start, out, lse=None, *, shared_len, scale,
-                         workspace, dev_error=None, stream=None) -> None:
-    """q: [total][nq][d] of the cache's type, dense within a row (a slice of a fused q/k/v row will do); out:
-    the same, dense; seqs [n], start [n + 1] int32; lse: float32 [total][nq] or None."""
+def lsp_prefix_attention_q4_workspace_bytes(cache: lsp_kv_cache, dtype, nq: int, n: int, total: int) -> int:
+    """dtype: of the rows, torch.bfloat16 or torch.float32."""
+    return _prefix_attention_q4_workspace_bytes(cache, _dtype_code(dtype), nq, n, total)
+
+
+def _attention_rows(cache, q, seqs, start, out, lse):
+    """Arguments that both attention calls take: (type, elements between rows, rows, heads, entries)."""
     shape, stride, d, n = q.shape, q.stride(), cache.d, seqs.numel()
-    if (stride[1] != d and shape[1] > 1 or stride[2] != 1 or shape[2] != d or out.shape != shape
+    if (len(shape) != 3 or stride[1] != d and shape[1] > 1 or stride[2] != 1 or shape[2] != d or out.shape != shape
             or not out.is_contiguous()):
         raise ValueError("q: [total][nq][d], dense within a row; out: the same shape, contiguous")
-    if _dtype_code(q.dtype) != cache.dtype or out.dtype != q.dtype:
-        raise ValueError("q and out: the cache's type")
+    code = _dtype_code(q.dtype)
+    if out.dtype != q.dtype:
+        raise ValueError("q and out: one type, the cache's type")
     if not _dense(seqs, _int32, n) or not _dense(start, _int32, n + 1):
         raise ValueError("seqs [n] and start [n + 1]: contiguous int32")
     if lse is not None and not _dense(lse, _float32, shape[0] * shape[1]):
         raise ValueError("lse: contiguous float32 [total][nq]")
-    _check(_prefix_attention(cache, layer, q.data_ptr(), stride[0], shape[1], seqs.data_ptr(), start.data_ptr(),
-                             n, shape[0], shared_len, scale, out.data_ptr(), _opt(lse), *_room(workspace),
+    return code, stride[0], shape[0], shape[1], n
+
+
+def lsp_prefix_attention(cache: lsp_kv_cache, layer, q, seqs, start, out, lse=None, *, shared_len, scale,
+                         workspace, dev_error=None, stream=None) -> None:
+    """q: [total][nq][d] of the cache's type, dense within a row (a slice of a fused q/k/v row will do); out:
+    the same, dense; seqs [n], start [n + 1] int32; lse: float32 [total][nq] or None."""
+    code, step, total, nq, n = _attention_rows(cache, q, seqs, start, out, lse)
+    if code != cache.dtype:
+        raise ValueError("q and out: the cache's type")
+    _check(_prefix_attention(cache, layer, q.data_ptr(), step, nq, seqs.data_ptr(), start.data_ptr(), n, total,
+                             shared_len, scale, out.data_ptr(), _opt(lse), *_room(workspace),
                              _word(dev_error), _stream(stream)), "lsp_prefix_attention")
+
+
+def lsp_prefix_attention_q4(cache: lsp_kv_cache, layer, q, seqs, start, out, lse=None, *, shared_len, scale,
+                            workspace, dev_error=None, stream=None) -> None:
+    """lsp_prefix_attention over a cache held in 4 bits: q and out bfloat16 or float32."""
+    code, step, total, nq, n = _attention_rows(cache, q, seqs, start, out, lse)
+    if cache.dtype != LSP_DTYPE_Q4:
+        raise ValueError("a cache held in 4 bits")
+    _check(_prefix_attention_q4(cache, layer, q.data_ptr(), code, step, nq, seqs.data_ptr(), start.data_ptr(), n, total,
+                                shared_len, scale, out.data_ptr(), _opt(lse), *_room(workspace),
+                                _word(dev_error), _stream(stream)), "lsp_prefix_attention_q4")
 
 
 def _row_stride(t, C, rows, V):
@@ -512,6 +586,32 @@ def lsp_verify_probs(target_probs, draft_probs, draft_tokens, u, e, accepted_len
                          u.data_ptr(), e.data_ptr(), C, B, V, ld_t, ld_q, accepted_len.data_ptr(),
                          next_token.data_ptr(), _opt(out_tokens), _word(dev_error), _stream(stream)),
            "lsp_verify_probs")
+
+
+def lsp_logprobs(logits, tokens, logprob, entropy=None, top=None, top_logprob=None, *, temperature=1.0, dev_error=None,
+                 stream=None) -> None:
+    """logits [rows][V] bfloat16 or float32, dense within a row (rows may overlap nothing and lie anywhere apart).
+    Contiguous: int32 tokens [rows] (-1: none) and top [rows][k], float32 logprob and entropy [rows], top_logprob
+    [rows][k]; all but logprob may be None."""
+    if logits.dim() != 2:
+        raise ValueError("logits: [rows][V]")
+    rows, V = logits.shape
+    stride, k = logits.stride(), 0
+    code = _dtype_code(logits.dtype)
+    if V > 1 and stride[1] != 1 or rows > 1 and stride[0] < V:
+        raise ValueError("logits: [rows][V], dense within a row")
+    if not _dense(tokens, _int32, rows) or not _dense(logprob, _float32, rows) or entropy is not None and not _dense(entropy, _float32, rows):
+        raise ValueError("tokens [rows]: contiguous int32; logprob and entropy [rows]: contiguous float32")
+    for t, dtype in ((top, _int32), (top_logprob, _float32)):
+        if t is not None:
+            if t.dim() != 2 or not _dense(t, dtype, rows * t.shape[1]):
+                raise ValueError("top: contiguous int32 [rows][k]; top_logprob: contiguous float32 [rows][k]")
+            k = t.shape[1]
+    if top is not None and top_logprob is not None and top.shape != top_logprob.shape:
+        raise ValueError("top and top_logprob: one shape")
+    _check(_logprobs(logits.data_ptr(), code, tokens.data_ptr(), rows, V, stride[0] if rows > 1 else V, temperature, k,
+                     logprob.data_ptr(), _opt(entropy), _opt(top), _opt(top_logprob), _word(dev_error), _stream(stream)),
+           "lsp_logprobs")
 
 
 EXPORTED = sorted(_f)
