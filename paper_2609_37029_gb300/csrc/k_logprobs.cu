@@ -7,11 +7,11 @@
 // One pass: every thread keeps (m, S, A) of its elements and moves them to a higher
 // m as 2^t times (S, A + S t).
 //
-// The k largest, from the same pass: a thread has a stripe of the row (every 512th
+// The k largest, from the same pass: a thread has a stripe of the row (every 256th
 // piece of 16 bytes), whose largest logit and its first place it knows at the end.
 // Each of the k largest elements is in one of the k stripes whose first are the
 // largest -- an element in any other stripe has k elements before it -- so those
-// stripes alone are read again (k of 512, mostly from L2), and what comes at or
+// stripes alone are read again (k of 256, mostly from L2), and what comes at or
 // before the k-th stripe's first goes to a list, some more than k elements as a
 // rule, which is ranked by counting.  Places decide between equal logits all the
 // way.  Should the list overflow (a row made for it: thousands of large elements in
@@ -33,7 +33,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kAhead = 4;                        // 16-byte pieces a thread has in flight
 constexpr int kList = 1024;                      // candidates of a CTA
@@ -90,6 +90,18 @@ struct Vec {
       }
     }
   }
+  // the largest and the smallest, NaN aside
+  __device__ static __forceinline__ void range(const uint4& v, const float* x, float* top, float* low) {
+    if constexpr (sizeof(T) == 2) {
+      const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
+      const __nv_bfloat162 a = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3])), b = __hmin2(__hmin2(p[0], p[1]), __hmin2(p[2], p[3]));
+      *top = fmaxf(__low2float(a), __high2float(a));
+      *low = fminf(__low2float(b), __high2float(b));
+    } else {
+      *top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+      *low = fminf(fminf(x[0], x[1]), fminf(x[2], x[3]));
+    }
+  }
 };
 
 // A CTA's part of a row, in places: the row's elements before its first 16-byte
@@ -110,29 +122,91 @@ struct Part {
   int tail_index;
 };
 
+struct Scale {
+  float c, inv;         // log2(e) / T, its reciprocal
+  float large;          // logits up to here leave every t finite
+};
+
 // Of a thread's elements: the largest logit and its place, and the sums relative to `m`.
 struct Stats {
-  float m, s, a, best;
+  float m, best;
+  float2 s, a;          // of every other element, to be added
   uint32_t place;
 };
 
+// (a0, a1) + b, a b, a + b and a b + c: two fp32 operations an instruction
+__device__ __forceinline__ float2 add2s(float a0, float a1, float b) {
+  float2 d;
+  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %4};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a0), "f"(a1), "f"(b));
+  return d;
+}
+__device__ __forceinline__ float2 mul2s(float2 a, float b) {
+  float2 d;
+  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %4};\n mul.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n .reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mov.b64 z, {%6, %7};\n"
+      " fma.rn.f32x2 x, x, y, z;\n mov.b64 {%0, %1}, x;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+
+// Elements x, of which top and low are the largest and the smallest (NaN aside).  As
+// long as logits stay within +-large, every t is finite, and e t = 0 where e = 0.
+// What is below (-inf, a banned token) is raised to where e is 0 already; a row of
+// larger numbers takes its steps one by one with t limited.
 template <int N>
-__device__ __forceinline__ void add_elems(Stats& st, const float* x, float top, float c) {
+__device__ __forceinline__ void add_elems(Stats& st, float* x, float top, float low, const Scale& k) {
   if (top > st.m) {
-    const float t = max_nan((st.m - top) * c, kLeast), r = ex2a(t);
-    st.a = r * (st.a + st.s * t);
-    st.s *= r;
+    const float t = max_nan((st.m - top) * k.c, kLeast), r = ex2a(t);
+    st.a = make_float2(r * (st.a.x + st.s.x * t), r * (st.a.y + st.s.y * t));
+    st.s = make_float2(r * st.s.x, r * st.s.y);
     st.m = top;
   }
-  float s[2] = {0.f, 0.f}, a[2] = {0.f, 0.f};
+  if (!(low > -k.large) || fabsf(st.m) > k.large) {
+    if (fabsf(st.m) > k.large) {
+#pragma unroll 1
+      for (int i = 0; i < N; ++i) {
+        float y = x[0];                          // (no indexed registers)
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float t = max_nan((x[i] - st.m) * c, kLeast), e = ex2a(t);
-    s[i & 1] += e;
-    a[i & 1] = fmaf(e, t, a[i & 1]);
+        for (int e = 1; e < N; ++e) y = e == i ? x[e] : y;
+        const float t = max_nan((y - st.m) * k.c, kLeast), e = ex2a(t);
+        st.s.x += e;
+        st.a.x = fmaf(e, t, st.a.x);
+      }
+      return;
+    }
+    // (200 / c below m; where m's last place is more than that, some of those below)
+    const float least = st.m - fmaxf(200.0f * k.inv, fabsf(st.m) * 0x1p-20f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = max_nan(x[i], least);
   }
-  st.s += s[0] + s[1];
-  st.a += a[0] + a[1];
+#pragma unroll
+  for (int i = 0; i < N; i += 2) {
+    const float2 t = mul2s(add2s(x[i], x[i + 1], -st.m), k.c), e = make_float2(ex2a(t.x), ex2a(t.y));
+    st.s = add2(st.s, e);
+    st.a = fma2(e, t, st.a);
+  }
+}
+
+__device__ __forceinline__ void add_one(Stats& st, float x, uint32_t place, const Scale& k) {
+  if (x > st.best) st.best = x, st.place = place;
+  float pair[2] = {x, -INFINITY};
+  add_elems<2>(st, pair, x, -INFINITY, k);
 }
 
 __device__ __forceinline__ unsigned long long block_max(unsigned long long v, Smem& sm) {
@@ -243,7 +317,7 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, i
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const LogprobsParams p, int cluster) {
+__global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobsParams p, int cluster) {
   constexpr int VE = Vec<T>::kElems;
   __shared__ Smem sm;
   griddep_wait();
@@ -266,6 +340,7 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const LogprobsPar
     return;
   }
   const float c = kLog2e / p.temperature;
+  const Scale scale = {c, p.temperature * 0.69314718055994531f, 1e38f / fmaxf(c, 1.0f)};
   Part<T> part;
   part.z = static_cast<const T*>(p.z) + (int64_t)row * p.ld;
   const int off = (int)((16 - (reinterpret_cast<uintptr_t>(part.z) & 15)) & 15) / (int)sizeof(T);
@@ -277,13 +352,11 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const LogprobsPar
   part.tail_index = part.body + pieces * VE;
   part.tail = rank == cluster - 1 ? p.V - part.tail_index : 0;
   part.tail_at = ((part.pieces + kThreads - 1) / kThreads + 1) * kThreads;
-  Stats st = {kLowest, 0.f, 0.f, -INFINITY, 0u};
+  Stats st = {kLowest, -INFINITY, {0.f, 0.f}, {0.f, 0.f}, 0u};
   // (a thread's first place, for stripes of -inf alone)
   st.place = tid < part.head ? tid : tid < part.pieces ? kThreads + tid : part.tail_at + tid;
   if (tid < part.head) {
-    const float x = to_f(part.z[tid]);
-    if (x > st.best) st.best = x, st.place = tid;
-    add_elems<1>(st, &x, x, c);
+    add_one(st, to_f(part.z[tid]), tid, scale);
   }
   for (int i0 = tid; i0 < part.pieces; i0 += kThreads * kAhead) {
     uint4 v[kAhead];
@@ -293,19 +366,15 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const LogprobsPar
 #pragma unroll
     for (int q = 0; q < kAhead; ++q) {
       if (i0 + q * kThreads >= part.pieces) break;
-      float x[VE];
+      float x[VE], top, low;
       Vec<T>::unpack(v[q], x);
-      float top = x[0];
-#pragma unroll
-      for (int e = 1; e < VE; ++e) top = fmaxf(top, x[e]);
+      Vec<T>::range(v[q], x, &top, &low);
       if (top > st.best) st.best = top, st.place = kThreads + i0 + q * kThreads;
-      add_elems<VE>(st, x, top, c);
+      add_elems<VE>(st, x, top, low, scale);
     }
   }
   if (tid < part.tail) {
-    const float x = to_f(part.z[part.tail_index + tid]);
-    if (x > st.best) st.best = x, st.place = part.tail_at + tid;
-    add_elems<1>(st, &x, x, c);
+    add_one(st, to_f(part.z[part.tail_index + tid]), part.tail_at + tid, scale);
   }
   // the CTA's sums
   const float wm = warp_max(st.m);
@@ -316,7 +385,7 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const LogprobsPar
   for (int o = kWarps / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   {
     const float t = max_nan((st.m - m) * c, kLeast), r = ex2a(t);
-    const float s = warp_sum(r * st.s), a = warp_sum(r * (st.a + st.s * t));
+    const float s = warp_sum(r * (st.s.x + st.s.y)), a = warp_sum(r * (st.a.x + st.a.y + (st.s.x + st.s.y) * t));
     if (lane == 0) sm.red2[warp] = make_float2(s, a);
   }
   __syncthreads();
@@ -368,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, 2) logprobs_kernel(const LogprobsPar
 int choose_cluster(int rows, int V, int es, int num_sms) {
   const int64_t pieces = (int64_t)V * es / 16;
   int n = 1;
-  while (n < kMaxCluster && (int64_t)rows * n < 4 * num_sms && pieces > (int64_t)kThreads * n) n *= 2;
+  while (n < kMaxCluster && (int64_t)rows * n < 12 * num_sms && pieces > (int64_t)kThreads * n) n *= 2;
   return n;
 }
 

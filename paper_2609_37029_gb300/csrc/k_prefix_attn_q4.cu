@@ -71,6 +71,17 @@ struct Smem {
 template <int HD>
 size_t smem_bytes(int n) { return sizeof(Smem<HD>) + (size_t)n * (sizeof(PrefixSeq) + sizeof(int64_t)) + sizeof(int64_t) + 128; }
 
+struct Place {                                   // of the ring: a stage, and the parity of its use
+  uint32_t stage, phase;
+  __device__ __forceinline__ void next(uint32_t count) {
+    if (++stage == count) stage = 0, phase ^= 1;
+  }
+};
+template <bool kX>
+struct BoolTag {
+  static constexpr bool value = kX;
+};
+
 __device__ __forceinline__ float ex2a(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -113,7 +124,8 @@ __device__ __forceinline__ void load_role(const PrefixAttnParams& p, Smem<HD>& s
   const int block_codes = p.page * (HD / 2);
   PrefixSegs<1, kKeys> segs(p, sm.sched, line_base, info, blockIdx.x);
   PrefixSeg g;
-  uint32_t k = 0, fill = 0;
+  uint32_t k = 0;
+  Place ring = {0, 1};                           // (the first uses wait for nobody)
   bool more, shared = true;
   do {
     more = shared && segs.next_shared(g);
@@ -136,13 +148,13 @@ __device__ __forceinline__ void load_role(const PrefixAttnParams& p, Smem<HD>& s
       return lane < runs && kb < g.kb1 && pos < g.k_end ? g.tab[pos >> page_bits] : -1;
     };
     int pg = entry(g.kb0);
-    for (int kb = g.kb0; kb < g.kb1; ++kb, ++fill) {
+    for (int kb = g.kb0; kb < g.kb1; ++kb, ring.next(St::kCount)) {
       const int next = entry(kb + 1);
       const int pos = g.k0 + kb * kKeys + lane * run;
       const bool mine = lane < runs && pos < g.k_end, held = mine && pg >= 0 && pg < p.pages;
-      const uint32_t st = fill % St::kCount, bar = smem_u32(&sm.full[st]);
-      if (!tc_wait(smem_u32(&sm.empty[st]), ((fill / St::kCount) & 1) ^ 1, &sm.abort, p.err)) return;
-      uint8_t* at = sm.ring[st];
+      const uint32_t bar = smem_u32(&sm.full[ring.stage]);
+      if (!tc_wait(smem_u32(&sm.empty[ring.stage]), ring.phase, &sm.abort, p.err)) return;
+      uint8_t* at = sm.ring[ring.stage];
       if (mine && !held) {                       // a page of no pool: scales of 0
         set_err(p.err, LSP_DEV_BAD_SEQ);
         for (uint32_t i = 0; i < scales; i += 16) {
@@ -173,7 +185,7 @@ __device__ __forceinline__ void load_role(const PrefixAttnParams& p, Smem<HD>& s
 // A warp's part of the products of a segment.
 template <typename T, int HD>
 __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm, const PrefixSeg& g, int rg, int kg, int kgs,
-                                         uint32_t& fill, float (&o)[HD / 16][4], float2& m_out, float2& l_out) {
+                                         Place& ring, float (&o)[HD / 16][4], float2& m_out, float2& l_out) {
   using St = Stage<HD>;
   constexpr int P = kPieces<T>, kQ = HD / 8;     // registers of a row's quarter, of one piece
   constexpr int kWordsK = HD / 32, kWordsV = HD / 64;
@@ -217,119 +229,131 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
     lim[i] = row < rows ? min(g.see0 + row / p.rep, g.k_end) : INT_MAX;
   }
   const int least = min(g.see0 + 8 * rg / p.rep, g.k_end);
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  // maximum of the base-2 scores, the raw score from which on it is raised, sum of the weights
+  float m[2] = {-INFINITY, -INFINITY}, reach[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < HD / 16; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[i][e] = 0.f;
-  const int ka = key_at(r), kv[4] = {key_at(2 * t), key_at(2 * t + 1), key_at(2 * t) + 8, key_at(2 * t + 1) + 8};
-  for (int kb = g.kb0; kb < g.kb1; ++kb, ++fill) {
-    const uint32_t st = fill % St::kCount;
-    if (!tc_wait(smem_u32(&sm.full[st]), (fill / St::kCount) & 1, &sm.abort, p.err)) return false;
-    const uint8_t* at = sm.ring[st];
-    const int key0 = g.k0 + kb * kKeys;
-    const bool edge = key0 + kKeys > least;
-    for (int sl0 = kg; sl0 < kSlices && live; sl0 += kgs) {
-      const int k16 = sl0 * kSlice;
-      // scores
-      float s[4] = {0.f, 0.f, 0.f, 0.f};
-      {
-        uint32_t wa[kWordsK], wb[kWordsK];
-        const uint8_t* a = at + (k16 + ka) * (HD / 2) + t * (HD / 8);
-        if constexpr (HD == 128) {
-          const uint4 x = *reinterpret_cast<const uint4*>(a), y = *reinterpret_cast<const uint4*>(a + 8 * (HD / 2));
-          wa[0] = x.x; wa[1] = x.y; wa[2] = x.z; wa[3] = x.w;
-          wb[0] = y.x; wb[1] = y.y; wb[2] = y.z; wb[3] = y.w;
-        } else {
-          const uint2 x = *reinterpret_cast<const uint2*>(a), y = *reinterpret_cast<const uint2*>(a + 8 * (HD / 2));
-          wa[0] = x.x; wa[1] = x.y;
-          wb[0] = y.x; wb[1] = y.y;
+  // where the lane's words and scales lie in a stage: of keys r and r + 8, of values 2t (2t + 8) and 2t + 1 (2t + 9)
+  const int ka = key_at(r), kv[2] = {key_at(2 * t), key_at(2 * t + 1)};
+  const int k_at = ka * (HD / 2) + t * (HD / 8), ks_at = 2 * St::kCodes + ka * (HD / 16) + (HD == 128 ? t : t >> 1) * 2;
+  int v_at[2], vs_at[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    v_at[j] = St::kCodes + kv[j] * (HD / 2) + r * (HD / 16);
+    vs_at[j] = 2 * St::kCodes + St::kScales + kv[j] * (HD / 16) + (HD == 128 ? r >> 1 : r >> 2) * 2;
+  }
+  const Q4Consts consts;
+  // 16 keys, the first of them key `key` of the sequence, from `codes` and `scales` on; edge: some row does not see some key
+  auto slice = [&](const uint8_t* codes, const uint8_t* scales, int key, auto edge) {
+    constexpr bool kEdge = decltype(edge)::value;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    {
+      uint32_t wa[kWordsK], wb[kWordsK];
+      const uint8_t* a = codes + k_at;
+      if constexpr (HD == 128) {
+        const uint4 x = *reinterpret_cast<const uint4*>(a), y = *reinterpret_cast<const uint4*>(a + 8 * (HD / 2));
+        wa[0] = x.x; wa[1] = x.y; wa[2] = x.z; wa[3] = x.w;
+        wb[0] = y.x; wb[1] = y.y; wb[2] = y.z; wb[3] = y.w;
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(a), y = *reinterpret_cast<const uint2*>(a + 8 * (HD / 2));
+        wa[0] = x.x; wa[1] = x.y;
+        wb[0] = y.x; wb[1] = y.y;
+      }
+      const uint32_t sa = *reinterpret_cast<const uint16_t*>(scales + ks_at) * 0x10001u;
+      const uint32_t sb = *reinterpret_cast<const uint16_t*>(scales + ks_at + 8 * (HD / 16)) * 0x10001u;
+#pragma unroll
+      for (int i = 0; i < kWordsK; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t x[4] = {q4_pair(consts, wa[i] >> (8 * h), sa), q4_pair(consts, wb[i] >> (8 * h), sb),
+                                 q4_pair(consts, wa[i] >> (8 * h + 4), sa), q4_pair(consts, wb[i] >> (8 * h + 4), sb)};
+#pragma unroll
+          for (int k = 0; k < P; ++k) mma_bf16(s, x, q[k][4 * i + 2 * h], q[k][4 * i + 2 * h + 1]);
         }
-        const uint16_t* scales = reinterpret_cast<const uint16_t*>(at + 2 * St::kCodes) + (k16 + ka) * (HD / 32) + (HD == 128 ? t : t >> 1);
-        const uint32_t sa = scales[0] * 0x10001u, sb = scales[8 * (HD / 32)] * 0x10001u;
+    }
+    // rows 2t, 2t + 1 (s[0], s[1]) of key ka, and (s[2], s[3]) of key ka + 8
+    if (kEdge) {
 #pragma unroll
-        for (int i = 0; i < kWordsK; ++i)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t x[4] = {q4_pair(wa[i] >> (8 * h), sa), q4_pair(wb[i] >> (8 * h), sb), q4_pair(wa[i] >> (8 * h + 4), sa),
-                                   q4_pair(wb[i] >> (8 * h + 4), sb)};
-#pragma unroll
-            for (int k = 0; k < P; ++k) mma_bf16(s, x, q[k][4 * i + 2 * h], q[k][4 * i + 2 * h + 1]);
-          }
-      }
-      // rows 2t, 2t + 1 (s[0], s[1]) of key ka, and (s[2], s[3]) of key ka + 8
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s[e] *= sl;
-        if (edge && key0 + k16 + ka + (e & 2) * 4 >= lim[e & 1]) s[e] = -INFINITY;
-      }
-      bool raise[2];
+      for (int e = 0; e < 4; ++e)
+        if (key + ka + (e & 2) * 4 >= lim[e & 1]) s[e] = -INFINITY;
+    }
+    // (in raw scores: m is the running maximum, and a row is raised where a score exceeds it by kRaise in base 2)
+    const bool raise = fmaxf(s[0], s[2]) > reach[0] || fmaxf(s[1], s[3]) > reach[1];
+    if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float top = fmaxf(s[i], s[i + 2]);
-        raise[i] = top > m[i] + kRaise || (m[i] == -INFINITY && top > -INFINITY);
-      }
-      if (__any_sync(0xffffffffu, raise[0] || raise[1])) {
+        float top = fmaxf(s[i], s[i + 2]);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float top = fmaxf(s[i], s[i + 2]);
+        for (int w = 4; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+        if (!(top > reach[i])) continue;
+        top *= sl;
+        const float keep = ex2a(m[i] - top);     // (0 for the first)
+        m[i] = top;
+        reach[i] = (top + kRaise) / sl;
+        l[i] *= keep;
 #pragma unroll
-          for (int w = 4; w < 32; w <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-          if (!(top > m[i] + kRaise || (m[i] == -INFINITY && top > -INFINITY))) continue;
-          const float keep = ex2a(m[i] - top);   // (0 for the first)
-          m[i] = top;
-          l[i] *= keep;
-#pragma unroll
-          for (int d = 0; d < HD / 16; ++d) o[d][i] *= keep, o[d][i + 2] *= keep;
-        }
-      }
-      uint32_t b0[P], b1[P];
-      {
-        float w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          w[e] = ex2a(s[e] - (m[e & 1] == -INFINITY ? 0.f : m[e & 1]));
-          l[e & 1] += w[e];
-        }
-        // (bf16: the weights of the product are rounded to 2^-9 of each, their sum is not: the other operand is bf16,
-        // and the rounding of the output outweighs it)
-        split_pair<P>(w[0], w[1], b0);
-        split_pair<P>(w[2], w[3], b1);
-#pragma unroll
-        for (int k = 0; k < P; ++k) b0[k] = transpose8(b0[k]), b1[k] = transpose8(b1[k]);
-      }
-      // values
-      uint32_t w[4][kWordsV], sv[4];
-      const uint16_t* scales = reinterpret_cast<const uint16_t*>(at + 2 * St::kCodes + St::kScales) + k16 * (HD / 32) + (HD == 128 ? r >> 1 : r >> 2);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint8_t* a = at + St::kCodes + (k16 + kv[j]) * (HD / 2) + r * (HD / 16);
-        if constexpr (HD == 128) {
-          const uint2 x = *reinterpret_cast<const uint2*>(a);
-          w[j][0] = x.x; w[j][1] = x.y;
-        } else {
-          w[j][0] = *reinterpret_cast<const uint32_t*>(a);
-        }
-        sv[j] = scales[kv[j] * (HD / 32)];
-        // slots of a page past the last key hold anything: their weights are 0, and 0 x V must be 0
-        if (edge && key0 + k16 + kv[j] >= g.k_end) sv[j] = 0;
-      }
-      const uint32_t sa = sv[0] | sv[1] << 16, sb = sv[2] | sv[3] << 16;
-#pragma unroll
-      for (int i = 0; i < kWordsV; ++i) {
-        const uint32_t lo_a = __byte_perm(w[0][i], w[1][i], 0x5410), hi_a = __byte_perm(w[0][i], w[1][i], 0x7632);
-        const uint32_t lo_b = __byte_perm(w[2][i], w[3][i], 0x5410), hi_b = __byte_perm(w[2][i], w[3][i], 0x7632);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t x[4] = {q4_pair(lo_a >> (4 * k), sa), q4_pair(hi_a >> (4 * k), sa), q4_pair(lo_b >> (4 * k), sb),
-                                 q4_pair(hi_b >> (4 * k), sb)};
-#pragma unroll
-          for (int c = 0; c < P; ++c) mma_bf16(o[4 * i + k], x, b0[c], b1[c]);
-        }
+        for (int d = 0; d < HD / 16; ++d) o[d][i] *= keep, o[d][i + 2] *= keep;
       }
     }
-    __syncwarp();
-    if (lane == 0) mbar_arrive(smem_u32(&sm.empty[st]));
+    uint32_t b0[P], b1[P];
+    {
+      float w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        w[e] = ex2a(fmaf(s[e], sl, kEdge && m[e & 1] == -INFINITY ? 0.f : -m[e & 1]));
+        l[e & 1] += w[e];
+      }
+      // (bf16: the weights of the product are rounded to 2^-9 of each, their sum is not: the other operand is bf16,
+      // and the rounding of the output outweighs it)
+      split_pair<P>(w[0], w[1], b0);
+      split_pair<P>(w[2], w[3], b1);
+#pragma unroll
+      for (int k = 0; k < P; ++k) b0[k] = transpose8(b0[k]), b1[k] = transpose8(b1[k]);
+    }
+    uint32_t w[4][kWordsV], sv[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint8_t* a = codes + v_at[j & 1] + (j >> 1) * 8 * (HD / 2);
+      if constexpr (HD == 128) {
+        const uint2 x = *reinterpret_cast<const uint2*>(a);
+        w[j][0] = x.x; w[j][1] = x.y;
+      } else {
+        w[j][0] = *reinterpret_cast<const uint32_t*>(a);
+      }
+      sv[j] = *reinterpret_cast<const uint16_t*>(scales + vs_at[j & 1] + (j >> 1) * 8 * (HD / 16));
+      // slots of a page past the last key hold anything: their weights are 0, and 0 x V must be 0
+      if (kEdge && key + kv[j & 1] + (j >> 1) * 8 >= g.k_end) sv[j] = 0;
+    }
+    const uint32_t sa = sv[0] | sv[1] << 16, sb = sv[2] | sv[3] << 16;
+#pragma unroll
+    for (int i = 0; i < kWordsV; ++i) {
+      const uint32_t lo_a = __byte_perm(w[0][i], w[1][i], 0x5410), hi_a = __byte_perm(w[0][i], w[1][i], 0x7632);
+      const uint32_t lo_b = __byte_perm(w[2][i], w[3][i], 0x5410), hi_b = __byte_perm(w[2][i], w[3][i], 0x7632);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t x[4] = {q4_pair(consts, lo_a >> (4 * k), sa), q4_pair(consts, hi_a >> (4 * k), sa),
+                               q4_pair(consts, lo_b >> (4 * k), sb), q4_pair(consts, hi_b >> (4 * k), sb)};
+#pragma unroll
+        for (int c = 0; c < P; ++c) mma_bf16(o[4 * i + k], x, b0[c], b1[c]);
+      }
+    }
+  };
+  for (int kb = g.kb0; kb < g.kb1; ++kb) {
+    if (!tc_wait(smem_u32(&sm.full[ring.stage]), ring.phase, &sm.abort, p.err)) return false;
+    if (live) {
+      const uint8_t* at = sm.ring[ring.stage];
+      const int key0 = g.k0 + kb * kKeys;
+      if (key0 + kKeys > least) {
+        for (int i = kg; i < kSlices; i += kgs) slice(at + i * kSlice * (HD / 2), at + i * kSlice * (HD / 16), key0 + i * kSlice, BoolTag<true>());
+      } else {
+        for (int i = kg; i < kSlices; i += kgs) slice(at + i * kSlice * (HD / 2), at + i * kSlice * (HD / 16), key0 + i * kSlice, BoolTag<false>());
+      }
+      __syncwarp();
+    }
+    if (lane == 0) mbar_arrive(smem_u32(&sm.empty[ring.stage]));
+    ring.next(St::kCount);
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i)
@@ -343,7 +367,8 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
 template <typename T, int HD>
 __device__ __forceinline__ void multiply_role(const PrefixAttnParams& p, Smem<HD>& sm) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, t = lane & 3;
-  uint32_t fill = 0, met = 0;
+  Place ring = {0, 0};
+  uint32_t met = 0;
   // the multiplying warps wait for each other (within the limit of every wait: one of them may have given up)
   auto meet = [&]() {
     __syncwarp();
@@ -364,7 +389,7 @@ __device__ __forceinline__ void multiply_role(const PrefixAttnParams& p, Smem<HD
     const int rg = warp & (rgs - 1), kg = warp / rgs;
     float o[HD / 16][4];
     float2 m, l;
-    if (!multiply<T, HD>(p, sm, g, rg, kg, kgs, fill, o, m, l)) break;
+    if (!multiply<T, HD>(p, sm, g, rg, kg, kgs, ring, o, m, l)) break;
     if (r == 0) {
       sm.merge_ml[warp][2 * t] = make_float2(m.x, l.x);
       sm.merge_ml[warp][2 * t + 1] = make_float2(m.y, l.y);

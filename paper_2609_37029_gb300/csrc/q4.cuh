@@ -17,43 +17,65 @@ constexpr uint32_t kQ4Zero = 0x88888888u;        // eight codes of 0
 __device__ __forceinline__ uint32_t bf2_bits(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t*>(&x); }
 __device__ __forceinline__ __nv_bfloat162 bits_bf2(uint32_t x) { return *reinterpret_cast<__nv_bfloat162*>(&x); }
 
+// What unpacking takes besides, in registers: a loop that has them as immediate
+// operands moves them there for every pair.
+struct Q4Consts {
+  uint32_t mask, one, minus;
+  __device__ __forceinline__ Q4Consts() {
+    asm volatile("mov.b32 %0, 0x000F000F;" : "=r"(mask));
+    asm volatile("mov.b32 %0, 0x43004300;" : "=r"(one));         // 128.0
+    asm volatile("mov.b32 %0, 0xC308C308;" : "=r"(minus));       // -136.0
+  }
+};
+
 // Two elements (codes in the low 4 bits of each half of w) times two scales, as a pair of bfloat16.
-__device__ __forceinline__ uint32_t q4_pair(uint32_t w, uint32_t scales) {
+__device__ __forceinline__ uint32_t q4_pair(const Q4Consts& k, uint32_t w, uint32_t scales) {
   uint32_t x;
-  asm("lop3.b32 %0, %1, 0x000F000F, 0x43004300, 0xEA;" : "=r"(x) : "r"(w));      // (w & mask) | 128.0
-  return bf2_bits(__hmul2(__hsub2(bits_bf2(x), bits_bf2(0x43084308u)), bits_bf2(scales)));
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(x) : "r"(w), "r"(k.mask), "r"(k.one));      // (w & mask) | 128.0
+  return bf2_bits(__hmul2(__hadd2(bits_bf2(x), bits_bf2(k.minus)), bits_bf2(scales)));
 }
 
 // The scale of a group from the greatest |x| of its values (as bits, so that what is
 // not finite counts as greater than what is): the least number of five significant
-// bits with 7 s >= a.  a / 7 correctly rounded and cut to five bits is that number,
-// or the one before it; 7 s is exact.
+// bits with 7 s >= a.  A quotient that is never below a / 7 and hardly above it, cut
+// to five bits, is that number or the one before it; 7 s is exact and tells.
 __device__ __forceinline__ float q4_scale(uint32_t a_bits) {
   if (a_bits >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
   const float a = __uint_as_float(a_bits);
-  const uint32_t bits = __float_as_uint(__fdiv_rn(a, 7.0f)) & ~0x7FFFFu;
-  const float low = __uint_as_float(bits);
-  return 7.0f * low < a ? __uint_as_float(bits + 0x80000u) : low;
+  const uint32_t bits = __float_as_uint(__fmul_ru(a, 0.14285715f)) & ~0x7FFFFu;  // (the next number above 1/7)
+  return 7.0f * __uint_as_float(bits) < a ? __uint_as_float(bits + 0x80000u) : __uint_as_float(bits);
 }
 
-// Eight codes of a group.  The product with the reciprocal names a whole number that
-// is the nearest or next to it; what is left over is exact (r s has eight bits, and
-// the difference no more than x's) and says which, ties to the even one.
-__device__ __forceinline__ uint32_t q4_codes(const float* x, float s) {
+// Eight codes of a group, by x / s and a sum whose last place is the whole number:
+// 1.5 2^23 + 8 + c, so that codes are the low bits (rounded to nearest, ties to even;
+// the 8 moves no tie).  What the quotient may not do is reach a tie, or leave one:
+//   f32   it is the correctly rounded one: the reciprocal and one step of the exact
+//         remainder (Markstein 1990).  Ties n + 1/2 are fp32 numbers, and an x next
+//         to s (n + 1/2) lies at least half a last place of the quotient from it.
+//   bf16  (x of eight significant bits) a quotient is a tie, or at least 2^-4 / (2 31)
+//         > 2^-10 from one; rounded to multiples of 2^-12 first, it stays what it is.
+template <bool kShort>                           // x of eight significant bits
+__device__ __forceinline__ uint32_t q4_codes(float* x, float s) {
   if (!(s > 0.0f)) return kQ4Zero;                // an empty group, or one that is NaN
-  const float up = s < 1.1754944e-30f ? 18446744073709551616.0f : 1.0f;          // (2^64: reciprocals stay finite)
-  s *= up;
-  const float inv = 1.0f / s, half = 0.5f * s;
+  if (s < 1e-30f) {                              // (times 2^64: reciprocals stay finite)
+    s *= 18446744073709551616.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= 18446744073709551616.0f;
+  }
+  const float inv = __frcp_rn(s);
   uint32_t w = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float y = x[e] * up, r = rintf(y * inv), rest = fmaf(-r, s, y);
-    int c = (int)r;
-    if (rest > half || (rest == half && (c & 1))) ++c;
-    else if (rest < -half || (rest == -half && (c & 1))) --c;
-    w |= (uint32_t)(c + 8) << (16 * (e & 1) + 4 * (e >> 1));
+    float y;
+    if constexpr (kShort) {
+      y = fmaf(x[e], inv, 3072.0f) + (12582920.0f - 3072.0f);
+    } else {
+      const float q = x[e] * inv;
+      y = fmaf(fmaf(-q, s, x[e]), inv, q) + 12582920.0f;
+    }
+    w += __float_as_uint(y) << (16 * (e & 1) + 4 * (e >> 1));
   }
-  return w;
+  return w - 0x4B400000u * 0x11111111u;          // (the upper bits of the eight numbers)
 }
 
 }  // namespace lsp
