@@ -29,4 +29,11 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+struct Place {                                   // of the ring: a stage, and the parity of its use
+  uint32_t stage, phase;
+  __device__ __forceinline__ void next(uint32_t count) {
+    if (++stage == count) stage = 0, phase ^= 1;
+  }
+};
+
 }  // namespace lsp

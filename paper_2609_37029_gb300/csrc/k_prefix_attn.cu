@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
           u = tile / kUnitTiles;
           shared_at = (tile % kUnitTiles) * tile_rows + (t - tile * p.tok_tile) * p.rep + hr;
           const bool last = u + 1 == p.units;
-          shared_cost = last ? block_cost<kUnitTiles>(p, p.total - u * kUnitTiles * p.tok_tile) : kCostTwo;
+          shared_cost = last ? block_cost(p, p.total - u * kUnitTiles * p.tok_tile) : p.cost.many;
           pieces = s_pieces[last];
           shared = p.splits * pieces;
           shared_first = shared_place(s, g * p.splits, u) - s.whole_line;
@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
         for (int u = 0; u < unit; ++u)
           first += (int64_t)item_length<kUnitTiles>(p, r, u, own_blocks<kUnitTiles, kBlock>(p, r, s.base, u)) * p.nkv;
         blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, unit);
-        cost = block_cost<kUnitTiles>(p, r.rows - unit * kUnitTiles * p.tok_tile);
+        cost = block_cost(p, r.rows - unit * kUnitTiles * p.tok_tile);
         const int len = item_length<kUnitTiles>(p, r, unit, blocks);
         first += (int64_t)g * len;
         if (blocks > 0) {
@@ -336,7 +336,7 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
         if (c >= s.ctas) return -1;
         // a CTA may have a piece of the item without any of its blocks
         const int price = sh ? shared_cost : cost;
-        if (blocks_before(s, begin[c + 1] - place, nb, price) <= blocks_before(s, begin[c] - place, nb, price)) return -1;
+        if (blocks_before(p, s, begin[c + 1] - place, nb, price) <= blocks_before(p, s, begin[c] - place, nb, price)) return -1;
         return sh ? shared_rows<kUnitTiles>(p, s, item, c) + shared_at : own_rows<kUnitTiles>(p, r, unit, g, c) + own_at;
       };
       // the first segment of this lane for the maxima, and for the sums
@@ -515,15 +515,31 @@ int choose_splits(int heads, int units, int blocks, int grid) {
 struct Shape {
   int tile, unit_tiles, block, per_sm;
 };
+
+// Costs in units of 0.37 us.  few_rows: rows that a block is cheaper with.
+PrefixCosts costs(int few_rows, int few, int many, int segment) {
+  PrefixCosts c = {few_rows, few, many, segment, {}};
+  const int group[4] = {few, few * kPrefixTogether, many, many * kPrefixTogether};
+  for (int i = 0; i < 4; ++i) c.inverse[i] = (uint32_t)((((uint64_t)1 << 32) + group[i] - 1) / group[i]);
+  return c;
+}
+PrefixCosts attn_costs(const PrefixAttnParams& p) {
+  // ... over a cache in 4 bits: both are as long as it takes to unpack a block (16 requests of 17 rows over 32K 170 us,
+  // with the costs below 198)
+  if (p.tc && p.q4) return costs(p.tok_tile * p.rep, 5, 5, 11);
+  // one row tile 1.1 us a block, two 1.46, a segment 1.9 (16 requests over 32K, bf16)
+  if (p.tc) return costs(p.tok_tile * p.rep, 3, 4, 5);
+  // (the fp32 kernel's warps have eight rows each, and those without rows leave the block to the others)
+  return costs(32, 3, 4, 5);
+}
 Shape attn_shape(const PrefixAttnParams& p, int dtype) {
+  if (p.tc) return {kPrefixTcRows, kPrefixTcTiles, kPrefixTcKeys, 1};
   if (p.q4) return {kPrefixQ4Rows, 1, kPrefixQ4Keys, prefix_q4_per_sm(dtype, p.d)};
-  if (dtype == LSP_DTYPE_BF16) return {kPrefixTcRows, kPrefixTcTiles, kPrefixTcKeys, 1};
   return {kFmaRows, 1, kFmaKeys, p.d == 64 ? kFmaPerSm<64> : kFmaPerSm<128>};
 }
 
-}  // namespace
-
-size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms) {
+size_t plan(PrefixAttnParams* p, int dtype, int num_sms, bool tc) {
+  p->tc = tc;
   const Shape sh = attn_shape(*p, dtype);
   p->tok_tile = sh.tile / p->rep;
   p->units = (p->total + p->tok_tile * sh.unit_tiles - 1) / (p->tok_tile * sh.unit_tiles);
@@ -534,7 +550,26 @@ size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms) {
   const int64_t rows = (int64_t)p->tok_tile * p->rep * sh.unit_tiles, items = std::max<int64_t>((int64_t)p->nkv * p->units, p->grid);
   p->part_rows = (items + 2 * p->grid) * rows + (int64_t)p->nkv * p->rep * p->total;
   p->part_rows = (p->part_rows + 3) / 4 * 4;
+  p->cost = attn_costs(*p);
   return align256((size_t)p->part_rows * sizeof(float2)) + (size_t)p->part_rows * p->d * sizeof(float);
+}
+
+// Rows of bf16 over a cache in 4 bits: which kernel.
+bool q4_on_tc(const PrefixAttnParams& p) {
+  if (p.n > prefix_tc_q4_seqs(p.d)) return false;
+  const int64_t shared = p.shared_len >= 1024 ? (int64_t)p.total * p.rep : 0, own = (int64_t)((p.total + p.n - 1) / p.n) * p.rep;
+  return std::max(shared, own) > 16;
+}
+
+}  // namespace
+
+size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms) {
+  return plan(p, dtype, num_sms, dtype == LSP_DTYPE_BF16 && (!p->q4 || q4_on_tc(*p)));
+}
+
+size_t prefix_attn_workspace(PrefixAttnParams p, int dtype, int num_sms) {
+  const size_t own = plan(&p, dtype, num_sms, dtype == LSP_DTYPE_BF16);
+  return p.q4 && p.tc ? std::max(own, plan(&p, dtype, num_sms, false)) : own;
 }
 
 int launch_prefix_attention(PrefixAttnParams p, int dtype, void* ws, cudaStream_t s) {
@@ -542,8 +577,8 @@ int launch_prefix_attention(PrefixAttnParams p, int dtype, void* ws, cudaStream_
   p.part_ml = reinterpret_cast<float2*>(w);
   w += align256((size_t)p.part_rows * sizeof(float2));
   p.part_o = reinterpret_cast<float*>(w);
+  if (p.tc) return p.d == 128 ? launch_tc<128>(p, s) : launch_tc<64>(p, s);
   if (p.q4) return p.d == 128 ? launch_q4<128>(p, dtype, s) : launch_q4<64>(p, dtype, s);
-  if (dtype == LSP_DTYPE_BF16) return p.d == 128 ? launch_tc<128>(p, s) : launch_tc<64>(p, s);
   return p.d == 128 ? launch_fma<128>(p, s) : launch_fma<64>(p, s);
 }
 

@@ -71,26 +71,10 @@ struct Smem {
 template <int HD>
 size_t smem_bytes(int n) { return sizeof(Smem<HD>) + (size_t)n * (sizeof(PrefixSeq) + sizeof(int64_t)) + sizeof(int64_t) + 128; }
 
-struct Place {                                   // of the ring: a stage, and the parity of its use
-  uint32_t stage, phase;
-  __device__ __forceinline__ void next(uint32_t count) {
-    if (++stage == count) stage = 0, phase ^= 1;
-  }
-};
-template <bool kX>
-struct BoolTag {
-  static constexpr bool value = kX;
-};
-
 __device__ __forceinline__ float ex2a(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
-}
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-               "l"(src), "r"(bytes), "r"(bar)
-               : "memory");
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {     // of an 8 x 8 matrix of 16-bit elements
   uint32_t y;

@@ -41,6 +41,11 @@
 // that PV(j) reads, and the products of one thread complete in order.  TMEM:
 // scores of stream t at columns 128 t, sums at 256 + 128 t.
 //
+// Over a cache in 4 bits (kQ4; format: q4.cuh) four more warps, 12 to 15, come
+// between the loads and the ring: warp 8 copies a tile's codes and scales into one of
+// a few places behind it, and the four write its 128 keys as bf16 where TMA would
+// have put them.
+//
 // The maximum is raised (and the sums rescaled) only when it would grow by more
 // than 2^8, as attention kernels in the literature do: weights stay below 2^8 and
 // the sums, in fp32, lose nothing.
@@ -48,13 +53,17 @@
 
 #include "barrier_wait.cuh"
 #include "prefix_sched.cuh"
+#include "q4.cuh"
 
 namespace lsp {
 namespace {
 
 constexpr int kRows = kPrefixTcRows, kKeys = kPrefixTcKeys, kTiles = kPrefixTcTiles;
-constexpr int kThreads = 384;
-constexpr int kLoadWarp = 8, kMmaWarp = 9;       // the second products' warp and the plan's follow
+constexpr int kLoadWarp = 8, kMmaWarp = 9, kUnpackWarp = 12;    // the second products' warp and the plan's come between
+constexpr int kUnpackWarps = 4;
+constexpr size_t kMostSmem = 227 * 1024;         // of a CTA
+template <bool kQ4>
+constexpr int kThreads = 32 * (kQ4 ? kUnpackWarp + kUnpackWarps : kUnpackWarp);
 constexpr int kAhead = 4;                        // segments planned ahead
 constexpr int kFirstKeys = 64;                   // keys whose weights are handed over before the rest's (when chosen 0.75 ms over 128K; 32: 0.79, 96: 0.81)
 constexpr float kLog2e = 1.4426950408889634f;
@@ -81,12 +90,23 @@ struct TcMisc {
   } planned[kAhead];
   PrefixSched sched;
   float2 lone_ml[2][kRows];                      // stream 1's maximum and sum of segments with one row tile, by turns
-  int64_t line_base[kPrefixMaxSeqs + 1];
-  PrefixSeq info[kPrefixMaxSeqs];
+  uint64_t packed_full[4], packed_empty[4];      // kQ4: tiles in 4 bits
+  int packed_keys[4];                            // keys of one; -1: no more tiles
 };
 
+// A tile of a cache in 4 bits: codes, then scales.
 template <int HD>
-constexpr size_t tc_smem() { return TcShape<HD>::kMisc + sizeof(TcMisc) + 1024; }
+struct Packed {
+  static constexpr int kCodes = kKeys * HD / 2, kBytes = kCodes + kKeys * HD / 16;
+  static constexpr int kMost = 4;                // places, as far as there is room
+};
+
+// Shared memory: query tiles and ring, TcMisc, places in the line and sequences of the batch, packed tiles.
+__host__ __device__ constexpr size_t tc_seqs(int n) { return ((size_t)n * (sizeof(PrefixSeq) + sizeof(int64_t)) + sizeof(int64_t) + 127) & ~(size_t)127; }
+template <int HD>
+constexpr size_t tc_smem(int n, int packed) {
+  return TcShape<HD>::kMisc + ((sizeof(TcMisc) + 127) & ~(size_t)127) + tc_seqs(n) + (size_t)packed * Packed<HD>::kBytes + 1024;
+}
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* map, uint32_t bar, int x, int y, int z) {
   asm volatile(
@@ -169,6 +189,18 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+__device__ __forceinline__ void ld_shared2(uint32_t at, uint32_t& x, uint32_t& y) {
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint32_t ld_shared_u16(uint32_t at) {
+  uint32_t x;
+  asm volatile("ld.shared.u16 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+  return x;
+}
+__device__ __forceinline__ void st_shared4(uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
 __device__ __forceinline__ float ex2a(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -228,9 +260,9 @@ __device__ __forceinline__ uint32_t value_tile(const Jobs& j, int i) { return j.
 
 // The plan of the CTA's segments, handed on through shared memory: finding the
 // next one takes some 500 cycles, which nobody should spend between two segments.
-__device__ __forceinline__ void plan_role(const PrefixAttnParams& p, TcMisc* m) {
+__device__ __forceinline__ void plan_role(const PrefixAttnParams& p, TcMisc* m, const int64_t* line_base, const PrefixSeq* info) {
   const int lane = threadIdx.x & 31;
-  PrefixSegs<kTiles, kKeys> segs(p, m->sched, m->line_base, m->info, blockIdx.x);
+  PrefixSegs<kTiles, kKeys> segs(p, m->sched, line_base, info, blockIdx.x);
   PrefixSeg g;
   uint32_t k = 0;
   auto publish = [&](bool more) {
@@ -267,6 +299,24 @@ struct SegReader {
   }
 };
 
+// The query tiles of a segment.
+template <int HD>
+__device__ __forceinline__ bool load_queries(const PrefixAttnParams& p, const CUtensorMap* mq, uint32_t sm, TcMisc* m,
+                                             const PrefixSeg& g, const Jobs& jobs, uint32_t& nq) {
+  using Sh = TcShape<HD>;
+  const int tiles = jobs.lone ? 1 : 2;
+  for (int t = 0; t < tiles; ++t, ++nq) {
+    const uint32_t slot = nq & 1, bar = smem_u32(&m->q_full[slot]);
+    if (!tc_wait(smem_u32(&m->q_empty[slot]), ((nq >> 1) & 1) ^ 1, &m->abort, p.err)) return false;
+    if ((threadIdx.x & 31) == 0) {
+      mbar_expect_tx(bar, (uint32_t)(Sh::kHalves * p.tok_tile * p.rep * 128));
+      for (int h = 0; h < Sh::kHalves; ++h)
+        tma_load_3d(sm + slot * Sh::kTile + h * Sh::kHalf, mq, bar, 64 * h, g.head * p.rep, g.t0 + t * p.tok_tile);
+    }
+  }
+  return true;
+}
+
 template <int HD>
 __device__ __forceinline__ void load_role(const PrefixAttnParams& p, const CUtensorMap* mq, const CUtensorMap* mk,
                                           const CUtensorMap* mv, uint32_t sm, TcMisc* m, SegReader segs) {
@@ -278,16 +328,7 @@ __device__ __forceinline__ void load_role(const PrefixAttnParams& p, const CUten
   PrefixSeg g;
   while (segs.next(g)) {
     const Jobs jobs = seg_jobs(p, g);
-    const int tiles = jobs.lone ? 1 : 2;
-    for (int t = 0; t < tiles; ++t, ++nq) {
-      const uint32_t slot = nq & 1, bar = smem_u32(&m->q_full[slot]);
-      if (!tc_wait(smem_u32(&m->q_empty[slot]), ((nq >> 1) & 1) ^ 1, &m->abort, p.err)) return;
-      if (lane == 0) {
-        mbar_expect_tx(bar, (uint32_t)(Sh::kHalves * p.tok_tile * p.rep * 128));
-        for (int h = 0; h < Sh::kHalves; ++h)
-          tma_load_3d(sm + slot * Sh::kTile + h * Sh::kHalf, mq, bar, 64 * h, g.head * p.rep, g.t0 + t * p.tok_tile);
-      }
-    }
+    if (!load_queries<HD>(p, mq, sm, m, g, jobs, nq)) return;
     // lane l loads page l of a block; a page past the keys or outside the pool reads as zeros
     auto entry = [&](int kb) {
       const int pos = g.k0 + kb * kKeys + lane * box;
@@ -326,6 +367,128 @@ __device__ __forceinline__ void load_role(const PrefixAttnParams& p, const CUten
       if (i + lead < blocks && !load(mk, g.kb0 + i + lead, lead == 2 ? e2 : e1)) return;
       e0 = e1;
       e1 = e2;
+    }
+  }
+}
+
+// Codes and scales of the tiles, in the order of the ring's places, and the query tiles.
+template <int HD>
+__device__ __forceinline__ void load_packed_role(const PrefixAttnParams& p, const CUtensorMap* mq, uint32_t sm, uint8_t* packed,
+                                                 int count, TcMisc* m, SegReader segs) {
+  using Pk = Packed<HD>;
+  const int lane = threadIdx.x & 31;
+  const int run = min(p.page, kKeys), runs = kKeys / run, page_bits = 31 - __clz(p.page);
+  const uint32_t codes = run * (HD / 2), scales = run * (HD / 16);
+  const int block_codes = p.page * (HD / 2);
+  uint32_t nq = 0;
+  Place place = {0, 1};                          // (the first uses wait for nobody)
+  PrefixSeg g;
+  while (segs.next(g)) {
+    const Jobs jobs = seg_jobs(p, g);
+    if (!load_queries<HD>(p, mq, sm, m, g, jobs, nq)) return;
+    // lane l loads run l of a block
+    auto entry = [&](int kb) {
+      const int pos = g.k0 + kb * kKeys + lane * run;
+      return lane < runs && kb < g.kb1 && pos < g.k_end ? g.tab[pos >> page_bits] : -1;
+    };
+    auto load = [&](const char* pool, int kb, int pg) {
+      const uint32_t at = place.stage, bar = smem_u32(&m->packed_full[at]);
+      const int first = g.k0 + kb * kKeys, pos = first + lane * run;
+      const bool mine = lane < runs && pos < g.k_end, held = mine && pg >= 0 && pg < p.pages;
+      if (!tc_wait(smem_u32(&m->packed_empty[at]), place.phase, &m->abort, p.err)) return false;
+      uint8_t* to = packed + at * Pk::kBytes;
+      if (mine && !held) {                       // a page of no pool: scales of 0
+        set_err(p.err, LSP_DEV_BAD_SEQ);
+        for (uint32_t i = 0; i < scales; i += 16) *reinterpret_cast<uint4*>(to + Pk::kCodes + lane * scales + i) = make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
+      }
+      const int n = __popc(__ballot_sync(0xffffffffu, held));
+      __syncwarp();
+      if (lane == 0) {
+        m->packed_keys[at] = min(g.k_end - first, kKeys);
+        mbar_expect_tx(bar, n * (codes + scales));
+      }
+      __syncwarp();
+      if (held) {
+        const int slot = pos & (p.page - 1);
+        const char* block = pool + (int64_t)pg * p.s_page + (int64_t)g.head * p.s_head;
+        bulk_load(smem_u32(to) + lane * codes, block + slot * (HD / 2), codes, bar);
+        bulk_load(smem_u32(to) + Pk::kCodes + lane * scales, block + block_codes + slot * (HD / 16), scales, bar);
+      }
+      place.next(count);
+      return true;
+    };
+    // first uses: keys lead values by one job (two streams' worth where both take every block)
+    const int lead = jobs.lone ? 2 : 1, blocks = g.kb1 - g.kb0;
+    int e0 = entry(g.kb0), e1 = entry(g.kb0 + 1);
+    if (!load(p.k, g.kb0, e0)) return;
+    if (lead == 2 && blocks > 1 && !load(p.k, g.kb0 + 1, e1)) return;
+    for (int i = 0; i < blocks; ++i) {
+      const int e2 = entry(g.kb0 + i + 2);
+      if (!load(p.v, g.kb0 + i, e0)) return;
+      if (i + lead < blocks && !load(p.k, g.kb0 + i + lead, lead == 2 ? e2 : e1)) return;
+      e0 = e1;
+      e1 = e2;
+    }
+  }
+  const uint32_t at = place.stage;
+  if (!tc_wait(smem_u32(&m->packed_empty[at]), place.phase, &m->abort, p.err)) return;
+  if (lane == 0) {
+    m->packed_keys[at] = -1;
+    mbar_arrive(smem_u32(&m->packed_full[at]));
+  }
+  __syncwarp();
+}
+
+// Tiles from 4 bits to bf16, 32 keys of each to a warp.  A lane takes two words of codes, 16 dims, at a time: a
+// warp's words lie side by side, and eight lanes store to eight different columns of 16 bytes (lanes of the second
+// half of a row's dims begin with their second word).
+template <int HD>
+__device__ __forceinline__ void unpack_role(const PrefixAttnParams& p, int warp, uint8_t* smp, const uint8_t* packed, int count,
+                                            TcMisc* m) {
+  using Sh = TcShape<HD>;
+  using Pk = Packed<HD>;
+  constexpr int kPairs = HD / 16, kKeysOf = 32 / kPairs, kSteps = 32 / kKeysOf;  // pairs of words of a key; keys of a step
+  const int lane = threadIdx.x & 31, pair = lane & (kPairs - 1), first = 32 * warp + lane / kPairs;
+  const bool second = pair >= 4;                 // of the row's halves of 64 dims
+  const uint32_t base = smem_u32(packed) + first * (HD / 2) + pair * 8, scale_base = smem_u32(packed) + Pk::kCodes + first * (HD / 16) + (pair >> 1) * 2;
+  const uint32_t to = smem_u32(smp) + Sh::kRing + (second ? Sh::kHalf : 0u) + first * 128;
+  const int column = (2 * pair & 7) | (second ? 1 : 0);
+  const Q4Consts consts;
+  Place place = {0, 0}, ring = {0, 1};
+  for (;; place.next(count), ring.next(Sh::kStages)) {
+    const uint32_t at = place.stage, st = ring.stage;
+    if (!tc_wait(smem_u32(&m->packed_full[at]), place.phase, &m->abort, p.err)) return;
+    const int keys = m->packed_keys[at];
+    if (keys < 0) return;
+    uint32_t w[kSteps][2], s[kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      ld_shared2(base + at * Pk::kBytes + i * kKeysOf * (HD / 2), w[i][0], w[i][1]);
+      s[i] = ld_shared_u16(scale_base + at * Pk::kBytes + i * kKeysOf * (HD / 16));
+    }
+    if (keys < kKeys) {                          // slots of a page past the last key hold anything
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i)
+        if (first + i * kKeysOf >= keys) s[i] = 0;
+    }
+    if (!tc_wait(smem_u32(&m->empty[st]), ring.phase, &m->abort, p.err)) return;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const uint32_t scale = s[i] * 0x10001u, row = to + st * Sh::kTile + i * kKeysOf * 128;
+      const int key = first + i * kKeysOf;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t x = second ? w[i][1 - e] : w[i][e];
+        st_shared4(row + (((column ^ e ^ key) & 7) << 4), q4_pair(consts, x, scale), q4_pair(consts, x >> 4, scale),
+                   q4_pair(consts, x >> 8, scale), q4_pair(consts, x >> 12, scale));
+      }
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      mbar_arrive(smem_u32(&m->full[st]));
+      mbar_arrive(smem_u32(&m->packed_empty[at]));
     }
   }
 }
@@ -462,7 +625,7 @@ __device__ __forceinline__ void mma_role(const PrefixAttnParams& p, int t, uint3
   }
 }
 
-template <int HD>
+template <int HD, bool kQ4>
 __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, uint8_t* smp, uint32_t tmem, TcMisc* m,
                                              SegReader segs) {
   const int lane = threadIdx.x & 31, quad = (threadIdx.x >> 5) & 3, row = quad * 32 + lane;
@@ -511,7 +674,7 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
           if (raise) mx = b;
         }
       }
-      if (jobs.lone || t == 0) {
+      if (!kQ4 && (jobs.lone || t == 0)) {       // (unpacked tiles have zeros there)
         // slots of a page past the last key hold anything: their weights are 0, and 0 x V must be 0
         // (where both streams use the tile, stream 1's turn comes after stream 0's)
         const int keys = g.k_end - g.k0 - kb * kKeys;
@@ -622,23 +785,30 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
   }
 }
 
-template <int HD>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int HD, bool kQ4>
+__global__ void __launch_bounds__(kThreads<kQ4>, 1)
     prefix_attn_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
-                          const __grid_constant__ CUtensorMap mv, const PrefixAttnParams p) {
+                          const __grid_constant__ CUtensorMap mv, const PrefixAttnParams p, int count) {
   extern __shared__ uint8_t tc_raw[];
   uint8_t* smp = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tc_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   TcMisc* m = reinterpret_cast<TcMisc*>(smp + TcShape<HD>::kMisc);
+  PrefixSeq* info = reinterpret_cast<PrefixSeq*>(smp + TcShape<HD>::kMisc + ((sizeof(TcMisc) + 127) & ~(size_t)127));
+  int64_t* line_base = reinterpret_cast<int64_t*>(info + p.n);
+  uint8_t* packed = reinterpret_cast<uint8_t*>(info) + tc_seqs(p.n);
   const uint32_t sm = smem_u32(smp);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, cta = blockIdx.x;
   if (threadIdx.x == kLoadWarp * 32) {
     for (int i = 0; i < 8; ++i) {
-      mbar_init(smem_u32(&m->full[i]), 1);
+      mbar_init(smem_u32(&m->full[i]), kQ4 ? kUnpackWarps : 1);
       mbar_init(smem_u32(&m->empty[i]), 2);
     }
     for (int i = 0; i < kAhead; ++i) {
       mbar_init(smem_u32(&m->seg_full[i]), 1);
       mbar_init(smem_u32(&m->seg_empty[i]), 11);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(smem_u32(&m->packed_full[i]), 1);
+      mbar_init(smem_u32(&m->packed_empty[i]), kUnpackWarps);
     }
     for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&m->lone_full[i]), 4);
     mbar_init(smem_u32(&m->drain), 2);
@@ -655,14 +825,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     m->abort = 0;
     fence_barrier_init();
     tma_prefetch_desc(&mq);
-    tma_prefetch_desc(&mk);
-    tma_prefetch_desc(&mv);
+    if (!kQ4) {
+      tma_prefetch_desc(&mk);
+      tma_prefetch_desc(&mv);
+    }
   }
   if (warp == kMmaWarp) tmem_alloc(smem_u32(&m->tmem), 512);
   griddep_wait();
   griddep_launch();
   if (warp == 0) {
-    const PrefixSched sc = build_sched<kTiles, kKeys>(p, m->line_base, m->info, cta == 0);
+    const PrefixSched sc = build_sched<kTiles, kKeys>(p, line_base, info, cta == 0);
     if (lane == 0) m->sched = sc;
   }
   tc_fence_before();
@@ -670,18 +842,30 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = m->tmem;
   const SegReader segs{m, p.err};
-  // registers: 384 threads x 168 at launch = 256 x 200 (softmax) + 128 x 96 and some left over
+  // registers: 384 threads x 168 at launch = 256 x 200 (softmax) + 128 x 96 and some left over;
+  // with the unpacking warps 512 x 128 = 256 x 184 + 256 x 72
   if (warp >= kLoadWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
-    if (warp == kLoadWarp)
-      load_role<HD>(p, &mq, &mk, &mv, sm, m, segs);
+    if constexpr (kQ4)
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    else
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+    if (warp == kLoadWarp) {
+      if constexpr (kQ4)
+        load_packed_role<HD>(p, &mq, sm, packed, count, m, segs);
+      else
+        load_role<HD>(p, &mq, &mk, &mv, sm, m, segs);
+    } else if (kQ4 && warp >= kUnpackWarp)
+      unpack_role<HD>(p, warp - kUnpackWarp, smp, packed, count, m);
     else if (warp < kMmaWarp + 2)
       mma_role<HD>(p, warp - kMmaWarp, sm, tmem, m, segs);
     else
-      plan_role(p, m);
+      plan_role(p, m, line_base, info);
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
-    softmax_role<HD>(p, warp >> 2, smp, tmem, m, segs);
+    if constexpr (kQ4)
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    else
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
+    softmax_role<HD, kQ4>(p, warp >> 2, smp, tmem, m, segs);
   }
   tc_fence_before();
   __syncthreads();
@@ -704,35 +888,56 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
 }
 
+// The most sequences that leave room for so many packed tiles.
 template <int HD>
+constexpr int most_seqs(int packed) {
+  int n = kPrefixMaxSeqs;
+  while (n > 0 && tc_smem<HD>(n, packed) > kMostSmem) --n;
+  return n;
+}
+
+template <int HD, bool kQ4>
 int launch(const PrefixAttnParams& p, cudaStream_t s) {
   static bool set[8] = {};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return LSP_ERR_CUDA;
   if (dev >= 8 || !set[dev]) {
-    if (cudaFuncSetAttribute(prefix_attn_tc_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc_smem<HD>()) != cudaSuccess)
+    if (cudaFuncSetAttribute(prefix_attn_tc_kernel<HD, kQ4>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem) != cudaSuccess)
       return LSP_ERR_CUDA;
     if (dev < 8) set[dev] = true;
   }
-  CUtensorMap mq, mk, mv;
+  constexpr int four = most_seqs<HD>(4), three = most_seqs<HD>(3);
+  const int packed = !kQ4 ? 0 : p.n <= four ? 4 : p.n <= three ? 3 : 2;
+  CUtensorMap mq = {}, mk = {}, mv = {};
   int rc;
   {
     const uint64_t dims[3] = {HD, (uint64_t)p.nq, (uint64_t)p.total}, st[2] = {HD * 2, (uint64_t)p.q_stride * 2};
     const uint32_t box[3] = {64, (uint32_t)p.rep, (uint32_t)p.tok_tile};
     if ((rc = tmap_bf16_sw128(&mq, p.q, 3, dims, st, box)) != LSP_OK) return rc;
   }
-  const uint64_t dims[4] = {HD, (uint64_t)p.page, (uint64_t)p.nkv, (uint64_t)p.pages};
-  const uint64_t st[3] = {(uint64_t)p.s_slot * 2, (uint64_t)p.s_head * 2, (uint64_t)p.s_page * 2};
-  const uint32_t box[4] = {64, (uint32_t)std::min(p.page, kKeys), 1, 1};
-  if ((rc = tmap_bf16_sw128(&mk, p.k, 4, dims, st, box)) != LSP_OK || (rc = tmap_bf16_sw128(&mv, p.v, 4, dims, st, box)) != LSP_OK)
-    return rc;
-  return launch_pdl(prefix_attn_tc_kernel<HD>, dim3(p.grid), dim3(kThreads), tc_smem<HD>(), s, mq, mk, mv, p) == cudaSuccess
+  if constexpr (!kQ4) {
+    const uint64_t dims[4] = {HD, (uint64_t)p.page, (uint64_t)p.nkv, (uint64_t)p.pages};
+    const uint64_t st[3] = {(uint64_t)p.s_slot * 2, (uint64_t)p.s_head * 2, (uint64_t)p.s_page * 2};
+    const uint32_t box[4] = {64, (uint32_t)std::min(p.page, kKeys), 1, 1};
+    if ((rc = tmap_bf16_sw128(&mk, p.k, 4, dims, st, box)) != LSP_OK || (rc = tmap_bf16_sw128(&mv, p.v, 4, dims, st, box)) != LSP_OK)
+      return rc;
+  }
+  return launch_pdl(prefix_attn_tc_kernel<HD, kQ4>, dim3(p.grid), dim3(kThreads<kQ4>), tc_smem<HD>(p.n, packed), s, mq, mk, mv, p,
+                    packed) == cudaSuccess
              ? LSP_OK
              : LSP_ERR_CUDA;
 }
 
 }  // namespace
 
-int launch_prefix_attn_tc(const PrefixAttnParams& p, cudaStream_t s) { return p.d == 128 ? launch<128>(p, s) : launch<64>(p, s); }
+int prefix_tc_q4_seqs(int d) {
+  constexpr int wide = most_seqs<128>(2), narrow = most_seqs<64>(2);
+  return d == 128 ? wide : narrow;
+}
+
+int launch_prefix_attn_tc(const PrefixAttnParams& p, cudaStream_t s) {
+  if (p.q4) return p.d == 128 ? launch<128, true>(p, s) : launch<64, true>(p, s);
+  return p.d == 128 ? launch<128, false>(p, s) : launch<64, false>(p, s);
+}
 
 }  // namespace lsp

@@ -297,6 +297,12 @@ int launch_pages_read(const KvCache& c, const int* seqs, const int* start, int n
                       int total, int es, bool q4, unsigned* err, cudaStream_t s);
 
 // ------------------------------------------------------------------ shared-prefix attention
+constexpr int kPrefixTogether = 4;   // key blocks that a cut keeps together (prefix_sched.cuh)
+constexpr int kPrefixInverseBits = 26;
+struct PrefixCosts {
+  int few_rows, few, many, segment;  // each cost * kPrefixTogether below 2^(32 - kPrefixInverseBits)
+  uint32_t inverse[4];               // ceil(2^32 / x) for x = few, few * kPrefixTogether, many, many * kPrefixTogether
+};
 struct PrefixAttnParams {
   const char* k;            // the layer's pools
   const char* v;
@@ -316,10 +322,12 @@ struct PrefixAttnParams {
   unsigned* err;
   // plan (prefix_attn_plan) and workspace
   int tok_tile;             // rows of q (tokens) in a tile: tile rows / rep
+  bool tc;                  // on the tensor cores' own memory (k_prefix_attn_tc.cu)
   int units;                // units of tiles that cover all rows
   int splits;               // key ranges of the shared pages
   int num_sms;
   int grid;                 // CTAs of the main kernel
+  PrefixCosts cost;         // of the chosen kernel
   int64_t part_rows;        // rows of partial results the workspace holds
   float* part_o;            // [part_rows][d] unnormalised sums
   float2* part_ml;          // [part_rows] (running maximum of the base-2 scores, sum)
@@ -327,10 +335,12 @@ struct PrefixAttnParams {
 constexpr int kPrefixMaxSeqs = 1024;
 constexpr int kPrefixMaxRep = 64;
 constexpr int kPrefixMaxGrid = 1024;  // CTAs of the main kernel
-// Fills the plan fields; returns the workspace bytes.
+// Fills the plan fields; returns the workspace bytes (of the chosen kernel; of any that the call may take).
 size_t prefix_attn_plan(PrefixAttnParams* p, int dtype, int num_sms);
-// bf16 on the tensor cores; the joining kernel is the caller's.
+size_t prefix_attn_workspace(PrefixAttnParams p, int dtype, int num_sms);
+// rows of bf16, over a cache of bf16 or in 4 bits, on the tensor cores; the joining kernel is the caller's.
 int launch_prefix_attn_tc(const PrefixAttnParams& p, cudaStream_t s);
+int prefix_tc_q4_seqs(int d);         // sequences it has room for, over a cache in 4 bits
 constexpr int kPrefixTcRows = 128, kPrefixTcKeys = 128, kPrefixTcTiles = 2;   // tile rows, key block, tiles of a unit
 // rows of bf16 or f32 over a cache in 4 bits
 int launch_prefix_attn_q4(const PrefixAttnParams& p, int dtype, cudaStream_t s);

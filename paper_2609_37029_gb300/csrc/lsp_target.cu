@@ -109,7 +109,7 @@ size_t attn_workspace(const lsp_kv_cache* cache, int dtype, int nq, int n, int t
   PrefixAttnParams p = {};
   int sms = 0;
   if (check_shape(cache) != LSP_OK || attn_shape(cache, nq, n, total, &p) != LSP_OK || num_sms(&sms) != LSP_OK) return 0;
-  return total == 0 ? 0 : prefix_attn_plan(&p, dtype, sms);
+  return total == 0 ? 0 : prefix_attn_workspace(p, dtype, sms);
 }
 
 int attention(const lsp_kv_cache* cache, int layer, const void* q, int dtype, int64_t q_stride, int nq, const int32_t* seqs,

@@ -51,19 +51,15 @@ struct PrefixSched {
   int together;         // key blocks that a cut keeps together in a short item
 };
 
-// What work costs a CTA, for dealing it out, in units of 0.37 us: a key block
-// against one and against two row tiles (1.1 and 1.46 us measured at 16 requests
-// over 32K), and what a segment takes besides (1.9 us).  The fp32 kernel's warps
-// have eight rows each, and those without rows leave the block to the others.
-constexpr int kCostOne = 3, kCostTwo = 4, kCostSegment = 5;
+// What work costs a CTA, for dealing it out, is the kernel's (PrefixCosts): a key
+// block against few and against many rows, and what a segment takes besides.
+//
 // A segment of the tensor cores costs as much as two blocks, so a cut leaves four
 // together in a short item (of up to kShort), unless there is less work than CTAs;
-// a block of the fp32 kernel takes longer than what comes with it.
-constexpr int kTogether = 4, kShort = 8;
-template <int kUnitTiles>
+// a block of the other kernels takes longer than what comes with it.
+constexpr int kTogether = kPrefixTogether, kShort = 8;
 __device__ __forceinline__ int block_cost(const PrefixAttnParams& p, int tokens) {
-  if (kUnitTiles == 1) return tokens * p.rep > 32 ? kCostTwo : kCostOne;
-  return tokens > p.tok_tile ? kCostTwo : kCostOne;
+  return tokens * p.rep > p.cost.few_rows ? p.cost.many : p.cost.few;
 }
 struct __align__(16) PrefixSeq {
   int seq, first, rows, len;    // row of the table (-1: none), first row of q, rows, tokens
@@ -125,7 +121,7 @@ __device__ __forceinline__ int own_units(const PrefixAttnParams& p, const Prefix
 // Length on the line of an own item of a unit with `blocks` key blocks:
 template <int kUnitTiles>
 __device__ __forceinline__ int item_length(const PrefixAttnParams& p, const PrefixSeq& r, int u, int blocks) {
-  return blocks > 0 ? kCostSegment + blocks * block_cost<kUnitTiles>(p, r.rows - u * kUnitTiles * p.tok_tile) : 0;
+  return blocks > 0 ? p.cost.segment + blocks * block_cost(p, r.rows - u * kUnitTiles * p.tok_tile) : 0;
 }
 
 // Built by one warp of every CTA; line_base [n + 1], info [n] in shared memory.
@@ -151,8 +147,8 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
   s.items = s.blocks > 0 ? p.nkv * p.splits * p.units : 0;
   s.whole = s.items / p.grid * p.grid;
   const int most = s.range + (s.longer > 0);
-  s.len_two = kCostSegment + most * kCostTwo;
-  s.len_last = kCostSegment + most * block_cost<kUnitTiles>(p, p.total - (p.units - 1) * kUnitTiles * p.tok_tile);
+  s.len_two = p.cost.segment + most * p.cost.many;
+  s.len_last = p.cost.segment + most * block_cost(p, p.total - (p.units - 1) * kUnitTiles * p.tok_tile);
   s.len_range = (int64_t)(p.units - 1) * s.len_two + s.len_last;
   s.whole_line = (int64_t)(s.whole / p.units) * s.len_range + (int64_t)(s.whole % p.units) * s.len_two;
   s.shared_line = (int64_t)(s.items / p.units) * s.len_range - s.whole_line;
@@ -177,8 +173,8 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
   }
   if (lane == 0) line_base[p.n] = line;
   s.line = s.shared_line + line;
-  const int least = kCostOne;
-  const bool small = s.line < (int64_t)p.grid * (kCostSegment + kTogether * least);
+  const int least = p.cost.few;
+  const bool small = s.line < (int64_t)p.grid * (p.cost.segment + kTogether * least);
   s.together = kUnitTiles == 1 || small ? 1 : kTogether;
   s.ctas = small ? max(min((int)s.line / least, p.grid), 1) : p.grid;
   return s;
@@ -237,14 +233,13 @@ struct PrefixSeg {
 // Key blocks of an item of the line (of `blocks`, each of `cost`) that belong to
 // the places before `at` of it: single ones or groups, the first with the
 // segment's cost, go to where they begin.
-__device__ __forceinline__ int blocks_before(const PrefixSched& s, int64_t at, int blocks, int cost) {
-  if (at <= kCostSegment) return at > 0 ? min(blocks <= kShort ? s.together : 1, blocks) : 0;
+__device__ __forceinline__ int blocks_before(const PrefixAttnParams& p, const PrefixSched& s, int64_t at, int blocks, int cost) {
+  if (at <= p.cost.segment) return at > 0 ? min(blocks <= kShort ? s.together : 1, blocks) : 0;
   const int together = blocks <= kShort ? s.together : 1, group = together * cost;
-  const int64_t n = at - kCostSegment + group - 1;
+  const int64_t n = at - p.cost.segment + group - 1;
   // n / group, by ceil(2^32 / group): exact below 2^32 / group
-  static_assert(kCostOne == 3 && kCostTwo == 4 && kTogether == 4, "the groups' inverses");
-  const uint32_t inverse = cost == kCostOne ? (together == 1 ? 1431655766u : 357913942u) : (together == 1 ? 1u << 30 : 1u << 28);
-  const int64_t groups = n < (1 << 28) ? (int64_t)__umulhi((uint32_t)n, inverse) : long_div(n, group);
+  const uint32_t inverse = p.cost.inverse[(cost == p.cost.few ? 0 : 2) + (together > 1)];
+  const int64_t groups = n < (1 << kPrefixInverseBits) ? (int64_t)__umulhi((uint32_t)n, inverse) : long_div(n, group);
   return (int)min(groups * together, (int64_t)blocks);
 }
 
@@ -287,13 +282,13 @@ struct PrefixSegs {
         gs = (int)div_floor(place, s.len_range);
         const int64_t rel = place - gs * s.len_range;
         u = (int)min(div_floor(rel, s.len_two), (int64_t)(p.units - 1));
-        const int cost = u + 1 < p.units ? kCostTwo : block_cost<kUnitTiles>(p, p.total - u * kUnitTiles * p.tok_tile);
+        const int cost = u + 1 < p.units ? p.cost.many : block_cost(p, p.total - u * kUnitTiles * p.tok_tile);
         const int64_t to = rel - (int64_t)u * s.len_two + 1, from = max(to - (mid - x), (int64_t)0);
         mid -= to - from;
         split = gs % p.splits;
         const int blocks = range_blocks(s, split);
-        c0 = blocks_before(s, from, blocks, cost);
-        c1 = blocks_before(s, to, blocks, cost);
+        c0 = blocks_before(p, s, from, blocks, cost);
+        c1 = blocks_before(p, s, to, blocks, cost);
       } else {
         x = max(x, min(end, s.shared_line));
         return false;
@@ -334,9 +329,9 @@ struct PrefixSegs {
       g.head = (int)div_floor(rel, len);
       const int64_t from = rel - g.head * len, to = min(len, from + (end - x));
       x += to - from;
-      const int i0 = u * kUnitTiles * p.tok_tile, cost = block_cost<kUnitTiles>(p, r.rows - i0);
-      g.kb0 = blocks_before(s, from, blocks, cost);
-      g.kb1 = blocks_before(s, to, blocks, cost);
+      const int i0 = u * kUnitTiles * p.tok_tile, cost = block_cost(p, r.rows - i0);
+      g.kb0 = blocks_before(p, s, from, blocks, cost);
+      g.kb1 = blocks_before(p, s, to, blocks, cost);
       if (g.kb0 >= g.kb1) continue;
       g.tab = p.table + (size_t)r.seq * p.max_pages;
       g.t0 = r.first + i0;

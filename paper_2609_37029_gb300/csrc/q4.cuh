@@ -12,6 +12,19 @@
 namespace lsp {
 
 constexpr int kQ4Group = 32;
+
+template <bool kX>
+struct BoolTag {
+  static constexpr bool value = kX;
+};
+
+// A run of a block's codes or scales into shared memory (addresses and bytes multiples of 16).
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+
 constexpr uint32_t kQ4Zero = 0x88888888u;        // eight codes of 0
 
 __device__ __forceinline__ uint32_t bf2_bits(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t*>(&x); }
