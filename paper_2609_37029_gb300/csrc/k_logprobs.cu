@@ -7,51 +7,63 @@
 // One pass: every thread keeps (m, S, A) of its elements and moves them to a higher
 // m as 2^t times (S, A + S t).
 //
-// The k largest, from the same pass: a thread has a stripe of the row (every 256th
-// piece of 16 bytes), whose largest logit and its first place it knows at the end.
-// Each of the k largest elements is in one of the k stripes whose first are the
-// largest -- an element in any other stripe has k elements before it -- so those
-// stripes alone are read again (k of 256, mostly from L2), and what comes at or
-// before the k-th stripe's first goes to a list, some more than k elements as a
-// rule, which is ranked by counting.  Places decide between equal logits all the
-// way.  Should the list overflow (a row made for it: thousands of large elements in
-// few stripes), the elements are taken one at a time instead, k passes over L2.
+// The k largest, from the same pass: a thread has a stripe of the CTA's part (every
+// 128th piece of 16 bytes), of which it knows at the end the piece with the largest
+// logit (the first of several), and the largest of the others.  Each of the k largest
+// elements is in one of the k stripes whose first are the largest -- an element in any
+// other stripe has k elements before it -- so of those stripes the piece with the
+// largest is read again, and the whole stripe where another piece reaches the k-th
+// stripe's first too (a few of a hundred).  What comes at or before that goes to a
+// list, some more than k elements as a rule, which is ranked by counting.  Places
+// decide between equal logits all the way.  Should the list overflow (a row made for
+// it: hundreds of large elements in few stripes), the elements are taken one at a time
+// instead, k passes over L2.
 //
-// A row is split over a cluster of CTAs, whose first joins the parts out of the
-// others' shared memory: no workspace, no second launch.
-//
-// Bound by memory.
+// A row is split over a cluster of CTAs, which hand their parts to the first of them
+// through its shared memory: no workspace, no second launch.  The CTAs stay for as
+// many rows as fall to them; a warp of each copies the rows' next pieces into a ring
+// meanwhile (40 KB, four CTAs on an SM), so that memory is read on while a row's last
+// steps, which are rounds of latency, are taken.
 #include <algorithm>
+#include <cstddef>
 
-#include <cooperative_groups.h>
-
-#include "common.cuh"
+#include "barrier_wait.cuh"
 #include "lsp_internal.h"
+#include "q4.cuh"
 
 namespace lsp {
 namespace {
 
-namespace cg = cooperative_groups;
-
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kThreads = 128, kWarps = kThreads / 32;      // that add up; a warp more loads, and one joins a row's parts
 constexpr int kMaxCluster = 8;
-constexpr int kAhead = 4;                        // 16-byte pieces a thread has in flight
-constexpr int kList = 1024;                      // candidates of a CTA
+constexpr int kPerSm = 4;
+constexpr int kRounds = 4;                       // pieces of a thread in a stage
+constexpr int kStages = 5, kStageBytes = kRounds * kThreads * 16;
+constexpr int kStripes = kThreads;               // of a CTA's part: stripe i, of thread i, has its pieces i, i + kStripes, ...
+constexpr int kList = 512;                       // candidates of a CTA
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLeast = -150.0f;                // 2^t is 0 from here on
 constexpr float kLowest = -3.402823466e38f;
 
+// What a CTA has of a row, in the shared memory of its cluster's first.
+struct Partial {
+  float m, s, a;
+  unsigned long long sorted[kLogprobsMaxK];      // its k largest elements: key and place, 0: none
+};
+
 struct Smem {
+  alignas(128) uint8_t ring[kStages][kStageBytes];
+  Partial part[2][kMaxCluster];                  // by turns
   unsigned long long list[kList];
-  unsigned long long sorted[kLogprobsMaxK];      // of the CTA: key and place, 0: none
-  unsigned long long all[kMaxCluster * kLogprobsMaxK];
-  uint32_t stripe[kThreads];
+  unsigned long long sorted[kLogprobsMaxK];
+  uint32_t stripe[kStripes];
   float red[kWarps];
   float2 red2[kWarps];
   unsigned long long best[kWarps];
   uint32_t least[kWarps];
-  int count, stripes;
-  float m, s, a;
+  uint64_t full[kStages], empty[kStages];
+  uint64_t parts[2], taken[2];                   // the cluster's parts of a row are there; the first has read them
+  int count, stripes, abort;
 };
 
 __device__ __forceinline__ float ex2a(float x) {
@@ -65,13 +77,20 @@ __device__ __forceinline__ float max_nan(float a, float b) {     // NaN if eithe
   return y;
 }
 
-// Whole numbers that order as the logits do (-0 as 0; NaN below all); 0 stands for no element.
+// Whole numbers of a type's width that order as its logits do (-0 as 0; NaN below all); 0 stands for no element.
+template <typename T>
+constexpr int kKeyBits = 8 * (int)sizeof(T);
+template <typename T>
 __device__ __forceinline__ uint32_t key_of(float x) {
   if (x != x) return 1u;
   const uint32_t u = __float_as_uint(x + 0.0f);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  return (u & 0x80000000u ? ~u : u | 0x80000000u) >> (32 - kKeyBits<T>);
 }
-__device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
+template <typename T>
+__device__ __forceinline__ float of_key(uint32_t k) {
+  k <<= 32 - kKeyBits<T>;
+  return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k & (sizeof(T) == 2 ? 0xFFFF0000u : 0xFFFFFFFFu));
+}
 // Key and place in one: the larger, and of equal ones the first, is the larger.
 __device__ __forceinline__ unsigned long long entry(uint32_t key, uint32_t at) { return (unsigned long long)key << 32 | ~at; }
 
@@ -90,6 +109,10 @@ struct Vec {
       }
     }
   }
+  __device__ static __forceinline__ uint4 none() {
+    const uint32_t inf = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+    return make_uint4(inf, inf, inf, inf);
+  }
   // the largest and the smallest, NaN aside
   __device__ static __forceinline__ void range(const uint4& v, const float* x, float* top, float* low) {
     if constexpr (sizeof(T) == 2) {
@@ -105,21 +128,15 @@ struct Vec {
 };
 
 // A CTA's part of a row, in places: the row's elements before its first 16-byte
-// boundary (place tid < head), the part's pieces (places kThreads + i), and the
+// boundary (place tid < head), the part's pieces (places kStripes + i), and the
 // elements behind the last piece (from place `tail_at` on).  Places rise with the index.
 template <typename T>
 struct Part {
   const T* z;
   int head, body, first, pieces, tail, tail_at;  // body: index of the row's first piece; first: of the part's, in pieces
-  __device__ __forceinline__ uint4 piece(uint32_t place) const {
-    return __ldcg(reinterpret_cast<const uint4*>(z + body) + (first + (int)(place - kThreads)));
-  }
-  __device__ __forceinline__ int index(uint32_t place) const {   // of a place's first element
-    if (place < kThreads) return (int)place;
-    if (place < (uint32_t)tail_at) return body + (first + (int)(place - kThreads)) * Vec<T>::kElems;
-    return tail_index + (int)(place - tail_at);
-  }
   int tail_index;
+  __device__ __forceinline__ uint4 piece(int i) const { return __ldcg(reinterpret_cast<const uint4*>(z + body) + (first + i)); }
+  __device__ __forceinline__ int index(int i) const { return body + (first + i) * Vec<T>::kElems; }   // of a piece's first element
 };
 
 struct Scale {
@@ -127,10 +144,12 @@ struct Scale {
   float large;          // logits up to here leave every t finite
 };
 
-// Of a thread's elements: the largest logit and its place, and the sums relative to `m`.
+// Of a thread's elements: the sums relative to `m`; of its stripe the largest logit, its piece's place, and the largest
+// of the other pieces.
 struct Stats {
-  float m, best;
+  float m, reach;
   float2 s, a;          // of every other element, to be added
+  float best, other;
   uint32_t place;
 };
 
@@ -165,17 +184,20 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   return d;
 }
 
-// Elements x, of which top and low are the largest and the smallest (NaN aside).  As
-// long as logits stay within +-large, every t is finite, and e t = 0 where e = 0.
-// What is below (-inf, a banned token) is raised to where e is 0 already; a row of
-// larger numbers takes its steps one by one with t limited.
+// Elements x, of which top and low are the largest and the smallest (NaN aside).  The
+// sums move to a higher m when an element exceeds theirs by 2^8 (they are fp32: what
+// is added meanwhile loses nothing).  As long as logits stay within +-large, every t
+// is finite, and e t = 0 where e = 0.  What is below (-inf, a banned token) is raised
+// to where e is 0 already; a row of larger numbers takes its steps one by one with t
+// limited.
 template <int N>
 __device__ __forceinline__ void add_elems(Stats& st, float* x, float top, float low, const Scale& k) {
-  if (top > st.m) {
+  if (top > st.reach) {
     const float t = max_nan((st.m - top) * k.c, kLeast), r = ex2a(t);
     st.a = make_float2(r * (st.a.x + st.s.x * t), r * (st.a.y + st.s.y * t));
     st.s = make_float2(r * st.s.x, r * st.s.y);
     st.m = top;
+    st.reach = top + 8.0f * k.inv;
   }
   if (!(low > -k.large) || fabsf(st.m) > k.large) {
     if (fabsf(st.m) > k.large) {
@@ -195,48 +217,66 @@ __device__ __forceinline__ void add_elems(Stats& st, float* x, float top, float 
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = max_nan(x[i], least);
   }
+  float2 s[2] = {st.s, {0.f, 0.f}}, a[2] = {st.a, {0.f, 0.f}};
 #pragma unroll
   for (int i = 0; i < N; i += 2) {
     const float2 t = mul2s(add2s(x[i], x[i + 1], -st.m), k.c), e = make_float2(ex2a(t.x), ex2a(t.y));
-    st.s = add2(st.s, e);
-    st.a = fma2(e, t, st.a);
+    s[(i >> 1) & 1] = add2(s[(i >> 1) & 1], e);
+    a[(i >> 1) & 1] = fma2(e, t, a[(i >> 1) & 1]);
   }
+  st.s = add2(s[0], s[1]);
+  st.a = add2(a[0], a[1]);
 }
 
-__device__ __forceinline__ void add_one(Stats& st, float x, uint32_t place, const Scale& k) {
-  if (x > st.best) st.best = x, st.place = place;
+__device__ __forceinline__ void add_one(Stats& st, float x, const Scale& k) {
   float pair[2] = {x, -INFINITY};
   add_elems<2>(st, pair, x, -INFINITY, k);
+}
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Among the threads that add up.
+__device__ __forceinline__ void meet() { named_bar(1, kThreads); }
+__device__ __forceinline__ int count_all(bool x) {
+  int n;
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.popc.aligned.u32 %0, 1, %2, p;\n}"
+      : "=r"(n)
+      : "r"((uint32_t)x), "n"(kThreads)
+      : "memory");
+  return n;
 }
 
 __device__ __forceinline__ unsigned long long block_max(unsigned long long v, Smem& sm) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
-  __syncthreads();
+  meet();
   if (lane == 0) sm.best[warp] = v;
-  __syncthreads();
+  meet();
   v = sm.best[lane & (kWarps - 1)];
 #pragma unroll
   for (int o = kWarps / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
   return v;
 }
 
-// sm.sorted = the k largest elements of the part (0 where it has fewer).
+// sm.sorted = the k largest elements of the part (0 where it has fewer); head, tail: this thread's single elements.
 template <typename T>
-__device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, int k, Smem& sm) {
+__device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, float head, float tail, int k, Smem& sm) {
   constexpr int VE = Vec<T>::kElems;
-  const int tid = threadIdx.x;
-  const int rounds = (part.pieces + kThreads - 1) / kThreads;    // pieces of a stripe
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int rounds = (part.pieces + kStripes - 1) / kStripes;    // pieces of a stripe
   const bool some = tid < part.head || tid < part.pieces || tid < part.tail;
-  const uint32_t key = some ? key_of(st.best) : 0u;
+  const uint32_t key = some ? key_of<T>(st.best) : 0u;
   if (tid == 0) sm.count = sm.stripes = 0;
   if (tid < k) sm.sorted[tid] = 0;
   // the largest `cut` that k stripes reach, bit by bit; among equal ones, the place that makes them k
   uint32_t cut = 0, last = 0xFFFFFFFFu;
-  int reach = kThreads;
-  for (uint32_t bit = 1u << 31; bit; bit >>= 1) {
-    const int n = __syncthreads_count(key >= (cut | bit));
+  int reach = kStripes;
+  for (uint32_t bit = 1u << (kKeyBits<T> - 1); bit; bit >>= 1) {
+    const int n = count_all(key >= (cut | bit));
     if (n >= k) {
       cut |= bit;
       reach = n;
@@ -245,43 +285,56 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, i
   }
   if (reach == k) {                              // the least of theirs
     const uint32_t least = __reduce_min_sync(0xffffffffu, key >= cut ? key : 0xFFFFFFFFu);
-    if ((tid & 31) == 0) sm.least[tid >> 5] = least;
-    __syncthreads();
-    cut = __reduce_min_sync(0xffffffffu, sm.least[tid & (kWarps - 1)]);
+    if (lane == 0) sm.least[warp] = least;
+    meet();
+    cut = __reduce_min_sync(0xffffffffu, sm.least[lane & (kWarps - 1)]);
   } else if (cut > 0) {
-    uint32_t below = 0;                          // places < below leave less than k stripes
-    for (uint32_t bit = 1u << 31; bit; bit >>= 1) {
-      const uint32_t x = below | bit;
-      if (__syncthreads_count(key > cut || (key == cut && st.place < x)) < k) below = x;
-    }
-    last = below;
+    last = 0;                                    // places below it leave less than k stripes
+    for (uint32_t bit = 1u << (31 - __clz(part.tail_at + kStripes)); bit; bit >>= 1)
+      if (count_all(key > cut || (key == cut && st.place < (last | bit))) < k) last |= bit;
   }
   auto in = [&](uint32_t e_key, uint32_t place) { return e_key > cut || (e_key == cut && place <= last); };
-  if (some && in(key, st.place)) sm.stripe[atomicAdd(&sm.stripes, 1)] = tid;
-  __syncthreads();
-  const int per = rounds + 2;                    // places of a stripe
   auto put = [&](float x, uint32_t place, int index) {
-    const uint32_t e = key_of(x);
+    const uint32_t e = key_of<T>(x);
     if (!in(e, place)) return;
     const int at = atomicAdd(&sm.count, 1);
     if (at < kList) sm.list[at] = entry(e, (uint32_t)index);
   };
-  for (int i = tid; i < sm.stripes * per; i += kThreads) {
-    const int stripe = (int)sm.stripe[i / per], j = i % per;
-    if (j == 0) {
-      if (stripe < part.head) put(to_f(part.z[stripe]), stripe, stripe);
-    } else if (j <= rounds) {
-      const uint32_t place = (uint32_t)j * kThreads + stripe;
-      if ((j - 1) * kThreads + stripe >= part.pieces) continue;
-      float x[VE];
-      Vec<T>::unpack(part.piece(place), x);
+  auto put_piece = [&](const uint4& v, int i) {
+    float x[VE];
+    Vec<T>::unpack(v, x);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) put(x[e], place, part.index(place) + e);
-    } else if (stripe < part.tail) {
-      put(to_f(part.z[part.tail_index + stripe]), part.tail_at + stripe, part.tail_index + stripe);
+    for (int e = 0; e < VE; ++e) put(x[e], kStripes + i, part.index(i) + e);
+  };
+  if (some && in(key, st.place)) {
+    if (tid < part.head) put(head, tid, tid);
+    if (tid < part.tail) put(tail, part.tail_at + tid, part.tail_index + tid);
+    // (another piece with the largest logit lies behind, and has the place to decide; a single element counts as a piece)
+    if (key_of<T>(st.other) >= cut)
+      sm.stripe[atomicAdd(&sm.stripes, 1)] = tid;
+    else if (st.place >= kStripes && st.place < (uint32_t)part.tail_at)
+      put_piece(part.piece((int)st.place - kStripes), (int)st.place - kStripes);
+  }
+  meet();
+  // a warp takes stripes in turn, a lane every 32nd piece, some of them in flight together
+  constexpr int kOnce = 4;
+  const int stripes = sm.stripes;
+  for (int x = warp; x < stripes; x += kWarps) {
+    const int stripe = (int)sm.stripe[x];
+    for (int j = lane; j - lane < rounds; j += 32 * kOnce) {
+      uint4 v[kOnce];
+      int at[kOnce];                             // of the part's pieces
+#pragma unroll
+      for (int q = 0; q < kOnce; ++q) {
+        at[q] = (j + 32 * q) * kStripes + stripe;
+        if (at[q] < part.pieces) v[q] = part.piece(at[q]);
+      }
+#pragma unroll
+      for (int q = 0; q < kOnce; ++q)
+        if (at[q] < part.pieces) put_piece(v[q], at[q]);
     }
   }
-  __syncthreads();
+  meet();
   const int n = sm.count;
   if (n <= kList) {
     for (int i = tid; i < n; i += kThreads) {
@@ -290,22 +343,22 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, i
       for (int j = 0; j < n; ++j) rank += sm.list[j] > mine;
       if (rank < k) sm.sorted[rank] = mine;
     }
-    __syncthreads();
+    meet();
     return;
   }
   unsigned long long before = ~0ull;
   for (int r = 0; r < k; ++r) {
     unsigned long long best = 0;
     auto see = [&](float x, int index) {
-      const unsigned long long e = entry(key_of(x), (uint32_t)index);
+      const unsigned long long e = entry(key_of<T>(x), (uint32_t)index);
       if (e < before && e > best) best = e;
     };
     if (tid < part.head) see(to_f(part.z[tid]), tid);
     for (int i = tid; i < part.pieces; i += kThreads) {
       float x[VE];
-      Vec<T>::unpack(part.piece(kThreads + i), x);
+      Vec<T>::unpack(part.piece(i), x);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) see(x[e], part.index(kThreads + i) + e);
+      for (int e = 0; e < VE; ++e) see(x[e], part.index(i) + e);
     }
     if (tid < part.tail) see(to_f(part.z[part.tail_index + tid]), part.tail_index + tid);
     best = block_max(best, sm);
@@ -313,34 +366,41 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, i
     before = best;
     if (best == 0) break;
   }
-  __syncthreads();
+  meet();
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobsParams p, int cluster) {
-  constexpr int VE = Vec<T>::kElems;
-  __shared__ Smem sm;
-  griddep_wait();
-  griddep_launch();
-  cg::cluster_group group = cg::this_cluster();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int row = blockIdx.x / cluster, rank = blockIdx.x - row * cluster;
-  const int token = p.tokens[row];
-  if (token < 0 || token >= p.V) {               // (every CTA of the cluster)
-    if (rank > 0) return;
-    if (tid < p.k) {
-      if (p.top) p.top[(int64_t)row * p.k + tid] = -1;
-      if (p.top_logprob) p.top_logprob[(int64_t)row * p.k + tid] = -INFINITY;
+// The rows with a token that fall to cluster `mine` of `clusters`, in order; for whole warps.
+struct Rows {
+  const int32_t* tokens;
+  int rows, V, clusters;
+  int skip;                                      // rows with a token until the next of this cluster's
+  int at = 0, token = -1;                        // the next 32 rows; token: of the lane's row
+  unsigned left = 0;
+  __device__ __forceinline__ bool valid(int t) const { return t >= 0 && t < V; }
+  __device__ __forceinline__ int next(int* of) { // -1: no more
+    for (;;) {
+      const int n = __popc(left);
+      if (n > skip) {
+        for (; skip > 0; --skip) left &= left - 1;
+        const int lane = __ffs(left) - 1;
+        left &= left - 1;
+        skip = clusters - 1;
+        *of = __shfl_sync(0xffffffffu, token, lane);
+        return at - 32 + lane;
+      }
+      skip -= n;
+      if (at >= rows) return -1;
+      const int r = at + (threadIdx.x & 31);
+      token = r < rows ? tokens[r] : -1;
+      left = __ballot_sync(0xffffffffu, valid(token));
+      at += 32;
     }
-    if (tid == 0) {
-      p.logprob[row] = -INFINITY;
-      if (p.entropy) p.entropy[row] = 0.f;
-      if (token != -1) set_err(p.err, LSP_DEV_BAD_TOKEN);
-    }
-    return;
   }
-  const float c = kLog2e / p.temperature;
-  const Scale scale = {c, p.temperature * 0.69314718055994531f, 1e38f / fmaxf(c, 1.0f)};
+};
+
+template <typename T>
+__device__ __forceinline__ Part<T> part_of(const LogprobsParams& p, int row, int rank, int cluster) {
+  constexpr int VE = Vec<T>::kElems;
   Part<T> part;
   part.z = static_cast<const T*>(p.z) + (int64_t)row * p.ld;
   const int off = (int)((16 - (reinterpret_cast<uintptr_t>(part.z) & 15)) & 15) / (int)sizeof(T);
@@ -351,115 +411,286 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobsPar
   part.head = rank == 0 ? part.body : 0;
   part.tail_index = part.body + pieces * VE;
   part.tail = rank == cluster - 1 ? p.V - part.tail_index : 0;
-  part.tail_at = ((part.pieces + kThreads - 1) / kThreads + 1) * kThreads;
-  Stats st = {kLowest, -INFINITY, {0.f, 0.f}, {0.f, 0.f}, 0u};
-  // (a thread's first place, for stripes of -inf alone)
-  st.place = tid < part.head ? tid : tid < part.pieces ? kThreads + tid : part.tail_at + tid;
-  if (tid < part.head) {
-    add_one(st, to_f(part.z[tid]), tid, scale);
-  }
-  for (int i0 = tid; i0 < part.pieces; i0 += kThreads * kAhead) {
-    uint4 v[kAhead];
-#pragma unroll
-    for (int q = 0; q < kAhead; ++q)
-      if (i0 + q * kThreads < part.pieces) v[q] = part.piece(kThreads + i0 + q * kThreads);
-#pragma unroll
-    for (int q = 0; q < kAhead; ++q) {
-      if (i0 + q * kThreads >= part.pieces) break;
-      float x[VE], top, low;
-      Vec<T>::unpack(v[q], x);
-      Vec<T>::range(v[q], x, &top, &low);
-      if (top > st.best) st.best = top, st.place = kThreads + i0 + q * kThreads;
-      add_elems<VE>(st, x, top, low, scale);
-    }
-  }
-  if (tid < part.tail) {
-    add_one(st, to_f(part.z[part.tail_index + tid]), part.tail_at + tid, scale);
-  }
-  // the CTA's sums
-  const float wm = warp_max(st.m);
-  if (lane == 0) sm.red[warp] = wm;
-  __syncthreads();
-  float m = sm.red[lane & (kWarps - 1)];
-#pragma unroll
-  for (int o = kWarps / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  {
-    const float t = max_nan((st.m - m) * c, kLeast), r = ex2a(t);
-    const float s = warp_sum(r * (st.s.x + st.s.y)), a = warp_sum(r * (st.a.x + st.a.y + (st.s.x + st.s.y) * t));
-    if (lane == 0) sm.red2[warp] = make_float2(s, a);
-  }
-  __syncthreads();
-  if (tid == 0) {
-    float s = 0.f, a = 0.f;
-    for (int w = 0; w < kWarps; ++w) s += sm.red2[w].x, a += sm.red2[w].y;
-    sm.m = m; sm.s = s; sm.a = a;
-  }
-  if (p.k > 0) part_top<T>(part, st, p.k, sm);
-  if (cluster > 1) group.sync(); else __syncthreads();
-  if (rank == 0) {
-    float top = kLowest;
-    for (int r = 0; r < cluster; ++r) top = fmaxf(top, *group.map_shared_rank(&sm.m, r));
-    float s = 0.f, a = 0.f;
-    for (int r = 0; r < cluster; ++r) {
-      const float rs = *group.map_shared_rank(&sm.s, r), t = max_nan((*group.map_shared_rank(&sm.m, r) - top) * c, kLeast), x = ex2a(t);
-      s += x * rs;
-      a += x * (*group.map_shared_rank(&sm.a, r) + rs * t);
-    }
-    const bool none = !(s > 0.f) || !isfinite(top);      // no distribution
-    const float nan = __uint_as_float(0x7FC00000u), ln_s = logf(s);
-    if (tid == 0) {
-      p.logprob[row] = none ? nan : (to_f(part.z[token]) - top) / p.temperature - ln_s;
-      if (p.entropy) p.entropy[row] = none ? nan : fmaxf(ln_s - a / s * 0.69314718055994531f, 0.f);
-    }
-    if (p.k > 0) {
-      const int n = cluster * p.k;
-      for (int i = tid; i < n; i += kThreads) sm.all[i] = group.map_shared_rank(sm.sorted, i / p.k)[i % p.k];
-      __syncthreads();
-      for (int i = tid; i < n; i += kThreads) {
-        const unsigned long long mine = sm.all[i];
-        int at = 0;
-        if (cluster > 1) {
-          for (int j = 0; j < n; ++j) at += sm.all[j] > mine;
-        } else {
-          at = i;
-        }
-        if (at >= p.k || mine == 0) continue;    // (k <= V: k elements there are)
-        const int64_t to = (int64_t)row * p.k + at;
-        if (p.top) p.top[to] = none ? -1 : (int)~(uint32_t)mine;
-        if (p.top_logprob) p.top_logprob[to] = none ? nan : (of_key((uint32_t)(mine >> 32)) - top) / p.temperature - ln_s;
-      }
-    }
-  }
-  if (cluster > 1) group.sync();                 // the first CTA has read the others' parts
+  part.tail_at = ((part.pieces + kStripes - 1) / kStripes + 1) * kStripes;
+  return part;
 }
 
-// CTAs of a row: enough that they fill the GPU twice over, while each has two rounds of loads.
+template <typename T>
+__device__ __forceinline__ void load_role(const LogprobsParams& p, Smem& sm, Rows rows, int rank, int cluster) {
+  Place ring = {0, 1};                           // (the first uses wait for nobody)
+  int token;
+  for (int row = rows.next(&token); row >= 0; row = rows.next(&token)) {
+    const Part<T> part = part_of<T>(p, row, rank, cluster);
+    const char* from = reinterpret_cast<const char*>(part.z + part.body) + (int64_t)part.first * 16;
+    for (int i = 0; i < part.pieces; i += kRounds * kThreads, ring.next(kStages)) {
+      const uint32_t bar = smem_u32(&sm.full[ring.stage]), bytes = min(part.pieces - i, kRounds * kThreads) * 16;
+      if (!tc_wait(smem_u32(&sm.empty[ring.stage]), ring.phase, &sm.abort, p.err)) return;
+      if ((threadIdx.x & 31) == 0) {
+        mbar_expect_tx(bar, bytes);
+        bulk_load(smem_u32(sm.ring[ring.stage]), from + (int64_t)i * 16, bytes, bar);
+      }
+      __syncwarp();
+    }
+  }
+}
+
+// Shared memory of the cluster's CTA `rank`, and its barriers.
+__device__ __forceinline__ uint32_t in_cta(uint32_t at, int rank) {
+  uint32_t x;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(x) : "r"(at), "r"(rank));
+  return x;
+}
+__device__ __forceinline__ void store_far(uint32_t at, unsigned long long x) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at), "l"(x) : "memory");
+}
+__device__ __forceinline__ void arrive_far(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+struct ClusterWait : BarrierWait {
+  __device__ __forceinline__ bool ready() const {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void add_role(const LogprobsParams& p, Smem& sm, Rows rows, int rank, int cluster) {
+  constexpr int VE = Vec<T>::kElems;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const float c = kLog2e / p.temperature;
+  const Scale scale = {c, p.temperature * 0.69314718055994531f, 1e38f / fmaxf(c, 1.0f)};
+  // A wait that gives up leaves the row wrong, but its steps are taken all the same: the barriers of the CTA have no
+  // limit, so its threads leave together, behind a row.
+  bool failed = false;
+  auto wait = [&](uint64_t* bar, uint32_t parity) { failed |= !tc_wait(smem_u32(bar), parity, &sm.abort, p.err); };
+  Place ring = {0, 0};
+  int token;
+  uint32_t turn = 0;
+  for (int row = rows.next(&token); row >= 0; row = rows.next(&token), ++turn) {
+    const Part<T> part = part_of<T>(p, row, rank, cluster);
+    float head = 0.f, tail = 0.f;
+    if (tid < part.head) head = to_f(part.z[tid]);
+    if (tid < part.tail) tail = to_f(part.z[part.tail_index + tid]);
+    Stats st = {kLowest, kLowest, {0.f, 0.f}, {0.f, 0.f}, -INFINITY, -INFINITY, 0u};
+    // (a thread's first place, for stripes of -inf alone)
+    st.place = tid < part.head ? tid : tid < part.pieces ? kStripes + tid : part.tail_at + tid;
+    for (int i0 = 0; i0 < part.pieces; i0 += kRounds * kThreads, ring.next(kStages)) {
+      wait(&sm.full[ring.stage], ring.phase);
+      uint4 v[kRounds];
+#pragma unroll
+      for (int q = 0; q < kRounds; ++q) v[q] = reinterpret_cast<const uint4*>(sm.ring[ring.stage])[q * kThreads + tid];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sm.empty[ring.stage]));
+      float x[kRounds * VE], top = -INFINITY, low = INFINITY;
+#pragma unroll
+      for (int q = 0; q < kRounds; ++q) {
+        const int i = i0 + q * kThreads + tid;
+        if (i >= part.pieces) v[q] = Vec<T>::none();       // (-inf: nothing is added, none is the largest)
+        float a, b;
+        Vec<T>::unpack(v[q], x + q * VE);
+        Vec<T>::range(v[q], x + q * VE, &a, &b);
+        st.other = fmaxf(st.other, fminf(a, st.best));
+        if (a > st.best) st.best = a, st.place = kStripes + i;
+        top = fmaxf(top, a);
+        low = fminf(low, b);
+      }
+      add_elems<kRounds * VE>(st, x, top, low, scale);
+    }
+    if (tid < part.head) {                       // (the first of its stripe: it goes before an equal one)
+      st.other = fmaxf(st.other, fminf(head, st.best));
+      if (head >= st.best) st.best = head, st.place = tid;
+      add_one(st, head, scale);
+    }
+    if (tid < part.tail) {
+      st.other = fmaxf(st.other, fminf(tail, st.best));
+      if (tail > st.best) st.best = tail, st.place = part.tail_at + tid;
+      add_one(st, tail, scale);
+    }
+    // the CTA's sums
+    const float wm = warp_max(st.m);
+    if (lane == 0) sm.red[warp] = wm;
+    meet();
+    float m = sm.red[lane & (kWarps - 1)];
+#pragma unroll
+    for (int o = kWarps / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    {
+      const float t = max_nan((st.m - m) * c, kLeast), r = ex2a(t), s = st.s.x + st.s.y;
+      const float ws = warp_sum(r * s), wa = warp_sum(r * (st.a.x + st.a.y + s * t));
+      if (lane == 0) sm.red2[warp] = make_float2(ws, wa);
+    }
+    if (p.k > 0) part_top<T>(part, st, head, tail, p.k, sm); else meet();
+    // ... to the first CTA (its place is free once the row before the last is joined)
+    if (warp == 0) {
+      const uint32_t mine = smem_u32(&sm.part[turn & 1][rank]), far = in_cta(mine, 0);
+      failed |= !warp_wait(ClusterWait{{smem_u32(&sm.taken[turn & 1]), ((turn >> 1) & 1) ^ 1, &sm.abort, p.err}}, kWaitLimitNs);
+      if (lane == 0) {
+        float s = 0.f, a = 0.f;
+        for (int w = 0; w < kWarps; ++w) s += sm.red2[w].x, a += sm.red2[w].y;
+        store_far(far, (unsigned long long)__float_as_uint(s) << 32 | __float_as_uint(m));
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(far + 8), "f"(a) : "memory");
+      }
+      if (lane < p.k) store_far(far + (uint32_t)offsetof(Partial, sorted) + 8 * lane, sm.sorted[lane]);
+      arrive_far(in_cta(smem_u32(&sm.parts[turn & 1]), 0));      // (every lane, for what it has stored)
+    }
+    if (count_all(failed) > 0) break;            // (and the row's lists are read)
+  }
+}
+
+// The warp of a cluster's first CTA that joins the parts of a row.
+template <typename T>
+__device__ __forceinline__ void join_role(const LogprobsParams& p, Smem& sm, Rows rows, int cluster) {
+  const int lane = threadIdx.x & 31;
+  const float c = kLog2e / p.temperature;
+  const float nan = __uint_as_float(0x7FC00000u);
+  int token;
+  uint32_t turn = 0;
+  for (int row = rows.next(&token); row >= 0; row = rows.next(&token), ++turn) {
+    const float z = to_f(static_cast<const T*>(p.z)[(int64_t)row * p.ld + token]);
+    if (!warp_wait(ClusterWait{{smem_u32(&sm.parts[turn & 1]), (turn >> 1) & 1, &sm.abort, p.err}}, kWaitLimitNs)) return;
+    const Partial* all = sm.part[turn & 1];
+    float top = kLowest;
+    for (int r = 0; r < cluster; ++r) top = fmaxf(top, all[r].m);
+    float s = 0.f, a = 0.f;
+    for (int r = 0; r < cluster; ++r) {
+      const float t = max_nan((all[r].m - top) * c, kLeast), x = ex2a(t);
+      s += x * all[r].s;
+      a += x * (all[r].a + all[r].s * t);
+    }
+    const bool none = !(s > 0.f) || !isfinite(top);              // no distribution
+    const float ln_s = logf(s);
+    if (lane == 0) {
+      p.logprob[row] = none ? nan : (z - top) / p.temperature - ln_s;
+      if (p.entropy) p.entropy[row] = none ? nan : fmaxf(ln_s - a / s * 0.69314718055994531f, 0.f);
+    }
+    // lane r has the first that is left of part r's list; the largest of those goes to lane i in round i
+    uint32_t key = 0, at = 0, won_key = 0, won_at = 0;
+    int next = 0;
+    auto pull = [&]() {
+      const unsigned long long x = lane < cluster && next < p.k ? all[lane].sorted[next] : 0;
+      key = (uint32_t)(x >> 32);
+      at = (uint32_t)x;
+      ++next;
+    };
+    pull();
+    for (int i = 0; i < p.k; ++i) {
+      const uint32_t k = __reduce_max_sync(0xffffffffu, key), w = __reduce_max_sync(0xffffffffu, key == k ? at : 0u);
+      if (lane == i) won_key = k, won_at = w;
+      if (key == k && at == w) pull();
+    }
+    if (lane < p.k) {                            // (k <= V: there are k elements)
+      const int64_t to = (int64_t)row * p.k + lane;
+      if (p.top) p.top[to] = none ? -1 : (int)~won_at;
+      if (p.top_logprob) p.top_logprob[to] = none ? nan : (of_key<T>(won_key) - top) / p.temperature - ln_s;
+    }
+    __syncwarp();
+    if (lane < cluster) arrive_far(in_cta(smem_u32(&sm.taken[turn & 1]), lane));
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads + 64, kPerSm) logprobs_kernel(const LogprobsParams p, int cluster) {
+  extern __shared__ uint8_t raw[];
+  Smem& sm = *reinterpret_cast<Smem*>((reinterpret_cast<uintptr_t>(raw) + 127) & ~static_cast<uintptr_t>(127));
+  const int tid = threadIdx.x, rank = blockIdx.x % cluster;
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(smem_u32(&sm.full[i]), 1);
+      mbar_init(smem_u32(&sm.empty[i]), kWarps);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&sm.parts[i]), 32 * cluster);
+      mbar_init(smem_u32(&sm.taken[i]), 1);
+    }
+    sm.abort = 0;
+    fence_barrier_init();
+  }
+  cluster_sync();                                // (barriers are there before another CTA arrives at them)
+  griddep_wait();
+  griddep_launch();
+  const Rows rows{p.tokens, p.rows, p.V, (int)gridDim.x / cluster, (int)blockIdx.x / cluster};
+  if (tid >= kThreads + 32) {
+    if (rank == 0) join_role<T>(p, sm, rows, cluster);
+  } else if (tid >= kThreads) {
+    load_role<T>(p, sm, rows, rank, cluster);
+  } else {
+    // rows without a token
+    for (int r = blockIdx.x * kThreads + tid; r < p.rows; r += gridDim.x * kThreads) {
+      const int token = p.tokens[r];
+      if (rows.valid(token)) continue;
+      for (int i = 0; i < p.k; ++i) {
+        if (p.top) p.top[(int64_t)r * p.k + i] = -1;
+        if (p.top_logprob) p.top_logprob[(int64_t)r * p.k + i] = -INFINITY;
+      }
+      p.logprob[r] = -INFINITY;
+      if (p.entropy) p.entropy[r] = 0.f;
+      if (token != -1) set_err(p.err, LSP_DEV_BAD_TOKEN);
+    }
+    add_role<T>(p, sm, rows, rank, cluster);
+  }
+  __syncthreads();
+  // Every load has been waited for, unless a wait gave up: then loads may still be landing, and the CTA stays for
+  // them (bounded).
+  if (*reinterpret_cast<volatile int*>(&sm.abort) && tid == 0) {
+    const uint64_t t0 = global_ns();
+    while (global_ns() - t0 < 1000000ull) {}
+  }
+  cluster_sync();                                // (nobody stores into a CTA that is gone)
+}
+
+// CTAs of a row: enough that the rows go round the GPU a few times, while each has a round of loads.
 int choose_cluster(int rows, int V, int es, int num_sms) {
   const int64_t pieces = (int64_t)V * es / 16;
   int n = 1;
-  while (n < kMaxCluster && (int64_t)rows * n < 12 * num_sms && pieces > (int64_t)kThreads * n) n *= 2;
+  while (n < kMaxCluster && (int64_t)rows * n < 4 * kPerSm * num_sms && pieces > (int64_t)kThreads * n) n *= 2;
   return n;
+}
+
+template <typename T>
+int launch(const LogprobsParams& p, int num_sms, cudaStream_t s) {
+  static bool set[8] = {};
+  const int smem = (int)sizeof(Smem) + 128;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return LSP_ERR_CUDA;
+  if (dev >= 8 || !set[dev]) {
+    if (cudaFuncSetAttribute(logprobs_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return LSP_ERR_CUDA;
+    if (dev < 8) set[dev] = true;
+  }
+  const int cluster = choose_cluster(p.rows, p.V, (int)sizeof(T), num_sms);
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kThreads + 64);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  // as many clusters as run at once: what is left over would come behind all the others' rows
+  static int most[8][4] = {};
+  const int log = 31 - __builtin_clz(cluster);
+  int at_once = dev < 8 ? most[dev][log] : 0;
+  if (at_once == 0) {
+    cfg.gridDim = dim3((unsigned)(kPerSm * num_sms / cluster * cluster));
+    if (cudaOccupancyMaxActiveClusters(&at_once, logprobs_kernel<T>, &cfg) != cudaSuccess || at_once < 1) return LSP_ERR_CUDA;
+    if (dev < 8) most[dev][log] = at_once;
+  }
+  cfg.numAttrs = 2;
+  cfg.gridDim = dim3((unsigned)(std::min(p.rows, at_once) * cluster));
+  return cudaLaunchKernelEx(&cfg, logprobs_kernel<T>, p, cluster) == cudaSuccess ? LSP_OK : LSP_ERR_CUDA;
 }
 
 }  // namespace
 
 int launch_logprobs(const LogprobsParams& p, int dtype, int num_sms, cudaStream_t s) {
-  const int cluster = choose_cluster(p.rows, p.V, dtype == LSP_DTYPE_BF16 ? 2 : 4, num_sms);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(p.rows * cluster));
-  cfg.blockDim = dim3(kThreads);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cluster;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  const cudaError_t e = dtype == LSP_DTYPE_BF16 ? cudaLaunchKernelEx(&cfg, logprobs_kernel<bf16>, p, cluster)
-                                                : cudaLaunchKernelEx(&cfg, logprobs_kernel<float>, p, cluster);
-  return e == cudaSuccess ? LSP_OK : LSP_ERR_CUDA;
+  return dtype == LSP_DTYPE_BF16 ? launch<bf16>(p, num_sms, s) : launch<float>(p, num_sms, s);
 }
 
 }  // namespace lsp
