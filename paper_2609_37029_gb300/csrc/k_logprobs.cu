@@ -8,7 +8,7 @@
 // m as 2^t times (S, A + S t).
 //
 // The k largest, from the same pass: a thread has a stripe of the CTA's part (every
-// 128th piece of 16 bytes), of which it knows at the end the piece with the largest
+// 128th piece of 64 bytes), of which it knows at the end the piece with the largest
 // logit (the first of several), and the largest of the others.  Each of the k largest
 // elements is in one of the k stripes whose first are the largest -- an element in any
 // other stripe has k elements before it -- so of those stripes the piece with the
@@ -37,8 +37,8 @@ namespace {
 constexpr int kThreads = 128, kWarps = kThreads / 32;      // that add up; a warp more loads, and one joins a row's parts
 constexpr int kMaxCluster = 8;
 constexpr int kPerSm = 4;
-constexpr int kRounds = 4;                       // pieces of a thread in a stage
-constexpr int kStages = 5, kStageBytes = kRounds * kThreads * 16;
+constexpr int kPieceBytes = 64;                  // of a row, for a thread at a time
+constexpr int kStages = 5, kStageBytes = kThreads * kPieceBytes;
 constexpr int kStripes = kThreads;               // of a CTA's part: stripe i, of thread i, has its pieces i, i + kStripes, ...
 constexpr int kList = 512;                       // candidates of a CTA
 constexpr float kLog2e = 1.4426950408889634f;
@@ -95,10 +95,11 @@ __device__ __forceinline__ float of_key(uint32_t k) {
 __device__ __forceinline__ unsigned long long entry(uint32_t key, uint32_t at) { return (unsigned long long)key << 32 | ~at; }
 
 template <typename T>
-struct Vec {
-  static constexpr int kElems = 16 / (int)sizeof(T);
-  __device__ static __forceinline__ void unpack(const uint4& v, float* x) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+struct Piece {
+  static constexpr int kElems = kPieceBytes / (int)sizeof(T), kOf = 16 / (int)sizeof(T);
+  uint4 v[4];
+  __device__ __forceinline__ void unpack(int q, float* x) const {        // its q-th 16 bytes
+    const uint32_t w[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (sizeof(T) == 2) {
@@ -109,65 +110,58 @@ struct Vec {
       }
     }
   }
-  __device__ static __forceinline__ uint4 none() {
-    const uint32_t inf = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
-    return make_uint4(inf, inf, inf, inf);
-  }
-  // the largest and the smallest, NaN aside
-  __device__ static __forceinline__ void range(const uint4& v, const float* x, float* top, float* low) {
+  __device__ __forceinline__ float top() const { // the largest, NaN aside
+    float t;
     if constexpr (sizeof(T) == 2) {
-      const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
-      const __nv_bfloat162 a = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3])), b = __hmin2(__hmin2(p[0], p[1]), __hmin2(p[2], p[3]));
-      *top = fmaxf(__low2float(a), __high2float(a));
-      *low = fminf(__low2float(b), __high2float(b));
+      __nv_bfloat162 m[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) m[q] = __hmax2(__hmax2(bits_bf2(v[q].x), bits_bf2(v[q].y)), __hmax2(bits_bf2(v[q].z), bits_bf2(v[q].w)));
+      const __nv_bfloat162 a = __hmax2(__hmax2(m[0], m[1]), __hmax2(m[2], m[3]));
+      t = fmaxf(__low2float(a), __high2float(a));
     } else {
-      *top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-      *low = fminf(fminf(x[0], x[1]), fminf(x[2], x[3]));
+      t = -INFINITY;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float x[4];
+        unpack(q, x);
+        t = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), t);
+      }
     }
+    return t;
   }
 };
 
 // A CTA's part of a row, in places: the row's elements before its first 16-byte
-// boundary (place tid < head), the part's pieces (places kStripes + i), and the
-// elements behind the last piece (from place `tail_at` on).  Places rise with the index.
+// boundary (place tid < head), the part's pieces from there on (places kStripes + i),
+// and the elements behind the last piece (from place `tail_at` on).  Places rise with
+// the index.
 template <typename T>
 struct Part {
   const T* z;
   int head, body, first, pieces, tail, tail_at;  // body: index of the row's first piece; first: of the part's, in pieces
   int tail_index;
-  __device__ __forceinline__ uint4 piece(int i) const { return __ldcg(reinterpret_cast<const uint4*>(z + body) + (first + i)); }
-  __device__ __forceinline__ int index(int i) const { return body + (first + i) * Vec<T>::kElems; }   // of a piece's first element
+  __device__ __forceinline__ uint4 quarter(int i, int q) const { return __ldcg(reinterpret_cast<const uint4*>(z + body) + 4 * (int64_t)(first + i) + q); }
+  __device__ __forceinline__ int index(int i) const { return body + (first + i) * Piece<T>::kElems; }   // of a piece's first element
 };
 
 struct Scale {
   float c, inv;         // log2(e) / T, its reciprocal
-  float large;          // logits up to here leave every t finite
+  float large;          // logits up to here: t is finite, and what ref rounds off below 2^-4
 };
 
-// Of a thread's elements: the sums relative to `m`; of its stripe the largest logit, its piece's place, and the largest
-// of the other pieces.
+// Of a thread's elements: the largest of those that have been m, and sums of 2^t and
+// 2^t t with t = z c - ref, ref = m c rounded (what that rounds off is the same for all
+// and is taken back at the end); of its stripe the largest logit, its piece's place,
+// and the largest of the other pieces.
 struct Stats {
-  float m, reach;
+  float m, ref;
+  float least;          // logits below count nothing and are raised to here; NaN: t = (z - m) c, limited, one by one
   float2 s, a;          // of every other element, to be added
   float best, other;
   uint32_t place;
 };
 
-// (a0, a1) + b, a b, a + b and a b + c: two fp32 operations an instruction
-__device__ __forceinline__ float2 add2s(float a0, float a1, float b) {
-  float2 d;
-  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %4};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a0), "f"(a1), "f"(b));
-  return d;
-}
-__device__ __forceinline__ float2 mul2s(float2 a, float b) {
-  float2 d;
-  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %4};\n mul.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b));
-  return d;
-}
+// a + b and a b + c: two fp32 operations an instruction
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   float2 d;
   asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
@@ -184,53 +178,82 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   return d;
 }
 
-// Elements x, of which top and low are the largest and the smallest (NaN aside).  The
-// sums move to a higher m when an element exceeds theirs by 2^8 (they are fp32: what
-// is added meanwhile loses nothing).  As long as logits stay within +-large, every t
-// is finite, and e t = 0 where e = 0.  What is below (-inf, a banned token) is raised
-// to where e is 0 already; a row of larger numbers takes its steps one by one with t
-// limited.
-template <int N>
-__device__ __forceinline__ void add_elems(Stats& st, float* x, float top, float low, const Scale& k) {
-  if (top > st.reach) {
-    const float t = max_nan((st.m - top) * k.c, kLeast), r = ex2a(t);
-    st.a = make_float2(r * (st.a.x + st.s.x * t), r * (st.a.y + st.s.y * t));
-    st.s = make_float2(r * st.s.x, r * st.s.y);
-    st.m = top;
-    st.reach = top + 8.0f * k.inv;
-  }
-  if (!(low > -k.large) || fabsf(st.m) > k.large) {
-    if (fabsf(st.m) > k.large) {
-#pragma unroll 1
-      for (int i = 0; i < N; ++i) {
-        float y = x[0];                          // (no indexed registers)
+// The sums move to a higher m when an element, `top`, exceeds theirs by 2^8 (they are
+// fp32: what is added meanwhile loses nothing).
+__device__ __forceinline__ void raise(Stats& st, float top, const Scale& k) {
+  if (!((top - st.m) * k.c > 8.0f)) return;
+  const bool was = st.least == st.least, fine = fabsf(top) <= k.large;
+  const float ref = top * k.c, t = max_nan(was && fine ? st.ref - ref : (st.m - top) * k.c, kLeast), r = ex2a(t);
+  st.a = make_float2(r * (st.a.x + st.s.x * t), r * (st.a.y + st.s.y * t));
+  st.s = make_float2(r * st.s.x, r * st.s.y);
+  st.m = top;
+  st.ref = ref;
+  // (200 / c below m; where m's last place is more than that, some of those below)
+  st.least = fine ? top - fmaxf(200.0f * k.inv, fabsf(top) * 0x1p-20f) : __uint_as_float(0x7FC00000u);
+}
+__device__ __forceinline__ void add_limited(Stats& st, float x, const Scale& k) {
+  const float t = max_nan((x - st.m) * k.c, kLeast), e = ex2a(t);
+  st.s.x += e;
+  st.a.x = fmaf(e, t, st.a.x);
+}
+
+// A piece at `place`.  As long as m stays within +-large, every t is finite, and e t = 0
+// where e = 0: what is far below (-inf, a banned token) is raised to where e is 0 already.
+template <typename T>
+__device__ __forceinline__ void add_piece(Stats& st, Piece<T>& v, uint32_t place, const Scale& k) {
+  const float top = v.top();
+  st.other = fmaxf(st.other, fminf(top, st.best));
+  if (top > st.best) st.best = top, st.place = place;
+  raise(st, top, k);
+  if (st.least != st.least) {                    // nothing but -inf so far, or logits too large
 #pragma unroll
-        for (int e = 1; e < N; ++e) y = e == i ? x[e] : y;
-        const float t = max_nan((y - st.m) * k.c, kLeast), e = ex2a(t);
-        st.s.x += e;
-        st.a.x = fmaf(e, t, st.a.x);
-      }
-      return;
+    for (int q = 0; q < 4; ++q) {
+      float x[Piece<T>::kOf];
+      v.unpack(q, x);
+#pragma unroll
+      for (int i = 0; i < Piece<T>::kOf; ++i) add_limited(st, x[i], k);
     }
-    // (200 / c below m; where m's last place is more than that, some of those below)
-    const float least = st.m - fmaxf(200.0f * k.inv, fabsf(st.m) * 0x1p-20f);
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = max_nan(x[i], least);
+    return;
   }
+  const float2 c = make_float2(k.c, k.c), ref = make_float2(-st.ref, -st.ref);
+  const __nv_bfloat16 low = __float2bfloat16_rd(st.least);
+  const __nv_bfloat162 low2 = __halves2bfloat162(low, low);
   float2 s[2] = {st.s, {0.f, 0.f}}, a[2] = {st.a, {0.f, 0.f}};
 #pragma unroll
-  for (int i = 0; i < N; i += 2) {
-    const float2 t = mul2s(add2s(x[i], x[i + 1], -st.m), k.c), e = make_float2(ex2a(t.x), ex2a(t.y));
-    s[(i >> 1) & 1] = add2(s[(i >> 1) & 1], e);
-    a[(i >> 1) & 1] = fma2(e, t, a[(i >> 1) & 1]);
+  for (int q = 0; q < 4; ++q) {
+    float x[Piece<T>::kOf];
+    if constexpr (sizeof(T) == 2) {
+      v.v[q] = make_uint4(bf2_bits(__hmax2_nan(bits_bf2(v.v[q].x), low2)), bf2_bits(__hmax2_nan(bits_bf2(v.v[q].y), low2)),
+                          bf2_bits(__hmax2_nan(bits_bf2(v.v[q].z), low2)), bf2_bits(__hmax2_nan(bits_bf2(v.v[q].w), low2)));
+      v.unpack(q, x);
+    } else {
+      v.unpack(q, x);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = max_nan(x[i], st.least);
+    }
+#pragma unroll
+    for (int i = 0; i < Piece<T>::kOf; i += 2) {
+      const float2 t = fma2(make_float2(x[i], x[i + 1]), c, ref), e = make_float2(ex2a(t.x), ex2a(t.y));
+      s[(i >> 1) & 1] = add2(s[(i >> 1) & 1], e);
+      a[(i >> 1) & 1] = fma2(e, t, a[(i >> 1) & 1]);
+    }
   }
   st.s = add2(s[0], s[1]);
   st.a = add2(a[0], a[1]);
 }
-
+// The pieces are over: sums relative to m.
+__device__ __forceinline__ void settle(Stats& st, const Scale& k) {
+  if (st.least != st.least) return;
+  const float off = fmaf(st.m, k.c, -st.ref), f = ex2a(-off);
+  st.a = make_float2(f * (st.a.x - off * st.s.x), f * (st.a.y - off * st.s.y));
+  st.s = make_float2(f * st.s.x, f * st.s.y);
+  st.least = __uint_as_float(0x7FC00000u);
+}
+// A single element, behind that.
 __device__ __forceinline__ void add_one(Stats& st, float x, const Scale& k) {
-  float pair[2] = {x, -INFINITY};
-  add_elems<2>(st, pair, x, -INFINITY, k);
+  raise(st, x, k);
+  st.least = __uint_as_float(0x7FC00000u);
+  add_limited(st, x, k);
 }
 
 __device__ __forceinline__ void cluster_sync() {
@@ -265,9 +288,7 @@ __device__ __forceinline__ unsigned long long block_max(unsigned long long v, Sm
 // sm.sorted = the k largest elements of the part (0 where it has fewer); head, tail: this thread's single elements.
 template <typename T>
 __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, float head, float tail, int k, Smem& sm) {
-  constexpr int VE = Vec<T>::kElems;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int rounds = (part.pieces + kStripes - 1) / kStripes;    // pieces of a stripe
   const bool some = tid < part.head || tid < part.pieces || tid < part.tail;
   const uint32_t key = some ? key_of<T>(st.best) : 0u;
   if (tid == 0) sm.count = sm.stripes = 0;
@@ -300,11 +321,23 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, f
     const int at = atomicAdd(&sm.count, 1);
     if (at < kList) sm.list[at] = entry(e, (uint32_t)index);
   };
-  auto put_piece = [&](const uint4& v, int i) {
-    float x[VE];
-    Vec<T>::unpack(v, x);
+  auto load_piece = [&](int i) {
+    Piece<T> v;
 #pragma unroll
-    for (int e = 0; e < VE; ++e) put(x[e], kStripes + i, part.index(i) + e);
+    for (int q = 0; q < 4; ++q) v.v[q] = part.quarter(i, q);
+    return v;
+  };
+  auto each = [&](const Piece<T>& v, int i, auto f) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      float x[Piece<T>::kOf];
+      v.unpack(q, x);
+#pragma unroll
+      for (int e = 0; e < Piece<T>::kOf; ++e) f(x[e], part.index(i) + q * Piece<T>::kOf + e);
+    }
+  };
+  auto put_piece = [&](const Piece<T>& v, int i) {
+    each(v, i, [&](float x, int index) { put(x, kStripes + i, index); });
   };
   if (some && in(key, st.place)) {
     if (tid < part.head) put(head, tid, tid);
@@ -313,26 +346,13 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, f
     if (key_of<T>(st.other) >= cut)
       sm.stripe[atomicAdd(&sm.stripes, 1)] = tid;
     else if (st.place >= kStripes && st.place < (uint32_t)part.tail_at)
-      put_piece(part.piece((int)st.place - kStripes), (int)st.place - kStripes);
+      put_piece(load_piece((int)st.place - kStripes), (int)st.place - kStripes);
   }
   meet();
-  // a warp takes stripes in turn, a lane every 32nd piece, some of them in flight together
-  constexpr int kOnce = 4;
+  // a warp takes stripes in turn, a lane every 32nd piece
   const int stripes = sm.stripes;
   for (int x = warp; x < stripes; x += kWarps) {
-    const int stripe = (int)sm.stripe[x];
-    for (int j = lane; j - lane < rounds; j += 32 * kOnce) {
-      uint4 v[kOnce];
-      int at[kOnce];                             // of the part's pieces
-#pragma unroll
-      for (int q = 0; q < kOnce; ++q) {
-        at[q] = (j + 32 * q) * kStripes + stripe;
-        if (at[q] < part.pieces) v[q] = part.piece(at[q]);
-      }
-#pragma unroll
-      for (int q = 0; q < kOnce; ++q)
-        if (at[q] < part.pieces) put_piece(v[q], at[q]);
-    }
+    for (int i = lane * kStripes + (int)sm.stripe[x]; i < part.pieces; i += 32 * kStripes) put_piece(load_piece(i), i);
   }
   meet();
   const int n = sm.count;
@@ -354,12 +374,7 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, f
       if (e < before && e > best) best = e;
     };
     if (tid < part.head) see(to_f(part.z[tid]), tid);
-    for (int i = tid; i < part.pieces; i += kThreads) {
-      float x[VE];
-      Vec<T>::unpack(part.piece(i), x);
-#pragma unroll
-      for (int e = 0; e < VE; ++e) see(x[e], part.index(i) + e);
-    }
+    for (int i = tid; i < part.pieces; i += kThreads) each(load_piece(i), i, see);
     if (tid < part.tail) see(to_f(part.z[part.tail_index + tid]), part.tail_index + tid);
     best = block_max(best, sm);
     if (tid == 0) sm.sorted[r] = best;
@@ -400,7 +415,7 @@ struct Rows {
 
 template <typename T>
 __device__ __forceinline__ Part<T> part_of(const LogprobsParams& p, int row, int rank, int cluster) {
-  constexpr int VE = Vec<T>::kElems;
+  constexpr int VE = Piece<T>::kElems;
   Part<T> part;
   part.z = static_cast<const T*>(p.z) + (int64_t)row * p.ld;
   const int off = (int)((16 - (reinterpret_cast<uintptr_t>(part.z) & 15)) & 15) / (int)sizeof(T);
@@ -421,13 +436,13 @@ __device__ __forceinline__ void load_role(const LogprobsParams& p, Smem& sm, Row
   int token;
   for (int row = rows.next(&token); row >= 0; row = rows.next(&token)) {
     const Part<T> part = part_of<T>(p, row, rank, cluster);
-    const char* from = reinterpret_cast<const char*>(part.z + part.body) + (int64_t)part.first * 16;
-    for (int i = 0; i < part.pieces; i += kRounds * kThreads, ring.next(kStages)) {
-      const uint32_t bar = smem_u32(&sm.full[ring.stage]), bytes = min(part.pieces - i, kRounds * kThreads) * 16;
+    const char* from = reinterpret_cast<const char*>(part.z + part.body) + (int64_t)part.first * kPieceBytes;
+    for (int i = 0; i < part.pieces; i += kThreads, ring.next(kStages)) {
+      const uint32_t bar = smem_u32(&sm.full[ring.stage]), bytes = min(part.pieces - i, kThreads) * kPieceBytes;
       if (!tc_wait(smem_u32(&sm.empty[ring.stage]), ring.phase, &sm.abort, p.err)) return;
       if ((threadIdx.x & 31) == 0) {
         mbar_expect_tx(bar, bytes);
-        bulk_load(smem_u32(sm.ring[ring.stage]), from + (int64_t)i * 16, bytes, bar);
+        bulk_load(smem_u32(sm.ring[ring.stage]), from + (int64_t)i * kPieceBytes, bytes, bar);
       }
       __syncwarp();
     }
@@ -460,10 +475,9 @@ struct ClusterWait : BarrierWait {
 
 template <typename T>
 __device__ __forceinline__ void add_role(const LogprobsParams& p, Smem& sm, Rows rows, int rank, int cluster) {
-  constexpr int VE = Vec<T>::kElems;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const float c = kLog2e / p.temperature;
-  const Scale scale = {c, p.temperature * 0.69314718055994531f, 1e38f / fmaxf(c, 1.0f)};
+  const Scale scale = {c, p.temperature * 0.69314718055994531f, fminf(1e38f, 1e6f / c)};
   // A wait that gives up leaves the row wrong, but its steps are taken all the same: the barriers of the CTA have no
   // limit, so its threads leave together, behind a row.
   bool failed = false;
@@ -476,31 +490,20 @@ __device__ __forceinline__ void add_role(const LogprobsParams& p, Smem& sm, Rows
     float head = 0.f, tail = 0.f;
     if (tid < part.head) head = to_f(part.z[tid]);
     if (tid < part.tail) tail = to_f(part.z[part.tail_index + tid]);
-    Stats st = {kLowest, kLowest, {0.f, 0.f}, {0.f, 0.f}, -INFINITY, -INFINITY, 0u};
+    Stats st = {kLowest, kLowest, __uint_as_float(0x7FC00000u), {0.f, 0.f}, {0.f, 0.f}, -INFINITY, -INFINITY, 0u};
     // (a thread's first place, for stripes of -inf alone)
     st.place = tid < part.head ? tid : tid < part.pieces ? kStripes + tid : part.tail_at + tid;
-    for (int i0 = 0; i0 < part.pieces; i0 += kRounds * kThreads, ring.next(kStages)) {
+    for (int i0 = 0; i0 < part.pieces; i0 += kThreads, ring.next(kStages)) {
       wait(&sm.full[ring.stage], ring.phase);
-      uint4 v[kRounds];
+      Piece<T> v;
+      // (eight lanes, 64 bytes apart, read eight different 16 bytes of 128; the order within a piece does not matter)
 #pragma unroll
-      for (int q = 0; q < kRounds; ++q) v[q] = reinterpret_cast<const uint4*>(sm.ring[ring.stage])[q * kThreads + tid];
+      for (int q = 0; q < 4; ++q) v.v[q] = reinterpret_cast<const uint4*>(sm.ring[ring.stage])[4 * tid + ((q + (lane >> 1)) & 3)];
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&sm.empty[ring.stage]));
-      float x[kRounds * VE], top = -INFINITY, low = INFINITY;
-#pragma unroll
-      for (int q = 0; q < kRounds; ++q) {
-        const int i = i0 + q * kThreads + tid;
-        if (i >= part.pieces) v[q] = Vec<T>::none();       // (-inf: nothing is added, none is the largest)
-        float a, b;
-        Vec<T>::unpack(v[q], x + q * VE);
-        Vec<T>::range(v[q], x + q * VE, &a, &b);
-        st.other = fmaxf(st.other, fminf(a, st.best));
-        if (a > st.best) st.best = a, st.place = kStripes + i;
-        top = fmaxf(top, a);
-        low = fminf(low, b);
-      }
-      add_elems<kRounds * VE>(st, x, top, low, scale);
+      if (i0 + tid < part.pieces) add_piece(st, v, kStripes + i0 + tid, scale);
     }
+    settle(st, scale);
     if (tid < part.head) {                       // (the first of its stripe: it goes before an equal one)
       st.other = fmaxf(st.other, fminf(head, st.best));
       if (head >= st.best) st.best = head, st.place = tid;
@@ -644,7 +647,7 @@ __global__ void __launch_bounds__(kThreads + 64, kPerSm) logprobs_kernel(const L
 
 // CTAs of a row: enough that the rows go round the GPU a few times, while each has a round of loads.
 int choose_cluster(int rows, int V, int es, int num_sms) {
-  const int64_t pieces = (int64_t)V * es / 16;
+  const int64_t pieces = (int64_t)V * es / kPieceBytes;
   int n = 1;
   while (n < kMaxCluster && (int64_t)rows * n < 4 * kPerSm * num_sms && pieces > (int64_t)kThreads * n) n *= 2;
   return n;
