@@ -645,11 +645,13 @@ __global__ void __launch_bounds__(kThreads + 64, kPerSm) logprobs_kernel(const L
   cluster_sync();                                // (nobody stores into a CTA that is gone)
 }
 
-// CTAs of a row: enough that the rows go round the GPU a few times, while each has a round of loads.
+// CTAs of a row: a part costs some 5 us besides reading it, so no more than fill the GPU's SMs more than twice over
+// (rows of 151936, k = 20: 190 of fp32 43, 38, 43 and 44 us with 1, 2, 4 and 8; 500 76, 77, 81, 89; 64 31, 23, 20, 20),
+// while each has a round of loads.
 int choose_cluster(int rows, int V, int es, int num_sms) {
   const int64_t pieces = (int64_t)V * es / kPieceBytes;
   int n = 1;
-  while (n < kMaxCluster && (int64_t)rows * n < 4 * kPerSm * num_sms && pieces > (int64_t)kThreads * n) n *= 2;
+  while (n < kMaxCluster && (int64_t)rows * n * 5 < 12 * num_sms && pieces > (int64_t)kThreads * n) n *= 2;
   return n;
 }
 
