@@ -228,25 +228,23 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
     v_at[j] = St::kCodes + kv[j] * (HD / 2) + r * (HD / 16);
     vs_at[j] = 2 * St::kCodes + St::kScales + kv[j] * (HD / 16) + (HD == 128 ? r >> 1 : r >> 2) * 2;
   }
+  const uint32_t ring_at = smem_u32(sm.ring), full_at = smem_u32(sm.full), empty_at = smem_u32(sm.empty);
   const Q4Consts consts;
   // 16 keys, the first of them key `key` of the sequence, from `codes` and `scales` on; edge: some row does not see some key
-  auto slice = [&](const uint8_t* codes, const uint8_t* scales, int key, auto edge) {
+  auto slice = [&](uint32_t codes, uint32_t scales, int key, auto edge) {
     constexpr bool kEdge = decltype(edge)::value;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     {
       uint32_t wa[kWordsK], wb[kWordsK];
-      const uint8_t* a = codes + k_at;
       if constexpr (HD == 128) {
-        const uint4 x = *reinterpret_cast<const uint4*>(a), y = *reinterpret_cast<const uint4*>(a + 8 * (HD / 2));
+        const uint4 x = ld_shared4(codes + k_at), y = ld_shared4(codes + k_at + 8 * (HD / 2));
         wa[0] = x.x; wa[1] = x.y; wa[2] = x.z; wa[3] = x.w;
         wb[0] = y.x; wb[1] = y.y; wb[2] = y.z; wb[3] = y.w;
       } else {
-        const uint2 x = *reinterpret_cast<const uint2*>(a), y = *reinterpret_cast<const uint2*>(a + 8 * (HD / 2));
-        wa[0] = x.x; wa[1] = x.y;
-        wb[0] = y.x; wb[1] = y.y;
+        ld_shared2(codes + k_at, wa[0], wa[1]);
+        ld_shared2(codes + k_at + 8 * (HD / 2), wb[0], wb[1]);
       }
-      const uint32_t sa = *reinterpret_cast<const uint16_t*>(scales + ks_at) * 0x10001u;
-      const uint32_t sb = *reinterpret_cast<const uint16_t*>(scales + ks_at + 8 * (HD / 16)) * 0x10001u;
+      const uint32_t sa = ld_shared_u16(scales + ks_at) * 0x10001u, sb = ld_shared_u16(scales + ks_at + 8 * (HD / 16)) * 0x10001u;
 #pragma unroll
       for (int i = 0; i < kWordsK; ++i)
 #pragma unroll
@@ -299,14 +297,12 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
     uint32_t w[4][kWordsV], sv[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint8_t* a = codes + v_at[j & 1] + (j >> 1) * 8 * (HD / 2);
-      if constexpr (HD == 128) {
-        const uint2 x = *reinterpret_cast<const uint2*>(a);
-        w[j][0] = x.x; w[j][1] = x.y;
-      } else {
-        w[j][0] = *reinterpret_cast<const uint32_t*>(a);
-      }
-      sv[j] = *reinterpret_cast<const uint16_t*>(scales + vs_at[j & 1] + (j >> 1) * 8 * (HD / 16));
+      const uint32_t a = codes + v_at[j & 1] + (j >> 1) * 8 * (HD / 2);
+      if constexpr (HD == 128)
+        ld_shared2(a, w[j][0], w[j][1]);
+      else
+        w[j][0] = ld_shared(a);
+      sv[j] = ld_shared_u16(scales + vs_at[j & 1] + (j >> 1) * 8 * (HD / 16));
       // slots of a page past the last key hold anything: their weights are 0, and 0 x V must be 0
       if (kEdge && key + kv[j & 1] + (j >> 1) * 8 >= g.k_end) sv[j] = 0;
     }
@@ -325,9 +321,9 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
     }
   };
   for (int kb = g.kb0; kb < g.kb1; ++kb) {
-    if (!tc_wait(smem_u32(&sm.full[ring.stage]), ring.phase, &sm.abort, p.err)) return false;
+    if (!tc_wait(full_at + 8 * ring.stage, ring.phase, &sm.abort, p.err)) return false;
     if (live) {
-      const uint8_t* at = sm.ring[ring.stage];
+      const uint32_t at = ring_at + ring.stage * St::kBytes;
       const int key0 = g.k0 + kb * kKeys;
       if (key0 + kKeys > least) {
         for (int i = kg; i < kSlices; i += kgs) slice(at + i * kSlice * (HD / 2), at + i * kSlice * (HD / 16), key0 + i * kSlice, BoolTag<true>());
@@ -336,7 +332,7 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
       }
       __syncwarp();
     }
-    if (lane == 0) mbar_arrive(smem_u32(&sm.empty[ring.stage]));
+    if (lane == 0) mbar_arrive(empty_at + 8 * ring.stage);
     ring.next(St::kCount);
   }
 #pragma unroll

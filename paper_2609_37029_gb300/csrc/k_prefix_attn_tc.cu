@@ -189,18 +189,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-__device__ __forceinline__ void ld_shared2(uint32_t at, uint32_t& x, uint32_t& y) {
-  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(at) : "memory");
-}
-__device__ __forceinline__ uint32_t ld_shared_u16(uint32_t at) {
-  uint32_t x;
-  asm volatile("ld.shared.u16 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
-  return x;
-}
-__device__ __forceinline__ void st_shared4(uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
-  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
-}
-
 __device__ __forceinline__ float ex2a(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
