@@ -554,11 +554,14 @@ size_t plan(PrefixAttnParams* p, int dtype, int num_sms, bool tc) {
   return align256((size_t)p->part_rows * sizeof(float2)) + (size_t)p->part_rows * p->d * sizeof(float);
 }
 
-// Rows of bf16 over a cache in 4 bits: which kernel.
+// Rows of bf16 over a cache in 4 bits: which kernel.  That of registers unpacks for 8 rows at a time, with little
+// else to do per key; a tile of the tensor cores takes what it takes, whatever its rows.  (4 bits, 32 heads on 8: 16
+// requests of 1, 4 and 9 rows with 8K of their own 39, 53 and 109 us, on the tensor cores 68, 70 and 74; 16 of one row over
+// a shared 4K and 32K 39 and 94, 34 and 49; 32 of one row and head over 8K, with 2K of their own, 76 and 94.)
 bool q4_on_tc(const PrefixAttnParams& p) {
   if (p.n > prefix_tc_q4_seqs(p.d)) return false;
-  const int64_t shared = p.shared_len >= 1024 ? (int64_t)p.total * p.rep : 0, own = (int64_t)((p.total + p.n - 1) / p.n) * p.rep;
-  return std::max(shared, own) > 16;
+  const int64_t shared = p.shared_len >= p.page ? (int64_t)p.total * p.rep : 0, own = (int64_t)((p.total + p.n - 1) / p.n) * p.rep;
+  return shared > 32 || own > 16;
 }
 
 }  // namespace

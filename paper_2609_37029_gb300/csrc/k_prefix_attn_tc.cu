@@ -98,7 +98,6 @@ struct TcMisc {
 template <int HD>
 struct Packed {
   static constexpr int kCodes = kKeys * HD / 2, kBytes = kCodes + kKeys * HD / 16;
-  static constexpr int kMost = 4;                // places, as far as there is room
 };
 
 // Shared memory: query tiles and ring, TcMisc, places in the line and sequences of the batch, packed tiles.
