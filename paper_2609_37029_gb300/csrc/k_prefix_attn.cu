@@ -524,11 +524,11 @@ PrefixCosts costs(int few_rows, int few, int many, int segment) {
   return c;
 }
 PrefixCosts attn_costs(const PrefixAttnParams& p) {
-  // ... over a cache in 4 bits: both are as long as it takes to unpack a block (16 requests of 17 rows over 32K 170 us,
-  // with the costs below 198)
-  if (p.tc && p.q4) return costs(p.tok_tile * p.rep, 5, 5, 11);
-  // one row tile 1.1 us a block, two 1.46, a segment 1.9 (16 requests over 32K, bf16)
-  if (p.tc) return costs(p.tok_tile * p.rep, 3, 4, 5);
+  // one row tile 1.1 us a block, two 1.46, a segment 1.9 (16 requests over 32K, bf16); over a cache in 4 bits both are as
+  // long as it takes to unpack a block (16 requests of 17 rows over 32K 172 us, with the costs of bf16 198)
+  if (p.tc) return p.q4 ? costs(p.tok_tile * p.rep, 5, 5, 8) : costs(p.tok_tile * p.rep, 3, 4, 5);
+  // unpacked again for every 8 rows (32 of one row over 8K and up to 4K of their own 52 us, with the costs below 76)
+  if (p.q4) return costs(8, 4, 10, 8);
   // (the fp32 kernel's warps have eight rows each, and those without rows leave the block to the others)
   return costs(32, 3, 4, 5);
 }
