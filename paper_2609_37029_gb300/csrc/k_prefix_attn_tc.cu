@@ -91,9 +91,10 @@ struct TcMisc {
   PrefixSched sched;
   float2 lone_ml[2][kRows];                      // stream 1's maximum and sum of segments with one row tile, by turns
   uint64_t packed_full[4], packed_empty[4];      // kQ4: tiles in 4 bits
-  int packed_keys[4];                            // keys of one; -1: no more tiles
+  int packed_keys[4];                            // keys of one, + kLone where one stream alone takes it; -1: no more tiles
 };
 
+constexpr int kLone = 256;
 // A tile of a cache in 4 bits: codes, then scales.
 template <int HD>
 struct Packed {
@@ -392,7 +393,7 @@ __device__ __forceinline__ void load_packed_role(const PrefixAttnParams& p, cons
       const int n = __popc(__ballot_sync(0xffffffffu, held));
       __syncwarp();
       if (lane == 0) {
-        m->packed_keys[at] = min(g.k_end - first, kKeys);
+        m->packed_keys[at] = min(g.k_end - first, kKeys) + (jobs.lone ? kLone : 0);
         mbar_expect_tx(bar, n * (codes + scales));
       }
       __syncwarp();
@@ -446,8 +447,8 @@ __device__ __forceinline__ void unpack_role(const PrefixAttnParams& p, int warp,
   for (;; place.next(count), ring.next(Sh::kStages)) {
     const uint32_t at = place.stage, st = ring.stage;
     if (!tc_wait(smem_u32(&m->packed_full[at]), place.phase, &m->abort, p.err)) return;
-    const int keys = m->packed_keys[at];
-    if (keys < 0) return;
+    const int word = m->packed_keys[at], keys = word & (kLone - 1);
+    if (word < 0) return;
     uint32_t w[kSteps][2], s[kSteps];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
@@ -474,6 +475,7 @@ __device__ __forceinline__ void unpack_role(const PrefixAttnParams& p, int warp,
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) {
+      if (warp == 0 && word >= kLone) mbar_arrive(smem_u32(&m->empty[st]));      // (for the stream without use for it)
       mbar_arrive(smem_u32(&m->full[st]));
       mbar_arrive(smem_u32(&m->packed_empty[at]));
     }
@@ -492,8 +494,10 @@ __device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, 
 // branch a product took 2.7 times as long).  Both streams come to every tile of
 // the ring and every query tile in order, and each arrives at it once: when its
 // products are done with the tile, or at once where it has no use for it.  So
-// neither is ever more than a phase from the other.
-template <int HD>
+// neither is ever more than a phase from the other.  (kQ4: where the streams take
+// alternate blocks, what a tile's stream alone comes to, the unpacking warps have
+// arrived for the other: the ring does not wait for a stream that is busy elsewhere.)
+template <int HD, bool kQ4>
 __device__ __forceinline__ void mma_role(const PrefixAttnParams& p, int t, uint32_t sm, uint32_t tmem, TcMisc* m,
                                          SegReader segs) {
   using Sh = TcShape<HD>;
@@ -509,6 +513,7 @@ __device__ __forceinline__ void mma_role(const PrefixAttnParams& p, int t, uint3
   auto wait = [&](uint32_t bar, uint32_t parity) { return tc_wait(bar, parity, &m->abort, p.err); };
   auto landed = [&](uint32_t tile) { return wait(full + 8 * (tile & (Sh::kStages - 1)), (tile / Sh::kStages) & 1); };
   auto pass = [&](uint32_t upto) {               // the other stream's tiles
+    if (kQ4) seen = upto;
     for (; seen < upto; ++seen) {
       if (!landed(seen)) return false;
       if (elect_one()) mbar_arrive(empty + 8 * (seen & (Sh::kStages - 1)));
@@ -844,7 +849,7 @@ __global__ void __launch_bounds__(kThreads<kQ4>, 1)
     } else if (kQ4 && warp >= kUnpackWarp)
       unpack_role<HD>(p, warp - kUnpackWarp, smp, packed, count, m);
     else if (warp < kMmaWarp + 2)
-      mma_role<HD>(p, warp - kMmaWarp, sm, tmem, m, segs);
+      mma_role<HD, kQ4>(p, warp - kMmaWarp, sm, tmem, m, segs);
     else
       plan_role(p, m, line_base, info);
   } else {
