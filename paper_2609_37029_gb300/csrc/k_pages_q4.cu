@@ -91,8 +91,9 @@ struct Eight {                                   // contiguous elements of a row
   }
 };
 
-// Unit u of a CTA: operand u & 1 (keys, values) of its row u >> 1.
-template <typename T>
+// Unit u of a CTA: operand u & 1 (keys, values) of its row u >> 1.  A lane has every 32nd word of the row: always the
+// same word of a head, of every (32 / words of a head)-th head.
+template <typename T, int HD>
 __global__ void __launch_bounds__(kThreads) pages_write_q4_kernel(const KvCache c, const int* seqs, const int* start, int n,
                                                                   const char* k_new, const char* v_new, int64_t row_bytes,
                                                                   int total, int per, unsigned* err) {
@@ -101,36 +102,33 @@ __global__ void __launch_bounds__(kThreads) pages_write_q4_kernel(const KvCache 
   griddep_launch();
   find_rows(c, seqs, start, n, total, per, rows, err);
   const int lane = threadIdx.x & 31;
-  const int per_head = c.d / 8, shift = 31 - __clz(per_head), words = c.nkv * per_head;
-  const int codes = c.page * (c.d / 2);          // bytes of a block's codes
+  constexpr int kPerHead = HD / 8, kHeads = 32 / kPerHead;       // words of a head, heads of a step
+  const int word = lane & (kPerHead - 1), steps = (c.nkv + kHeads - 1) / kHeads;
   for (int u = threadIdx.x >> 5; u < 2 * per; u += kThreads / 32) {
     const Row r = rows.row[u >> 1];
     if (r.kind != kHeld) continue;
-    const char* from = (u & 1 ? v_new : k_new) + (int64_t)(blockIdx.x * per + (u >> 1)) * row_bytes;
-    char* page = (u & 1 ? c.v : c.k) + (int64_t)r.page * c.s_page;
-    for (int i0 = 0; i0 < words; i0 += 32 * kBatch) {
+    const char* from = (u & 1 ? v_new : k_new) + (int64_t)(blockIdx.x * per + (u >> 1)) * row_bytes + lane * 8 * (int)sizeof(T);
+    char* block = (u & 1 ? c.v : c.k) + (int64_t)r.page * c.s_page + (int64_t)(lane / kPerHead) * c.s_head;
+    const int code_at = (r.slot * kPerHead + word) * 4, scale_at = c.page * (HD / 2) + (r.slot * (kPerHead / 4) + (word >> 2)) * 2;
+    for (int i0 = 0; i0 < steps; i0 += kBatch, from += kBatch * 32 * 8 * (int)sizeof(T)) {
+      const int left = c.nkv - i0 * kHeads - lane / kPerHead;    // heads from this lane's on
       Eight<T> v[kBatch];
 #pragma unroll
-      for (int q = 0; q < kBatch; ++q) {
-        const int i = i0 + 32 * q + lane;
-        if (i < words) v[q].load(from + (int64_t)i * 8 * sizeof(T));
-      }
+      for (int q = 0; q < kBatch; ++q)
+        if (q * kHeads < left) v[q].load(from + q * 32 * 8 * (int)sizeof(T));
 #pragma unroll
-      for (int q = 0; q < kBatch; ++q) {
-        const int i = i0 + 32 * q + lane;
-        if (i0 + 32 * q >= words) break;
-        uint32_t a = i < words ? v[q].most() : 0;
+      for (int q = 0; q < kBatch; ++q, block += kHeads * c.s_head) {
+        if (i0 + q >= steps) break;
+        const bool mine = q * kHeads < left;
+        uint32_t a = mine ? v[q].most() : 0;
         a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));  // (a group's four lanes end a row together)
         a = max(a, __shfl_xor_sync(0xffffffffu, a, 2));
-        if (i < words) {
+        if (mine) {
           const float s = q4_scale(a);
           float x[8];
           v[q].get(x);
-          char* block = page + (int64_t)(i >> shift) * c.s_head;
-          const int word = i & (per_head - 1);
-          reinterpret_cast<uint32_t*>(block)[r.slot * per_head + word] = q4_codes<sizeof(T) == 2>(x, s);
-          if ((word & 3) == 0)
-            reinterpret_cast<uint16_t*>(block + codes)[r.slot * (per_head >> 2) + (word >> 2)] = (uint16_t)(__float_as_uint(s) >> 16);
+          *reinterpret_cast<uint32_t*>(block + code_at) = q4_codes<sizeof(T) == 2>(x, s);
+          if ((word & 3) == 0) *reinterpret_cast<uint16_t*>(block + scale_at) = (uint16_t)(__float_as_uint(s) >> 16);
         }
         __syncwarp();
       }
@@ -211,7 +209,8 @@ dim3 row_grid(int total) { return dim3((unsigned)((total + rows_per_cta(total) -
 
 int launch_pages_write_q4(const KvCache& c, const int* seqs, const int* start, int n, const void* k_new, const void* v_new,
                           int64_t row_bytes, int total, int es, unsigned* err, cudaStream_t s) {
-  const auto kernel = es == 2 ? pages_write_q4_kernel<bf16> : pages_write_q4_kernel<float>;
+  const auto kernel = es == 2 ? (c.d == 128 ? pages_write_q4_kernel<bf16, 128> : pages_write_q4_kernel<bf16, 64>)
+                              : (c.d == 128 ? pages_write_q4_kernel<float, 128> : pages_write_q4_kernel<float, 64>);
   return status(launch_pdl(kernel, row_grid(total), dim3(kThreads), 0, s, c, seqs, start, n, static_cast<const char*>(k_new),
                            static_cast<const char*>(v_new), row_bytes, total, rows_per_cta(total), err));
 }

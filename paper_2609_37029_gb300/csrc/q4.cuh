@@ -99,7 +99,11 @@ __device__ __forceinline__ uint32_t q4_codes(float* x, float s) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] *= 18446744073709551616.0f;
   }
-  const float inv = __frcp_rn(s);
+  float inv;
+  if constexpr (kShort)
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));      // (2^-23 of it: what is off by that is rounded away)
+  else
+    inv = __frcp_rn(s);
   uint32_t w = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
