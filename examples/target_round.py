@@ -6,11 +6,16 @@ the drafter proposes B tokens from its fixed-size state (lsp_draft); the target
 takes the committed token and the proposals as B + 1 new rows of its cache
 (lsp_pages_reserve, then per layer lsp_pages_write and lsp_prefix_attention, the
 prompt's pages read once for all requests); lsp_verify_probs accepts r of the
-proposals and gives the next committed token; lsp_pages_trim gives back the
-rejected rows; lsp_view_update folds the r + 1 kept rows into the drafter's state.
-The prompt itself runs once, and lsp_pages_fork hands its pages to the requests.
+proposals and gives the next committed token; lsp_logprobs gives what a server
+answers beside the tokens; lsp_pages_trim gives back the rejected rows;
+lsp_view_update folds the r + 1 kept rows into the drafter's state.  The prompt
+itself runs once, and lsp_pages_fork hands its pages to the requests.
 
-    python examples/target_round.py [--rounds 8] [--prompt 500] [--temperature 1]
+With --cache q4 the cache is held in 4 bits (lsp_pages_write_q4,
+lsp_prefix_attention_q4).  At the end the drafter's state of the first request is
+built again from the cache (lsp_pages_read), as a server does that dropped it.
+
+    python examples/target_round.py [--rounds 8] [--prompt 500] [--temperature 1] [--cache bf16|q4]
 """
 import argparse
 import os
@@ -29,15 +34,15 @@ def whole(x):
 class Target:
     """The toy target and its paged cache: sequence 0 is the prompt, 1..C its continuations."""
 
-    def __init__(self, s, weights, most_tokens, page=64, seed=5):
-        self.s, self.w = s, weights
+    def __init__(self, s, weights, most_tokens, page=64, seed=5, q4=False):
+        self.s, self.w, self.q4 = s, weights, q4
         g = torch.Generator(device="cuda").manual_seed(seed)
         self.qkv, self.back = ([torch.randn(o, i, generator=g, device="cuda").mul_(i ** -0.5).to(s.torch_dtype)
                                 for _ in range(s.L)]
                                for o, i in (((s.nq + 2 * s.nkv) * s.d, s.H), (s.H, s.nq * s.d)))
         held = -(-most_tokens // page)
-        pool = (2, s.L, (s.C + 1) * held, s.nkv, page, s.d)
-        self.k, self.v = torch.zeros(pool, dtype=s.torch_dtype, device="cuda")
+        pool = (2, s.L, (s.C + 1) * held, s.nkv, page, s.d * 9 // 16 if q4 else s.d)
+        self.k, self.v = torch.zeros(pool, dtype=torch.uint8 if q4 else s.torch_dtype, device="cuda")
         self.table = torch.full((s.C + 1, held), -1, dtype=torch.int32, device="cuda")
         self.len = torch.zeros(s.C + 1, dtype=torch.int32, device="cuda")
         self.refs = torch.zeros(pool[2], dtype=torch.int32, device="cuda")
@@ -49,8 +54,13 @@ class Target:
         """New rows (tokens [total], rows [start[i], start[i+1]) of sequence seqs[i], add[i] of them) through
         the target: k, v [L][total][nkv][d], hidden states [L][total][H] and fp32 logits [total][V]."""
         s, c, total = self.s, self.cache, tokens.numel()
-        ws = torch.empty(lsp.lsp_prefix_attention_workspace_bytes(c, s.nq, seqs.numel(), total), dtype=torch.uint8,
-                         device="cuda")
+        if self.q4:
+            room = lsp.lsp_prefix_attention_q4_workspace_bytes(c, s.torch_dtype, s.nq, seqs.numel(), total)
+            write, attend = lsp.lsp_pages_write_q4, lsp.lsp_prefix_attention_q4
+        else:
+            room = lsp.lsp_prefix_attention_workspace_bytes(c, s.nq, seqs.numel(), total)
+            write, attend = lsp.lsp_pages_write, lsp.lsp_prefix_attention
+        ws = torch.empty(room, dtype=torch.uint8, device="cuda")
         lsp.lsp_pages_reserve(c, seqs, add, self.pages_ws, self.error)
         x = self.w["embed"][tokens.long()].float() * s.H ** 0.5
         k, v, h = [], [], []
@@ -58,15 +68,23 @@ class Target:
             y = (rms(x).to(s.torch_dtype) @ self.qkv[layer].T).view(total, s.nq + 2 * s.nkv, s.d)
             q, kn, vn = y.split([s.nq, s.nkv, s.nkv], dim=1)         # slices of the fused rows, no copy
             out = torch.empty(total, s.nq, s.d, dtype=s.torch_dtype, device="cuda")
-            lsp.lsp_pages_write(c, layer, seqs, start, kn, vn, self.error)
-            lsp.lsp_prefix_attention(c, layer, q, seqs, start, out, shared_len=shared, scale=s.d ** -0.5, workspace=ws,
-                                     dev_error=self.error)
+            write(c, layer, seqs, start, kn, vn, self.error)
+            attend(c, layer, q, seqs, start, out, shared_len=shared, scale=s.d ** -0.5, workspace=ws, dev_error=self.error)
             x = x + (out.view(total, -1) @ self.back[layer].T).float()
             k.append(kn)
             v.append(vn)
             h.append(x.to(s.torch_dtype))
         logits = (rms(x).to(s.torch_dtype) @ self.w["lm_head"].T).float()
         return torch.stack(k), torch.stack(v), torch.stack(h), logits
+
+    def read(self, seq, tokens):
+        """k, v [L][tokens][nkv][d] of a sequence's last tokens, as the cache holds them."""
+        s = self.s
+        k, v = torch.empty(2, s.L, tokens, s.nkv, s.d, dtype=s.torch_dtype, device="cuda")
+        seqs, start = whole([seq]), whole([0, tokens])
+        for layer in range(s.L):
+            lsp.lsp_pages_read(self.cache, layer, seqs, start, k[layer], v[layer], self.error)
+        return k, v
 
 
 def rms(x):
@@ -81,14 +99,14 @@ def distribution(logits, temperature):
 
 
 class Generation:
-    def __init__(self, s, prompt, rounds, temperature=0.0, seed=11):
-        """prompt: int32 [P] of token ids; the cache has room for `rounds` rounds."""
+    def __init__(self, s, prompt, rounds, temperature=0.0, seed=11, q4=False):
+        """prompt: int32 [P] of token ids; the cache has room for `rounds` rounds, in 4 bits with q4."""
         self.s, self.T, self.seed, self.round = s, temperature, seed, 0
         self.gen = torch.Generator(device="cuda").manual_seed(seed)
         w = synth.make_weights(s, device="cuda")
         self.weights, self.held = lsp.make_weights(w), w
         self.prompt = prompt.numel()
-        self.target = t = Target(s, w, self.prompt + (rounds + 1) * (s.B + 1))
+        self.target = t = Target(s, w, self.prompt + (rounds + 1) * (s.B + 1), q4=q4)
         self.seqs = whole(list(range(1, s.C + 1)))
         self.start = whole([i * (s.B + 1) for i in range(s.C + 1)])
         self.add = whole([s.B + 1] * s.C)
@@ -105,6 +123,8 @@ class Generation:
         self.committed = (p / self.exponentials(s.C)).argmax(-1).to(torch.int32)
         self.len = torch.full((s.C,), self.prompt, dtype=torch.int32, device="cuda")
         self.tokens = [[int(a)] for a in self.committed]
+        self.logprobs = [[] for _ in range(s.C)]                    # (log probability, entropy, top tokens, theirs) a token
+        self.boundary = h[:, -1:].expand(-1, s.C, -1).clone()       # hidden states of each request's last folded row [L][C][H]
         self.accepted = []
 
     def exponentials(self, rows):
@@ -128,6 +148,7 @@ class Generation:
         out = torch.empty(s.C, s.B + 1, dtype=torch.int32, device="cuda")
         u = torch.rand(s.C, s.B, generator=self.gen, device="cuda")
         lsp.lsp_verify_probs(p, q, y, u, self.exponentials(s.C), r, nxt, out_tokens=out, dev_error=t.error)
+        lp, entropy, top, top_lp = self.answers(z, out)
         keep = r + 1                                                # the committed token and the accepted ones
         self.len += keep
         lsp.lsp_pages_trim(t.cache, self.seqs, self.len, t.error)
@@ -137,8 +158,31 @@ class Generation:
         got = r.tolist()                                            # the round's result, on the host
         for b, row in enumerate(out.tolist()):
             self.tokens[b] += row[:got[b] + 1]
+            at = [b * (s.B + 1) + i for i in range(got[b] + 1)]
+            self.logprobs[b] += list(zip(lp[at].tolist(), entropy[at].tolist(), top[at].tolist(), top_lp[at].tolist()))
+            self.boundary[:, b] = h[:, at[-1]]
         self.accepted.append(got)
         return got
+
+    def answers(self, logits, out, k=3):
+        """Log probability and entropy of every emitted token, and the k likeliest in its place (-1: none emitted)."""
+        rows = logits.shape[0]
+        lp, entropy, top_lp = (torch.empty(*x, device="cuda") for x in ((rows,), (rows,), (rows, k)))
+        top = torch.empty(rows, k, dtype=torch.int32, device="cuda")
+        lsp.lsp_logprobs(logits, out.view(-1), lp, entropy, top, top_lp, temperature=self.T or 1.0, dev_error=self.target.error)
+        return lp, entropy, top, top_lp
+
+    def rebuild(self, b):
+        """A drafter state of request b alone, from what the cache holds of it."""
+        s = self.s.with_(C=1)
+        n = int(self.len[b])
+        k, v = self.target.read(b + 1, n)
+        h = torch.zeros(s.L, n, s.H, dtype=s.torch_dtype, device="cuda")
+        h[:, -1] = self.boundary[:, b]                              # (all that the state takes of them)
+        state = lsp.lsp_state_create(lsp.make_config(s))
+        lsp.lsp_state_init(state, self.held["G"])
+        lsp.lsp_view_update(state, k[None], v[None], h[None], whole([n]))
+        return state
 
     def check(self):
         """Raises if a kernel saw something wrong in any of the rounds."""
@@ -156,14 +200,18 @@ def main():
     ap.add_argument("--rounds", type=int, default=8)
     ap.add_argument("--prompt", type=int, default=500)
     ap.add_argument("--temperature", type=float, default=1.0)
+    ap.add_argument("--cache", choices=["bf16", "q4"], default="bf16")
     a = ap.parse_args()
     s = synth.SMALL.with_(layer_scale=False)
     prompt = torch.randint(0, s.V, (a.prompt,), generator=torch.Generator().manual_seed(3), dtype=torch.int32).cuda()
-    run = Generation(s, prompt, a.rounds, a.temperature)
+    run = Generation(s, prompt, a.rounds, a.temperature, q4=a.cache == "q4")
     for i in range(a.rounds):
         print(f"round {i}: accepted {run.step()} of {s.B}")
     run.check()
     live = int((run.target.refs > 0).sum())
+    said = [x[0] for row in run.logprobs for x in row]
+    print(f"mean log probability of {len(said)} tokens {sum(said) / len(said):.3f}")
+    lsp.lsp_state_destroy(run.rebuild(0))
     print(f"{sum(map(len, run.tokens))} tokens for {s.C} continuations of a prompt of {a.prompt}; {live} pages live")
     run.close()
 

@@ -90,7 +90,7 @@ __device__ __forceinline__ float q4_scale(uint32_t a_bits) {
 //         remainder (Markstein 1990).  Ties n + 1/2 are fp32 numbers, and an x next
 //         to s (n + 1/2) lies at least half a last place of the quotient from it.
 //   bf16  (x of eight significant bits) a quotient is a tie, or at least 2^-4 / (2 31)
-//         > 2^-10 from one; rounded to multiples of 2^-12 first, it stays what it is.
+//         > 2^-10 from one; rounded to multiples of 2^-13 first, it stays what it is.
 template <bool kShort>                           // x of eight significant bits
 __device__ __forceinline__ uint32_t q4_codes(float* x, float s) {
   if (!(s > 0.0f)) return kQ4Zero;                // an empty group, or one that is NaN
@@ -109,7 +109,7 @@ __device__ __forceinline__ uint32_t q4_codes(float* x, float s) {
   for (int e = 0; e < 8; ++e) {
     float y;
     if constexpr (kShort) {
-      y = fmaf(x[e], inv, 3072.0f) + (12582920.0f - 3072.0f);
+      y = fmaf(x[e], inv, 1536.0f) + (12582920.0f - 1536.0f);
     } else {
       const float q = x[e] * inv;
       y = fmaf(fmaf(-q, s, x[e]), inv, q) + 12582920.0f;

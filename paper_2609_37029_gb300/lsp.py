@@ -590,7 +590,7 @@ def lsp_verify_probs(target_probs, draft_probs, draft_tokens, u, e, accepted_len
 
 def lsp_logprobs(logits, tokens, logprob, entropy=None, top=None, top_logprob=None, *, temperature=1.0, dev_error=None,
                  stream=None) -> None:
-    """logits [rows][V] bfloat16 or float32, dense within a row (rows may overlap nothing and lie anywhere apart).
+    """logits [rows][V] bfloat16 or float32, dense within a row (which may be followed by anything).
     Contiguous: int32 tokens [rows] (-1: none) and top [rows][k], float32 logprob and entropy [rows], top_logprob
     [rows][k]; all but logprob may be None."""
     if logits.dim() != 2:

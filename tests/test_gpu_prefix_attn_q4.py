@@ -254,3 +254,61 @@ def test_long_context_split_over_the_whole_gpu(lsp, dtype):
             tol = (2 ** -8 + 2 ** -10) * (size + want.abs()) if dtype == "bf16" else 4e-5 * size
             assert ((out[r0 + i].double() - want).abs() <= tol).all()
             assert (z[r0 + i].double() - torch.logsumexp(s, -1)).abs().max() < 2e-5 + 2e-6 * 12
+
+
+def check_by_sequence(pool, t, q, lens, rows, out, z):
+    """Sequence by sequence in fp64, one KV head, nothing shared."""
+    from tests.q4_common import held
+    kk, vv = (torch.from_numpy(held(x)).cuda() for x in pool)
+    d, page, at = q.shape[2], pool[0].shape[3], 0
+    tol = (lambda size, want: (2 ** -8 + 2 ** -10) * (size + want.abs())) if q.dtype == torch.bfloat16 else (lambda size, want: 4e-5 * size)
+    for b, (n, r) in enumerate(zip(lens, rows)):
+        pages = t[0][b, :-(-n // page)].long()
+        k, v = (x[0, pages, 0].reshape(-1, d)[:n].double() for x in (kk, vv))
+        s = torch.einsum("rhd,nd->rhn", q[at:at + r].double(), k) * d ** -0.5
+        seen = torch.arange(n, device="cuda")[None] <= torch.arange(n - r, n, device="cuda")[:, None]
+        s = s.masked_fill(~seen[:, None], -torch.inf)
+        w = torch.softmax(s, -1)
+        want, size = w @ v, w @ v.abs()
+        assert bool(((out[at:at + r].double() - want).abs() <= tol(size, want)).all()), b
+        lse = torch.logsumexp(s, -1)
+        assert bool(((z[at:at + r].double() - lse).abs() <= 2e-5 + 2e-6 * lse.abs()).all()), b
+        at += r
+
+
+# 64 heads on one KV head: a tile of the tensor cores has two tokens, so 1 and 2 rows are one tile, 3 and 4 two
+@pytest.mark.parametrize("order", [(4, 1), (3, 2, 1), (4, 4, 1, 1), (1, 4, 1, 3, 9)])
+@pytest.mark.parametrize("d,blocks", [(64, 2), (128, 3)])
+def test_one_and_two_row_tiles_by_turns(lsp, order, d, blocks):
+    n = 400
+    rows = [order[i % len(order)] for i in range(n)]
+    lens = [128 * (1 + i % blocks) + 7 + 5 * i % 113 for i in range(n)]
+    pool, t, q = case(lens, rows, 0, nq=64, nkv=1, d=d, dtype="bf16", page=16)
+    seqs = list(range(n))
+    out, z = attend(lsp, pool, t, q, seqs, rows, 0)
+    check_by_sequence(pool, t, q, lens, rows, out, z)
+    for fill in (0, 0x5A):
+        again, z2 = attend(lsp, pool, t, q, seqs, rows, 0, fill=fill)
+        assert torch.equal(out, again) and torch.equal(z, z2)
+
+
+@pytest.mark.parametrize("n", [150, 180, 480, 700, 1024])
+@pytest.mark.parametrize("dtype", list(DT))
+def test_batches_around_what_there_is_room_for(lsp, n, dtype):
+    """The schedule of a batch lies in shared memory: more sequences leave room for fewer tiles, or for another kernel."""
+    rows = [1 + i % 2 for i in range(n)]
+    lens = [20 + 37 * i % 150 for i in range(n)]
+    pool, t, q = case(lens, rows, 0, nq=20, nkv=1, d=128, dtype=dtype, page=32)
+    out, z = attend(lsp, pool, t, q, list(range(n)), rows, 0)
+    check_by_sequence(pool, t, q, lens, rows, out, z)
+
+
+def test_the_workspace_of_a_call_is_enough_whatever_is_shared(lsp):
+    """It is asked for before it is known how much is shared, and the kernel is chosen by that."""
+    for n, q in ((1, 1), (3, 1), (16, 1), (40, 1), (4, 9), (2, 300)):
+        lens, rows = [2 * 64 + 300 + i for i in range(n)], [q] * n
+        pool, t, x = case(lens, rows, 128, nq=8, nkv=2, d=64, dtype="bf16", page=64)
+        oc = oracle_cache(*pool, *t)
+        for shared in (0, 64, 128):
+            out, z = attend(lsp, pool, t, x, list(range(n)), rows, shared)
+            compare(oc, x, list(range(n)), rows, out, z)
