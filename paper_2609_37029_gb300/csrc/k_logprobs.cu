@@ -156,6 +156,7 @@ struct Scale {
 struct Stats {
   float m, ref;
   float least;          // logits below count nothing and are raised to here; NaN: t = (z - m) c, limited, one by one
+  uint32_t low;         // the same as a pair of bf16, rounded down
   float2 s, a;          // of every other element, to be added
   float best, other;
   uint32_t place;
@@ -190,6 +191,8 @@ __device__ __forceinline__ void raise(Stats& st, float top, const Scale& k) {
   st.ref = ref;
   // (200 / c below m; where m's last place is more than that, some of those below)
   st.least = fine ? top - fmaxf(200.0f * k.inv, fabsf(top) * 0x1p-20f) : __uint_as_float(0x7FC00000u);
+  const __nv_bfloat16 low = __float2bfloat16_rd(st.least);
+  st.low = bf2_bits(__halves2bfloat162(low, low));
 }
 __device__ __forceinline__ void add_limited(Stats& st, float x, const Scale& k) {
   const float t = max_nan((x - st.m) * k.c, kLeast), e = ex2a(t);
@@ -216,8 +219,7 @@ __device__ __forceinline__ void add_piece(Stats& st, Piece<T>& v, uint32_t place
     return;
   }
   const float2 c = make_float2(k.c, k.c), ref = make_float2(-st.ref, -st.ref);
-  const __nv_bfloat16 low = __float2bfloat16_rd(st.least);
-  const __nv_bfloat162 low2 = __halves2bfloat162(low, low);
+  const __nv_bfloat162 low2 = bits_bf2(st.low);
   float2 s[2] = {st.s, {0.f, 0.f}}, a[2] = {st.a, {0.f, 0.f}};
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
@@ -315,7 +317,9 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, f
       if (count_all(key > cut || (key == cut && st.place < (last | bit))) < k) last |= bit;
   }
   auto in = [&](uint32_t e_key, uint32_t place) { return e_key > cut || (e_key == cut && place <= last); };
+  const float least = of_key<T>(cut);            // (most elements are below it, and go no further)
   auto put = [&](float x, uint32_t place, int index) {
+    if (cut > 0 && !(x >= least)) return;
     const uint32_t e = key_of<T>(x);
     if (!in(e, place)) return;
     const int at = atomicAdd(&sm.count, 1);
@@ -491,7 +495,7 @@ __device__ __forceinline__ void add_role(const LogprobsParams& p, Smem& sm, Rows
     float head = 0.f, tail = 0.f;
     if (tid < part.head) head = to_f(part.z[tid]);
     if (tid < part.tail) tail = to_f(part.z[part.tail_index + tid]);
-    Stats st = {kLowest, kLowest, __uint_as_float(0x7FC00000u), {0.f, 0.f}, {0.f, 0.f}, -INFINITY, -INFINITY, 0u};
+    Stats st = {kLowest, kLowest, __uint_as_float(0x7FC00000u), 0u, {0.f, 0.f}, {0.f, 0.f}, -INFINITY, -INFINITY, 0u};
     // (a thread's first place, for stripes of -inf alone)
     st.place = tid < part.head ? tid : tid < part.pieces ? kStripes + tid : part.tail_at + tid;
     for (int i0 = 0; i0 < part.pieces; i0 += kThreads, ring.next(kStages)) {
