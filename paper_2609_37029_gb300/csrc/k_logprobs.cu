@@ -24,6 +24,12 @@
 // many rows as fall to them; a warp of each copies the rows' next pieces into a ring
 // meanwhile (40 KB, four CTAs on an SM), so that memory is read on while a row's last
 // steps, which are rounds of latency, are taken.
+//
+// Rows of 151936 on 608 CTAs: 1088 of bf16 with k = 5 in 75 us (330 MB, 4.4 TB/s; 72
+// with k = 0: two rows fall to most CTAs and one to some, which is 11 us of it), 190 of
+// fp32 among 272 with k = 20 in 32 us (116 MB, 3.6 TB/s), of which some 6 are the start and
+// the last rows' selection.  With a launch's CTAs for each part instead, without the
+// ring: 97 and 50.
 #include <algorithm>
 #include <cstddef>
 

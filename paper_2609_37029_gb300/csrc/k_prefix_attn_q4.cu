@@ -23,9 +23,20 @@
 // (8 / row groups)-th slice of 16 keys.  At its end the warps of the same rows add
 // up through shared memory.
 //
-// Few rows (decoding) leave the values to be unpacked as the work: 2 x 3.75
-// instructions for a pair of keys' values and one product for 256 of them, beside
-// 0.56 bytes of memory a value.
+// Few rows (decoding) leave the values to be unpacked as the work: 3.75 instructions
+// for a pair of them (shift, mask and magic number, minus 136, times the scale), half
+// of those on the half-rate integer pipe, and one product for 256, beside 0.56 bytes
+// of memory a value.  Measured (bf16, 32 heads on 8 of 128): 32 requests of one row
+// over 500 to 16000 tokens of their own 101 us in all for 354 MB (3.5 TB/s).  Without
+// any work on the blocks that is 76 us: 57 at 6.2 TB/s, 6 until the first block is there
+// (lengths, schedule, first segment, page, block: a chain of loads), 12 for the last
+// segments' sums and the join.  The other 25 are the multiplying warps': some 440
+// instructions for 16 keys, 0.62 of the issue slots and half of the integer pipe.
+// Tried and dropped: a fourth stage (106), one CTA an SM with twice the registers
+// (123), four row tiles a warp for 9 to 64 rows (16 requests of one row over 32K: 90
+// us, with one tile 89: products of 8 columns are as slow as unpacking), shifts as
+// products in the other pipe (108 to 122).  Rows past 16 an item go to the tensor cores'
+// own memory (k_prefix_attn_tc.cu), which takes a block's time whatever its rows.
 #include <algorithm>
 
 #include "barrier_wait.cuh"
