@@ -607,7 +607,7 @@ int lsp_verify_probs(const void* target_probs, const void* draft_probs, int dtyp
  * A row whose largest logit is not finite (all -inf, a +inf) or that has a NaN has
  * no distribution: NaN in logprob, entropy and top_logprob; top still holds k
  * tokens (+inf first, -inf after the finite ones, NaN last).
- * T in [2^-100, 2^100]; rows in [0, 2^27], V in [1, 2^30], ld >= V, k in [0, min(V, 32)].  One launch;
+ * T in [2^-100, 2^100]; rows in [0, 2^27], V in [1, 2^26], ld >= V, k in [0, min(V, 32)].  One launch;
  * each row is read once (the parts of it with its largest logits twice).  In fp32;
  * the same call gives the same bits.  How many rows there are decides how a row is
  * split: its sums may differ in their last bits, the tokens never. */

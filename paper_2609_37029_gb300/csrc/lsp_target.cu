@@ -272,7 +272,7 @@ int lsp_verify_probs(const void* target_probs, const void* draft_probs, int dtyp
 int lsp_logprobs(const void* logits, int dtype, const int32_t* tokens, int rows, int V, int64_t ld, float temperature, int k,
                  float* logprob, float* entropy, int32_t* top, float* top_logprob, uint32_t* dev_error, lsp_stream_t stream) {
   if (!is_float(dtype) || rows < 0 || k < 0 || !(temperature >= 0x1p-100f && temperature <= 0x1p100f)) return LSP_ERR_ARG;
-  if (rows > (1 << 27) || V < 1 || V > (1 << 30) || ld < V || ld >= ((int64_t)1 << 40) || k > kLogprobsMaxK || k > V) return LSP_ERR_SHAPE;
+  if (rows > (1 << 27) || V < 1 || V > (1 << 26) || ld < V || ld >= ((int64_t)1 << 40) || k > kLogprobsMaxK || k > V) return LSP_ERR_SHAPE;
   if (rows == 0) return LSP_OK;
   if (!logits || !tokens || !logprob || !aligned(logits, esize(dtype)) ||
       !words(tokens, logprob, entropy, top, top_logprob, dev_error))

@@ -176,6 +176,28 @@ def test_a_row_does_not_depend_on_the_others(lsp):
     check(z[:1], tokens[:1], 20, 1.0, one)
 
 
+@pytest.mark.parametrize("rows,V,k", [(70001, 7, 3), (9000, 40, 32), (3000, 600, 5)])
+def test_many_short_rows(lsp, rows, V, k):
+    """A cluster goes through hundreds of rows, some without a token, in any run of 32."""
+    g = torch.Generator().manual_seed(rows)
+    z = (torch.randn(rows, V, generator=g) * 3).cuda()
+    tokens = torch.randint(0, V, (rows,), generator=g, dtype=torch.int32)
+    tokens[torch.rand(rows, generator=g) < 0.3] = -1
+    tokens[5000:5500] = -1
+    tokens = tokens.cuda()
+    out = call(lsp, z, tokens, k)
+    live = tokens >= 0
+    lp = torch.log_softmax(z.double(), -1)
+    want = lp.gather(1, tokens.clamp(min=0).long()[:, None])[:, 0]
+    assert bool((out[0][~live] == -torch.inf).all()) and bool((out[1][~live] == 0).all())
+    assert bool((out[2][~live] == -1).all()) and bool((out[3][~live] == -torch.inf).all())
+    assert float((out[0].double() - want)[live].abs().max()) <= 3e-5
+    assert float((out[1].double() + (lp.exp() * lp).sum(-1))[live].abs().max()) <= 2e-4
+    order = torch.sort(z, descending=True, stable=True).indices[:, :k]
+    assert torch.equal(out[2][live], order[live].int())
+    assert float((out[3].double() - lp.gather(1, order))[live].abs().max()) <= 3e-5
+
+
 def test_streams_and_graphs(lsp):
     z, tokens = logits(20, 40001, "f32", 3).cuda(), ints(range(20))
     want = call(lsp, z, tokens, 6)

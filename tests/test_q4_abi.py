@@ -103,7 +103,7 @@ def test_logprobs(lsp):
                dict(T=float("nan")), dict(T=float("inf")), dict(T=1e-38), dict(T=1e38), dict(z=0x1002), dict(dtype=0, z=0x1001), dict(tokens=0x2002),
                dict(logprob=0x3001), dict(entropy=0x4002), dict(top=0x5001), dict(tl=0x6002), dict(err=0x7001)):
         assert call(**kw) == A, kw
-    for kw in (dict(V=0), dict(V=2 ** 30 + 1, ld=2 ** 31), dict(ld=99), dict(k=33), dict(V=4, ld=4), dict(rows=2 ** 27 + 1), dict(ld=2 ** 40)):
+    for kw in (dict(V=0), dict(V=2 ** 26 + 1, ld=2 ** 31), dict(ld=99), dict(k=33), dict(V=4, ld=4), dict(rows=2 ** 27 + 1), dict(ld=2 ** 40)):
         assert call(**kw) == S, kw
     assert call(rows=0, z=None) == lsp.LSP_OK
 
