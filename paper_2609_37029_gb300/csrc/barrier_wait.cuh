@@ -29,6 +29,15 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// Arrival of a warp at the barrier behind which a copy may write over what it has read
+// in shared memory.  An arrival does not wait for loads that are on their way, and the
+// copy does not queue behind them: so it is made to need them.  read: bits of every
+// load's result; zero: a 0 that the compiler does not know of.
+__device__ __forceinline__ void arrive_after_reads(uint32_t bar, uint32_t read, uint32_t zero) {
+  const uint32_t none = __ballot_sync(0xffffffffu, (read & zero) != 0);          // (0, once every lane has its values)
+  if ((threadIdx.x & 31) == 0) mbar_arrive(bar + none);
+}
+
 struct Place {                                   // of the ring: a stage, and the parity of its use
   uint32_t stage, phase;
   __device__ __forceinline__ void next(uint32_t count) {

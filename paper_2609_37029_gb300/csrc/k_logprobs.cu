@@ -493,7 +493,7 @@ __device__ __forceinline__ void add_role(const LogprobsParams& p, Smem& sm, Rows
   bool failed = false;
   auto wait = [&](uint64_t* bar, uint32_t parity) { failed |= !tc_wait(smem_u32(bar), parity, &sm.abort, p.err); };
   Place ring = {0, 0};
-  const uint32_t ring_at = smem_u32(sm.ring) + tid * kPieceBytes;
+  const uint32_t ring_at = smem_u32(sm.ring) + tid * kPieceBytes, zero = (uint32_t)p.V >> 31;
   int token;
   uint32_t turn = 0;
   for (int row = rows.next(&token); row >= 0; row = rows.next(&token), ++turn) {
@@ -510,8 +510,7 @@ __device__ __forceinline__ void add_role(const LogprobsParams& p, Smem& sm, Rows
       // (eight lanes, 64 bytes apart, read eight different 16 bytes of 128; the order within a piece does not matter)
 #pragma unroll
       for (int q = 0; q < 4; ++q) v.v[q] = ld_shared4(ring_at + ring.stage * kStageBytes + ((q + (lane >> 1)) & 3) * 16);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sm.empty[ring.stage]));
+      arrive_after_reads(smem_u32(&sm.empty[ring.stage]), v.v[0].x ^ v.v[1].x ^ v.v[2].x ^ v.v[3].x, zero);
       if (i0 + tid < part.pieces) add_piece(st, v, kStripes + i0 + tid, scale);
     }
     settle(st, scale);

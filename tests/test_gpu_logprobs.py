@@ -198,6 +198,25 @@ def test_many_short_rows(lsp, rows, V, k):
     assert float((out[3].double() - lp.gather(1, order))[live].abs().max()) <= 3e-5
 
 
+@pytest.mark.parametrize("rows,V,dtype", [(272, 151936, "f32"), (700, 151936, "bf16"), (40, 300007, "f32")])
+def test_the_same_call_gives_the_same_bits(lsp, rows, V, dtype):
+    """Long rows through the ring, call behind call: no piece is lost to the copy that follows it, or taken twice."""
+    z = torch.randn(rows, V, device="cuda", generator=torch.Generator("cuda").manual_seed(V)).mul_(2.5).to(DT[dtype])
+    tokens = ints(range(rows))
+    outs = []
+    for _ in range(100):
+        outs.append([torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(rows, 5, dtype=torch.int32, device="cuda"),
+                     torch.empty(rows, 5, device="cuda")])
+        lsp.lsp_logprobs(z, tokens, *outs[-1])
+    torch.cuda.synchronize()
+    for out in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(outs[0], out))
+    for at in range(0, rows, 50):
+        lp = torch.log_softmax(z[at:at + 50].double(), -1)
+        want = lp.gather(1, tokens[at:at + 50].long()[:, None])[:, 0]
+        assert float((outs[0][0][at:at + 50].double() - want).abs().max()) <= 3e-5
+
+
 def test_streams_and_graphs(lsp):
     z, tokens = logits(20, 40001, "f32", 3).cuda(), ints(range(20))
     want = call(lsp, z, tokens, 6)
