@@ -240,6 +240,8 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
     vs_at[j] = 2 * St::kCodes + St::kScales + kv[j] * (HD / 16) + (HD == 128 ? r >> 1 : r >> 2) * 2;
   }
   const uint32_t ring_at = smem_u32(sm.ring), full_at = smem_u32(sm.full), empty_at = smem_u32(sm.empty);
+  const uint32_t zero = (uint32_t)p.n >> 31;
+  uint32_t read = 0;
   const Q4Consts consts;
   // 16 keys, the first of them key `key` of the sequence, from `codes` and `scales` on; edge: some row does not see some key
   auto slice = [&](uint32_t codes, uint32_t scales, int key, auto edge) {
@@ -318,6 +320,7 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
       if (kEdge && key + kv[j & 1] + (j >> 1) * 8 >= g.k_end) sv[j] = 0;
     }
     const uint32_t sa = sv[0] | sv[1] << 16, sb = sv[2] | sv[3] << 16;
+    read = sa ^ sb ^ w[0][0] ^ w[1][0] ^ w[2][0] ^ w[3][0];      // (the keys' words the votes above have needed)
 #pragma unroll
     for (int i = 0; i < kWordsV; ++i) {
       const uint32_t lo_a = __byte_perm(w[0][i], w[1][i], 0x5410), hi_a = __byte_perm(w[0][i], w[1][i], 0x7632);
@@ -341,9 +344,8 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
       } else {
         for (int i = kg; i < kSlices; i += kgs) slice(at + i * kSlice * (HD / 2), at + i * kSlice * (HD / 16), key0 + i * kSlice, BoolTag<false>());
       }
-      __syncwarp();
     }
-    if (lane == 0) mbar_arrive(empty_at + 8 * ring.stage);
+    arrive_after_reads(empty_at + 8 * ring.stage, read, zero);
     ring.next(St::kCount);
   }
 #pragma unroll

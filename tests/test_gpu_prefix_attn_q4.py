@@ -312,3 +312,21 @@ def test_the_workspace_of_a_call_is_enough_whatever_is_shared(lsp):
         for shared in (0, 64, 128):
             out, z = attend(lsp, pool, t, x, list(range(n)), rows, shared)
             compare(oc, x, list(range(n)), rows, out, z)
+
+
+@pytest.mark.parametrize("rows,shared,dtype", [(1, 0, "bf16"), (1, 4096, "bf16"), (9, 8192, "bf16"), (3, 2048, "f32")])
+def test_the_same_call_gives_the_same_bits(lsp, rows, shared, dtype):
+    """Long sequences through the rings of both kernels, call behind call."""
+    n = 24
+    lens = [shared + rows + 400 * i % 5000 for i in range(n)]
+    pool, t, q = case(lens, [rows] * n, shared, nq=32, nkv=8, d=128, dtype=dtype, page=64)
+    c = lsp.make_kv_cache(*pool, *t)
+    ws = torch.empty(lsp.lsp_prefix_attention_q4_workspace_bytes(c, q.dtype, 32, n, n * rows), dtype=torch.uint8, device="cuda")
+    ids, start = ints(range(n)), ints(range(0, n * rows + 1, rows))
+    outs = []
+    for _ in range(60):
+        outs.append((torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")))
+        lsp.lsp_prefix_attention_q4(c, 0, q, ids, start, *outs[-1], shared_len=shared, scale=128 ** -0.5, workspace=ws)
+    torch.cuda.synchronize()
+    for out in outs[1:]:
+        assert torch.equal(out[0], outs[0][0]) and torch.equal(out[1], outs[0][1])
