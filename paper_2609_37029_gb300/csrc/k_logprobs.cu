@@ -25,9 +25,9 @@
 // meanwhile (40 KB, four CTAs on an SM), so that memory is read on while a row's last
 // steps, which are rounds of latency, are taken.
 //
-// Rows of 151936 on 608 CTAs: 1088 of bf16 with k = 5 in 75 us (330 MB, 4.4 TB/s; 72
+// Rows of 151936 on 608 CTAs: 1088 of bf16 with k = 5 in 76 us (330 MB, 4.4 TB/s; 72
 // with k = 0: two rows fall to most CTAs and one to some, which is 11 us of it), 190 of
-// fp32 among 272 with k = 20 in 32 us (116 MB, 3.6 TB/s), of which some 6 are the start and
+// fp32 among 272 with k = 20 in 33 us (115 MB, 3.5 TB/s), of which some 6 are the start and
 // the last rows' selection.  With a launch's CTAs for each part instead, without the
 // ring: 97 and 50.
 #include <algorithm>
@@ -510,8 +510,9 @@ __device__ __forceinline__ void add_role(const LogprobsParams& p, Smem& sm, Rows
       // (eight lanes, 64 bytes apart, read eight different 16 bytes of 128; the order within a piece does not matter)
 #pragma unroll
       for (int q = 0; q < 4; ++q) v.v[q] = ld_shared4(ring_at + ring.stage * kStageBytes + ((q + (lane >> 1)) & 3) * 16);
-      arrive_after_reads(smem_u32(&sm.empty[ring.stage]), v.v[0].x ^ v.v[1].x ^ v.v[2].x ^ v.v[3].x, zero);
       if (i0 + tid < part.pieces) add_piece(st, v, kStripes + i0 + tid, scale);
+      // (the sum needs all of the piece; as soon as the loads are there, in front of the piece, is 1 % slower)
+      arrive_after_reads(smem_u32(&sm.empty[ring.stage]), __float_as_uint(st.s.x), zero);
     }
     settle(st, scale);
     if (tid < part.head) {                       // (the first of its stripe: it goes before an equal one)
