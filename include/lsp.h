@@ -605,12 +605,13 @@ int lsp_verify_probs(const void* target_probs, const void* draft_probs, int dtyp
  *   top     device int32 [rows][k], top_logprob device float [rows][k]; either may
  *           be NULL, and both are not written with k = 0
  * A row whose largest logit is not finite (all -inf, a +inf) or that has a NaN has
- * no distribution: NaN in logprob, entropy and top_logprob; top still holds k
- * tokens (+inf first, -inf after the finite ones, NaN last).
- * T in [2^-100, 2^100]; rows in [0, 2^27], V in [1, 2^26], ld >= V, k in [0, min(V, 32)].  One launch;
- * each row is read once (the parts of it with its largest logits twice).  In fp32;
- * the same call gives the same bits.  How many rows there are decides how a row is
- * split: its sums may differ in their last bits, the tokens never. */
+ * no distribution: NaN in logprob, entropy and top_logprob, -1 in top.  (In other
+ * rows tokens of -inf follow the finite ones, with top_logprob -inf.)
+ * T in [2^-100, 2^100]; rows in [0, 2^27], V in [1, 2^26], ld >= V, k in
+ * [0, min(V, 32)].  One launch; each row is read once (the parts of it with its
+ * largest logits twice).  In fp32; the same call gives the same bits.  How many rows
+ * there are decides how a row is split: its sums may differ in their last bits, the
+ * tokens never. */
 int lsp_logprobs(const void* logits, int dtype, const int32_t* tokens, int rows, int V, int64_t ld,
                  float temperature, int k, float* logprob, float* entropy, int32_t* top,
                  float* top_logprob, uint32_t* dev_error, lsp_stream_t stream);
