@@ -96,6 +96,9 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {     // of an 8 x 8 
 // (rows of 64 bytes: reads of keys then meet no bank twice, reads of values two at most).
 __device__ __forceinline__ int key_at(int m) { return m ^ ((m >> 1) & 1); }
 
+// A value that is the same in all of a warp, as one that the compiler knows to be.
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+
 // Pairs of x, y as kPieces bf16 numbers each, of falling size.
 template <int P>
 __device__ __forceinline__ void split_pair(float x, float y, uint32_t* out) {
@@ -359,7 +362,7 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
 
 template <typename T, int HD>
 __device__ __forceinline__ void multiply_role(const PrefixAttnParams& p, Smem<HD>& sm) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, t = lane & 3;
+  const int lane = threadIdx.x & 31, warp = uniform(threadIdx.x >> 5), r = lane >> 2, t = lane & 3;
   Place ring = {0, 0};
   uint32_t met = 0;
   // the multiplying warps wait for each other (within the limit of every wait: one of them may have given up)
@@ -371,9 +374,13 @@ __device__ __forceinline__ void multiply_role(const PrefixAttnParams& p, Smem<HD
   for (uint32_t k = 0;; ++k) {
     const uint32_t at = k % kAhead;
     if (!tc_wait(smem_u32(&sm.seg_full[at]), (k / kAhead) & 1, &sm.abort, p.err)) break;
-    const bool more = sm.planned[at].more;
+    const bool more = uniform(sm.planned[at].more) != 0;
     PrefixSeg g;
-    if (more) g = sm.planned[at].g;
+    if (more) {
+      g = sm.planned[at].g;
+      g.head = uniform(g.head), g.t0 = uniform(g.t0), g.tokens = uniform(g.tokens);
+      g.k0 = uniform(g.k0), g.kb0 = uniform(g.kb0), g.kb1 = uniform(g.kb1), g.k_end = uniform(g.k_end), g.see0 = uniform(g.see0);
+    }
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&sm.seg_empty[at]));
     if (!more) break;
