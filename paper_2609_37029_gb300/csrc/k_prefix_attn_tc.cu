@@ -436,7 +436,7 @@ __device__ __forceinline__ void load_packed_role(const PrefixAttnParams& p, cons
   __syncwarp();
 }
 
-// Tiles from 4 bits to bf16, 32 keys of each to a warp.  A lane takes two words of codes, 16 dims, at a time: a
+// Tiles from 4 bits to bf16, eighths of the values, 32 keys of each to a warp.  A lane takes two words of codes, 16 dims, at a time: a
 // warp's words lie side by side, and eight lanes store to eight different columns of 16 bytes (lanes of the second
 // half of a row's dims begin with their second word).
 template <int HD>
@@ -450,7 +450,7 @@ __device__ __forceinline__ void unpack_role(const PrefixAttnParams& p, int warp,
   const uint32_t base = smem_u32(packed) + first * (HD / 2) + pair * 8, scale_base = smem_u32(packed) + Pk::kCodes + first * (HD / 16) + (pair >> 1) * 2;
   const uint32_t to = smem_u32(smp) + Sh::kRing + (second ? Sh::kHalf : 0u) + first * 128;
   const int column = (2 * pair & 7) | (second ? 1 : 0);
-  const Q4Consts consts;
+  const Q4Eighths consts;
   Place place = {0, 0}, ring = {0, 1};
   for (;; place.next(count), ring.next(Sh::kStages)) {
     const uint32_t at = place.stage, st = ring.stage;
@@ -475,9 +475,9 @@ __device__ __forceinline__ void unpack_role(const PrefixAttnParams& p, int warp,
       const int key = first + i * kKeysOf;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const uint32_t x = second ? w[i][1 - e] : w[i][e];
-        st_shared4(row + (((column ^ e ^ key) & 7) << 4), q4_pair(consts, x, scale), q4_pair(consts, x >> 4, scale),
-                   q4_pair(consts, x >> 8, scale), q4_pair(consts, x >> 12, scale));
+        uint32_t x[4];
+        q4_eighths(consts, second ? w[i][1 - e] : w[i][e], scale, x);
+        st_shared4(row + (((column ^ e ^ key) & 7) << 4), x[0], x[1], x[2], x[3]);
       }
     }
     fence_proxy_async_smem();
@@ -631,7 +631,8 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
   const int lane = threadIdx.x & 31, quad = (threadIdx.x >> 5) & 3, row = quad * 32 + lane;
   const uint32_t ts = tmem + ((uint32_t)(quad * 32) << 16) + 128u * t, to = ts + 256u;
   const int tok = row / p.rep;
-  const float sl = p.scale * kLog2e;
+  constexpr float kUnit = kQ4 ? 8.0f : 1.0f;     // (unpacked tiles hold eighths)
+  const float sl = kUnit * p.scale * kLog2e;
   uint32_t ns = 0, no = 0, no1 = 0;              // jobs; segments of this stream, of stream 1 (as stream 0 sees them)
   uint32_t lones = 0, tiles = 0;                 // segments that both streams add up; ring tiles of the segments before
   PrefixSeg g;
@@ -752,6 +753,8 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
         w1 = other.x == -INFINITY ? 0.f : ex2a((other.x - top) * sl);
         mx = top;
         sum = sum * w0 + other.y * w1;
+        w0 *= kUnit;
+        w1 *= kUnit;
       }
       ++no1;
     }
@@ -766,6 +769,9 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
         tmem_ld32(to + 128 + c, x);
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = o[e] * w0 + x[e] * w1;
+      } else if (kQ4) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) o[e] *= kUnit;
       }
       if (c + 32 == HD) {                        // the sums are in registers: the next segment may start
         tc_fence_before();

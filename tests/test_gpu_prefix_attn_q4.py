@@ -314,6 +314,36 @@ def test_the_workspace_of_a_call_is_enough_whatever_is_shared(lsp):
             compare(oc, x, list(range(n)), rows, out, z)
 
 
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("rows", [[2, 1], [40, 35]])
+@pytest.mark.parametrize("k_by,v_by", [(60, -120), (-110, 100)])
+def test_very_large_and_very_small_values(lsp, rows, k_by, v_by, dtype):
+    """Powers of two change no rounding while results are normal numbers: keys times 2^k_by under queries times
+    2^-k_by, and values times 2^v_by, give the bits of what they are without them.  Values of 2^-120 give sums below
+    2^-126, whose last place is 2^-149: some 300 products and four roundings of a sum lose at most 1200 times half of
+    that, 2^-139.  Beside that the output is rounded once more: by half a last place, 2^-134 of a bf16 subnormal, and
+    where the lost bits cross a tie by a whole one (2^-8, 2^-23 of it)."""
+    lens, shared = [300, 277], 128
+    pool, t, q = case(lens, rows, shared, nq=4, nkv=2, d=128, dtype=dtype, page=32, seed=5)
+    want, lse = attend(lsp, pool, t, q, [0, 1], rows, shared)
+    scaled = []
+    for x, by in zip(pool, (k_by, v_by)):
+        page, d = x.shape[3], x.shape[4] // 9 * 16
+        y = x.clone().flatten(3)
+        bits = y[..., page * d // 2:].view(torch.bfloat16)
+        bits.copy_((bits.double() * 2.0 ** by).bfloat16())
+        scaled.append(y.unflatten(-1, (page, -1)))
+    out, z = attend(lsp, scaled, t, (q.double() * 2.0 ** -k_by).to(q.dtype), [0, 1], rows, shared)
+    want = want.double() * 2.0 ** v_by
+    off = (out.double() - want).abs()
+    assert torch.equal(z, lse)
+    if v_by > 0:
+        assert float(off.max()) == 0
+    else:
+        step, least = (2 ** -8, 2 ** -134) if dtype == "bf16" else (2 ** -23, 2 ** -150)
+        assert bool((off <= step * want.abs() + least + 2 ** -139).all())
+
+
 @pytest.mark.parametrize("rows,shared,dtype", [(1, 0, "bf16"), (1, 4096, "bf16"), (9, 8192, "bf16"), (3, 2048, "f32")])
 def test_the_same_call_gives_the_same_bits(lsp, rows, shared, dtype):
     """Long sequences through the rings of both kernels, call behind call."""
