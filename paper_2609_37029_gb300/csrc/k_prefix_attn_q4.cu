@@ -27,12 +27,14 @@
 // for a pair of them (shift, mask and magic number, minus 136, times the scale), half
 // of those on the half-rate integer pipe, and one product for 256, beside 0.56 bytes
 // of memory a value.  Measured (bf16, 32 heads on 8 of 128): 32 requests of one row
-// over 500 to 16000 tokens of their own 101 us in all for 354 MB (3.5 TB/s).  Without
+// over 500 to 16000 tokens of their own 95 us in all for 354 MB (3.7 TB/s).  Without
 // any work on the blocks that is 76 us: 57 at 6.2 TB/s, 6 until the first block is there
 // (lengths, schedule, first segment, page, block: a chain of loads), 12 for the last
-// segments' sums and the join.  The other 25 are the multiplying warps': some 440
-// instructions for 16 keys, 0.62 of the issue slots and half of the integer pipe.
-// Tried and dropped: a fourth stage (106), one CTA an SM with twice the registers
+// segments' sums and the join.  The other 20 are the multiplying warps': some 430
+// instructions for 16 keys, 0.65 of the issue slots and half of the integer pipe.
+// Tried and dropped: a fourth stage (nothing), stages given back ahead of the second
+// product (100: spills), scores in two chains of products (nothing), eighths in three
+// steps a pair (101 for values or both, 98 for keys; they pay in k_prefix_attn_tc.cu), one CTA an SM with twice the registers
 // (123), four row tiles a warp for 9 to 64 rows (16 requests of one row over 32K: 90
 // us, with one tile 89: products of 8 columns are as slow as unpacking), shifts as
 // products in the other pipe (108 to 122).  Rows past 16 an item go to the tensor cores'
@@ -271,6 +273,18 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
           for (int k = 0; k < P; ++k) mma_bf16(s, x, q[k][4 * i + 2 * h], q[k][4 * i + 2 * h + 1]);
         }
     }
+    uint32_t vw[4][kWordsV], sv[4];              // (read while the scores are on their way)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t a = codes + v_at[j & 1] + (j >> 1) * 8 * (HD / 2);
+      if constexpr (HD == 128)
+        ld_shared2(a, vw[j][0], vw[j][1]);
+      else
+        vw[j][0] = ld_shared(a);
+      sv[j] = ld_shared_u16(scales + vs_at[j & 1] + (j >> 1) * 8 * (HD / 16));
+      // slots of a page past the last key hold anything: their weights are 0, and 0 x V must be 0
+      if (kEdge && key + kv[j & 1] + (j >> 1) * 8 >= g.k_end) sv[j] = 0;
+    }
     // rows 2t, 2t + 1 (s[0], s[1]) of key ka, and (s[2], s[3]) of key ka + 8
     if (kEdge) {
 #pragma unroll
@@ -310,24 +324,12 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
 #pragma unroll
       for (int k = 0; k < P; ++k) b0[k] = transpose8(b0[k]), b1[k] = transpose8(b1[k]);
     }
-    uint32_t w[4][kWordsV], sv[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t a = codes + v_at[j & 1] + (j >> 1) * 8 * (HD / 2);
-      if constexpr (HD == 128)
-        ld_shared2(a, w[j][0], w[j][1]);
-      else
-        w[j][0] = ld_shared(a);
-      sv[j] = ld_shared_u16(scales + vs_at[j & 1] + (j >> 1) * 8 * (HD / 16));
-      // slots of a page past the last key hold anything: their weights are 0, and 0 x V must be 0
-      if (kEdge && key + kv[j & 1] + (j >> 1) * 8 >= g.k_end) sv[j] = 0;
-    }
     const uint32_t sa = sv[0] | sv[1] << 16, sb = sv[2] | sv[3] << 16;
-    read = sa ^ sb ^ w[0][0] ^ w[1][0] ^ w[2][0] ^ w[3][0];      // (the keys' words the votes above have needed)
+    read = sa ^ sb ^ vw[0][0] ^ vw[1][0] ^ vw[2][0] ^ vw[3][0];      // (the keys' words the votes above have needed)
 #pragma unroll
     for (int i = 0; i < kWordsV; ++i) {
-      const uint32_t lo_a = __byte_perm(w[0][i], w[1][i], 0x5410), hi_a = __byte_perm(w[0][i], w[1][i], 0x7632);
-      const uint32_t lo_b = __byte_perm(w[2][i], w[3][i], 0x5410), hi_b = __byte_perm(w[2][i], w[3][i], 0x7632);
+      const uint32_t lo_a = __byte_perm(vw[0][i], vw[1][i], 0x5410), hi_a = __byte_perm(vw[0][i], vw[1][i], 0x7632);
+      const uint32_t lo_b = __byte_perm(vw[2][i], vw[3][i], 0x5410), hi_b = __byte_perm(vw[2][i], vw[3][i], 0x7632);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t x[4] = {q4_pair(consts, lo_a >> (4 * k), sa), q4_pair(consts, hi_a >> (4 * k), sa),

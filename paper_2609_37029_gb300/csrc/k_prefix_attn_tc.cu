@@ -44,15 +44,17 @@
 // Over a cache in 4 bits (kQ4; format: q4.cuh) four more warps, 12 to 15, come
 // between the loads and the ring: warp 8 copies a tile's codes and scales into one of
 // a few places behind it, and the four write its 128 keys as bf16 where TMA would
-// have put them: some 800 cycles a tile next to the softmax (75 values a lane and
-// 1000 cycles of the products), half of it the integer and 16-bit pipes' own.  16
-// requests of 17 rows over 32K 156 to 164 us (0.91 PFLOP/s), with the unpacking left out
-// 141: what is left over bf16's 133 are registers (184 a thread for the softmax) and
-// issue slots, not the copy.  16 of one row over 32K 45 to 47 us, as with bf16: 10 until
-// the first scores, 22 for 14 blocks, 4 for the segment's sums, 10 for the join.
+// have put them, as eighths (three steps a pair; as they are, in four, 156 and 46.5 us
+// below): some 700 cycles a tile next to the softmax (75 values a lane and 1000 cycles of
+// the products), half of it the integer and 16-bit pipes' own.  16 requests of 17 rows
+// over 32K 153 to 159 us (0.94 PFLOP/s), with the unpacking left out 141: what is left
+// over bf16's 133 are registers (184 a thread for the softmax) and issue slots, not the
+// copy.  16 of one row over 32K 45 us, as with bf16: 10 until the first scores, 21 for 14
+// blocks, which the unpacking bounds, 4 for the segment's sums, 10 for the join.
 // Tried and dropped: codes straight from memory into registers (the prefetched ones
 // hold too few bytes in flight, 512 us), the next tile's words fetched early (spills, or
-// nothing gained), softmax warps without rows standing aside (nothing).
+// nothing gained), places given back before the words are unpacked (nothing), the next
+// blocks fetched into L2 (172 and 48), softmax warps without rows standing aside (nothing).
 //
 // The maximum is raised (and the sums rescaled) only when it would grow by more
 // than 2^8, as attention kernels in the literature do: weights stay below 2^8 and
