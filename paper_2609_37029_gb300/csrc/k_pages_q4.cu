@@ -6,8 +6,8 @@
 // sides.  Four threads share a group and its scale.
 //
 // Prompts of 1500 to 9000 tokens (41 thousand tokens, 8 heads of 128, bf16): written
-// in 45 us (5.0 TB/s: 0.72 of the issue slots, half of the integer pipe), read back in 36
-// (5.9 TB/s).  A round's 272 rows take 2 to 3 us each, which is latency: entry, length,
+// in 42 us (5.1 TB/s: 0.73 of the issue slots, half of the integer pipe), read back in 38
+// (5.7 TB/s).  A round's 272 rows take 2 to 3 us each, which is latency: entry, length,
 // page, row.
 #include <algorithm>
 
@@ -19,6 +19,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBatch = 4;                        // words a lane has in flight
+
+// A value that is the same in all of a warp, as one that the compiler knows to be.
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 
 // Row t of a call: the page and slot of its token.  kNone: a row of no entry.
 enum RowKind { kNone, kBad, kStray, kHeld };
@@ -109,9 +112,11 @@ __global__ void __launch_bounds__(kThreads) pages_write_q4_kernel(const KvCache 
   const int lane = threadIdx.x & 31;
   constexpr int kPerHead = HD / 8, kHeads = 32 / kPerHead;       // words of a head, heads of a step
   const int word = lane & (kPerHead - 1), steps = (c.nkv + kHeads - 1) / kHeads;
-  for (int u = threadIdx.x >> 5; u < 2 * per; u += kThreads / 32) {
-    const Row r = rows.row[u >> 1];
-    if (r.kind != kHeld) continue;
+  for (int u = uniform(threadIdx.x >> 5); u < 2 * per; u += kThreads / 32) {
+    Row r = rows.row[u >> 1];
+    if (uniform(r.kind) != kHeld) continue;
+    r.page = uniform(r.page);
+    r.slot = uniform(r.slot);
     const char* from = (u & 1 ? v_new : k_new) + (int64_t)(blockIdx.x * per + (u >> 1)) * row_bytes + lane * 8 * (int)sizeof(T);
     char* block = (u & 1 ? c.v : c.k) + (int64_t)r.page * c.s_page + (int64_t)(lane / kPerHead) * c.s_head;
     const int code_at = (r.slot * kPerHead + word) * 4, scale_at = c.page * (HD / 2) + (r.slot * (kPerHead / 4) + (word >> 2)) * 2;

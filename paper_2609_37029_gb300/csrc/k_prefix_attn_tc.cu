@@ -205,23 +205,6 @@ __device__ __forceinline__ float ex2a(float x) {
   return y;
 }
 
-// (a0, a1) * (b, b) + (c, c) and (a0, a1) + (b0, b1): two fp32 operations an instruction
-__device__ __forceinline__ float2 fma2(float a0, float a1, float b, float c) {
-  float2 d;
-  asm("{\n .reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %4};\n mov.b64 z, {%5, %5};\n"
-      " fma.rn.f32x2 x, x, y, z;\n mov.b64 {%0, %1}, x;\n}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a0), "f"(a1), "f"(b), "f"(c));
-  return d;
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
-      : "=f"(d.x), "=f"(d.y)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-
 // Maximum of 64 scores of a row (four chains); edge: those from `left` on become -inf.
 __device__ __forceinline__ float row_max64(uint32_t* r, int left, bool edge) {
   if (edge) {
@@ -694,6 +677,7 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
         }
       }
       const float base = mx == -INFINITY ? 0.f : -mx * sl;
+      const float2 sl2 = make_float2(sl, sl), base2 = make_float2(base, base);
       float2 acc[4];
 #pragma unroll
       for (int c = 0; c < 4; ++c) acc[c] = make_float2(0.f, 0.f);
@@ -702,7 +686,7 @@ __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, u
         uint32_t w[16];
 #pragma unroll
         for (int c = 0; c < 32; c += 2) {
-          const float2 x = fma2(__uint_as_float(r[32 * h + c]), __uint_as_float(r[32 * h + c + 1]), sl, base);
+          const float2 x = fma2(make_float2(__uint_as_float(r[32 * h + c]), __uint_as_float(r[32 * h + c + 1])), sl2, base2);
           const float2 e = make_float2(ex2a(x.x), ex2a(x.y));
           acc[(c >> 1) & 3] = add2(acc[(c >> 1) & 3], e);
           w[c >> 1] = pack_bf16(e.x, e.y);

@@ -54,6 +54,23 @@ constexpr uint32_t kQ4Zero = 0x88888888u;        // eight codes of 0
 __device__ __forceinline__ uint32_t bf2_bits(__nv_bfloat162 x) { return *reinterpret_cast<uint32_t*>(&x); }
 __device__ __forceinline__ __nv_bfloat162 bits_bf2(uint32_t x) { return *reinterpret_cast<__nv_bfloat162*>(&x); }
 
+// a + b and a b + c: two fp32 operations an instruction
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 x, y;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n .reg .b64 x, y, z;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mov.b64 z, {%6, %7};\n"
+      " fma.rn.f32x2 x, x, y, z;\n mov.b64 {%0, %1}, x;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+
 // What unpacking takes besides, in registers: a loop that has them as immediate
 // operands moves them there for every pair.
 struct Q4Consts {
@@ -127,16 +144,19 @@ __device__ __forceinline__ uint32_t q4_codes(float* x, float s) {
   else
     inv = __frcp_rn(s);
   uint32_t w = 0;
+  const float2 inv2 = make_float2(inv, inv);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float y;
+  for (int e = 0; e < 8; e += 2) {
+    const float2 x2 = make_float2(x[e], x[e + 1]);
+    float2 y;
     if constexpr (kShort) {
-      y = fmaf(x[e], inv, 1536.0f) + (12582920.0f - 1536.0f);
+      y = add2(fma2(x2, inv2, make_float2(1536.0f, 1536.0f)), make_float2(12582920.0f - 1536.0f, 12582920.0f - 1536.0f));
     } else {
-      const float q = x[e] * inv;
-      y = fmaf(fmaf(-q, s, x[e]), inv, q) + 12582920.0f;
+      const float2 q = make_float2(x2.x * inv, x2.y * inv);
+      y = add2(fma2(fma2(make_float2(-q.x, -q.y), make_float2(s, s), x2), inv2, q), make_float2(12582920.0f, 12582920.0f));
     }
-    w += __float_as_uint(y) << (16 * (e & 1) + 4 * (e >> 1));
+    w += __float_as_uint(y.x) << (2 * e);
+    w += __float_as_uint(y.y) << (2 * e + 16);
   }
   return w - 0x4B400000u * 0x11111111u;          // (the upper bits of the eight numbers)
 }
