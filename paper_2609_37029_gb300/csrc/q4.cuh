@@ -132,9 +132,9 @@ __device__ __forceinline__ float q4_scale(uint32_t a_bits) {
 //         > 2^-10 from one; rounded to multiples of 2^-13 first, it stays what it is.
 template <bool kShort>                           // x of eight significant bits
 __device__ __forceinline__ uint32_t q4_codes(float* x, float s) {
-  if (!(s > 0.0f)) return kQ4Zero;                // an empty group, or one that is NaN
-  if (s < 1e-30f) {                              // (times 2^64: reciprocals stay finite)
-    s *= 18446744073709551616.0f;
+  if (!(s >= 1e-30f)) {
+    if (!(s > 0.0f)) return kQ4Zero;             // an empty group, or one that is NaN
+    s *= 18446744073709551616.0f;                // (times 2^64: reciprocals stay finite)
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] *= 18446744073709551616.0f;
   }
