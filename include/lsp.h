@@ -553,7 +553,8 @@ size_t lsp_prefix_attention_q4_workspace_bytes(const lsp_kv_cache* cache, int dt
 
 /* lsp_prefix_attention over a cache of dtype Q4, whose keys and values enter as
  * the numbers they stand for: the same rows, shared pages and results, for q and
- * out of `dtype` BF16 or F32.  Nothing is unpacked to memory.  bf16: scores and
+ * out of `dtype` BF16 or F32.  (One past bfloat16's largest number enters as
+ * infinity or as itself.)  Nothing is unpacked to memory.  bf16: scores and
  * sums in fp32, weights rounded to bf16 for the product with V.  f32: q and the
  * weights enter the tensor cores as sums of three bf16 numbers each (24 bits), the
  * products are exact and summed in fp32.  workspace: at least
