@@ -540,7 +540,9 @@ size_t lsp_prefix_attention_workspace_bytes(const lsp_kv_cache* cache, int nq, i
  * (LSP_DEV_BAD_SEQ); table entries outside the pool read as zero keys and values
  * (LSP_DEV_BAD_SEQ).  What lies in unused slots of a page is never seen,
  * whatever its bits; the keys and values of a sequence's own tokens are taken
- * to be finite.  bf16: scores and sums in fp32, weights rounded to bf16 for
+ * to be finite (a NaN in a key makes out and lse NaN in the rows that see it, one
+ * in a row's query in that row; one in a value reaches rows of the call that do
+ * not see it yet).  bf16: scores and sums in fp32, weights rounded to bf16 for
  * the product with V; f32: fp32 throughout. */
 int lsp_prefix_attention(const lsp_kv_cache* cache, int layer, const void* q, int64_t q_stride,
                          int nq, const int32_t* seqs, const int32_t* start, int n, int total,
@@ -554,7 +556,9 @@ size_t lsp_prefix_attention_q4_workspace_bytes(const lsp_kv_cache* cache, int dt
 /* lsp_prefix_attention over a cache of dtype Q4, whose keys and values enter as
  * the numbers they stand for: the same rows, shared pages and results, for q and
  * out of `dtype` BF16 or F32.  (One past bfloat16's largest number enters as
- * infinity or as itself.)  Nothing is unpacked to memory.  bf16: scores and
+ * infinity or as itself.)  A group that is NaN makes NaN, in the rows that see it
+ * and no others, of out and lse if it is a key's, of its dims of out if it is a
+ * value's, whatever its weight.  Nothing is unpacked to memory.  bf16: scores and
  * sums in fp32, weights rounded to bf16 for the product with V.  f32: q and the
  * weights enter the tensor cores as sums of three bf16 numbers each (24 bits), the
  * products are exact and summed in fp32.  workspace: at least

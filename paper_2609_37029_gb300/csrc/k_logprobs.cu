@@ -77,11 +77,6 @@ __device__ __forceinline__ float ex2a(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float max_nan(float a, float b) {     // NaN if either is
-  float y;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-  return y;
-}
 
 // Whole numbers of a type's width that order as its logits do (-0 as 0; NaN below all); 0 stands for no element.
 template <typename T>

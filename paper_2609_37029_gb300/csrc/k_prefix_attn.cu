@@ -6,7 +6,9 @@
 //
 // with the keys cut into segments, each leaving (sum_j 2^(s2_j - m2) v_j, m2,
 // l) in base 2, s2 = s log2(e); prefix_join_kernel adds a row's segments with
-// weights 2^(m2_seg - max m2).
+// weights 2^(m2_seg - max m2).  m2 is -inf where the row sees no key of the segment.
+// A running maximum passes over scores that are NaN, but l does not: the join takes
+// such a segment's maximum as NaN, and out and lse become so.
 //
 // prefix_attn_fma_kernel: f32 storage, fp32 multiply-adds, 64 rows x 64 keys a
 // step, 4 x 4 scores and 4 x (HD / 16) sums a thread.  Where rows fill the tiles (16
@@ -362,7 +364,7 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
         if (row_m >= 0) {
 #pragma unroll
           for (int k = 0; k < kHeads; ++k)
-            if (k < heads) m[k] = fmaxf(m[k], p.part_ml[row_m + k].x);
+            if (k < heads) m[k] = max_nan(m[k], part_max(p.part_ml[row_m + k]));
         }
         if ((q += 32) >= all) break;
         row_m = row_of(q);
@@ -370,24 +372,27 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
       bool some = false;
 #pragma unroll
       for (int k = 0; k < kHeads; ++k) {
-        m[k] = warp_max(m[k]);
-        some |= m[k] > -INFINITY;
+#pragma unroll
+        for (int w = 16; w > 0; w >>= 1) m[k] = max_nan(m[k], __shfl_xor_sync(0xffffffffu, m[k], w));
+        some |= m[k] != -INFINITY;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) o[k][e] = 0.f;
       }
       for (int q0 = 0; q0 < all && some; q0 += 32 * kWarps) {
         const int64_t row = q0 == 0 ? row_s : row_of(q0 + lane * kWarps + part);
-        float x[kHeads];
+        float x[kHeads];                           // the segment's weight; below 0: it has none, and its sums are not read
         bool any = false;
 #pragma unroll
         for (int k = 0; k < kHeads; ++k) {
-          x[k] = 0.f;
+          x[k] = -1.f;
           if (row >= 0 && k < heads) {
             const float2 ml = p.part_ml[row + k];
-            x[k] = ml.x == -INFINITY ? 0.f : ex2a(ml.x - m[k]);
-            l[k] += x[k] * ml.y;
+            if (part_max(ml) != -INFINITY) {
+              x[k] = ex2a(part_max(ml) - m[k]);
+              l[k] += x[k] * ml.y;
+            }
           }
-          any |= x[k] > 0.f;
+          any |= x[k] >= 0.f;                      // (a weight of 0 still takes NaN along)
         }
         for (unsigned left = __ballot_sync(0xffffffffu, any); left;) {
           float y[kAhead][kHeads][kVec], f[kAhead][kHeads];
@@ -399,10 +404,10 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
             const int64_t at = __shfl_sync(0xffffffffu, row, src);
 #pragma unroll
             for (int k = 0; k < kHeads; ++k) {
-              f[a][k] = on ? __shfl_sync(0xffffffffu, x[k], src) : 0.f;
+              f[a][k] = on ? __shfl_sync(0xffffffffu, x[k], src) : -1.f;
 #pragma unroll
               for (int e = 0; e < kVec; ++e) y[a][k][e] = 0.f;
-              if (f[a][k] > 0.f) {
+              if (f[a][k] >= 0.f) {
                 if constexpr (kVec == 4) {
                   const float4 z = *part_chunk<HD>(p.part_o, at + k, lane);
                   y[a][k][0] = z.x; y[a][k][1] = z.y; y[a][k][2] = z.z; y[a][k][3] = z.w;
@@ -443,7 +448,7 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
 #pragma unroll
       for (int k = 0; k < kHeads; ++k) {
         if (k >= heads) break;
-        const float inv = l[k] > 0.f ? 1.f / l[k] : 0.f;
+        const float inv = l[k] == 0.f ? 0.f : 1.f / l[k];
         const int64_t to = (int64_t)t * p.nq + g * p.rep + hr + k;
         T* out = static_cast<T*>(p.out) + to * HD + lane * kVec;
         if constexpr (sizeof(T) == 2 && kVec == 4)

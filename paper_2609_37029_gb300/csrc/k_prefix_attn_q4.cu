@@ -285,6 +285,28 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
       // slots of a page past the last key hold anything: their weights are 0, and 0 x V must be 0
       if (kEdge && key + kv[j & 1] + (j >> 1) * 8 >= g.k_end) sv[j] = 0;
     }
+    if (kEdge) {
+      // A value that is NaN must not enter the sums of rows that do not see it (0 x NaN): it is left out, and the
+      // lane's dims of the rows that see it become NaN.  (Eighths of the others cannot be infinite.)
+      bool lost = false;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) lost |= (sv[j] & 0x7F80u) == 0x7F80u;
+      if (__any_sync(0xffffffffu, lost)) {
+        uint32_t hit = 0;                        // keys of the slice, of the lane's group of dims
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if ((sv[j] & 0x7F80u) == 0x7F80u) hit |= 1u << (kv[j & 1] + (j >> 1) * 8), sv[j] = 0;
+        hit |= __shfl_xor_sync(0xffffffffu, hit, 1);
+        hit |= __shfl_xor_sync(0xffffffffu, hit, 2);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int seen = lim[i] - key;
+          if (seen <= 0 || !(hit & (seen < 16 ? (1u << seen) - 1 : 0xFFFFu))) continue;
+#pragma unroll
+          for (int d = 0; d < HD / 16; ++d) o[d][i] = o[d][i + 2] = __uint_as_float(0x7FC00000u);
+        }
+      }
+    }
     // rows 2t, 2t + 1 (s[0], s[1]) of key ka, and (s[2], s[3]) of key ka + 8
     if (kEdge) {
 #pragma unroll
@@ -316,6 +338,7 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
       for (int e = 0; e < 4; ++e) {
         w[e] = ex2a(fmaf(s[e], sl, kEdge && m[e & 1] == -INFINITY ? 0.f : -m[e & 1]));
         l[e & 1] += w[e];
+        if (kEdge) w[e] *= 8.0f;                 // (for the values' eighths)
       }
       // (bf16: the weights of the product are rounded to 2^-9 of each, their sum is not: the other operand is bf16,
       // and the rounding of the output outweighs it)
@@ -324,7 +347,11 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
 #pragma unroll
       for (int k = 0; k < P; ++k) b0[k] = transpose8(b0[k]), b1[k] = transpose8(b1[k]);
     }
-    const uint32_t sa = sv[0] | sv[1] << 16, sb = sv[2] | sv[3] << 16;
+    uint32_t sa = sv[0] | sv[1] << 16, sb = sv[2] | sv[3] << 16;
+    if (kEdge) {
+      sa = bf2_bits(__hmul2(bits_bf2(sa), bits_bf2(0x3E003E00u)));           // (exact: scales are multiples of 2^-130)
+      sb = bf2_bits(__hmul2(bits_bf2(sb), bits_bf2(0x3E003E00u)));
+    }
     read = sa ^ sb ^ vw[0][0] ^ vw[1][0] ^ vw[2][0] ^ vw[3][0];      // (the keys' words the votes above have needed)
 #pragma unroll
     for (int i = 0; i < kWordsV; ++i) {
@@ -357,7 +384,7 @@ __device__ __forceinline__ bool multiply(const PrefixAttnParams& p, Smem<HD>& sm
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int w = 4; w < 32; w <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], w);
-  m_out = make_float2(m[0], m[1]);
+  m_out = make_float2(part_max(make_float2(m[0], l[0])), part_max(make_float2(m[1], l[1])));
   l_out = make_float2(l[0], l[1]);
   return true;
 }
@@ -404,7 +431,7 @@ __device__ __forceinline__ void multiply_role(const PrefixAttnParams& p, Smem<HD
       const int row = 2 * t + i;
       const float mine = i ? m.y : m.x;
       float top = mine;
-      for (int j = 0; j < kgs; ++j) top = fmaxf(top, sm.merge_ml[j * rgs + rg][row].x);
+      for (int j = 0; j < kgs; ++j) top = max_nan(top, sm.merge_ml[j * rgs + rg][row].x);
       const float f = mine == -INFINITY ? 0.f : ex2a(mine - top);
 #pragma unroll
       for (int d0 = 0; d0 < HD / 32; ++d0) {
@@ -431,10 +458,10 @@ __device__ __forceinline__ void multiply_role(const PrefixAttnParams& p, Smem<HD
       *part_chunk<HD>(p.part_o, g.part + row, c) = x;
       if (c == 0) {
         float top = -INFINITY, sum = 0.f;
-        for (int j = 0; j < kgs; ++j) top = fmaxf(top, sm.merge_ml[j * rgs + (row >> 3)][row & 7].x);
+        for (int j = 0; j < kgs; ++j) top = max_nan(top, sm.merge_ml[j * rgs + (row >> 3)][row & 7].x);
         for (int j = 0; j < kgs; ++j) {
           const float2 y = sm.merge_ml[j * rgs + (row >> 3)][row & 7];
-          if (y.x > -INFINITY) sum += y.y * ex2a(y.x - top);
+          if (y.x != -INFINITY) sum += y.y * ex2a(y.x - top);
         }
         p.part_ml[g.part + row] = make_float2(top, sum);
       }

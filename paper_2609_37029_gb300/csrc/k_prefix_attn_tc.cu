@@ -102,6 +102,8 @@ struct TcMisc {
   float2 lone_ml[2][kRows];                      // stream 1's maximum and sum of segments with one row tile, by turns
   uint64_t packed_full[4], packed_empty[4];      // kQ4: tiles in 4 bits
   int packed_keys[4];                            // keys of one, + kLone where one stream alone takes it; -1: no more tiles
+  uint64_t landed;                               // kQ4: a tile that load_packed_role looks through
+  int lost;                                      // and whether one of them was changed
 };
 
 constexpr int kLone = 256;
@@ -352,7 +354,22 @@ __device__ __forceinline__ void load_role(const PrefixAttnParams& p, const CUten
   }
 }
 
-// Codes and scales of the tiles, in the order of the ring's places, and the query tiles.
+// A value that is NaN must not enter the sums of rows that do not see it (0 x NaN): in tiles of which rows see a part, its
+// scale becomes 0 here, and spoil_rows makes the sums of the rows that see it NaN.  Scales [from, to) of the tile.
+__device__ __forceinline__ void leave_out(uint16_t* scales, int from, int to, int* lost) {
+#pragma unroll 1
+  for (int x = max(from, 0) + (threadIdx.x & 31); x < to; x += 32)
+    if ((scales[x] & 0x7F80) == 0x7F80) {
+      scales[x] = 0;
+      *lost = 1;
+    }
+  fence_proxy_async_smem();
+  __syncwarp();
+}
+
+// Codes and scales of the tiles, in the order of the ring's places, and the query tiles.  Tiles of values that not every
+// row sees all of, one or two of a sequence, are waited for and looked through here (16 requests of 17 rows over 32K
+// 152 us; code for that in the unpacking or the softmax warps slowed every tile: 158 to 188).
 template <int HD>
 __device__ __forceinline__ void load_packed_role(const PrefixAttnParams& p, const CUtensorMap* mq, uint32_t sm, uint8_t* packed,
                                                  int count, TcMisc* m, SegReader segs) {
@@ -361,7 +378,7 @@ __device__ __forceinline__ void load_packed_role(const PrefixAttnParams& p, cons
   const int run = min(p.page, kKeys), runs = kKeys / run, page_bits = 31 - __clz(p.page);
   const uint32_t codes = run * (HD / 2), scales = run * (HD / 16);
   const int block_codes = p.page * (HD / 2);
-  uint32_t nq = 0;
+  uint32_t nq = 0, looked = 0;
   Place place = {0, 1};                          // (the first uses wait for nobody)
   PrefixSeg g;
   while (segs.next(g)) {
@@ -372,9 +389,12 @@ __device__ __forceinline__ void load_packed_role(const PrefixAttnParams& p, cons
       const int pos = g.k0 + kb * kKeys + lane * run;
       return lane < runs && kb < g.kb1 && pos < g.k_end ? g.tab[pos >> page_bits] : -1;
     };
-    auto load = [&](const char* pool, int kb, int pg) {
-      const uint32_t at = place.stage, bar = smem_u32(&m->packed_full[at]);
-      const int first = g.k0 + kb * kKeys, pos = first + lane * run;
+    auto load = [&](const char* pool, int kb, int pg, bool values) {
+      const uint32_t at = place.stage;
+      const int first = g.k0 + kb * kKeys, keys = min(g.k_end - first, kKeys), seen = g.see0 - first;
+      const bool look = values && seen < keys;
+      const uint32_t bar = smem_u32(look ? &m->landed : &m->packed_full[at]);
+      const int pos = first + lane * run;
       const bool mine = lane < runs && pos < g.k_end, held = mine && pg >= 0 && pg < p.pages;
       if (!tc_wait(smem_u32(&m->packed_empty[at]), place.phase, &m->abort, p.err)) return false;
       uint8_t* to = packed + at * Pk::kBytes;
@@ -386,7 +406,7 @@ __device__ __forceinline__ void load_packed_role(const PrefixAttnParams& p, cons
       const int n = __popc(__ballot_sync(0xffffffffu, held));
       __syncwarp();
       if (lane == 0) {
-        m->packed_keys[at] = min(g.k_end - first, kKeys) + (jobs.lone ? kLone : 0);
+        m->packed_keys[at] = keys + (jobs.lone ? kLone : 0);
         mbar_expect_tx(bar, n * (codes + scales));
       }
       __syncwarp();
@@ -396,20 +416,28 @@ __device__ __forceinline__ void load_packed_role(const PrefixAttnParams& p, cons
         bulk_load(smem_u32(to) + lane * codes, block + slot * (HD / 2), codes, bar);
         bulk_load(smem_u32(to) + Pk::kCodes + lane * scales, block + block_codes + slot * (HD / 16), scales, bar);
       }
+      if (look) {
+        if (!tc_wait(bar, looked++ & 1, &m->abort, p.err)) return false;
+        leave_out(reinterpret_cast<uint16_t*>(to + Pk::kCodes), seen * (HD / 32), keys * (HD / 32), &m->lost);
+        if (lane == 0) mbar_arrive(smem_u32(&m->packed_full[at]));
+      }
       place.next(count);
       return true;
     };
     // first uses: keys lead values by one job (two streams' worth where both take every block)
     const int lead = jobs.lone ? 2 : 1, blocks = g.kb1 - g.kb0;
-    int e0 = entry(g.kb0), e1 = entry(g.kb0 + 1);
-    if (!load(p.k, g.kb0, e0)) return;
-    if (lead == 2 && blocks > 1 && !load(p.k, g.kb0 + 1, e1)) return;
-    for (int i = 0; i < blocks; ++i) {
-      const int e2 = entry(g.kb0 + i + 2);
-      if (!load(p.v, g.kb0 + i, e0)) return;
-      if (i + lead < blocks && !load(p.k, g.kb0 + i + lead, lead == 2 ? e2 : e1)) return;
-      e0 = e1;
-      e1 = e2;
+    int e0 = entry(g.kb0), e1 = entry(g.kb0 + 1), e2 = entry(g.kb0 + 2);         // pages of the blocks from v on
+    for (int k = 0, v = 0; v < blocks;) {
+      const bool values = k >= blocks || k >= v + lead;
+      if (!load(values ? p.v : p.k, g.kb0 + (values ? v : k), values || k == v ? e0 : k == v + 1 ? e1 : e2, values)) return;
+      if (values) {
+        ++v;
+        e0 = e1;
+        e1 = e2;
+        e2 = entry(g.kb0 + v + 2);
+      } else {
+        ++k;
+      }
     }
   }
   const uint32_t at = place.stage;
@@ -610,6 +638,39 @@ __device__ __forceinline__ void mma_role(const PrefixAttnParams& p, int t, uint3
   }
 }
 
+// The sums of stream t's rows that see a value that leave_out left out become NaN, in its dims: behind all segments, which
+// are gone through again.
+template <int HD>
+__device__ __forceinline__ void spoil_rows(const PrefixAttnParams& p, int t, int row, const PrefixSched& sched, const int64_t* line_base,
+                                           const PrefixSeq* info) {
+  const float nan = __uint_as_float(0x7FC00000u);
+  const int tok = row / p.rep;
+  PrefixSegs<kTiles, kKeys> segs(p, sched, line_base, info, blockIdx.x);
+  PrefixSeg g;
+  while (segs.next_shared(g)) {}                 // (every row sees all of their keys)
+  while (segs.next_own(g)) {
+    const bool lone = seg_jobs(p, g).lone;
+    const int i = (lone ? 0 : t * p.tok_tile) + tok;
+    const bool mine = tok < p.tok_tile && i < g.tokens && (t == 0 || !lone);
+    const int64_t at = g.part + (!lone && t ? p.tok_tile * p.rep : 0) + row;
+    const int begin = max(g.k0 + g.kb0 * kKeys, g.see0), end = min(g.k0 + g.kb1 * kKeys, g.k_end);
+#pragma unroll 1
+    for (int group = 0; group < HD / 32; ++group) {
+      int first = INT_MAX;
+      for (int pos = begin + (threadIdx.x & 31); pos < end; pos += 32) {
+        const int pg = g.tab[pos / p.page];
+        if (pg < 0 || pg >= p.pages) continue;
+        const char* block = p.v + (int64_t)pg * p.s_page + (int64_t)g.head * p.s_head + p.page * (HD / 2);
+        const uint16_t s = reinterpret_cast<const uint16_t*>(block)[(pos % p.page) * (HD / 32) + group];
+        if ((s & 0x7F80) == 0x7F80) first = min(first, pos);
+      }
+      first = __reduce_min_sync(0xffffffffu, first);
+      if (mine && first < g.see0 + i)
+        for (int c = 8 * group; c < 8 * group + 8; ++c) *part_chunk<HD>(p.part_o, at, c) = make_float4(nan, nan, nan, nan);
+    }
+  }
+}
+
 template <int HD, bool kQ4>
 __device__ __forceinline__ void softmax_role(const PrefixAttnParams& p, int t, uint8_t* smp, uint32_t tmem, TcMisc* m,
                                              SegReader segs) {
@@ -804,6 +865,7 @@ __global__ void __launch_bounds__(kThreads<kQ4>, 1)
     }
     for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&m->lone_full[i]), 4);
     mbar_init(smem_u32(&m->drain), 2);
+    mbar_init(smem_u32(&m->landed), 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&m->turn[i]), 1);
       mbar_init(smem_u32(&m->q_full[i]), 1);
@@ -815,6 +877,7 @@ __global__ void __launch_bounds__(kThreads<kQ4>, 1)
       mbar_init(smem_u32(&m->o_free[i]), 4);
     }
     m->abort = 0;
+    m->lost = 0;
     fence_barrier_init();
     tma_prefetch_desc(&mq);
     if (!kQ4) {
@@ -858,6 +921,7 @@ __global__ void __launch_bounds__(kThreads<kQ4>, 1)
     else
       asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     softmax_role<HD, kQ4>(p, warp >> 2, smp, tmem, m, segs);
+    if (kQ4 && __any_sync(0xffffffffu, *reinterpret_cast<volatile int*>(&m->lost))) spoil_rows<HD>(p, warp >> 2, threadIdx.x & 127, m->sched, line_base, info);
   }
   tc_fence_before();
   __syncthreads();

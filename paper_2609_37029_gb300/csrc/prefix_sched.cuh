@@ -219,6 +219,9 @@ __device__ __forceinline__ float4* part_chunk(float* part_o, int64_t r, int c) {
   return reinterpret_cast<float4*>(part_o) + ((r >> 2) * (HD / 4) + c) * 4 + (r & 3);
 }
 
+// The maximum of what a segment leaves (its running maximum and sum): NaN where a score was.
+__device__ __forceinline__ float part_max(float2 ml) { return ml.y == ml.y ? ml.x : ml.y; }
+
 // What a CTA works on at a time: the rows of a unit and a range of key blocks.
 struct PrefixSeg {
   const int32_t* tab;   // row of the table
