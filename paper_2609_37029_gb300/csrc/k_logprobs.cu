@@ -556,7 +556,8 @@ __device__ __forceinline__ void join_role(const LogprobsParams& p, Smem& sm, Row
     const bool none = !(s > 0.f) || !isfinite(top);              // no distribution
     const float ln_s = logf(s);
     if (lane == 0) {
-      p.logprob[row] = none ? nan : (z - top) / p.temperature - ln_s;
+      // (S may come out below 1 by what its terms are rounded)
+      p.logprob[row] = none ? nan : fminf((z - top) / p.temperature - ln_s, 0.f);
       if (p.entropy) p.entropy[row] = none ? nan : fmaxf(ln_s - a / s * 0.69314718055994531f, 0.f);
     }
     // lane r has the first that is left of part r's list; the largest of those goes to lane i in round i
@@ -577,7 +578,7 @@ __device__ __forceinline__ void join_role(const LogprobsParams& p, Smem& sm, Row
     if (lane < p.k) {                            // (k <= V: there are k elements)
       const int64_t to = (int64_t)row * p.k + lane;
       if (p.top) p.top[to] = none ? -1 : (int)~won_at;
-      if (p.top_logprob) p.top_logprob[to] = none ? nan : (of_key<T>(won_key) - top) / p.temperature - ln_s;
+      if (p.top_logprob) p.top_logprob[to] = none ? nan : fminf((of_key<T>(won_key) - top) / p.temperature - ln_s, 0.f);
     }
     __syncwarp();
     if (lane < cluster) arrive_far(in_cta(smem_u32(&sm.taken[turn & 1]), lane));
