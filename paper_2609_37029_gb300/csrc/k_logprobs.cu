@@ -164,11 +164,17 @@ struct Stats {
 };
 
 // The sums move to a higher m when an element, `top`, exceeds theirs by 2^8 (they are
-// fp32: what is added meanwhile loses nothing).
-__device__ __forceinline__ void raise(Stats& st, float top, const Scale& k) {
+// fp32: what is added meanwhile loses nothing).  They are relative to ref, or where least is NaN to m itself, and so
+// afterwards; single: to m.
+__device__ __forceinline__ void raise(Stats& st, float top, const Scale& k, bool single) {
   if (!((top - st.m) * k.c > 8.0f)) return;
-  const bool was = st.least == st.least, fine = fabsf(top) <= k.large;
-  const float ref = top * k.c, t = max_nan(was && fine ? st.ref - ref : (st.m - top) * k.c, kLeast), r = ex2a(t);
+  const bool was = st.least == st.least, fine = !single && fabsf(top) <= k.large;
+  const float ref = top * k.c;
+  float t = was && fine ? st.ref - ref : (st.m - top) * k.c;
+  if (was && !fine) t -= fmaf(st.m, k.c, -st.ref);
+  if (!was && fine) t += fmaf(top, k.c, -ref);
+  t = max_nan(t, kLeast);
+  const float r = ex2a(t);
   st.a = make_float2(r * (st.a.x + st.s.x * t), r * (st.a.y + st.s.y * t));
   st.s = make_float2(r * st.s.x, r * st.s.y);
   st.m = top;
@@ -191,7 +197,7 @@ __device__ __forceinline__ void add_piece(Stats& st, Piece<T>& v, uint32_t place
   const float top = v.top();
   st.other = fmaxf(st.other, fminf(top, st.best));
   if (top > st.best) st.best = top, st.place = place;
-  raise(st, top, k);
+  raise(st, top, k, false);
   if (st.least != st.least) {                    // nothing but -inf so far, or logits too large
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -237,8 +243,7 @@ __device__ __forceinline__ void settle(Stats& st, const Scale& k) {
 }
 // A single element, behind that.
 __device__ __forceinline__ void add_one(Stats& st, float x, const Scale& k) {
-  raise(st, x, k);
-  st.least = __uint_as_float(0x7FC00000u);
+  raise(st, x, k, true);
   add_limited(st, x, k);
 }
 

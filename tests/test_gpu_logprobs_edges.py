@@ -1,5 +1,6 @@
 """lsp_logprobs where its arithmetic has least room: near-certain tokens, logits at the limit of its faster steps,
 filtered rows, rows at any address.  Tolerances: test_gpu_logprobs.py's."""
+import numpy as np
 import pytest
 import torch
 
@@ -33,3 +34,24 @@ def test_log_probabilities_are_never_positive(lsp, V, dtype):
     z[:, :], z[:, 5] = -float("inf"), 3.0            # the only token
     out = call(lsp, z, ints([5] * rows), 2)
     assert not out[0].any() and not out[1].any() and not out[3][:, 0].any()
+
+
+def frames(by):
+    """Rows whose threads meet a plateau first and a larger logit in their last piece, both next to +-1e6 / c,
+    c = log2(e) / T: up to there t = z c - ref, beyond it t = (z - m) c."""
+    V, limit = 131072, 1e6 * np.log(2)
+    z = np.zeros((24, V), np.float32)
+    for r in range(24):
+        low = by * limit - 6.0 + 0.0625 * 5 * r if by > 0 else by * limit - 7.0 + 0.0625 * 5 * r
+        z[r] = low
+        z[r].reshape(8, -1)[:, -2048::16] = np.float32(low) + np.float32(6.25)
+    return torch.from_numpy(z).cuda()
+
+
+@pytest.mark.parametrize("by", [1, -1])
+def test_logits_on_both_sides_of_the_limit_of_the_fast_steps(lsp, by):
+    z = frames(by)
+    tokens = ints([0, 131071 - 15] * 12)
+    check(z, tokens, 3, 1.0, call(lsp, z, tokens, 3))
+    # (the same x, everything by a power of two)
+    check(z / 1024, tokens, 3, 2.0 ** -10, call(lsp, z / 1024, tokens, 3, 2.0 ** -10))
