@@ -613,8 +613,9 @@ int lsp_verify_probs(const void* target_probs, const void* draft_probs, int dtyp
  * no distribution: NaN in logprob, entropy and top_logprob, -1 in top.  (In other
  * rows tokens of -inf follow the finite ones, with top_logprob -inf.)
  * T in [2^-100, 2^100]; rows in [0, 2^27], V in [1, 2^26], ld >= V, k in
- * [0, min(V, 32)].  One launch; each row is read once (the parts of it with its
- * largest logits twice).  In fp32; the same call gives the same bits.  How many rows
+ * [0, min(V, 32)].  One launch; each row is read once, and what may hold its k
+ * largest logits once more (k times where more than a thousand that belong there
+ * crowd into a few places of a row).  In fp32; the same call gives the same bits.  How many rows
  * there are decides how a row is split: its sums may differ in their last bits, the
  * tokens never. */
 int lsp_logprobs(const void* logits, int dtype, const int32_t* tokens, int rows, int V, int64_t ld,

@@ -13,11 +13,13 @@
 // elements is in one of the k stripes whose first are the largest -- an element in any
 // other stripe has k elements before it -- so of those stripes the piece with the
 // largest is read again, and the whole stripe where another piece reaches the k-th
-// stripe's first too (a few of a hundred).  What comes at or before that goes to a
-// list, some more than k elements as a rule, which is ranked by counting.  Places
-// decide between equal logits all the way.  Should the list overflow (a row made for
-// it: hundreds of large elements in few stripes), the elements are taken one at a time
-// instead, k passes over L2.
+// stripe's first too (a few of a hundred).  What is above that goes to a list, what
+// equals it to another, some more than k elements as a rule, and they are ranked by
+// counting.  Places decide between equal logits all the way.  Where more elements equal
+// the k-th stripe's first than the list holds (rows of which all but a few logits are
+// -inf, or of equal logits) the first of them are looked for from the start of the part.
+// Only a row made for it (more than a thousand larger elements in those stripes)
+// overflows the list of the others: then the stripes are read k times.
 //
 // A row is split over a cluster of CTAs, which hand their parts to the first of them
 // through its shared memory: no workspace, no second launch.  The CTAs stay for as
@@ -46,7 +48,10 @@ constexpr int kPerSm = 4;
 constexpr int kPieceBytes = 64;                  // of a row, for a thread at a time
 constexpr int kStages = 5, kStageBytes = kThreads * kPieceBytes;
 constexpr int kStripes = kThreads;               // of a CTA's part: stripe i, of thread i, has its pieces i, i + kStripes, ...
-constexpr int kList = 512;                       // candidates of a CTA
+// Candidates of a CTA: elements above the cut, of k pieces of 64 bytes (and the singles of as many threads) as a rule, and
+// places of elements that equal it.
+constexpr int kList = kLogprobsMaxK * 33, kTies = 256;
+constexpr uint32_t kWhole = 0x80000000u;         // of a stripe: all of it is read again
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLeast = -150.0f;                // 2^t is 0 from here on
 constexpr float kLowest = -3.402823466e38f;
@@ -60,7 +65,7 @@ struct Partial {
 struct Smem {
   alignas(128) uint8_t ring[kStages][kStageBytes];
   Partial part[2][kMaxCluster];                  // by turns
-  unsigned long long list[kList];
+  unsigned long long list[kList + kTies];        // above the cut; equal to it
   unsigned long long sorted[kLogprobsMaxK];
   uint32_t stripe[kStripes];
   float red[kWarps];
@@ -69,8 +74,9 @@ struct Smem {
   uint32_t least[kWarps];
   uint64_t full[kStages], empty[kStages];
   uint64_t parts[2], taken[2];                   // the cluster's parts of a row are there; the first has read them
-  int count, stripes, abort;
+  int count[2], stripes, abort;                  // of the lists
 };
+static_assert(kPerSm * (sizeof(Smem) + 128 + 1024) <= 228 * 1024, "CTAs of an SM");
 
 __device__ __forceinline__ float ex2a(float x) {
   float y;
@@ -282,7 +288,7 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, f
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool some = tid < part.head || tid < part.pieces || tid < part.tail;
   const uint32_t key = some ? key_of<T>(st.best) : 0u;
-  if (tid == 0) sm.count = sm.stripes = 0;
+  if (tid == 0) sm.count[0] = sm.count[1] = sm.stripes = 0;
   if (tid < k) sm.sorted[tid] = 0;
   // the largest `cut` that k stripes reach, bit by bit; among equal ones, the place that makes them k
   uint32_t cut = 0, last = 0xFFFFFFFFu;
@@ -311,8 +317,8 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, f
     if (cut > 0 && !(x >= least)) return;
     const uint32_t e = key_of<T>(x);
     if (!in(e, place)) return;
-    const int at = atomicAdd(&sm.count, 1);
-    if (at < kList) sm.list[at] = entry(e, (uint32_t)index);
+    const int tie = e == cut, at = atomicAdd(&sm.count[tie], 1);
+    if (at < (tie ? kTies : kList)) sm.list[at + (tie ? kList : 0)] = entry(e, (uint32_t)index);
   };
   auto load_piece = [&](int i) {
     Piece<T> v;
@@ -332,33 +338,79 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, f
   auto put_piece = [&](const Piece<T>& v, int i) {
     each(v, i, [&](float x, int index) { put(x, kStripes + i, index); });
   };
-  if (some && in(key, st.place)) {
+  const bool mine = some && in(key, st.place);
+  if (mine) {
     if (tid < part.head) put(head, tid, tid);
     if (tid < part.tail) put(tail, part.tail_at + tid, part.tail_index + tid);
     // (another piece with the largest logit lies behind, and has the place to decide; a single element counts as a piece)
-    if (key_of<T>(st.other) >= cut)
-      sm.stripe[atomicAdd(&sm.stripes, 1)] = tid;
-    else if (st.place >= kStripes && st.place < (uint32_t)part.tail_at)
+    const uint32_t other = key_of<T>(st.other);
+    if (other >= cut) sm.stripe[atomicAdd(&sm.stripes, 1)] = tid | (other > cut ? kWhole : 0u);
+    if ((other < cut || (other == cut && st.place > last)) && st.place >= kStripes && st.place < (uint32_t)part.tail_at)
       put_piece(load_piece((int)st.place - kStripes), (int)st.place - kStripes);
   }
   meet();
-  // a warp takes stripes in turn, a lane every 32nd piece
-  const int stripes = sm.stripes;
+  // a warp takes stripes in turn, a lane every 32nd piece; where the others equal the cut, up to the last place that counts
+  const int stripes = sm.stripes, tied = last < kStripes ? 0 : (int)min((uint32_t)part.pieces, last - kStripes + 1);
   for (int x = warp; x < stripes; x += kWarps) {
-    for (int i = lane * kStripes + (int)sm.stripe[x]; i < part.pieces; i += 32 * kStripes) put_piece(load_piece(i), i);
+    const uint32_t stripe = sm.stripe[x];
+    const int upto = stripe & kWhole ? part.pieces : tied;
+    for (int i = lane * kStripes + (int)(stripe & ~kWhole); i < upto; i += 32 * kStripes) put_piece(load_piece(i), i);
   }
   meet();
-  const int n = sm.count;
+  const int n = sm.count[0], ties = sm.count[1];
   if (n <= kList) {
-    for (int i = tid; i < n; i += kThreads) {
-      const unsigned long long mine = sm.list[i];
-      int rank = 0;
-      for (int j = 0; j < n; ++j) rank += sm.list[j] > mine;
-      if (rank < k) sm.sorted[rank] = mine;
+    // those that equal the cut behind the others
+    const int all = ties <= kTies ? n + ties : n;
+    for (int i = tid; i < all; i += kThreads) {
+      const bool tie = i >= n;
+      const unsigned long long* list = sm.list + (tie ? kList : 0);
+      const int len = tie ? ties : n;
+      const unsigned long long x = list[tie ? i - n : i];
+      int rank = tie ? n : 0;
+      for (int j = 0; j < len; ++j) rank += list[j] > x;
+      if (rank < k) sm.sorted[rank] = x;
+    }
+    if (n < k && ties > kTies) {
+      // more of them than the list holds (most of a filtered row, or one of equal logits): in the order of their index, as
+      // far as it takes
+      int found = n;
+      auto take = [&](uint32_t which, int index) {         // which: of this thread's next elements, from `index` on
+        const int count = __popc(which);
+        int before = count;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int x = __shfl_up_sync(0xffffffffu, before, o);
+          if (lane >= o) before += x;
+        }
+        meet();
+        if (lane == 31) sm.least[warp] = before;
+        meet();
+        int rank = found + before - count;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const int x = (int)sm.least[w];
+          if (w < warp) rank += x;
+          found += x;
+        }
+        for (; which && rank < k; which &= which - 1) sm.sorted[rank++] = entry(cut, (uint32_t)(index + __ffs(which) - 1));
+      };
+      take(tid < part.head && key_of<T>(head) == cut, tid);
+      for (int i0 = 0; i0 < part.pieces && found < k; i0 += kThreads) {
+        const int i = i0 + tid;
+        uint32_t which = 0;
+        if (i < part.pieces) each(load_piece(i), i, [&](float x, int index) { which |= (uint32_t)(x == least) << (index - part.index(i)); });
+        take(which, part.index(i));
+      }
+      if (found < k) take(tid < part.tail && key_of<T>(tail) == cut, part.tail_index + tid);
     }
     meet();
     return;
   }
+  // the stripes' elements, one alternative at a time
+  if (tid == 0) sm.stripes = 0;
+  meet();
+  if (mine) sm.stripe[atomicAdd(&sm.stripes, 1)] = tid;
+  meet();
   unsigned long long before = ~0ull;
   for (int r = 0; r < k; ++r) {
     unsigned long long best = 0;
@@ -366,9 +418,10 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, f
       const unsigned long long e = entry(key_of<T>(x), (uint32_t)index);
       if (e < before && e > best) best = e;
     };
-    if (tid < part.head) see(to_f(part.z[tid]), tid);
-    for (int i = tid; i < part.pieces; i += kThreads) each(load_piece(i), i, see);
-    if (tid < part.tail) see(to_f(part.z[part.tail_index + tid]), part.tail_index + tid);
+    if (mine && tid < part.head) see(head, tid);
+    for (int x = warp; x < sm.stripes; x += kWarps)
+      for (int i = lane * kStripes + (int)sm.stripe[x]; i < part.pieces; i += 32 * kStripes) each(load_piece(i), i, see);
+    if (mine && tid < part.tail) see(tail, part.tail_index + tid);
     best = block_max(best, sm);
     if (tid == 0) sm.sorted[r] = best;
     before = best;

@@ -55,3 +55,76 @@ def test_logits_on_both_sides_of_the_limit_of_the_fast_steps(lsp, by):
     check(z, tokens, 3, 1.0, call(lsp, z, tokens, 3))
     # (the same x, everything by a power of two)
     check(z / 1024, tokens, 3, 2.0 ** -10, call(lsp, z / 1024, tokens, 3, 2.0 ** -10))
+
+
+def filtered(rows, V, dtype, finite, seed, lowest=False):
+    """All but `finite` logits of a row are the type's way of saying never."""
+    g = torch.Generator().manual_seed(seed)
+    z = torch.full((rows, V), float(torch.finfo(DT[dtype]).min) if lowest else -float("inf"))
+    for r in range(rows):
+        at = torch.randperm(V, generator=g)[:finite]
+        z[r, at] = torch.randn(finite, generator=g) * 3
+    return z.to(DT[dtype])
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("lowest", [False, True])
+@pytest.mark.parametrize("rows,V,finite,k", [(3, 151936, 50, 20), (3, 151936, 5, 32), (2, 151937, 1, 32), (3, 20011, 31, 32),
+                                             (3, 2047, 3, 32), (400, 9001, 20, 20), (2, 33, 2, 32), (4, 600001, 900, 32)])
+def test_filtered_rows(lsp, rows, V, finite, k, lowest, dtype):
+    z = filtered(rows, V, dtype, finite, V + k, lowest).cuda()
+    tokens = z.argmax(-1).int()
+    check(z, tokens, k, 1.0, call(lsp, z, tokens, k))
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_ties_at_the_cut_in_the_head_the_tail_and_far_apart(lsp, dtype):
+    """More equal logits than a list of them holds, with larger ones among them, in rows that start at any address."""
+    V, k = 40013, 32
+    for by in range(4):
+        wide = torch.full((by + 5 * (V + 3),), -7.0)
+        z = wide[by:].as_strided((5, V), (V + 3, 1))
+        z[1, -300:] = 2.0                            # the ties are at the end
+        z[1, 0] = 2.0
+        z[2, 5::7] = 1.5                             # everywhere
+        z[2, 3], z[2, V - 1] = 1.75, 9.0
+        z[3, 1000:30000] = 4.0                       # in one stretch, with some larger ones
+        z[3, 1500:1520] = 5.0
+        z[4, ::2] = 1.0                              # larger ones in more places than alternatives
+        z[4, 100:30000:311] = 2.0
+        wide = wide.to(DT[dtype]).cuda()
+        z = wide[by:].as_strided((5, V), (V + 3, 1))
+        tokens = ints([0, V - 1, 3, 1500, 100])
+        for n in (1, 17, k):
+            check(z, tokens, n, 1.0, call(lsp, z, tokens, n))
+
+
+def elapsed(lsp, z, tokens, k):
+    out = [torch.empty(z.shape[0], device="cuda"), None, torch.empty(z.shape[0], k, dtype=torch.int32, device="cuda")]
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    best = float("inf")
+    for _ in range(6):
+        a.record()
+        for _ in range(5):
+            lsp.lsp_logprobs(z, tokens, *out)
+        b.record()
+        torch.cuda.synchronize()
+        best = min(best, a.elapsed_time(b))
+    return best
+
+
+@pytest.mark.parametrize("dtype,k", [("bf16", 20), ("bf16", 32), ("f32", 32)])
+def test_filtered_rows_take_no_longer_than_others(lsp, dtype, k):
+    """(Reading such rows again for every alternative takes 10 to 30 times as long.)"""
+    rows, V = 600, 151936
+    g = torch.Generator("cuda").manual_seed(1)
+    z = (torch.randn(rows, V, device="cuda", generator=g) * 2.5).to(DT[dtype])
+    tokens = ints([7] * rows)
+    usual = elapsed(lsp, z, tokens, k)
+    keep = torch.rand(rows, V, device="cuda", generator=g) < 50 / V
+    z = torch.where(keep, z, -float("inf"))
+    z[:, 7] = 1.0
+    assert elapsed(lsp, z, tokens, k) < 3 * usual
+    z = torch.sort(z.float(), descending=True).values.to(DT[dtype])        # the largest side by side
+    z[:, 7] = 1.0
+    assert elapsed(lsp, z, tokens, k) < 3 * usual
