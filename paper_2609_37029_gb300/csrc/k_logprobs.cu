@@ -185,8 +185,8 @@ __device__ __forceinline__ void raise(Stats& st, float top, const Scale& k, bool
   st.s = make_float2(r * st.s.x, r * st.s.y);
   st.m = top;
   st.ref = ref;
-  // (200 / c below m; where m's last place is more than that, some of those below)
-  st.least = fine ? top - fmaxf(200.0f * k.inv, fabsf(top) * 0x1p-20f) : __uint_as_float(0x7FC00000u);
+  // (200 / c below m, which is 10^6 / c at most: many of its last places)
+  st.least = fine ? top - 200.0f * k.inv : __uint_as_float(0x7FC00000u);
   const __nv_bfloat16 low = __float2bfloat16_rd(st.least);
   st.low = bf2_bits(__halves2bfloat162(low, low));
 }
