@@ -615,9 +615,9 @@ int lsp_verify_probs(const void* target_probs, const void* draft_probs, int dtyp
  * T in [2^-100, 2^100]; rows in [0, 2^27], V in [1, 2^26], ld >= V, k in
  * [0, min(V, 32)].  One launch; each row is read once, and what may hold its k
  * largest logits once more (k times where more than a thousand that belong there
- * crowd into a few places of a row).  In fp32; the same call gives the same bits.  How many rows
- * there are decides how a row is split: its sums may differ in their last bits, the
- * tokens never. */
+ * crowd into a few places of a row).  In fp32; the same call gives the same bits.
+ * How many rows there are, and a row's address modulo 16 bytes, decide how it is
+ * split: its sums may differ in their last bits, the tokens never. */
 int lsp_logprobs(const void* logits, int dtype, const int32_t* tokens, int rows, int V, int64_t ld,
                  float temperature, int k, float* logprob, float* entropy, int32_t* top,
                  float* top_logprob, uint32_t* dev_error, lsp_stream_t stream);

@@ -128,3 +128,20 @@ def test_filtered_rows_take_no_longer_than_others(lsp, dtype, k):
     z = torch.sort(z.float(), descending=True).values.to(DT[dtype])        # the largest side by side
     z[:, 7] = 1.0
     assert elapsed(lsp, z, tokens, k) < 3 * usual
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_a_row_at_any_address(lsp, dtype):
+    """The same row at several addresses: its sums may go another way, its tokens may not."""
+    V, k = 30011, 20
+    g = torch.Generator().manual_seed(3)
+    row = (torch.randn(V, generator=g) * 3).to(DT[dtype]).cuda()
+    row[::1000] = 12.5                               # equal ones among the largest
+    outs = []
+    for by in range(8):
+        wide = torch.zeros(V + 8, dtype=DT[dtype], device="cuda")
+        wide[by:by + V] = row
+        z = wide[by:by + V][None]
+        outs.append(call(lsp, z, ints([4321]), k))
+        check(z, ints([4321]), k, 1.0, outs[-1])
+    assert all(torch.equal(o[2], outs[0][2]) for o in outs)
