@@ -35,7 +35,7 @@ __device__ __forceinline__ float ex2a(float x) {
   return y;
 }
 
-constexpr int kFmaRows = 64, kFmaKeys = 64, kFmaThreads = 256;
+constexpr int kFmaRows = 64, kFmaKeys = kPrefixFmaKeys, kFmaThreads = 256;
 // CTAs of an SM: what is on its way in registers (HD / 16 float4) takes too many of them for two where HD = 128
 template <int HD>
 constexpr int kFmaPerSm = HD == 64 ? 2 : 1;
@@ -222,11 +222,11 @@ __global__ void __launch_bounds__(kFmaThreads, kFmaPerSm<HD>) prefix_attn_fma_ke
   griddep_launch();
   const int cta = blockIdx.x;
   if (threadIdx.x < 32) {
-    const PrefixSched s = build_sched<1, kFmaKeys>(p, sm.line_base, sm.info, cta == 0);
+    const PrefixSched s = build_sched<FmaWork>(p, sm.line_base, sm.info, cta == 0);
     if (threadIdx.x == 0) sm.sched = s;
   }
   __syncthreads();
-  PrefixSegs<1, kFmaKeys> segs(p, sm.sched, sm.line_base, sm.info, cta);
+  PrefixSegs<FmaWork> segs(p, sm.sched, sm.line_base, sm.info, cta);
   PrefixSeg seg;
   while (segs.next_shared(seg)) fma_segment<HD>(p, sm, seg);
   while (segs.next_own(seg)) fma_segment<HD>(p, sm, seg);
@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(kFmaThreads, kFmaPerSm<HD>) prefix_attn_fma_ke
 // the wait, and the work is laid out again should they differ.  (16 x 1 row over
 // 32K: 45.6 us; 43.7 without reading again, 49.5 with all of it after the wait.)
 constexpr int kJoinRows = 4, kJoinHeads = 4, kJoinPerSm = 4;
-template <typename T, int HD, int kUnitTiles, int kBlock, int kWarps, int kHeads>
+template <typename T, int HD, class W, int kWarps, int kHeads>
 __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoinPerSm) prefix_join_kernel(const PrefixAttnParams p) {
   static_assert(kWarps == 1 || kHeads == 1, "warps that share a row have one");
   constexpr int kVec = HD / 32, kAhead = kWarps > 1 ? 6 : 2;
@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
   bool waited = false, again = true;
   while (again) {
     if (warp == 0) {
-      const PrefixSched s = build_sched<kUnitTiles, kBlock>(p, line_base, info, false);
+      const PrefixSched s = build_sched<W>(p, line_base, info, false);
       if (lane == 0) s_sched = s;
     }
     __syncthreads();
@@ -303,23 +303,23 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
         const int tile_rows = p.tok_tile * p.rep;
         if (s.items > 0) {
           const int tile = t / p.tok_tile;
-          u = tile / kUnitTiles;
-          shared_at = (tile % kUnitTiles) * tile_rows + (t - tile * p.tok_tile) * p.rep + hr;
+          u = tile / W::kUnitTiles;
+          shared_at = (tile % W::kUnitTiles) * tile_rows + (t - tile * p.tok_tile) * p.rep + hr;
           const bool last = u + 1 == p.units;
-          shared_cost = last ? block_cost(p, p.total - u * kUnitTiles * p.tok_tile) : p.cost.many;
+          shared_cost = last ? block_cost<W>(p, p.total - u * W::kUnitTiles * p.tok_tile) : W::kMany;
           pieces = s_pieces[last];
           shared = p.splits * pieces;
           shared_first = shared_place(s, g * p.splits, u) - s.whole_line;
         }
         const int i = t - r.first, tile = i / p.tok_tile;
-        unit = tile / kUnitTiles;
-        own_at = (tile % kUnitTiles) * tile_rows + (i - tile * p.tok_tile) * p.rep + hr;
+        unit = tile / W::kUnitTiles;
+        own_at = (tile % W::kUnitTiles) * tile_rows + (i - tile * p.tok_tile) * p.rep + hr;
         first = s.shared_line + line_base[lo];
         for (int u = 0; u < unit; ++u)
-          first += (int64_t)item_length<kUnitTiles>(p, r, u, own_blocks<kUnitTiles, kBlock>(p, r, s.base, u)) * p.nkv;
-        blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, unit);
-        cost = block_cost(p, r.rows - unit * kUnitTiles * p.tok_tile);
-        const int len = item_length<kUnitTiles>(p, r, unit, blocks);
+          first += (int64_t)item_length<W>(p, r, u, own_blocks<W>(p, r, s.base, u)) * p.nkv;
+        blocks = own_blocks<W>(p, r, s.base, unit);
+        cost = block_cost<W>(p, r.rows - unit * W::kUnitTiles * p.tok_tile);
+        const int len = item_length<W>(p, r, unit, blocks);
         first += (int64_t)g * len;
         if (blocks > 0) {
           c0 = piece_at(first);
@@ -332,14 +332,14 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
         const bool sh = q < shared;
         const int range = sh && q >= pieces ? q / pieces : 0, k = sh ? q - range * pieces : q - shared;
         const int item = (g * p.splits + range) * p.units + u, nb = sh ? range_blocks(s, range) : blocks;
-        if (sh && item < s.whole) return k == 0 && nb > 0 ? shared_rows<kUnitTiles>(p, s, item, 0) + shared_at : -1;
+        if (sh && item < s.whole) return k == 0 && nb > 0 ? shared_rows<W>(p, s, item, 0) + shared_at : -1;
         const int64_t place = sh ? shared_first + range * s.len_range : first;
         const int c = (sh ? piece_at(place) : c0) + k;
         if (c >= s.ctas) return -1;
         // a CTA may have a piece of the item without any of its blocks
         const int price = sh ? shared_cost : cost;
-        if (blocks_before(p, s, begin[c + 1] - place, nb, price) <= blocks_before(p, s, begin[c] - place, nb, price)) return -1;
-        return sh ? shared_rows<kUnitTiles>(p, s, item, c) + shared_at : own_rows<kUnitTiles>(p, r, unit, g, c) + own_at;
+        if (blocks_before<W>(s, begin[c + 1] - place, nb, price) <= blocks_before<W>(s, begin[c] - place, nb, price)) return -1;
+        return sh ? shared_rows<W>(p, s, item, c) + shared_at : own_rows<W>(p, r, unit, g, c) + own_at;
       };
       // the first segment of this lane for the maxima, and for the sums
       int64_t row_m = row_of(lane), row_s = row_m;
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(32 * kJoinRows * kWarps, kWarps > 1 ? 2 : kJoi
   if (!waited) griddep_wait();
 }
 
-template <typename T, int HD, int kUnitTiles, int kBlock>
+template <typename T, int HD, class W>
 int launch_join(const PrefixAttnParams& p, cudaStream_t s) {
   const int64_t rows = (int64_t)p.total * p.nq;
   auto ctas = [&](int heads) { return ((int64_t)p.total * p.nkv * ((p.rep + heads - 1) / heads) + kJoinRows - 1) / kJoinRows; };
@@ -472,8 +472,8 @@ int launch_join(const PrefixAttnParams& p, cudaStream_t s) {
   // one warp for several 33.2; 512 rows 27.6 and 30.5; 2048 rows 53 and 42)
   const bool few = rows <= 2 * kJoinRows * (int64_t)p.num_sms;
   const cudaError_t e =
-      few ? launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 4, 1>, dim3((unsigned)ctas(1)), dim3(128 * kJoinRows), smem, s, p)
-          : launch_pdl(prefix_join_kernel<T, HD, kUnitTiles, kBlock, 1, kJoinHeads>, dim3((unsigned)std::min<int64_t>(ctas(kJoinHeads), kJoinPerSm * p.num_sms)),
+      few ? launch_pdl(prefix_join_kernel<T, HD, W, 4, 1>, dim3((unsigned)ctas(1)), dim3(128 * kJoinRows), smem, s, p)
+          : launch_pdl(prefix_join_kernel<T, HD, W, 1, kJoinHeads>, dim3((unsigned)std::min<int64_t>(ctas(kJoinHeads), kJoinPerSm * p.num_sms)),
                        dim3(32 * kJoinRows), smem, s, p);
   return e == cudaSuccess ? LSP_OK : LSP_ERR_CUDA;
 }
@@ -491,20 +491,21 @@ int launch_fma(const PrefixAttnParams& p, cudaStream_t s) {
   }
   if (launch_pdl(prefix_attn_fma_kernel<HD>, dim3(p.grid), dim3(kFmaThreads), sizeof(FmaSmem<HD>), s, p) != cudaSuccess)
     return LSP_ERR_CUDA;
-  return launch_join<float, HD, 1, kFmaKeys>(p, s);
+  return launch_join<float, HD, FmaWork>(p, s);
 }
 
 template <int HD>
 int launch_tc(const PrefixAttnParams& p, cudaStream_t s) {
   const int rc = launch_prefix_attn_tc(p, s);
-  return rc == LSP_OK ? launch_join<bf16, HD, kPrefixTcTiles, kPrefixTcKeys>(p, s) : rc;
+  if (rc != LSP_OK) return rc;
+  return p.q4 ? launch_join<bf16, HD, TcQ4Work>(p, s) : launch_join<bf16, HD, TcWork>(p, s);
 }
 
 template <int HD>
 int launch_q4(const PrefixAttnParams& p, int dtype, cudaStream_t s) {
   const int rc = launch_prefix_attn_q4(p, dtype, s);
   if (rc != LSP_OK) return rc;
-  return dtype == LSP_DTYPE_BF16 ? launch_join<bf16, HD, 1, kPrefixQ4Keys>(p, s) : launch_join<float, HD, 1, kPrefixQ4Keys>(p, s);
+  return dtype == LSP_DTYPE_BF16 ? launch_join<bf16, HD, Q4Work>(p, s) : launch_join<float, HD, Q4Work>(p, s);
 }
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -521,22 +522,6 @@ struct Shape {
   int tile, unit_tiles, block, per_sm;
 };
 
-// Costs in units of 0.37 us.  few_rows: rows that a block is cheaper with.
-PrefixCosts costs(int few_rows, int few, int many, int segment) {
-  PrefixCosts c = {few_rows, few, many, segment, {}};
-  const int group[4] = {few, few * kPrefixTogether, many, many * kPrefixTogether};
-  for (int i = 0; i < 4; ++i) c.inverse[i] = (uint32_t)((((uint64_t)1 << 32) + group[i] - 1) / group[i]);
-  return c;
-}
-PrefixCosts attn_costs(const PrefixAttnParams& p) {
-  // one row tile 1.1 us a block, two 1.46, a segment 1.9 (16 requests over 32K, bf16); over a cache in 4 bits both are as
-  // long as it takes to unpack a block (16 requests of 17 rows over 32K 172 us, with the costs of bf16 198)
-  if (p.tc) return p.q4 ? costs(p.tok_tile * p.rep, 5, 5, 8) : costs(p.tok_tile * p.rep, 3, 4, 5);
-  // unpacked again for every 8 rows (32 of one row over 8K and up to 4K of their own 52 us, with the costs below 76)
-  if (p.q4) return costs(8, 4, 10, 8);
-  // (the fp32 kernel's warps have eight rows each, and those without rows leave the block to the others)
-  return costs(32, 3, 4, 5);
-}
 Shape attn_shape(const PrefixAttnParams& p, int dtype) {
   if (p.tc) return {kPrefixTcRows, kPrefixTcTiles, kPrefixTcKeys, 1};
   if (p.q4) return {kPrefixQ4Rows, 1, kPrefixQ4Keys, prefix_q4_per_sm(dtype, p.d)};
@@ -555,7 +540,6 @@ size_t plan(PrefixAttnParams* p, int dtype, int num_sms, bool tc) {
   const int64_t rows = (int64_t)p->tok_tile * p->rep * sh.unit_tiles, items = std::max<int64_t>((int64_t)p->nkv * p->units, p->grid);
   p->part_rows = (items + 2 * p->grid) * rows + (int64_t)p->nkv * p->rep * p->total;
   p->part_rows = (p->part_rows + 3) / 4 * 4;
-  p->cost = attn_costs(*p);
   return align256((size_t)p->part_rows * sizeof(float2)) + (size_t)p->part_rows * p->d * sizeof(float);
 }
 

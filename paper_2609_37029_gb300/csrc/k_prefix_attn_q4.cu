@@ -122,7 +122,7 @@ __device__ __forceinline__ void load_role(const PrefixAttnParams& p, Smem<HD>& s
   const int run = min(p.page, kKeys), runs = kKeys / run, page_bits = 31 - __clz(p.page);
   const uint32_t codes = run * (HD / 2), scales = run * (HD / 16);
   const int block_codes = p.page * (HD / 2);
-  PrefixSegs<1, kKeys> segs(p, sm.sched, line_base, info, blockIdx.x);
+  PrefixSegs<Q4Work> segs(p, sm.sched, line_base, info, blockIdx.x);
   PrefixSeg g;
   uint32_t k = 0;
   Place ring = {0, 1};                           // (the first uses wait for nobody)
@@ -493,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm<T, HD>) prefix_attn_q4_kernel
   griddep_wait();
   griddep_launch();
   if (warp == kWarps) {
-    const PrefixSched s = build_sched<1, kKeys>(p, line_base, info, blockIdx.x == 0);
+    const PrefixSched s = build_sched<Q4Work>(p, line_base, info, blockIdx.x == 0);
     if (lane == 0) sm.sched = s;
   }
   __syncthreads();

@@ -60,6 +60,7 @@
 // than 2^8, as attention kernels in the literature do: weights stay below 2^8 and
 // the sums, in fp32, lose nothing.
 #include <algorithm>
+#include <type_traits>
 
 #include "barrier_wait.cuh"
 #include "prefix_sched.cuh"
@@ -243,9 +244,10 @@ __device__ __forceinline__ uint32_t value_tile(const Jobs& j, int i) { return j.
 
 // The plan of the CTA's segments, handed on through shared memory: finding the
 // next one takes some 500 cycles, which nobody should spend between two segments.
+template <class W>
 __device__ __forceinline__ void plan_role(const PrefixAttnParams& p, TcMisc* m, const int64_t* line_base, const PrefixSeq* info) {
   const int lane = threadIdx.x & 31;
-  PrefixSegs<kTiles, kKeys> segs(p, m->sched, line_base, info, blockIdx.x);
+  PrefixSegs<W> segs(p, m->sched, line_base, info, blockIdx.x);
   PrefixSeg g;
   uint32_t k = 0;
   auto publish = [&](bool more) {
@@ -639,13 +641,13 @@ __device__ __forceinline__ void mma_role(const PrefixAttnParams& p, int t, uint3
 }
 
 // The sums of stream t's rows that see a value that leave_out left out become NaN, in its dims: behind all segments, which
-// are gone through again.
+// are gone through again.  (Not inlined: 16 requests of 17 rows over 32K 153 us with it between the loops, 152 without.)
 template <int HD>
-__device__ __forceinline__ void spoil_rows(const PrefixAttnParams& p, int t, int row, const PrefixSched& sched, const int64_t* line_base,
+__device__ __noinline__ void spoil_rows(const PrefixAttnParams& p, int t, int row, const PrefixSched& sched, const int64_t* line_base,
                                            const PrefixSeq* info) {
   const float nan = __uint_as_float(0x7FC00000u);
   const int tok = row / p.rep;
-  PrefixSegs<kTiles, kKeys> segs(p, sched, line_base, info, blockIdx.x);
+  PrefixSegs<TcQ4Work> segs(p, sched, line_base, info, blockIdx.x);
   PrefixSeg g;
   while (segs.next_shared(g)) {}                 // (every row sees all of their keys)
   while (segs.next_own(g)) {
@@ -842,6 +844,7 @@ template <int HD, bool kQ4>
 __global__ void __launch_bounds__(kThreads<kQ4>, 1)
     prefix_attn_tc_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                           const __grid_constant__ CUtensorMap mv, const PrefixAttnParams p, int count) {
+  using Work = std::conditional_t<kQ4, TcQ4Work, TcWork>;
   extern __shared__ uint8_t tc_raw[];
   uint8_t* smp = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tc_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   TcMisc* m = reinterpret_cast<TcMisc*>(smp + TcShape<HD>::kMisc);
@@ -889,7 +892,7 @@ __global__ void __launch_bounds__(kThreads<kQ4>, 1)
   griddep_wait();
   griddep_launch();
   if (warp == 0) {
-    const PrefixSched sc = build_sched<kTiles, kKeys>(p, line_base, info, cta == 0);
+    const PrefixSched sc = build_sched<Work>(p, line_base, info, cta == 0);
     if (lane == 0) m->sched = sc;
   }
   tc_fence_before();
@@ -914,7 +917,7 @@ __global__ void __launch_bounds__(kThreads<kQ4>, 1)
     else if (warp < kMmaWarp + 2)
       mma_role<HD, kQ4>(p, warp - kMmaWarp, sm, tmem, m, segs);
     else
-      plan_role(p, m, line_base, info);
+      plan_role<Work>(p, m, line_base, info);
   } else {
     if constexpr (kQ4)
       asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");

@@ -297,12 +297,6 @@ int launch_pages_read(const KvCache& c, const int* seqs, const int* start, int n
                       int total, int es, bool q4, unsigned* err, cudaStream_t s);
 
 // ------------------------------------------------------------------ shared-prefix attention
-constexpr int kPrefixTogether = 4;   // key blocks that a cut keeps together (prefix_sched.cuh)
-constexpr int kPrefixInverseBits = 26;
-struct PrefixCosts {
-  int few_rows, few, many, segment;  // each cost * kPrefixTogether below 2^(32 - kPrefixInverseBits)
-  uint32_t inverse[4];               // ceil(2^32 / x) for x = few, few * kPrefixTogether, many, many * kPrefixTogether
-};
 struct PrefixAttnParams {
   const char* k;            // the layer's pools
   const char* v;
@@ -327,7 +321,6 @@ struct PrefixAttnParams {
   int splits;               // key ranges of the shared pages
   int num_sms;
   int grid;                 // CTAs of the main kernel
-  PrefixCosts cost;         // of the chosen kernel
   int64_t part_rows;        // rows of partial results the workspace holds
   float* part_o;            // [part_rows][d] unnormalised sums
   float2* part_ml;          // [part_rows] (running maximum of the base-2 scores, sum)
@@ -345,7 +338,7 @@ constexpr int kPrefixTcRows = 128, kPrefixTcKeys = 128, kPrefixTcTiles = 2;   //
 // rows of bf16 or f32 over a cache in 4 bits
 int launch_prefix_attn_q4(const PrefixAttnParams& p, int dtype, cudaStream_t s);
 int prefix_q4_per_sm(int dtype, int d);
-constexpr int kPrefixQ4Rows = 64, kPrefixQ4Keys = 128;
+constexpr int kPrefixQ4Rows = 64, kPrefixQ4Keys = 128, kPrefixFmaKeys = 64;
 // ws: prefix_attn_plan's bytes, 256-byte aligned.
 int launch_prefix_attention(PrefixAttnParams p, int dtype, void* ws, cudaStream_t s);
 

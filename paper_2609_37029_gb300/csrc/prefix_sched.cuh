@@ -51,15 +51,33 @@ struct PrefixSched {
   int together;         // key blocks that a cut keeps together in a short item
 };
 
-// What work costs a CTA, for dealing it out, is the kernel's (PrefixCosts): a key
-// block against few and against many rows, and what a segment takes besides.
+// A kernel's tiles of a unit and keys of a block, and what work costs a CTA of it, for
+// dealing it out, in units of 0.37 us: a key block against few and against many rows (more
+// than kFewRows; 0: than a tile's), and what a segment takes besides.  (Constants: as
+// parameters, with the join's divisions by them, attention of 16 requests of one row over
+// 32K took 49.3 us instead of 47.8.)
 //
 // A segment of the tensor cores costs as much as two blocks, so a cut leaves four
 // together in a short item (of up to kShort), unless there is less work than CTAs;
 // a block of the other kernels takes longer than what comes with it.
-constexpr int kTogether = kPrefixTogether, kShort = 8;
+template <int kUnitTiles_, int kBlock_, int kFewRows_, int kFew_, int kMany_, int kSegment_>
+struct PrefixWork {
+  static constexpr int kUnitTiles = kUnitTiles_, kBlock = kBlock_, kFewRows = kFewRows_, kFew = kFew_, kMany = kMany_, kSegment = kSegment_;
+};
+// one row tile 1.1 us a block, two 1.46, a segment 1.9 (16 requests over 32K)
+using TcWork = PrefixWork<kPrefixTcTiles, kPrefixTcKeys, 0, 3, 4, 5>;
+// over a cache in 4 bits both are as long as it takes to unpack a block (16 requests of 17 rows over 32K 172 us, with the
+// costs of bf16 198, when they were chosen)
+using TcQ4Work = PrefixWork<kPrefixTcTiles, kPrefixTcKeys, 0, 5, 5, 8>;
+// unpacked again for every 8 rows (32 of one row over 8K and up to 4K of their own 52 us, with the costs below 76)
+using Q4Work = PrefixWork<1, kPrefixQ4Keys, 8, 4, 10, 8>;
+// (the fp32 kernel's warps have eight rows each, and those without rows leave the block to the others)
+using FmaWork = PrefixWork<1, kPrefixFmaKeys, 32, 3, 4, 5>;
+
+constexpr int kTogether = 4, kShort = 8;
+template <class W>
 __device__ __forceinline__ int block_cost(const PrefixAttnParams& p, int tokens) {
-  return tokens * p.rep > p.cost.few_rows ? p.cost.many : p.cost.few;
+  return (W::kFewRows ? tokens * p.rep > W::kFewRows : tokens > p.tok_tile) ? W::kMany : W::kFew;
 }
 struct __align__(16) PrefixSeq {
   int seq, first, rows, len;    // row of the table (-1: none), first row of q, rows, tokens
@@ -108,10 +126,10 @@ __device__ __forceinline__ bool same_seq(const PrefixAttnParams& p, int i, const
 }
 
 // Own key blocks that unit u of a sequence has to see.
-template <int kUnitTiles, int kBlock>
+template <class W>
 __device__ __forceinline__ int own_blocks(const PrefixAttnParams& p, const PrefixSeq& r, int base, int u) {
-  const int upto = min(r.rows, (u + 1) * kUnitTiles * p.tok_tile);
-  return max(0, cdiv(r.len - r.rows + upto - base, kBlock));
+  const int upto = min(r.rows, (u + 1) * W::kUnitTiles * p.tok_tile);
+  return max(0, cdiv(r.len - r.rows + upto - base, W::kBlock));
 }
 
 __device__ __forceinline__ int own_units(const PrefixAttnParams& p, const PrefixSeq& r, int unit_tiles) {
@@ -119,13 +137,13 @@ __device__ __forceinline__ int own_units(const PrefixAttnParams& p, const Prefix
 }
 
 // Length on the line of an own item of a unit with `blocks` key blocks:
-template <int kUnitTiles>
+template <class W>
 __device__ __forceinline__ int item_length(const PrefixAttnParams& p, const PrefixSeq& r, int u, int blocks) {
-  return blocks > 0 ? p.cost.segment + blocks * block_cost(p, r.rows - u * kUnitTiles * p.tok_tile) : 0;
+  return blocks > 0 ? W::kSegment + blocks * block_cost<W>(p, r.rows - u * W::kUnitTiles * p.tok_tile) : 0;
 }
 
 // Built by one warp of every CTA; line_base [n + 1], info [n] in shared memory.
-template <int kUnitTiles, int kBlock>
+template <class W>
 __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, int64_t* line_base, PrefixSeq* info, bool report) {
   const int lane = threadIdx.x & 31;
   PrefixSched s;
@@ -141,14 +159,14 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) base = min(base, __shfl_xor_sync(0xffffffffu, base, o));
   s.base = max(base, 0) / p.page * p.page;
-  s.blocks = cdiv(s.base, kBlock);
+  s.blocks = cdiv(s.base, W::kBlock);
   s.range = s.blocks / p.splits;
   s.longer = s.blocks - s.range * p.splits;
   s.items = s.blocks > 0 ? p.nkv * p.splits * p.units : 0;
   s.whole = s.items / p.grid * p.grid;
   const int most = s.range + (s.longer > 0);
-  s.len_two = p.cost.segment + most * p.cost.many;
-  s.len_last = p.cost.segment + most * block_cost(p, p.total - (p.units - 1) * kUnitTiles * p.tok_tile);
+  s.len_two = W::kSegment + most * W::kMany;
+  s.len_last = W::kSegment + most * block_cost<W>(p, p.total - (p.units - 1) * W::kUnitTiles * p.tok_tile);
   s.len_range = (int64_t)(p.units - 1) * s.len_two + s.len_last;
   s.whole_line = (int64_t)(s.whole / p.units) * s.len_range + (int64_t)(s.whole % p.units) * s.len_two;
   s.shared_line = (int64_t)(s.items / p.units) * s.len_range - s.whole_line;
@@ -158,8 +176,8 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
     int64_t mine = 0;
     if (i < p.n) {
       const PrefixSeq r = info[i];               // this lane's own store
-      for (int u = 0, units = own_units(p, r, kUnitTiles); u < units; ++u)
-        mine += item_length<kUnitTiles>(p, r, u, own_blocks<kUnitTiles, kBlock>(p, r, s.base, u));
+      for (int u = 0, units = own_units(p, r, W::kUnitTiles); u < units; ++u)
+        mine += item_length<W>(p, r, u, own_blocks<W>(p, r, s.base, u));
       mine *= p.nkv;
     }
     int64_t x = mine;
@@ -173,9 +191,9 @@ __device__ __forceinline__ PrefixSched build_sched(const PrefixAttnParams& p, in
   }
   if (lane == 0) line_base[p.n] = line;
   s.line = s.shared_line + line;
-  const int least = p.cost.few;
-  const bool small = s.line < (int64_t)p.grid * (p.cost.segment + kTogether * least);
-  s.together = kUnitTiles == 1 || small ? 1 : kTogether;
+  const int least = W::kFew;
+  const bool small = s.line < (int64_t)p.grid * (W::kSegment + kTogether * least);
+  s.together = W::kUnitTiles == 1 || small ? 1 : kTogether;
   s.ctas = small ? max(min((int)s.line / least, p.grid), 1) : p.grid;
   return s;
 }
@@ -199,16 +217,16 @@ __device__ __forceinline__ int64_t shared_place(const PrefixSched& s, int head_r
 
 // Workspace rows: the first row of a segment; its second tile's rows follow its
 // first's (tok_tile * rep of them).  Shared items come before own ones.
-template <int kUnitTiles>
+template <class W>
 __device__ __forceinline__ int64_t shared_rows(const PrefixAttnParams& p, const PrefixSched& s, int item, int cta) {
-  return ((int64_t)item + (item >= s.whole ? cta : 0)) * kUnitTiles * p.tok_tile * p.rep;
+  return ((int64_t)item + (item >= s.whole ? cta : 0)) * W::kUnitTiles * p.tok_tile * p.rep;
 }
-template <int kUnitTiles>
+template <class W>
 __device__ __forceinline__ int64_t own_rows(const PrefixAttnParams& p, const PrefixSeq& r, int unit, int head, int cta) {
-  const int t0 = unit * kUnitTiles * p.tok_tile, tokens = min(r.rows - t0, kUnitTiles * p.tok_tile);
+  const int t0 = unit * W::kUnitTiles * p.tok_tile, tokens = min(r.rows - t0, W::kUnitTiles * p.tok_tile);
   const int64_t before = (int64_t)p.nkv * (r.first + t0) + (int64_t)head * tokens;
   const int64_t units = (int64_t)p.nkv * p.splits * p.units + p.grid + cta;
-  return units * kUnitTiles * p.tok_tile * p.rep + before * p.rep;
+  return units * W::kUnitTiles * p.tok_tile * p.rep + before * p.rep;
 }
 
 // Four dims (chunk c) of workspace row r.  Four rows are interleaved chunk by
@@ -233,21 +251,27 @@ struct PrefixSeg {
   int64_t part;         // its first row of the workspace
 };
 
+__host__ __device__ constexpr uint32_t inverse_of(int x) { return (uint32_t)((((uint64_t)1 << 32) + x - 1) / x); }
+
 // Key blocks of an item of the line (of `blocks`, each of `cost`) that belong to
 // the places before `at` of it: single ones or groups, the first with the
 // segment's cost, go to where they begin.
-__device__ __forceinline__ int blocks_before(const PrefixAttnParams& p, const PrefixSched& s, int64_t at, int blocks, int cost) {
-  if (at <= p.cost.segment) return at > 0 ? min(blocks <= kShort ? s.together : 1, blocks) : 0;
+template <class W>
+__device__ __forceinline__ int blocks_before(const PrefixSched& s, int64_t at, int blocks, int cost) {
+  if (at <= W::kSegment) return at > 0 ? min(blocks <= kShort ? s.together : 1, blocks) : 0;
   const int together = blocks <= kShort ? s.together : 1, group = together * cost;
-  const int64_t n = at - p.cost.segment + group - 1;
+  const int64_t n = at - W::kSegment + group - 1;
   // n / group, by ceil(2^32 / group): exact below 2^32 / group
-  const uint32_t inverse = p.cost.inverse[(cost == p.cost.few ? 0 : 2) + (together > 1)];
-  const int64_t groups = n < (1 << kPrefixInverseBits) ? (int64_t)__umulhi((uint32_t)n, inverse) : long_div(n, group);
+  constexpr int kBits = 26;
+  static_assert(kTogether * (W::kFew > W::kMany ? W::kFew : W::kMany) < (1 << (32 - kBits)), "the groups' inverses");
+  const uint32_t inverse = cost == W::kFew ? (together == 1 ? inverse_of(W::kFew) : inverse_of(kTogether * W::kFew))
+                                           : (together == 1 ? inverse_of(W::kMany) : inverse_of(kTogether * W::kMany));
+  const int64_t groups = n < (1 << kBits) ? (int64_t)__umulhi((uint32_t)n, inverse) : long_div(n, group);
   return (int)min(groups * together, (int64_t)blocks);
 }
 
 // The segments of a CTA: its whole items, and its piece [x, end) of the line.
-template <int kUnitTiles, int kBlock>
+template <class W>
 struct PrefixSegs {
   const PrefixAttnParams& p;
   const PrefixSched s;
@@ -285,13 +309,13 @@ struct PrefixSegs {
         gs = (int)div_floor(place, s.len_range);
         const int64_t rel = place - gs * s.len_range;
         u = (int)min(div_floor(rel, s.len_two), (int64_t)(p.units - 1));
-        const int cost = u + 1 < p.units ? p.cost.many : block_cost(p, p.total - u * kUnitTiles * p.tok_tile);
+        const int cost = u + 1 < p.units ? W::kMany : block_cost<W>(p, p.total - u * W::kUnitTiles * p.tok_tile);
         const int64_t to = rel - (int64_t)u * s.len_two + 1, from = max(to - (mid - x), (int64_t)0);
         mid -= to - from;
         split = gs % p.splits;
         const int blocks = range_blocks(s, split);
-        c0 = blocks_before(p, s, from, blocks, cost);
-        c1 = blocks_before(p, s, to, blocks, cost);
+        c0 = blocks_before<W>(s, from, blocks, cost);
+        c1 = blocks_before<W>(s, to, blocks, cost);
       } else {
         x = max(x, min(end, s.shared_line));
         return false;
@@ -301,11 +325,11 @@ struct PrefixSegs {
       g.kb1 = range_begin(s, split) + c1;
       g.tab = shared_tab;
       g.head = gs / p.splits;
-      g.t0 = u * kUnitTiles * p.tok_tile;
-      g.tokens = min(kUnitTiles * p.tok_tile, p.total - g.t0);
+      g.t0 = u * W::kUnitTiles * p.tok_tile;
+      g.tokens = min(W::kUnitTiles * p.tok_tile, p.total - g.t0);
       g.k0 = 0;
       g.k_end = g.see0 = s.base;
-      g.part = shared_rows<kUnitTiles>(p, s, gs * p.units + u, cta);
+      g.part = shared_rows<W>(p, s, gs * p.units + u, cta);
       return true;
     }
   }
@@ -319,30 +343,30 @@ struct PrefixSegs {
         if (line_base[mid] <= place) lo = mid; else hi = mid;
       }
       const PrefixSeq r = info[lo];
-      const int units = own_units(p, r, kUnitTiles);
+      const int units = own_units(p, r, W::kUnitTiles);
       int64_t rel = place - line_base[lo];
-      int u = 0, blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, 0);
-      int64_t len = item_length<kUnitTiles>(p, r, 0, blocks);
+      int u = 0, blocks = own_blocks<W>(p, r, s.base, 0);
+      int64_t len = item_length<W>(p, r, 0, blocks);
       while (rel >= len * p.nkv && u + 1 < units) {
         rel -= len * p.nkv;
-        blocks = own_blocks<kUnitTiles, kBlock>(p, r, s.base, ++u);
-        len = item_length<kUnitTiles>(p, r, u, blocks);
+        blocks = own_blocks<W>(p, r, s.base, ++u);
+        len = item_length<W>(p, r, u, blocks);
       }
       if (len <= 0) break;                       // (the line is made of items that have a length)
       g.head = (int)div_floor(rel, len);
       const int64_t from = rel - g.head * len, to = min(len, from + (end - x));
       x += to - from;
-      const int i0 = u * kUnitTiles * p.tok_tile, cost = block_cost(p, r.rows - i0);
-      g.kb0 = blocks_before(p, s, from, blocks, cost);
-      g.kb1 = blocks_before(p, s, to, blocks, cost);
+      const int i0 = u * W::kUnitTiles * p.tok_tile, cost = block_cost<W>(p, r.rows - i0);
+      g.kb0 = blocks_before<W>(s, from, blocks, cost);
+      g.kb1 = blocks_before<W>(s, to, blocks, cost);
       if (g.kb0 >= g.kb1) continue;
       g.tab = p.table + (size_t)r.seq * p.max_pages;
       g.t0 = r.first + i0;
-      g.tokens = min(kUnitTiles * p.tok_tile, r.rows - i0);
+      g.tokens = min(W::kUnitTiles * p.tok_tile, r.rows - i0);
       g.k0 = s.base;
       g.k_end = r.len;
       g.see0 = r.len - r.rows + i0 + 1;
-      g.part = own_rows<kUnitTiles>(p, r, u, g.head, cta);
+      g.part = own_rows<W>(p, r, u, g.head, cta);
       return true;
     }
     return false;
