@@ -561,7 +561,7 @@ size_t lsp_prefix_attention_q4_workspace_bytes(const lsp_kv_cache* cache, int dt
  * value's, whatever its weight.  Nothing is unpacked to memory.  bf16: scores and
  * sums in fp32, weights rounded to bf16 for the product with V.  f32: q and the
  * weights enter the tensor cores as sums of three bf16 numbers each (24 bits), the
- * products are exact and summed in fp32.  workspace: at least
+ * products are exact and summed in fp32.  scale up to 2^120.  workspace: at least
  * lsp_prefix_attention_q4_workspace_bytes, 256-byte aligned, not initialised. */
 int lsp_prefix_attention_q4(const lsp_kv_cache* cache, int layer, const void* q, int dtype,
                             int64_t q_stride, int nq, const int32_t* seqs, const int32_t* start, int n,

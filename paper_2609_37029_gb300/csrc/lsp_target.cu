@@ -123,6 +123,7 @@ int attention(const lsp_kv_cache* cache, int layer, const void* q, int dtype, in
   if (layer < 0 || layer >= c.layers || shared_len < 0 || !(scale > 0.f) || !std::isfinite(scale) || !seqs || !start ||
       !words(seqs, start, lse, dev_error))
     return LSP_ERR_ARG;
+  if (p.q4 && scale > 0x1p120f) return LSP_ERR_ARG;      // (its scores are of eighths: 8 log2(e) times it has to be finite)
   if (total == 0) return LSP_OK;
   const int es = esize(dtype);
   if (!q || !out || !aligned(q, 16) || !aligned(out, 16) || !workspace || !aligned(workspace, 256)) return LSP_ERR_ARG;

@@ -221,3 +221,11 @@ def test_logprobs_of_the_binding(lsp, dtype):
     wide = torch.zeros(6, 130, dtype=dtype)[:, 3:103]
     for kw in (dict(logits=wide), dict(entropy=None, top=None, top_logprob=None, dev_error=None), dict(top=None), dict(top_logprob=None)):
         refused(lsp, lsp.lsp_logprobs, {**base, **kw}, [])
+
+
+def test_attention_scales(lsp):
+    """Scores of eighths of the values have a factor of 8 log2(e) scale, which must be a number."""
+    def call(scale):
+        return lsp._f["lsp_prefix_attention_q4"](cache(lsp), 0, 0x7000, 0, 1024, 8, 16, 16, 2, 6, 10, scale, 0x8000, None, 0x9000, 0, None, None)
+    for scale in (1.5 * 2.0 ** 120, 2.0 ** 125, 3e38):
+        assert call(scale) == lsp.LSP_ERR_ARG
