@@ -27,11 +27,13 @@
 // meanwhile (40 KB, four CTAs on an SM), so that memory is read on while a row's last
 // steps, which are rounds of latency, are taken.
 //
-// Rows of 151936 on 608 CTAs: 1088 of bf16 with k = 5 in 76 us (330 MB, 4.4 TB/s; 72
+// Rows of 151936 on 608 CTAs: 1088 of bf16 with k = 5 in 78 us (330 MB, 4.2 TB/s; 72
 // with k = 0: two rows fall to most CTAs and one to some, which is 11 us of it), 190 of
-// fp32 among 272 with k = 20 in 33 us (115 MB, 3.5 TB/s), of which some 6 are the start and
-// the last rows' selection.  With a launch's CTAs for each part instead, without the
-// ring: 97 and 50.
+// fp32 among 272 with k = 20 in 33 us (115 MB, 3.5 TB/s; 380 parts, of which two fall to
+// some SMs and three to others), of which some 6 are the start and the selection.  With a
+// launch's CTAs for each part instead, without the ring: 97 and 50.  With k = 20, 600 rows
+// of bf16: 53 us, with 50 logits left by a filter 70, of equal logits 64, sorted 88 (with
+// one list for all candidates 52, 68, 1490, 1455).
 #include <algorithm>
 #include <cstddef>
 

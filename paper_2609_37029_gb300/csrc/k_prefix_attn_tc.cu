@@ -47,10 +47,13 @@
 // have put them, as eighths (three steps a pair; as they are, in four, 156 and 46.5 us
 // below): some 700 cycles a tile next to the softmax (75 values a lane and 1000 cycles of
 // the products), half of it the integer and 16-bit pipes' own.  16 requests of 17 rows
-// over 32K 153 to 159 us (0.94 PFLOP/s), with the unpacking left out 141: what is left
-// over bf16's 133 are registers (184 a thread for the softmax) and issue slots, not the
-// copy.  16 of one row over 32K 45 us, as with bf16: 10 until the first scores, 21 for 14
-// blocks, which the unpacking bounds, 4 for the segment's sums, 10 for the join.
+// over 32K 152 to 161 us (0.94 PFLOP/s); with the unpacking left out 141 where it took
+// 153, and what the rest over bf16's 133 is, no run has shown.  16 of one row over 32K
+// 41 us; when it took 45, 10 were until the first scores, 21 for 14 blocks, 4 for the
+// segment's sums, 10 for the join, and 41 in all with the unpacking left out: the
+// softmax's chain bounds the blocks more than the unpacking does.  A tile's way through
+// its place, load, unpacking and back, is a chain too: steps in the loading loop show
+// (one copy of its code for keys and values instead of five 42.3 -> 41.1 us).
 // Tried and dropped: codes straight from memory into registers (the prefetched ones
 // hold too few bytes in flight, 512 us), the next tile's words fetched early (spills, or
 // nothing gained), places given back before the words are unpacked (nothing), the next
