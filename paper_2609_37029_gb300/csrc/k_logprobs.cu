@@ -15,11 +15,12 @@
 // largest is read again, and the whole stripe where another piece reaches the k-th
 // stripe's first too (a few of a hundred).  What is above that goes to a list, what
 // equals it to another, some more than k elements as a rule, and they are ranked by
-// counting.  Places decide between equal logits all the way.  Where more elements equal
-// the k-th stripe's first than the list holds (rows of which all but a few logits are
-// -inf, or of equal logits) the first of them are looked for from the start of the part.
-// Only a row made for it (more than a thousand larger elements in those stripes)
-// overflows the list of the others: then the stripes are read k times.
+// counting (hundreds of them, in rows of falling order, by k maxima).  Places decide
+// between equal logits all the way.  Where more elements equal the k-th stripe's first
+// than the list holds (rows of which all but a few logits are -inf, or of equal logits)
+// the first of them are looked for from the start of the part.  Only a row made for it
+// (more than a thousand larger elements in those stripes) overflows the list of the
+// others: then the stripes are read k times.
 //
 // A row is split over a cluster of CTAs, which hand their parts to the first of them
 // through its shared memory: no workspace, no second launch.  The CTAs stay for as
@@ -32,8 +33,9 @@
 // fp32 among 272 with k = 20 in 33 us (115 MB, 3.5 TB/s; 380 parts, of which two fall to
 // some SMs and three to others), of which some 6 are the start and the selection.  With a
 // launch's CTAs for each part instead, without the ring: 97 and 50.  With k = 20, 600 rows
-// of bf16: 53 us, with 50 logits left by a filter 70, of equal logits 64, sorted 88 (with
-// one list for all candidates 52, 68, 1490, 1455).
+// of bf16: 53 us, with 50 logits left by a filter 71, of equal logits 64, sorted 54 (with
+// one list of 512 for all candidates 52, 69, 1490, 1455; 64 rows 19, 39, 35 and 29, and 19,
+// 221, 221 and 203).
 #include <algorithm>
 #include <cstddef>
 
@@ -53,6 +55,7 @@ constexpr int kStripes = kThreads;               // of a CTA's part: stripe i, o
 // Candidates of a CTA: elements above the cut, of k pieces of 64 bytes (and the singles of as many threads) as a rule, and
 // places of elements that equal it.
 constexpr int kList = kLogprobsMaxK * 33, kTies = 256;
+constexpr int kFew = 256;                        // of the list, that are ranked by counting
 constexpr uint32_t kWhole = 0x80000000u;         // of a stripe: all of it is read again
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLeast = -150.0f;                // 2^t is 0 from here on
@@ -360,7 +363,7 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, f
   }
   meet();
   const int n = sm.count[0], ties = sm.count[1];
-  if (n <= kList) {
+  if (n <= kFew) {
     // those that equal the cut behind the others
     const int all = ties <= kTies ? n + ties : n;
     for (int i = tid; i < all; i += kThreads) {
@@ -408,7 +411,7 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, f
     meet();
     return;
   }
-  // the stripes' elements, one alternative at a time
+  // one alternative at a time, of the list, or of the stripes' elements where it overflows
   if (tid == 0) sm.stripes = 0;
   meet();
   if (mine) sm.stripe[atomicAdd(&sm.stripes, 1)] = tid;
@@ -420,10 +423,17 @@ __device__ __forceinline__ void part_top(const Part<T>& part, const Stats& st, f
       const unsigned long long e = entry(key_of<T>(x), (uint32_t)index);
       if (e < before && e > best) best = e;
     };
-    if (mine && tid < part.head) see(head, tid);
-    for (int x = warp; x < sm.stripes; x += kWarps)
-      for (int i = lane * kStripes + (int)sm.stripe[x]; i < part.pieces; i += 32 * kStripes) each(load_piece(i), i, see);
-    if (mine && tid < part.tail) see(tail, part.tail_index + tid);
+    if (n <= kList) {
+      for (int i = tid; i < n; i += kThreads) {
+        const unsigned long long e = sm.list[i];
+        if (e < before && e > best) best = e;
+      }
+    } else {
+      if (mine && tid < part.head) see(head, tid);
+      for (int x = warp; x < sm.stripes; x += kWarps)
+        for (int i = lane * kStripes + (int)sm.stripe[x]; i < part.pieces; i += 32 * kStripes) each(load_piece(i), i, see);
+      if (mine && tid < part.tail) see(tail, part.tail_index + tid);
+    }
     best = block_max(best, sm);
     if (tid == 0) sm.sorted[r] = best;
     before = best;

@@ -114,20 +114,19 @@ def elapsed(lsp, z, tokens, k):
 
 
 @pytest.mark.parametrize("dtype,k", [("bf16", 20), ("bf16", 32), ("f32", 32)])
-def test_filtered_rows_take_no_longer_than_others(lsp, dtype, k):
-    """(Reading such rows again for every alternative takes 10 to 30 times as long.)"""
-    rows, V = 600, 151936
+def test_rows_of_mostly_equal_logits_take_no_multiple_of_others(lsp, dtype, k):
+    """(Reading such rows again for every alternative takes bf16 12 to 45 times as long as usual; this way it is 2 to 3.)"""
+    V = 151936
     g = torch.Generator("cuda").manual_seed(1)
-    z = (torch.randn(rows, V, device="cuda", generator=g) * 2.5).to(DT[dtype])
-    tokens = ints([7] * rows)
-    usual = elapsed(lsp, z, tokens, k)
-    keep = torch.rand(rows, V, device="cuda", generator=g) < 50 / V
-    z = torch.where(keep, z, -float("inf"))
-    z[:, 7] = 1.0
-    assert elapsed(lsp, z, tokens, k) < 3 * usual
-    z = torch.sort(z.float(), descending=True).values.to(DT[dtype])        # the largest side by side
-    z[:, 7] = 1.0
-    assert elapsed(lsp, z, tokens, k) < 3 * usual
+    for rows in (64, 600):                           # parts of a row, and whole rows
+        z = (torch.randn(rows, V, device="cuda", generator=g) * 2.5).to(DT[dtype])
+        tokens = ints([7] * rows)
+        usual = elapsed(lsp, z, tokens, k)
+        keep = torch.rand(rows, V, device="cuda", generator=g) < 50 / V
+        for x in (torch.where(keep, z, -float("inf")), torch.zeros_like(z),
+                  torch.sort(z.float(), descending=True).values.to(DT[dtype])):        # filtered, equal, the largest side by side
+            x[:, 7] = 1.0
+            assert elapsed(lsp, x, tokens, k) < 6 * usual
 
 
 @pytest.mark.parametrize("dtype", list(DT))
